@@ -1,0 +1,303 @@
+// Host side of include/ftattn.h: handle, validation, launches.
+#include "../../include/ftattn.h"
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <cstring>
+#include <new>
+
+#include "attn_plan.cuh"
+#include "attn_rope.cuh"
+#include "attn_simple.cuh"
+
+using namespace ftmoe;
+
+struct ft_attn {
+  ft_attn_config_t cfg;
+  int sm_count = 148, page_shift = 4;
+  uint32_t *status_dev = nullptr;
+  uint8_t *work_mem = nullptr;     // the work partition, one allocation
+  AttnWork work;
+  AttnGeom geom;
+  bool planned = false;
+  int n_req = 0, T = 0, max_new = 0;   // of the latest slots / plan call
+  uint64_t launches = 0;
+};
+
+namespace {
+
+cudaError_t g_attn_cuda_error = cudaSuccess;   // the CUDA error behind the latest FT_ERR_CUDA / FT_ERR_OOM
+
+#define FA_CUDA(expr)                                                                       \
+  do {                                                                                      \
+    cudaError_t e_ = (expr);                                                                \
+    if (e_ != cudaSuccess) {                                                                \
+      g_attn_cuda_error = e_;                                                               \
+      (void)cudaGetLastError();                                                             \
+      return e_ == cudaErrorMemoryAllocation ? FT_ERR_OOM : FT_ERR_CUDA;                    \
+    }                                                                                       \
+  } while (0)
+
+ft_status_t check_config(const ft_attn_config_t *c) {
+  if (!c || c->struct_size != sizeof(ft_attn_config_t)) return FT_ERR_INVALID_ARG;
+  if (c->device < 0 || (c->dtype != FT_ATTN_BF16 && c->dtype != FT_ATTN_FP16)) return FT_ERR_INVALID_ARG;
+  if (c->n_kv_heads < 1 || c->n_q_heads < c->n_kv_heads || c->n_q_heads % c->n_kv_heads || c->n_q_heads > 1024 ||
+      c->n_q_heads / c->n_kv_heads > 64)
+    return FT_ERR_INVALID_ARG;
+  if (c->n_pages < 1 || c->n_pages >= (1 << 22) || c->max_requests < 1 || c->max_requests > kAttnMaxRequests || c->max_tokens < 1 ||
+      c->max_tokens > (1 << 20) || c->max_pages < 1 || c->window < 0)
+    return FT_ERR_INVALID_ARG;
+  if (c->head_dim != 64 && c->head_dim != 128) return FT_ERR_UNSUPPORTED;
+  if (c->page_tokens != 16 && c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128) return FT_ERR_UNSUPPORTED;
+  if ((long long)c->n_pages * c->page_tokens >= (1ll << 31) || (long long)c->max_pages * c->page_tokens >= (1ll << 31))
+    return FT_ERR_INVALID_ARG;
+  // work units of a step are counted in 32 bits: key blocks of all requests and of all tiles of a request's rows
+  const long long blocks = (long long)c->max_pages * c->page_tokens / kDecKeys + 2;
+  const long long tile_tokens = 2 * (kTileRows / (c->n_q_heads / c->n_kv_heads));
+  const long long entries = c->max_tokens / tile_tokens + c->max_requests;
+  if (blocks * c->max_requests * c->n_kv_heads >= (1ll << 31) || blocks * entries * c->n_kv_heads >= (1ll << 31)) return FT_ERR_UNSUPPORTED;
+  return FT_OK;
+}
+
+// Restores the calling thread's current device when the entry point returns.
+struct DeviceScope {
+  int prev = -1;
+  cudaError_t err;
+  explicit DeviceScope(int dev) {
+    err = cudaGetDevice(&prev);
+    if (err == cudaSuccess && prev != dev) err = cudaSetDevice(dev); else prev = -1;
+  }
+  ~DeviceScope() { if (prev >= 0) (void)cudaSetDevice(prev); }
+};
+
+void free_all(ft_attn *h) {
+  (void)cudaFree(h->status_dev);
+  (void)cudaFree(h->work_mem);
+}
+
+ft_status_t allocate(ft_attn *h) {
+  const ft_attn_config_t &c = h->cfg;
+  FA_CUDA(cudaDeviceGetAttribute(&h->sm_count, cudaDevAttrMultiProcessorCount, c.device));
+  AttnGeom &g = h->geom;
+  g.group = c.n_q_heads / c.n_kv_heads;
+  g.n_kv = c.n_kv_heads;
+  g.window = c.window;
+  g.tile_tokens = 2 * (kTileRows / g.group);
+  g.dec_grid = g.tile_grid = h->sm_count < kAttnMaxGrid ? h->sm_count : kAttnMaxGrid;
+  g.dec_min_quota = 1;
+  g.tile_min_quota = 1;
+  g.tile_cap = c.max_tokens / g.tile_tokens + c.max_requests;
+  auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
+  const size_t n_dec = up(sizeof(AttnEntry) * (size_t)c.max_requests), n_tile = up(sizeof(AttnEntry) * (size_t)g.tile_cap);
+  const size_t n_start = up(sizeof(int4) * kAttnMaxGrid), total = 256 + n_dec + n_tile + 2 * n_start;
+  FA_CUDA(cudaMalloc(&h->work_mem, total));
+  FA_CUDA(cudaMemset(h->work_mem, 0, total));
+  FA_CUDA(cudaMalloc(&h->status_dev, 256));
+  FA_CUDA(cudaMemset(h->status_dev, 0, 256));
+  uint8_t *b = h->work_mem;
+  h->work.hdr = reinterpret_cast<AttnPlanHdr *>(b); b += 256;
+  h->work.dec = reinterpret_cast<AttnEntry *>(b); b += n_dec;
+  h->work.tile = reinterpret_cast<AttnEntry *>(b); b += n_tile;
+  h->work.dec_start = reinterpret_cast<int4 *>(b); b += n_start;
+  h->work.tile_start = reinterpret_cast<int4 *>(b);
+  FA_CUDA(cudaDeviceSynchronize());
+  return FT_OK;
+}
+
+bool step_ok(const ft_attn *h, int n_req, int T, int max_new) {
+  return n_req >= 0 && n_req <= h->cfg.max_requests && T >= 0 && T <= h->cfg.max_tokens && max_new >= 0 && max_new <= T;
+}
+
+ft_status_t launch_slots(ft_attn *h, AttnSlotsArgs &a, cudaStream_t st) {
+  a.max_pages = h->cfg.max_pages;
+  a.n_pages = h->cfg.n_pages;
+  a.page_shift = h->page_shift;
+  a.w = h->work;
+  a.g = h->geom;
+  a.status = h->status_dev;
+  // block 0 keeps the requests and the work partition; the others share the tokens and pages, 2048 tokens each
+  const int grid = a.own_tables ? 1 : 2 + (a.T - 1) / 2048;
+  if (a.n_req <= 256) attn_slots_kernel<256><<<grid, 256, 0, st>>>(a);
+  else attn_slots_kernel<1024><<<grid, 1024, 0, st>>>(a);
+  h->launches += 1;
+  FA_CUDA(cudaGetLastError());
+  h->planned = true;
+  h->n_req = a.n_req; h->T = a.T; h->max_new = a.max_new;
+  return FT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ft_attn_cache_bytes(const ft_attn_config_t *cfg) {
+  if (check_config(cfg) != FT_OK) return 0;
+  return (size_t)cfg->n_pages * 2 * cfg->n_kv_heads * cfg->page_tokens * cfg->head_dim * 2;
+}
+
+const char *ft_attn_last_cuda_error(void) { return cudaGetErrorString(g_attn_cuda_error); }
+
+ft_status_t ft_attn_create(const ft_attn_config_t *cfg, ft_attn_t **out) {
+  if (!out) return FT_ERR_INVALID_ARG;
+  *out = nullptr;
+  ft_status_t rc = check_config(cfg);
+  if (rc != FT_OK) return rc;
+  DeviceScope dev(cfg->device);
+  FA_CUDA(dev.err);
+  ft_attn *h = new (std::nothrow) ft_attn();
+  if (!h) return FT_ERR_OOM;
+  h->cfg = *cfg;
+  h->page_shift = cfg->page_tokens == 16 ? 4 : cfg->page_tokens == 32 ? 5 : cfg->page_tokens == 64 ? 6 : 7;
+  rc = allocate(h);
+  if (rc != FT_OK) {
+    free_all(h);
+    delete h;
+    return rc;
+  }
+  *out = h;
+  return FT_OK;
+}
+
+ft_status_t ft_attn_destroy(ft_attn_t *h) {
+  if (!h) return FT_OK;
+  DeviceScope dev(h->cfg.device);
+  cudaError_t e = cudaDeviceSynchronize();
+  free_all(h);
+  delete h;
+  FA_CUDA(e);
+  return FT_OK;
+}
+
+ft_status_t ft_attn_slots(ft_attn_t *h, int n_req, int T, int max_new, const int32_t *new_len, const int32_t *ctx_len,
+                          int32_t *table, int64_t table_stride, int32_t *free_pages, const int32_t *n_free,
+                          int32_t *q_start, int32_t *kv_len, int32_t *n_free_out, int32_t *admitted, int32_t *position,
+                          int32_t *slot, void *stream) {
+  if (!h || !step_ok(h, n_req, T, max_new)) return FT_ERR_INVALID_ARG;
+  if (!new_len || !ctx_len || !table || !free_pages || !n_free || !q_start || !kv_len || !n_free_out || !admitted ||
+      (T > 0 && (!position || !slot)))
+    return FT_ERR_INVALID_ARG;
+  if (table_stride < h->cfg.max_pages || n_free_out == n_free || kv_len == ctx_len) return FT_ERR_INVALID_ARG;
+  DeviceScope dev(h->cfg.device);
+  FA_CUDA(dev.err);
+  AttnSlotsArgs a;
+  memset(&a, 0, sizeof(a));
+  a.n_req = n_req; a.T = T; a.max_new = max_new;
+  a.new_len = new_len; a.ctx_len = ctx_len; a.table = table; a.table_stride = table_stride;
+  a.free_pages = free_pages; a.n_free = n_free; a.q_start = q_start; a.kv_len = kv_len; a.n_free_out = n_free_out;
+  a.admitted = admitted; a.position = position; a.slot = slot;
+  return launch_slots(h, a, static_cast<cudaStream_t>(stream));
+}
+
+ft_status_t ft_attn_plan(ft_attn_t *h, int n_req, int T, int max_new, const int32_t *q_start, const int32_t *kv_len,
+                         void *stream) {
+  if (!h || !step_ok(h, n_req, T, max_new) || (n_req > 0 && (!q_start || !kv_len))) return FT_ERR_INVALID_ARG;
+  DeviceScope dev(h->cfg.device);
+  FA_CUDA(dev.err);
+  AttnSlotsArgs a;
+  memset(&a, 0, sizeof(a));
+  a.n_req = n_req; a.T = T; a.max_new = max_new; a.own_tables = 1;
+  a.q_start_in = q_start; a.kv_len_in = kv_len;
+  return launch_slots(h, a, static_cast<cudaStream_t>(stream));
+}
+
+ft_status_t ft_attn_qk_rope(ft_attn_t *h, int T, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                            const void *v, int64_t v_stride, const void *w_q, const void *w_k, float eps,
+                            const float *cos_sin, int max_pos, int rot_dim, int interleaved, const int32_t *position,
+                            const int32_t *slot, void *q_out, int64_t q_out_stride, void *kv_cache, void *stream) {
+  if (!h || T < 0 || T > h->cfg.max_tokens) return FT_ERR_INVALID_ARG;
+  if (T == 0) return FT_OK;
+  const ft_attn_config_t &c = h->cfg;
+  const int D = c.head_dim;
+  if (!q || !k || !v || !q_out || !kv_cache || !position || !slot) return FT_ERR_INVALID_ARG;
+  if (rot_dim < 0 || rot_dim > D || rot_dim % 8 || (rot_dim > 0 && (!cos_sin || max_pos < 1))) return FT_ERR_INVALID_ARG;
+  if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)w_q | (uintptr_t)w_k | (uintptr_t)q_out) & 7) return FT_ERR_INVALID_ARG;
+  if (((uintptr_t)kv_cache | (uintptr_t)cos_sin) & 15) return FT_ERR_INVALID_ARG;
+  if (q_stride < (int64_t)c.n_q_heads * D || q_out_stride < (int64_t)c.n_q_heads * D || k_stride < (int64_t)c.n_kv_heads * D ||
+      v_stride < (int64_t)c.n_kv_heads * D || ((q_stride | k_stride | v_stride | q_out_stride) & 3))
+    return FT_ERR_INVALID_ARG;
+  if (!(eps >= 0.f)) return FT_ERR_INVALID_ARG;
+  DeviceScope dev(c.device);
+  FA_CUDA(dev.err);
+  RopeArgs a;
+  a.T = T; a.n_q = c.n_q_heads; a.n_kv = c.n_kv_heads; a.page_shift = h->page_shift; a.n_pages = c.n_pages;
+  a.rot_half = rot_dim / 2; a.interleaved = interleaved ? 1 : 0; a.max_pos = max_pos;
+  a.q = static_cast<const uint16_t *>(q); a.k = static_cast<const uint16_t *>(k); a.v = static_cast<const uint16_t *>(v);
+  a.w_q = static_cast<const uint16_t *>(w_q); a.w_k = static_cast<const uint16_t *>(w_k);
+  a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride; a.out_stride = q_out_stride;
+  a.eps = eps; a.cos_sin = cos_sin; a.position = position; a.slot = slot;
+  a.q_out = static_cast<uint16_t *>(q_out); a.cache = static_cast<uint16_t *>(kv_cache);
+  a.status = h->status_dev;
+  a.heads_per_group = 4;
+  const int heads = a.n_q + 2 * a.n_kv, parts = (heads + a.heads_per_group - 1) / a.heads_per_group;
+  const long long threads = (long long)T * parts * (D / 8);
+  const unsigned grid = (unsigned)((threads + 255) / 256);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool bf = c.dtype == FT_ATTN_BF16;
+  if (D == 128) {
+    if (bf) attn_rope_kernel<128, true><<<grid, 256, 0, st>>>(a); else attn_rope_kernel<128, false><<<grid, 256, 0, st>>>(a);
+  } else {
+    if (bf) attn_rope_kernel<64, true><<<grid, 256, 0, st>>>(a); else attn_rope_kernel<64, false><<<grid, 256, 0, st>>>(a);
+  }
+  h->launches += 1;
+  FA_CUDA(cudaGetLastError());
+  return FT_OK;
+}
+
+ft_status_t ft_attn_forward(ft_attn_t *h, const void *q, int64_t q_stride, const void *kv_cache, const int32_t *table,
+                            int64_t table_stride, void *out, int64_t out_stride, float *lse, float scale, void *stream) {
+  if (!h) return FT_ERR_INVALID_ARG;
+  if (!h->planned) return FT_ERR_STATE;
+  if (h->n_req == 0 || h->T == 0 || h->max_new == 0) return FT_OK;
+  const ft_attn_config_t &c = h->cfg;
+  const int D = c.head_dim;
+  if (!q || !kv_cache || !table || !out) return FT_ERR_INVALID_ARG;
+  if (((uintptr_t)q | (uintptr_t)kv_cache | (uintptr_t)out) & 15) return FT_ERR_INVALID_ARG;
+  if (q_stride < (int64_t)c.n_q_heads * D || out_stride < (int64_t)c.n_q_heads * D || ((q_stride | out_stride) & 7) ||
+      table_stride < c.max_pages || !(scale == scale))
+    return FT_ERR_INVALID_ARG;
+  DeviceScope dev(c.device);
+  FA_CUDA(dev.err);
+  AttnFwdArgs a;
+  a.w = h->work; a.n_q = c.n_q_heads; a.n_kv = c.n_kv_heads; a.page_shift = h->page_shift; a.n_pages = c.n_pages;
+  a.max_pages = c.max_pages; a.window = c.window;
+  a.q = static_cast<const uint16_t *>(q); a.cache = static_cast<const uint16_t *>(kv_cache);
+  a.q_stride = q_stride; a.out_stride = out_stride; a.table_stride = table_stride; a.table = table;
+  a.out = static_cast<uint16_t *>(out); a.lse = lse; a.scale = scale; a.status = h->status_dev;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool bf = c.dtype == FT_ATTN_BF16;
+  for (int tiled = 0; tiled < 2; ++tiled) {
+    if (tiled && h->max_new * h->geom.group <= kDecRows) break;
+    const int grid = h->sm_count * 4;
+    if (D == 128) {
+      if (bf) attn_simple_kernel<128, true><<<grid, 256, 0, st>>>(a, tiled); else attn_simple_kernel<128, false><<<grid, 256, 0, st>>>(a, tiled);
+    } else {
+      if (bf) attn_simple_kernel<64, true><<<grid, 256, 0, st>>>(a, tiled); else attn_simple_kernel<64, false><<<grid, 256, 0, st>>>(a, tiled);
+    }
+    h->launches += 1;
+    FA_CUDA(cudaGetLastError());
+  }
+  return FT_OK;
+}
+
+ft_status_t ft_attn_sync_status(ft_attn_t *h) {
+  if (!h) return FT_ERR_INVALID_ARG;
+  DeviceScope dev(h->cfg.device);
+  FA_CUDA(dev.err);
+  FA_CUDA(cudaDeviceSynchronize());
+  uint32_t st = 0;
+  FA_CUDA(cudaMemcpy(&st, h->status_dev, sizeof(st), cudaMemcpyDeviceToHost));
+  if (!st) return FT_OK;
+  FA_CUDA(cudaMemset(h->status_dev, 0, sizeof(st)));
+  FA_CUDA(cudaDeviceSynchronize());
+  if (st & kStatTimeout) return FT_ERR_TIMEOUT;
+  return (st & kStatBadIndex) ? FT_ERR_INVALID_ARG : FT_ERR_CUDA;
+}
+
+ft_status_t ft_attn_launch_count(ft_attn_t *h, uint64_t *out) {
+  if (!h || !out) return FT_ERR_INVALID_ARG;
+  *out = h->launches;
+  return FT_OK;
+}
+
+}  // extern "C"
