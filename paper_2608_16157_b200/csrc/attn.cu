@@ -9,6 +9,7 @@
 
 #include "attn_plan.cuh"
 #include "attn_rope.cuh"
+#include "attn_stream.cuh"
 #include "attn_simple.cuh"
 
 using namespace ftmoe;
@@ -20,6 +21,10 @@ struct ft_attn {
   uint8_t *work_mem = nullptr;     // the work partition, one allocation
   AttnWork work;
   AttnGeom geom;
+  float *part = nullptr;           // partial results of requests that several CTAs share
+  uint32_t *arrive = nullptr;      // their arrival counters
+  size_t arrive_bytes = 0;
+  void *encode = nullptr;          // cuTensorMapEncodeTiled
   bool planned = false;
   int n_req = 0, T = 0, max_new = 0;   // of the latest slots / plan call
   uint64_t launches = 0;
@@ -74,6 +79,50 @@ struct DeviceScope {
 void free_all(ft_attn *h) {
   (void)cudaFree(h->status_dev);
   (void)cudaFree(h->work_mem);
+  (void)cudaFree(h->part);
+  (void)cudaFree(h->arrive);
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// 16-bit elements, 128-byte swizzle: `rank` dimensions from the innermost, strides in elements.
+bool make_map(const ft_attn *h, CUtensorMap *tm, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *stride_elems,
+              const cuuint32_t *box) {
+  cuuint64_t strides[4];
+  const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
+  for (int i = 0; i + 1 < rank; ++i) strides[i] = stride_elems[i] * 2;
+  return reinterpret_cast<EncodeTiledFn>(h->encode)(tm, CU_TENSOR_MAP_DATA_TYPE_UINT16, rank, const_cast<void *>(base), dims, strides, box,
+                                                    ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The cache of a layer as [(page, keys or values, head)][tokens of the page][D]; a box is 64 elements of up to 64 tokens.
+bool make_cache_map(const ft_attn *h, CUtensorMap *tm, const void *cache) {
+  const ft_attn_config_t &c = h->cfg;
+  const cuuint64_t dims[3] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page_tokens, (cuuint64_t)c.n_pages * 2 * c.n_kv_heads};
+  const cuuint64_t strides[2] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page_tokens * c.head_dim};
+  const cuuint32_t box[3] = {64, (cuuint32_t)(c.page_tokens < kDecKeys ? c.page_tokens : kDecKeys), 1};
+  return make_map(h, tm, cache, 3, dims, strides, box);
+}
+
+template <int D>
+cudaError_t allow_smem() {
+  cudaError_t e = cudaFuncSetAttribute(attn_stream_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, StreamCfg<D>::kSmem);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(attn_stream_kernel<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, StreamCfg<D>::kSmem);
+  return e;
+}
+
+template <int D, bool BF16>
+void launch_forward(ft_attn *h, const CUtensorMap &tm, const AttnFwdArgs &a, cudaStream_t st) {
+  attn_stream_kernel<D, BF16><<<h->geom.dec_grid, kStreamThreads, StreamCfg<D>::kSmem, st>>>(tm, a);
+  h->launches += 1;
+  if (h->max_new * h->geom.group > kDecRows) {
+    attn_simple_kernel<D, BF16><<<h->sm_count * 4, 256, 0, st>>>(a);
+    h->launches += 1;
+  }
 }
 
 ft_status_t allocate(ft_attn *h) {
@@ -101,6 +150,16 @@ ft_status_t allocate(ft_attn *h) {
   h->work.tile = reinterpret_cast<AttnEntry *>(b); b += n_tile;
   h->work.dec_start = reinterpret_cast<int4 *>(b); b += n_start;
   h->work.tile_start = reinterpret_cast<int4 *>(b);
+  const size_t part = (size_t)g.dec_grid * 2 * (c.head_dim == 128 ? StreamCfg<128>::kPart : StreamCfg<64>::kPart) * sizeof(float);
+  FA_CUDA(cudaMalloc(&h->part, part));
+  h->arrive_bytes = (size_t)c.max_requests * c.n_kv_heads * sizeof(uint32_t);
+  FA_CUDA(cudaMalloc(&h->arrive, h->arrive_bytes));
+  FA_CUDA(cudaMemset(h->arrive, 0, h->arrive_bytes));
+  FA_CUDA(allow_smem<64>());
+  FA_CUDA(allow_smem<128>());
+  cudaDriverEntryPointQueryResult qres;
+  FA_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &h->encode, cudaEnableDefault, &qres));
+  if (!h->encode || qres != cudaDriverEntryPointSuccess) return FT_ERR_CUDA;
   FA_CUDA(cudaDeviceSynchronize());
   return FT_OK;
 }
@@ -259,24 +318,22 @@ ft_status_t ft_attn_forward(ft_attn_t *h, const void *q, int64_t q_stride, const
   DeviceScope dev(c.device);
   FA_CUDA(dev.err);
   AttnFwdArgs a;
-  a.w = h->work; a.n_q = c.n_q_heads; a.n_kv = c.n_kv_heads; a.page_shift = h->page_shift; a.n_pages = c.n_pages;
-  a.max_pages = c.max_pages; a.window = c.window;
+  a.w = h->work; a.n_q = c.n_q_heads; a.n_kv = c.n_kv_heads; a.group = h->geom.group; a.page_shift = h->page_shift;
+  a.n_pages = c.n_pages; a.window = c.window;
   a.q = static_cast<const uint16_t *>(q); a.cache = static_cast<const uint16_t *>(kv_cache);
   a.q_stride = q_stride; a.out_stride = out_stride; a.table_stride = table_stride; a.table = table;
-  a.out = static_cast<uint16_t *>(out); a.lse = lse; a.scale = scale; a.status = h->status_dev;
+  a.out = static_cast<uint16_t *>(out); a.lse = lse; a.scale_log2 = scale * 1.44269504088896f;
+  a.part = h->part; a.arrive = h->arrive; a.status = h->status_dev;
+  CUtensorMap tm;
+  if (!make_cache_map(h, &tm, kv_cache)) return FT_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool bf = c.dtype == FT_ATTN_BF16;
-  for (int tiled = 0; tiled < 2; ++tiled) {
-    if (tiled && h->max_new * h->geom.group <= kDecRows) break;
-    const int grid = h->sm_count * 4;
-    if (D == 128) {
-      if (bf) attn_simple_kernel<128, true><<<grid, 256, 0, st>>>(a, tiled); else attn_simple_kernel<128, false><<<grid, 256, 0, st>>>(a, tiled);
-    } else {
-      if (bf) attn_simple_kernel<64, true><<<grid, 256, 0, st>>>(a, tiled); else attn_simple_kernel<64, false><<<grid, 256, 0, st>>>(a, tiled);
-    }
-    h->launches += 1;
-    FA_CUDA(cudaGetLastError());
+  if (D == 128) {
+    if (bf) launch_forward<128, true>(h, tm, a, st); else launch_forward<128, false>(h, tm, a, st);
+  } else {
+    if (bf) launch_forward<64, true>(h, tm, a, st); else launch_forward<64, false>(h, tm, a, st);
   }
+  FA_CUDA(cudaGetLastError());
   return FT_OK;
 }
 
@@ -290,7 +347,11 @@ ft_status_t ft_attn_sync_status(ft_attn_t *h) {
   if (!st) return FT_OK;
   FA_CUDA(cudaMemset(h->status_dev, 0, sizeof(st)));
   FA_CUDA(cudaDeviceSynchronize());
-  if (st & kStatTimeout) return FT_ERR_TIMEOUT;
+  if (st & kStatTimeout) {      // a call that gave up may have left arrivals behind
+    FA_CUDA(cudaMemset(h->arrive, 0, h->arrive_bytes));
+    FA_CUDA(cudaDeviceSynchronize());
+    return FT_ERR_TIMEOUT;
+  }
   return (st & kStatBadIndex) ? FT_ERR_INVALID_ARG : FT_ERR_CUDA;
 }
 

@@ -1,30 +1,17 @@
 // Attention of the packed query rows over the paged cache, the plain form: one warp per (row, query head), one key at a
 // time, running maximum and sum.  Right for every case; every key is read once per query head and row.
 #pragma once
-#include "attn_plan.cuh"
-#include "attn_rope.cuh"
+#include "attn_stream.cuh"
 
 namespace ftmoe {
 
-struct AttnFwdArgs {
-  AttnWork w;
-  int32_t n_q, n_kv, page_shift, n_pages, max_pages, window;
-  const uint16_t *q, *cache;
-  long long q_stride, out_stride, table_stride;
-  const int32_t *table;
-  uint16_t *out;
-  float *lse;
-  float scale;
-  uint32_t *status;
-};
-
 template <int D, bool BF16>
-__global__ void __launch_bounds__(256) attn_simple_kernel(const AttnFwdArgs a, int tiled) {
+__global__ void __launch_bounds__(256) attn_simple_kernel(const AttnFwdArgs a) {
   constexpr int E = D / 32;
   const int lane = threadIdx.x & 31;
   const AttnPlanHdr hdr = *a.w.hdr;
-  const int n = tiled ? hdr.n_tile : hdr.n_dec;
-  const AttnEntry *list = tiled ? a.w.tile : a.w.dec;
+  const int n = hdr.n_tile;
+  const AttnEntry *list = a.w.tile;
   auto tof = [](uint16_t b) { return BF16 ? __uint_as_float((uint32_t)b << 16) : __half2float(__ushort_as_half(b)); };
   for (int ei = blockIdx.x; ei < n; ei += gridDim.x) {
     const AttnEntry e = list[ei];
@@ -33,7 +20,7 @@ __global__ void __launch_bounds__(256) attn_simple_kernel(const AttnFwdArgs a, i
       const uint16_t *q = a.q + (long long)(e.tok0 + i) * a.q_stride + h * D;
       float qv[E], o[E], m = -INFINITY, l = 0.f;
 #pragma unroll
-      for (int x = 0; x < E; ++x) { qv[x] = tof(q[x * 32 + lane]) * a.scale; o[x] = 0.f; }
+      for (int x = 0; x < E; ++x) { qv[x] = tof(q[x * 32 + lane]) * (a.scale_log2 * 0.693147180559945f); o[x] = 0.f; }
       const int lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
       for (int j = lo; j <= pos; ++j) {
         const int page = a.table[e.req * a.table_stride + (j >> a.page_shift)];

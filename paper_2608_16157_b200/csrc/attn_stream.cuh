@@ -1,0 +1,363 @@
+// Attention of requests with few query rows (n tokens x Hq/Hkv heads <= 16: single tokens, short drafts) over the paged
+// cache.  Every key and value is needed once per 16 rows and used for 4*16*D flops per 4*D bytes: bound by HBM.
+//
+// The key blocks (64 keys) of all requests and key/value heads form one flat list that is cut into equal shares, one
+// CTA per SM (the work partition of attn_plan.cuh), so the cache streams at an even rate whatever the lengths are.  A
+// producer warp brings a block's pages with TMA tile loads (128-byte swizzle) into a ring of 160 KB; the four consumer
+// warps take 16 keys each of every block: S = Q K^T and O += P V with mma.sync m16n8k16 (the rows on M), the running maximum
+// m and sum l of every row per warp:
+//   m' = max(m, max_j s_j),  l' = l 2^(m-m') + sum_j 2^(s_j-m'),  O' = O 2^(m-m') + sum_j 2^(s_j-m') v_j,  s in units of log2
+// P is rounded to the values' type for the second product (relative 2^-9 of each weight on average, below the rounding of
+// the result); l sums the unrounded weights; everything else stays in 32 bits.
+// At the end of a (request, head) the warps' (m, l, O) are joined in shared memory.  A request that was cut leaves its
+// parts in global memory; the CTA that arrives last (a counter per request and head) joins them in the order of the
+// CTAs, so results do not depend on who is last.
+// Values that no row attends to (behind the last token, before a window) are zeroed in shared memory before use: their
+// weights are 0, but what stands there may be NaN.
+#pragma once
+#include "attn_plan.cuh"
+#include "attn_rope.cuh"
+#include "tcgen.cuh"
+
+namespace ftmoe {
+
+struct AttnFwdArgs {
+  AttnWork w;
+  int32_t n_q, n_kv, group, page_shift, n_pages, window;
+  const uint16_t *q, *cache;
+  long long q_stride, out_stride, table_stride;
+  const int32_t *table;
+  uint16_t *out;
+  float *lse;
+  float scale_log2;       // scale * log2(e)
+  float *part;            // partial results of cut requests
+  uint32_t *arrive;       // arrival counters, zero between launches
+  uint32_t *status;
+};
+
+constexpr int kStreamWarps = 4, kStreamThreads = (kStreamWarps + 1) * 32;
+template <int D> struct StreamCfg {
+  static constexpr int kHalf = kDecKeys * D * 2;            // bytes of the keys (or values) of a block
+  static constexpr int kStage = 2 * kHalf;
+  static constexpr int kStages = D == 128 ? 5 : 10;
+  static constexpr int kRow = D + 8;                        // floats per row of the join buffer (bank-conflict free)
+  static constexpr int kJoin = kStreamWarps * kDecRows * kRow * 4;
+  static constexpr int kSmem = 1024 + kStages * kStage + kJoin + kStreamWarps * kDecRows * 8 + 2 * kStages * 8 + 64;
+  static constexpr int kPart = kDecRows * (D + 2);          // floats of one partial result: m[16], l[16], O[16][D]
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+template <bool BF16>
+__device__ __forceinline__ void mma_16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if (BF16)
+    mma_bf16(c, a[0], a[1], a[2], a[3], b0, b1);
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr));
+}
+__device__ __forceinline__ void named_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kStreamThreads, 1)
+attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) {
+  using Cfg = StreamCfg<D>;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  float *s_join = reinterpret_cast<float *>(smem + Cfg::kStages * Cfg::kStage);
+  float *s_ml = s_join + Cfg::kJoin / 4;                                  // [warp][16][m, l]
+  uint64_t *s_bar = reinterpret_cast<uint64_t *>(s_ml + kStreamWarps * kDecRows * 2);
+  volatile int *s_abort = reinterpret_cast<volatile int *>(s_bar + 2 * Cfg::kStages);
+  volatile int *s_last = s_abort + 1;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t ring = smem_u32(smem), bars = smem_u32(s_bar);
+  auto full_bar = [&](int s) { return bars + 8u * s; };
+  auto empty_bar = [&](int s) { return bars + 8u * (Cfg::kStages + s); };
+
+  const AttnPlanHdr hdr = *a.w.hdr;
+  const long long u_first = (long long)blockIdx.x * hdr.dec_quota;
+  if (u_first >= hdr.dec_units) return;
+  int left = (int)min((long long)hdr.dec_quota, hdr.dec_units - u_first);
+  const int4 st = a.w.dec_start[blockIdx.x];
+  if (tid == 0) {
+    for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), kStreamWarps); }
+    *s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  __syncthreads();
+
+  const int page_tokens = 1 << a.page_shift;
+  const int box_rows = min(page_tokens, kDecKeys), boxes = kDecKeys / box_rows;   // boxes of a block along its keys
+  int k = st.x, head = st.y, blk = st.z;
+  uint32_t it = 0;      // blocks of this CTA so far
+
+  if (warp == kStreamWarps) {
+    // ------------------------------ producer ------------------------------
+    // lane -> (box along the keys, 64-element chunk of D, keys or values)
+    constexpr int kChunks = D / 64;
+    const int per_box = 2 * kChunks;
+    const int bx = lane / per_box, ch = (lane % per_box) >> 1, is_v = lane & 1;
+    const bool owner = bx < boxes;
+    while (left > 0) {
+      const AttnEntry e = a.w.dec[k];
+      const int take = min(left, e.nb - blk);
+      const int hi = max(0, e.pos0 + e.n_tok), lo = a.window > 0 ? max(0, e.pos0 - a.window + 1) : 0;
+      const int32_t *row = a.table + (long long)e.req * a.table_stride;
+      auto page_of = [&](int b) -> int {       // page of this lane's box of block b, -1: nothing to load
+        const int key = (e.b0 + b) * kDecKeys + bx * box_rows;
+        if (!owner || key >= hi || key + box_rows <= lo) return -1;
+        return row[key >> a.page_shift];
+      };
+      int page = page_of(blk);
+      for (int b = blk; b < blk + take; ++b, ++it) {
+        const int next = b + 1 < blk + take ? page_of(b + 1) : -1;
+        const int key = (e.b0 + b) * kDecKeys + bx * box_rows;
+        const bool want = owner && key < hi && key + box_rows > lo;
+        if (want && (uint32_t)page >= (uint32_t)a.n_pages) {     // never followed: page 0 instead, and reported
+          atomicOr(a.status, kStatBadIndex);
+          page = 0;
+        }
+        const int s = it % Cfg::kStages;
+        mbar_wait(empty_bar(s), ((it / Cfg::kStages) & 1u) ^ 1u, s_abort, a.status);
+        if (*s_abort) break;
+        const uint32_t n = __popc(__ballot_sync(0xffffffffu, want));
+        if (lane == 0) mbar_expect_tx(full_bar(s), n * (uint32_t)(box_rows * 128));
+        __syncwarp();
+        if (want)
+          tma_load_3d(ring + s * Cfg::kStage + is_v * Cfg::kHalf + ch * (kDecKeys * 128) + bx * box_rows * 128, &tm, ch * 64,
+                      key & (page_tokens - 1), (page * 2 + is_v) * a.n_kv + head, full_bar(s));
+        page = next;
+      }
+      if (*s_abort) break;
+      left -= take;
+      blk = 0;
+      if (++head == a.n_kv) { head = 0; ++k; }
+    }
+    // copies of a CTA that gave up must land before its shared memory goes away
+    abort_drain(s_abort);
+    return;
+  }
+
+  // ------------------------------ consumers ------------------------------
+  const int g = lane >> 2, t4 = lane & 3;
+  const int key0 = warp * 16;                   // this warp's keys of a block
+  while (left > 0) {
+    const AttnEntry e = a.w.dec[k];
+    const int take = min(left, e.nb - blk);
+    const int hi = max(0, e.pos0 + e.n_tok), lo = a.window > 0 ? max(0, e.pos0 - a.window + 1) : 0;
+    const int rows = e.n_tok * a.group;
+    // query fragments: row r = token r / group, head of the group r % group
+    uint32_t q[D / 16][4];
+    int pos[2];
+    {
+      const uint16_t *qp[2];
+      bool ok[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = g + 8 * i, tok = r / a.group;
+        ok[i] = r < rows;
+        pos[i] = ok[i] ? e.pos0 + tok : -1;
+        qp[i] = a.q + (long long)(e.tok0 + (ok[i] ? tok : 0)) * a.q_stride + (head * a.group + (ok[i] ? r - tok * a.group : 0)) * D;
+      }
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          q[kk][i] = ok[i & 1] ? *reinterpret_cast<const uint32_t *>(qp[i & 1] + kk * 16 + (i >> 1) * 8 + t4 * 2) : 0u;
+    }
+    float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
+
+    for (int b = blk; b < blk + take; ++b, ++it) {
+      const int s = it % Cfg::kStages;
+      const bool ok = mbar_wait(full_bar(s), (it / Cfg::kStages) & 1u, s_abort, a.status);
+      const uint32_t kt = ring + s * Cfg::kStage, vt = kt + Cfg::kHalf;
+      const int base = (e.b0 + b) * kDecKeys + key0;                    // position of this warp's first key
+      if (ok && base < hi && base + 16 > lo) {
+        const bool edge = base + 16 > hi || base < lo;
+        if (edge) {
+#pragma unroll 1
+          for (int i = lane; i < 16 * (D / 8); i += 32) {
+            const int r = i / (D / 8), c = i % (D / 8), key = base + r;
+            if (key >= hi || key < lo)
+              asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(vt + (c >> 3) * (kDecKeys * 128) + (key0 + r) * 128 +
+                                                                        (((c & 7) ^ (r & 7)) << 4)),
+                           "r"(0u)
+                           : "memory");
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before the ring's next copy into these rows
+          __syncwarp();
+        }
+        // S: two 8-key tiles, each as two chains over D
+        float sc[2][2][4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) sc[i][j][x] = 0.f;
+        {
+          // matrices of an ldmatrix: (keys 0-7, d 0-7), (keys 0-7, d 8-15), (keys 8-15, d 0-7), (keys 8-15, d 8-15)
+          const int r = (lane & 7) + ((lane >> 4) << 3), cj = (lane >> 3) & 1;
+          const uint32_t ra = kt + (key0 + r) * 128;
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            uint32_t bm[4];
+            ldmatrix_x4(bm, ra + (kk >> 2) * (kDecKeys * 128) + ((((kk & 3) * 2 + cj) ^ (r & 7)) << 4));
+            mma_16<BF16>(sc[0][kk & 1], q[kk], bm[0], bm[1]);
+            mma_16<BF16>(sc[1][kk & 1], q[kk], bm[2], bm[3]);
+          }
+        }
+        float sv[2][4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) sv[i][x] = (sc[i][0][x] + sc[i][1][x]) * a.scale_log2;
+        if (base + 15 > e.pos0 || (a.window > 0 && base <= e.pos0 + e.n_tok - 1 - a.window)) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const int key = base + i * 8 + t4 * 2 + (x & 1), p = pos[x >> 1];
+              if (key > p || (a.window > 0 && key <= p - a.window)) sv[i][x] = -INFINITY;
+            }
+        }
+        uint32_t pa[4];
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2) {
+          float mx = fmaxf(fmaxf(sv[0][2 * h2], sv[0][2 * h2 + 1]), fmaxf(sv[1][2 * h2], sv[1][2 * h2 + 1]));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+          const float mn = fmaxf(m[h2], mx), base_m = mn == -INFINITY ? 0.f : mn;
+          const float f = ex2(m[h2] - base_m);
+          if (__any_sync(0xffffffffu, mn != m[h2])) {
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) { o[i][2 * h2] *= f; o[i][2 * h2 + 1] *= f; }
+            l[h2] *= f;
+          }
+          m[h2] = mn;
+          const float p0 = ex2(sv[0][2 * h2] - base_m), p1 = ex2(sv[0][2 * h2 + 1] - base_m);
+          const float p2 = ex2(sv[1][2 * h2] - base_m), p3 = ex2(sv[1][2 * h2 + 1] - base_m);
+          l[h2] += (p0 + p1) + (p2 + p3);
+          pa[h2] = pack_pair<BF16>(p0, p1);
+          pa[2 + h2] = pack_pair<BF16>(p2, p3);
+        }
+        {
+          // matrices: (keys 0-7, d 0-7), (keys 8-15, d 0-7), (keys 0-7, d 8-15), (keys 8-15, d 8-15), transposed
+          const int r = lane & 15, cj = lane >> 4;
+          const uint32_t ra = vt + (key0 + r) * 128;
+#pragma unroll
+          for (int nn = 0; nn < D / 16; ++nn) {
+            uint32_t bm[4];
+            ldmatrix_x4_trans(bm, ra + (nn >> 2) * (kDecKeys * 128) + ((((nn & 3) * 2 + cj) ^ (r & 7)) << 4));
+            mma_16<BF16>(o[2 * nn], pa, bm[0], bm[1]);
+            mma_16<BF16>(o[2 * nn + 1], pa, bm[2], bm[3]);
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(empty_bar(s));
+    }
+
+    // join the warps: (m, l) and O of every row
+#pragma unroll
+    for (int h2 = 0; h2 < 2; ++h2) {
+      l[h2] += __shfl_xor_sync(0xffffffffu, l[h2], 1);
+      l[h2] += __shfl_xor_sync(0xffffffffu, l[h2], 2);
+      if (t4 == 0) {
+        s_ml[(warp * kDecRows + g + 8 * h2) * 2] = m[h2];
+        s_ml[(warp * kDecRows + g + 8 * h2) * 2 + 1] = l[h2];
+      }
+      float *dst = s_join + (warp * kDecRows + g + 8 * h2) * Cfg::kRow + t4 * 2;
+      if (g + 8 * h2 < rows)
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) *reinterpret_cast<float2 *>(dst + i * 8) = make_float2(o[i][2 * h2], o[i][2 * h2 + 1]);
+    }
+    named_sync(1, kStreamWarps * 32);
+    const int u0 = e.unit0 * a.n_kv + head * e.nb;
+    const int c_first = u0 / hdr.dec_quota, c_last = (u0 + e.nb - 1) / hdr.dec_quota;
+    const bool whole = c_first == c_last;
+    constexpr int kCols = D / 4;                       // a thread owns 4 columns of every (128 / kCols)-th row
+    const int col = (tid % kCols) * 4, row0 = tid / kCols;
+    auto write_row = [&](int r, float mm, float ll, float4 v) {
+      const float inv = ll > 0.f ? 1.f / ll : 0.f;
+      const int tok = r / a.group, hq = head * a.group + r - tok * a.group;
+      const long long t = e.tok0 + tok;
+      *reinterpret_cast<uint2 *>(a.out + t * a.out_stride + hq * D + col) =
+          make_uint2(pack_pair<BF16>(v.x * inv, v.y * inv), pack_pair<BF16>(v.z * inv, v.w * inv));
+      if (a.lse && col == 0) a.lse[t * a.n_q + hq] = ll > 0.f ? (mm + log2f(ll)) * 0.693147180559945f : -INFINITY;
+    };
+    float *part = a.part + (size_t)(blockIdx.x * 2 + (blockIdx.x == c_first ? 1 : 0)) * Cfg::kPart;
+    for (int r = row0; r < rows; r += kStreamWarps * 32 / kCols) {
+      float mm = -INFINITY, ll = 0.f;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kStreamWarps; ++w) mm = fmaxf(mm, s_ml[(w * kDecRows + r) * 2]);
+      const float bm = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+      for (int w = 0; w < kStreamWarps; ++w) {
+        const float f = ex2(s_ml[(w * kDecRows + r) * 2] - bm);
+        const float4 x = *reinterpret_cast<const float4 *>(s_join + (w * kDecRows + r) * Cfg::kRow + col);
+        ll = fmaf(f, s_ml[(w * kDecRows + r) * 2 + 1], ll);
+        v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+      }
+      if (whole) {
+        write_row(r, mm, ll, v);
+      } else {
+        if (col == 0) { part[r] = mm; part[kDecRows + r] = ll; }
+        *reinterpret_cast<float4 *>(part + 2 * kDecRows + r * D + col) = v;
+      }
+    }
+    if (!whole) {
+      __threadfence();
+      named_sync(1, kStreamWarps * 32);
+      if (tid == 0) {
+        uint32_t *cnt = a.arrive + (size_t)k * a.n_kv + head;
+        const uint32_t n = (uint32_t)(c_last - c_first + 1);
+        const bool last = atomicAdd(cnt, 1u) == n - 1;
+        if (last) *cnt = 0u;
+        *s_last = last;
+        __threadfence();
+      }
+      named_sync(1, kStreamWarps * 32);
+      if (*s_last) {
+        for (int r = row0; r < rows; r += kStreamWarps * 32 / kCols) {
+          float mm = -INFINITY, ll = 0.f;
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+          for (int c = c_first; c <= c_last; ++c) {
+            const float *pc = a.part + (size_t)(c * 2 + (c == c_first ? 1 : 0)) * Cfg::kPart;
+            const float mc = __ldcg(pc + r), lc = __ldcg(pc + kDecRows + r);
+            const float4 x = __ldcg(reinterpret_cast<const float4 *>(pc + 2 * kDecRows + r * D + col));
+            const float mn = fmaxf(mm, mc), bm = mn == -INFINITY ? 0.f : mn;
+            const float f0 = ex2(mm - bm), f1 = ex2(mc - bm);
+            ll = ll * f0 + lc * f1;
+            v.x = v.x * f0 + x.x * f1; v.y = v.y * f0 + x.y * f1; v.z = v.z * f0 + x.z * f1; v.w = v.w * f0 + x.w * f1;
+            mm = mn;
+          }
+          write_row(r, mm, ll, v);
+        }
+      }
+    }
+    named_sync(1, kStreamWarps * 32);      // the join buffer is free again
+    left -= take;
+    blk = 0;
+    if (++head == a.n_kv) { head = 0; ++k; }
+  }
+  abort_drain(s_abort);
+}
+
+}  // namespace ftmoe
