@@ -10,7 +10,7 @@
 #include "attn_plan.cuh"
 #include "attn_rope.cuh"
 #include "attn_stream.cuh"
-#include "attn_simple.cuh"
+#include "attn_tile.cuh"
 
 using namespace ftmoe;
 
@@ -21,8 +21,10 @@ struct ft_attn {
   uint8_t *work_mem = nullptr;     // the work partition, one allocation
   AttnWork work;
   AttnGeom geom;
-  float *part = nullptr;           // partial results of requests that several CTAs share
-  uint32_t *arrive = nullptr;      // their arrival counters
+  float *part = nullptr;           // partial results of work items that several CTAs share: streaming kernel, tiled kernel
+  size_t part_tile = 0;            // floats before the second
+  uint32_t *arrive = nullptr;      // their arrival counters, in the same order
+  size_t arrive_tile = 0;
   size_t arrive_bytes = 0;
   void *encode = nullptr;          // cuTensorMapEncodeTiled
   bool planned = false;
@@ -107,22 +109,43 @@ bool make_cache_map(const ft_attn *h, CUtensorMap *tm, const void *cache) {
   return make_map(h, tm, cache, 3, dims, strides, box);
 }
 
-template <int D>
+// The packed queries as [T][key/value head][head of the group][D]; a box is 64 elements of all heads of a group, of the
+// tokens of one 128-row tile.
+bool make_query_map(const ft_attn *h, CUtensorMap *tm, const void *q, int64_t q_stride) {
+  const ft_attn_config_t &c = h->cfg;
+  const cuuint64_t D = c.head_dim, G = h->geom.group;
+  const cuuint64_t dims[4] = {D, G, (cuuint64_t)c.n_kv_heads, (cuuint64_t)h->T};
+  const cuuint64_t strides[3] = {D, G * D, (cuuint64_t)q_stride};
+  const cuuint32_t box[4] = {64, (cuuint32_t)G, 1, (cuuint32_t)(kTileRows / h->geom.group)};
+  return make_map(h, tm, q, 4, dims, strides, box);
+}
+
+template <int D, bool BF16>
 cudaError_t allow_smem() {
-  cudaError_t e = cudaFuncSetAttribute(attn_stream_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, StreamCfg<D>::kSmem);
+  cudaError_t e = cudaFuncSetAttribute(attn_stream_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, StreamCfg<D>::kSmem);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(attn_stream_kernel<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, StreamCfg<D>::kSmem);
+    e = cudaFuncSetAttribute(attn_tile_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, TileCfg<D>::kSmem);
   return e;
 }
 
 template <int D, bool BF16>
-void launch_forward(ft_attn *h, const CUtensorMap &tm, const AttnFwdArgs &a, cudaStream_t st) {
+ft_status_t launch_forward(ft_attn *h, AttnFwdArgs a, const void *cache, cudaStream_t st) {
+  CUtensorMap tm, tm_q;
+  if (!make_cache_map(h, &tm, cache)) return FT_ERR_CUDA;
+  a.part = h->part;
+  a.arrive = h->arrive;
   attn_stream_kernel<D, BF16><<<h->geom.dec_grid, kStreamThreads, StreamCfg<D>::kSmem, st>>>(tm, a);
   h->launches += 1;
+  FA_CUDA(cudaGetLastError());
   if (h->max_new * h->geom.group > kDecRows) {
-    attn_simple_kernel<D, BF16><<<h->sm_count * 4, 256, 0, st>>>(a);
+    if (!make_query_map(h, &tm_q, a.q, a.q_stride)) return FT_ERR_CUDA;
+    a.part = h->part + h->part_tile;
+    a.arrive = h->arrive + h->arrive_tile;
+    attn_tile_kernel<D, BF16><<<h->geom.tile_grid, kTileThreads, TileCfg<D>::kSmem, st>>>(tm_q, tm, a);
     h->launches += 1;
+    FA_CUDA(cudaGetLastError());
   }
+  return FT_OK;
 }
 
 ft_status_t allocate(ft_attn *h) {
@@ -150,13 +173,17 @@ ft_status_t allocate(ft_attn *h) {
   h->work.tile = reinterpret_cast<AttnEntry *>(b); b += n_tile;
   h->work.dec_start = reinterpret_cast<int4 *>(b); b += n_start;
   h->work.tile_start = reinterpret_cast<int4 *>(b);
-  const size_t part = (size_t)g.dec_grid * 2 * (c.head_dim == 128 ? StreamCfg<128>::kPart : StreamCfg<64>::kPart) * sizeof(float);
-  FA_CUDA(cudaMalloc(&h->part, part));
-  h->arrive_bytes = (size_t)c.max_requests * c.n_kv_heads * sizeof(uint32_t);
+  h->part_tile = (size_t)g.dec_grid * 2 * (c.head_dim == 128 ? StreamCfg<128>::kPart : StreamCfg<64>::kPart);
+  const size_t part = h->part_tile + (size_t)g.tile_grid * 4 * (c.head_dim == 128 ? TileCfg<128>::kPart : TileCfg<64>::kPart);
+  FA_CUDA(cudaMalloc(&h->part, part * sizeof(float)));
+  h->arrive_tile = (size_t)c.max_requests * c.n_kv_heads;
+  h->arrive_bytes = (h->arrive_tile + (size_t)g.tile_cap * c.n_kv_heads * 2) * sizeof(uint32_t);
   FA_CUDA(cudaMalloc(&h->arrive, h->arrive_bytes));
   FA_CUDA(cudaMemset(h->arrive, 0, h->arrive_bytes));
-  FA_CUDA(allow_smem<64>());
-  FA_CUDA(allow_smem<128>());
+  FA_CUDA((allow_smem<64, true>()));
+  FA_CUDA((allow_smem<64, false>()));
+  FA_CUDA((allow_smem<128, true>()));
+  FA_CUDA((allow_smem<128, false>()));
   cudaDriverEntryPointQueryResult qres;
   FA_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &h->encode, cudaEnableDefault, &qres));
   if (!h->encode || qres != cudaDriverEntryPointSuccess) return FT_ERR_CUDA;
@@ -322,19 +349,13 @@ ft_status_t ft_attn_forward(ft_attn_t *h, const void *q, int64_t q_stride, const
   a.n_pages = c.n_pages; a.window = c.window;
   a.q = static_cast<const uint16_t *>(q); a.cache = static_cast<const uint16_t *>(kv_cache);
   a.q_stride = q_stride; a.out_stride = out_stride; a.table_stride = table_stride; a.table = table;
-  a.out = static_cast<uint16_t *>(out); a.lse = lse; a.scale_log2 = scale * 1.44269504088896f;
-  a.part = h->part; a.arrive = h->arrive; a.status = h->status_dev;
-  CUtensorMap tm;
-  if (!make_cache_map(h, &tm, kv_cache)) return FT_ERR_CUDA;
+  a.out = static_cast<uint16_t *>(out); a.lse = lse; a.status = h->status_dev;
+  a.scale_log2 = scale * 1.44269504088896f;
+  if (a.scale_log2 == 0.f) a.scale_log2 = 1e-30f;   // equal weights without 0 * infinity in masked places
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool bf = c.dtype == FT_ATTN_BF16;
-  if (D == 128) {
-    if (bf) launch_forward<128, true>(h, tm, a, st); else launch_forward<128, false>(h, tm, a, st);
-  } else {
-    if (bf) launch_forward<64, true>(h, tm, a, st); else launch_forward<64, false>(h, tm, a, st);
-  }
-  FA_CUDA(cudaGetLastError());
-  return FT_OK;
+  if (D == 128) return bf ? launch_forward<128, true>(h, a, kv_cache, st) : launch_forward<128, false>(h, a, kv_cache, st);
+  return bf ? launch_forward<64, true>(h, a, kv_cache, st) : launch_forward<64, false>(h, a, kv_cache, st);
 }
 
 ft_status_t ft_attn_sync_status(ft_attn_t *h) {
