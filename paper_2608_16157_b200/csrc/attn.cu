@@ -60,7 +60,7 @@ ft_status_t check_config(const ft_attn_config_t *c) {
   if ((long long)c->n_pages * c->page_tokens >= (1ll << 31) || (long long)c->max_pages * c->page_tokens >= (1ll << 31))
     return FT_ERR_INVALID_ARG;
   // work units of a step are counted in 32 bits: key blocks of all requests and of all tiles of a request's rows
-  const long long blocks = (long long)c->max_pages * c->page_tokens / kDecKeys + 2;
+  const long long blocks = (long long)c->max_pages * c->page_tokens / kDecKeys + 2 + kTileCost;
   const long long tile_tokens = 2 * (kTileRows / (c->n_q_heads / c->n_kv_heads));
   const long long entries = c->max_tokens / tile_tokens + c->max_requests;
   if (blocks * c->max_requests * c->n_kv_heads >= (1ll << 31) || blocks * entries * c->n_kv_heads >= (1ll << 31)) return FT_ERR_UNSUPPORTED;

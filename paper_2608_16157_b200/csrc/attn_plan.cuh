@@ -18,10 +18,13 @@ constexpr int kDecRows = 16;           // query rows (tokens x heads of a group)
 constexpr int kDecKeys = 64;           // keys of one of its work units
 constexpr int kTileRows = 128;         // query rows of one tcgen05 tile; a work item of the tiled kernel is two of them
 constexpr int kTileKeys = 128;         // keys of one of its work units
+constexpr int kDecCost = 1, kTileCost = 3;   // of a work item besides its blocks, in units
 
 // One entry of the streaming list (a request with few rows) or of the tile list (up to 2 x 128 rows of a request).
-// The units of an entry are its key blocks b0 .. b0+nb-1 for each key/value head: unit (head h, block b) has the number
-// unit0*Hkv + h*nb + (b - b0).  CTA i evaluates the units [i*quota, (i+1)*quota).
+// The units of an entry are its key blocks b0 .. b0+nb-1 for each key/value head.  What an item costs besides its blocks
+// (queries, first scores, results) counts as `cost` units in front of them, so block b of head h stands at
+// unit0*Hkv + h*(nb + cost) + cost + (b - b0), unit0 being the sum of nb + cost of the entries before.  CTA i evaluates the
+// blocks that stand at [i*quota, (i+1)*quota).
 struct __align__(16) AttnEntry {
   int32_t req, tok0, n_tok, pos0;   // request, first packed row, rows, position of the first row
   int32_t b0, nb, unit0, pad;
@@ -91,16 +94,34 @@ __device__ __forceinline__ int count_le(const int32_t *a, int n, int v) {
   return lo;
 }
 
-// First unit of CTA c in a list of `n` entries.
-__device__ __forceinline__ int4 locate_unit(const AttnEntry *e, int n, int n_kv, int u) {
+// The first block at or behind position u in a list of `n` entries: entry, head, block.
+__device__ __forceinline__ int4 locate_unit(const AttnEntry *e, int n, int n_kv, int cost, int u) {
   int lo = 0, hi = n;                     // largest entry with unit0 * n_kv <= u
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (e[mid].unit0 * n_kv <= u) lo = mid; else hi = mid;
   }
-  const int rest = u - e[lo].unit0 * n_kv, nb = e[lo].nb;
-  return make_int4(lo, rest / nb, rest % nb, 0);
+  const int rest = u - e[lo].unit0 * n_kv, w = e[lo].nb + cost;
+  return make_int4(lo, rest / w, max(0, rest % w - cost), 0);
 }
+
+// A CTA's walk over its share: `take` blocks from block `blk` of (entry k, head).
+struct WorkWalk {
+  int k, head, blk, take, u;              // u: position of the item's first block
+  AttnEntry e;
+  // false: the share is done
+  __device__ __forceinline__ bool load(const AttnEntry *list, int n, int n_kv, int cost, int end) {
+    if (k >= n) return false;
+    e = list[k];
+    u = e.unit0 * n_kv + head * (e.nb + cost) + cost;
+    take = min(e.nb, end - u) - blk;
+    return take > 0;
+  }
+  __device__ __forceinline__ void next(int n_kv) {
+    blk = 0;
+    if (++head == n_kv) { head = 0; ++k; }
+  }
+};
 
 // Key blocks of `keys` keys that the rows at positions pos0 .. pos0+n-1 attend to: first block and count (at least one
 // block, so that rows that attend to nothing are still written).
@@ -121,12 +142,13 @@ __device__ void build_work(const AttnSlotsArgs &a, int n, int tok0, int kv, unsi
   int b0 = 0, nb = 0;
   if (dec) block_range(kv - n, n, g.window, kDecKeys, &b0, &nb);
   unsigned long long tot;
-  const unsigned long long inc = block_scan<NT>(pack2(dec ? 1u : 0u, (uint32_t)nb), s_warp, &tot);
+  const int w = dec ? nb + kDecCost : 0;
+  const unsigned long long inc = block_scan<NT>(pack2(dec ? 1u : 0u, (uint32_t)w), s_warp, &tot);
   const int n_dec = (int)(uint32_t)tot, dec_units = (int)(tot >> 32) * g.n_kv;
   if (dec) {
     AttnEntry e;
     e.req = tid; e.tok0 = tok0; e.n_tok = n; e.pos0 = kv - n; e.b0 = b0; e.nb = nb;
-    e.unit0 = (int)(inc >> 32) - nb; e.pad = 0;
+    e.unit0 = (int)(inc >> 32) - w; e.pad = 0;
     a.w.dec[(uint32_t)inc - 1] = e;
   }
   const int tiles = (n > 0 && !dec) ? (n + g.tile_tokens - 1) / g.tile_tokens : 0;
@@ -138,16 +160,16 @@ __device__ void build_work(const AttnSlotsArgs &a, int n, int tok0, int kv, unsi
   for (int base = 0; base < n_tile; base += NT) {
     const int t = base + tid;
     AttnEntry e;
-    e.nb = 0;
     if (t < n_tile) {
       const int r = count_le(s_tile, a.n_req, t);
       const int i = t - (r ? s_tile[r - 1] : 0), nr = s_q[r + 1] - s_q[r], first = i * g.tile_tokens;
       e.req = r; e.tok0 = s_q[r] + first; e.n_tok = min(g.tile_tokens, nr - first); e.pos0 = s_kv[r] - nr + first; e.pad = 0;
       block_range(e.pos0, e.n_tok, g.window, kTileKeys, &e.b0, &e.nb);
     }
-    const unsigned long long ui = block_scan<NT>((unsigned long long)e.nb, s_warp, &tot);
+    const int w = t < n_tile ? e.nb + kTileCost : 0;
+    const unsigned long long ui = block_scan<NT>((unsigned long long)w, s_warp, &tot);
     if (t < n_tile) {
-      e.unit0 = carry + (int)ui - e.nb;
+      e.unit0 = carry + (int)ui - w;
       a.w.tile[t] = e;
     }
     carry += (int)tot;
@@ -164,9 +186,9 @@ __device__ void build_work(const AttnSlotsArgs &a, int n, int tok0, int kv, unsi
   }
   __syncthreads();
   for (int c = tid; c < g.dec_grid; c += NT)
-    if ((long long)c * dec_quota < dec_units) a.w.dec_start[c] = locate_unit(a.w.dec, n_dec, g.n_kv, c * dec_quota);
+    if ((long long)c * dec_quota < dec_units) a.w.dec_start[c] = locate_unit(a.w.dec, n_dec, g.n_kv, kDecCost, c * dec_quota);
   for (int c = tid; c < g.tile_grid; c += NT)
-    if ((long long)c * tile_quota < tile_units) a.w.tile_start[c] = locate_unit(a.w.tile, n_tile, g.n_kv, c * tile_quota);
+    if ((long long)c * tile_quota < tile_units) a.w.tile_start[c] = locate_unit(a.w.tile, n_tile, g.n_kv, kTileCost, c * tile_quota);
 }
 
 // NT >= n_req: 256 threads for up to 256 requests, 1024 above.

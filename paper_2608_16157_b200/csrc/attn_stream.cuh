@@ -86,7 +86,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
   const AttnPlanHdr hdr = *a.w.hdr;
   const long long u_first = (long long)blockIdx.x * hdr.dec_quota;
   if (u_first >= hdr.dec_units) return;
-  int left = (int)min((long long)hdr.dec_quota, hdr.dec_units - u_first);
+  const int u_end = (int)min(u_first + hdr.dec_quota, (long long)hdr.dec_units);
   const int4 st = a.w.dec_start[blockIdx.x];
   if (tid == 0) {
     for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), kStreamWarps); }
@@ -98,7 +98,8 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
 
   const int page_tokens = 1 << a.page_shift;
   const int box_rows = min(page_tokens, kDecKeys), boxes = kDecKeys / box_rows;   // boxes of a block along its keys
-  int k = st.x, head = st.y, blk = st.z;
+  WorkWalk w;
+  w.k = st.x; w.head = st.y; w.blk = st.z;
   uint32_t it = 0;      // blocks of this CTA so far
 
   if (warp == kStreamWarps) {
@@ -108,9 +109,9 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
     const int per_box = 2 * kChunks;
     const int bx = lane / per_box, ch = (lane % per_box) >> 1, is_v = lane & 1;
     const bool owner = bx < boxes;
-    while (left > 0) {
-      const AttnEntry e = a.w.dec[k];
-      const int take = min(left, e.nb - blk);
+    for (; w.load(a.w.dec, hdr.n_dec, a.n_kv, kDecCost, u_end); w.next(a.n_kv)) {
+      const AttnEntry &e = w.e;
+      const int blk = w.blk, take = w.take, head = w.head;
       const int hi = max(0, e.pos0 + e.n_tok), lo = a.window > 0 ? max(0, e.pos0 - a.window + 1) : 0;
       const int32_t *row = a.table + (long long)e.req * a.table_stride;
       auto page_of = [&](int b) -> int {       // page of this lane's box of block b, -1: nothing to load
@@ -139,9 +140,6 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
         page = next;
       }
       if (*s_abort) break;
-      left -= take;
-      blk = 0;
-      if (++head == a.n_kv) { head = 0; ++k; }
     }
     // copies of a CTA that gave up must land before its shared memory goes away
     abort_drain(s_abort);
@@ -151,9 +149,9 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
   // ------------------------------ consumers ------------------------------
   const int g = lane >> 2, t4 = lane & 3;
   const int key0 = warp * 16;                   // this warp's keys of a block
-  while (left > 0) {
-    const AttnEntry e = a.w.dec[k];
-    const int take = min(left, e.nb - blk);
+  for (; w.load(a.w.dec, hdr.n_dec, a.n_kv, kDecCost, u_end); w.next(a.n_kv)) {
+    const AttnEntry &e = w.e;
+    const int blk = w.blk, take = w.take, head = w.head;
     const int hi = max(0, e.pos0 + e.n_tok), lo = a.window > 0 ? max(0, e.pos0 - a.window + 1) : 0;
     const int rows = e.n_tok * a.group;
     // query fragments: row r = token r / group, head of the group r % group
@@ -287,8 +285,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
         for (int i = 0; i < D / 8; ++i) *reinterpret_cast<float2 *>(dst + i * 8) = make_float2(o[i][2 * h2], o[i][2 * h2 + 1]);
     }
     named_sync(1, kStreamWarps * 32);
-    const int u0 = e.unit0 * a.n_kv + head * e.nb;
-    const int c_first = u0 / hdr.dec_quota, c_last = (u0 + e.nb - 1) / hdr.dec_quota;
+    const int c_first = w.u / hdr.dec_quota, c_last = (w.u + e.nb - 1) / hdr.dec_quota;
     const bool whole = c_first == c_last;
     constexpr int kCols = D / 4;                       // a thread owns 4 columns of every (128 / kCols)-th row
     const int col = (tid % kCols) * 4, row0 = tid / kCols;
@@ -305,13 +302,13 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
       float mm = -INFINITY, ll = 0.f;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < kStreamWarps; ++w) mm = fmaxf(mm, s_ml[(w * kDecRows + r) * 2]);
+      for (int i = 0; i < kStreamWarps; ++i) mm = fmaxf(mm, s_ml[(i * kDecRows + r) * 2]);
       const float bm = mm == -INFINITY ? 0.f : mm;
 #pragma unroll
-      for (int w = 0; w < kStreamWarps; ++w) {
-        const float f = ex2(s_ml[(w * kDecRows + r) * 2] - bm);
-        const float4 x = *reinterpret_cast<const float4 *>(s_join + (w * kDecRows + r) * Cfg::kRow + col);
-        ll = fmaf(f, s_ml[(w * kDecRows + r) * 2 + 1], ll);
+      for (int i = 0; i < kStreamWarps; ++i) {
+        const float f = ex2(s_ml[(i * kDecRows + r) * 2] - bm);
+        const float4 x = *reinterpret_cast<const float4 *>(s_join + (i * kDecRows + r) * Cfg::kRow + col);
+        ll = fmaf(f, s_ml[(i * kDecRows + r) * 2 + 1], ll);
         v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
       }
       if (whole) {
@@ -325,7 +322,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
       __threadfence();
       named_sync(1, kStreamWarps * 32);
       if (tid == 0) {
-        uint32_t *cnt = a.arrive + (size_t)k * a.n_kv + head;
+        uint32_t *cnt = a.arrive + (size_t)w.k * a.n_kv + head;
         const uint32_t n = (uint32_t)(c_last - c_first + 1);
         const bool last = atomicAdd(cnt, 1u) == n - 1;
         if (last) *cnt = 0u;
@@ -353,9 +350,6 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
       }
     }
     named_sync(1, kStreamWarps * 32);      // the join buffer is free again
-    left -= take;
-    blk = 0;
-    if (++head == a.n_kv) { head = 0; ++k; }
   }
   abort_drain(s_abort);
 }

@@ -6,36 +6,59 @@
 // request, as two tiles of 128 rows; its key blocks of 128 are its work units, cut into equal shares, one CTA per SM (the
 // work partition of attn_plan.cuh).  Roles of the warps:
 //   warp 9     brings Q (4-D TMA boxes: D, heads of the group, head, tokens) and the pages of K and V (128-byte swizzle)
-//   warp 8     issues tcgen05.mma: S_t = Q_t K^T into tensor memory, O_t += P_t V with P_t read from tensor memory
-//   warps 0-3, 4-7   softmax of tile 0 and 1: a thread owns a row, so maximum and sum need no exchange; P overwrites S
-// While one tile is in its softmax the tensor pipe works for the other.  The order of issue (PV_t of block j, then QK_t of
-// block j+1) makes the completion of S_t imply that O_t is at rest, so a row's rescaling of O_t in tensor memory needs no
-// barrier of its own; it is left out while the maximum grows by less than 2^8 (the result is the same: the sum is taken
-// with the same reference; 16-bit weights up to 2^8 have the same relative rounding).
+//   warp 8     issues tcgen05.mma: S_t = Q_t K^T into tensor memory, O_t += P_t V with P_t read from there
+//   warps 0-3, 4-7   softmax of tile 0 and 1: a thread owns a row, so maximum and sum need no exchange
+// While one tile is in its softmax the tensor pipe works for the other: one warp issues for both in turn, P_t V of block j and
+// then Q_t K^T of block j+1, which keeps the two out of step (two issuing warps fell into step: 4750 against 3870 clocks a
+// unit).  P overwrites its scores (tensor memory: 2 x (128 + D) columns) and is handed over in two halves of 64 keys.
+// No maximum is taken as a rule: a half block's weights are made with the row's present reference, and their sum tells
+// whether any exceeds 2^8; only then (and in a row's first half block) the maximum is taken, O rescaled in tensor memory and the
+// half repeated (the maximum is also taken where a mask is applied).  The result is the same, since weights and sum share one reference; 16-bit weights up to 2^8 have the same
+// relative rounding.
 // P is rounded to the values' type for the second product; scores, maxima, sums and O stay in 32 bits.
 #pragma once
+#include <type_traits>
+
 #include "attn_stream.cuh"
 
 namespace ftmoe {
 
-constexpr int kTileThreads = 320;
+constexpr int kTileThreads = 320, kTileHalf = 64;    // keys of half a block
 template <int D> struct TileCfg {
   static constexpr int kChunks = D / 64;                    // 64-element pieces of D: 128 rows x 128 bytes each
   static constexpr int kTile = 128 * D * 2;                 // bytes of 128 rows of Q, K or V
-  static constexpr int kStages = D == 128 ? 5 : 10;         // ring of K and V tiles
-  static constexpr int kBars = 2 * kStages + 2 + 8;
-  static constexpr int kSmem = 1024 + 2 * kTile + kStages * kTile + kBars * 8 + 64;
+  static constexpr int kStages = D == 128 ? 4 : 8;          // ring of K and V tiles
+  static constexpr int kStage = 8 * 4096;                   // results on their way out
+  static constexpr int kBars = 2 * kStages + 2 + 14;
+  static constexpr int kSmem = 1024 + 2 * kTile + kStages * kTile + kStage + kBars * 8 + 64;
   static constexpr int kPart = 128 * (D + 2);               // floats of one tile's partial result: m[128], l[128], O[D][128]
 };
 static_assert(TileCfg<128>::kSmem <= 232448 && TileCfg<64>::kSmem <= 232448, "shared memory of a CTA");
 
-__device__ __forceinline__ void umma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) { umma_bf16(d, a, b, idesc, acc); }
 __device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t acc) {
   asm volatile(
       "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
       " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
       "r"(a_tmem), "l"(b), "r"(idesc), "r"(acc)
       : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(p));
+  return p != 0;
+}
+// A value all lanes hold, in a uniform register.
+__device__ __forceinline__ int uniform(int v) { return __reduce_max_sync(0xffffffffu, v); }
+// Bounded wait without anything between the polls (limit: g_wait_polls, read once): a wait is on the critical path of every
+// block several times.  Returns false, after latching, if the phase never completes.
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, uint32_t limit, volatile int *abort_flag, uint32_t *status) {
+  for (uint32_t i = 0; i <= limit; ++i) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((i & 255u) == 255u && *abort_flag) return false;
+  }
+  *abort_flag = 1;
+  atomicOr(status, kStatTimeout);
+  return false;
 }
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
   asm volatile(
@@ -45,6 +68,12 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
       "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
       "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                 "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(taddr));
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
@@ -61,10 +90,36 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *tm,
       : "memory");
 }
 
+__device__ __forceinline__ uint64_t f2(float lo, float hi) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+  return v;
+}
+__device__ __forceinline__ void f2_split(uint64_t v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 // What a tile of a work item covers.
 struct TileSpan {
   int n, lo, hi, pos0;       // rows' tokens, keys [lo, hi) some row attends to, position of the first token
-  __device__ __forceinline__ bool active(int kb) const { return n > 0 && kb * kTileKeys < hi && (kb + 1) * kTileKeys > lo; }
+  // half blocks [first, last) that a part of the item's blocks [kb0, kb1) holds for the tile
+  __device__ __forceinline__ void halves(int kb0, int kb1, int *first, int *last) const {
+    *first = max(2 * kb0, lo / kTileHalf);
+    *last = n > 0 ? min(2 * kb1, (hi + kTileHalf - 1) / kTileHalf) : 0;
+    if (*last < *first) *last = *first;
+  }
 };
 __device__ __forceinline__ TileSpan tile_span(const AttnEntry &e, int t, int tokens, int window) {
   TileSpan s;
@@ -81,7 +136,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   using Cfg = TileCfg<D>;
   extern __shared__ unsigned char smem_raw[];
   unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  uint64_t *s_bar = reinterpret_cast<uint64_t *>(smem + (2 + Cfg::kStages) * Cfg::kTile);
+  unsigned char *s_stage = smem + (2 + Cfg::kStages) * Cfg::kTile;
+  uint64_t *s_bar = reinterpret_cast<uint64_t *>(s_stage + Cfg::kStage);
   uint32_t *s_tmem = reinterpret_cast<uint32_t *>(s_bar + Cfg::kBars);
   volatile int *s_abort = reinterpret_cast<volatile int *>(s_tmem + 1);
   volatile int *s_last = s_abort + 1;                        // [2]
@@ -91,20 +147,26 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   auto empty_bar = [&](int s) { return bars + 8u * (Cfg::kStages + s); };
   const uint32_t q_full = bars + 8u * (2 * Cfg::kStages), q_empty = q_full + 8;
   auto s_full = [&](int t) { return q_full + 16 + 8u * t; };
-  auto p_full = [&](int t) { return q_full + 32 + 8u * t; };
-  auto o_full = [&](int t) { return q_full + 48 + 8u * t; };
-  auto o_empty = [&](int t) { return q_full + 64 + 8u * t; };
+  auto p_full = [&](int t, uint32_t buf) { return q_full + 48 + 16u * t + 8u * buf; };
+  // (by the parity of the half's number: a waiter knows the one before the last on each to be complete)
+  auto pv_done = [&](int t, uint32_t i) { return q_full + 80 + 16u * t + 8u * (i & 1u); };
+  auto o_empty = [&](int t) { return q_full + 112 + 8u * t; };
 
+  const uint32_t limit = g_wait_polls;
   const AttnPlanHdr hdr = *a.w.hdr;
   const long long u_first = (long long)blockIdx.x * hdr.tile_quota;
   if (u_first >= hdr.tile_units) return;
-  int left = (int)min((long long)hdr.tile_quota, hdr.tile_units - u_first);
+  const int u_end = (int)min(u_first + hdr.tile_quota, (long long)hdr.tile_units);
   const int4 st = a.w.tile_start[blockIdx.x];
   if (tid == 0) {
     for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     mbar_init(q_full, 1);
     mbar_init(q_empty, 1);
-    for (int t = 0; t < 2; ++t) { mbar_init(s_full(t), 1); mbar_init(p_full(t), 4); mbar_init(o_full(t), 1); mbar_init(o_empty(t), 4); }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(s_full(t), 1);
+      for (int i = 0; i < 2; ++i) { mbar_init(p_full(t, i), 4); mbar_init(pv_done(t, i), 1); }
+      mbar_init(o_empty(t), 4);
+    }
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -119,302 +181,387 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   const uint32_t tmem = *s_tmem;
   const uint32_t tm_s = tmem, tm_o = tmem + 256;             // S_t (and P_t) at 128 t, O_t at 256 + D t
   const int tokens = kTileRows / a.group;                    // tokens of a tile
-  int k = st.x, head = st.y, blk = st.z;
+  WorkWalk w;
+  w.k = st.x; w.head = st.y; w.blk = st.z;
 
-  if (warp == 9) {
-    // ------------------------------ loads ------------------------------
-    const int page_tokens = 1 << a.page_shift;
-    const int box_rows = min(page_tokens, kDecKeys), boxes = kTileKeys / box_rows;
-    const int bx = lane / Cfg::kChunks, ch = lane % Cfg::kChunks;
-    const bool owner = bx < boxes;
-    uint32_t it = 0, items = 0;
-    while (left > 0 && !*s_abort) {
-      const AttnEntry e = a.w.tile[k];
-      const int take = min(left, e.nb - blk);
-      const int hi = max(0, e.pos0 + e.n_tok), lo = a.window > 0 ? max(0, e.pos0 - a.window + 1) : 0;
-      const int32_t *row = a.table + (long long)e.req * a.table_stride;
-      auto wanted = [&](int b) {
-        const int key = (e.b0 + b) * kTileKeys + bx * box_rows;
-        return owner && key < hi && key + box_rows > lo;
-      };
-      auto page_of = [&](int b) -> int { return wanted(b) ? row[((e.b0 + b) * kTileKeys + bx * box_rows) >> a.page_shift] : 0; };
-      int page = page_of(blk);
-      mbar_wait(q_empty, (items & 1u) ^ 1u, s_abort, a.status);
-      if (*s_abort) break;
-      if (lane == 0) {
-        const int n_tiles = e.n_tok > tokens ? 2 : 1;
-        mbar_expect_tx(q_full, (uint32_t)(n_tiles * Cfg::kChunks * tokens * a.group * 128));
-        for (int t = 0; t < n_tiles; ++t)
-          for (int c = 0; c < Cfg::kChunks; ++c)
-            tma_load_4d(q_smem + t * Cfg::kTile + c * 16384, &tm_q, c * 64, 0, head, e.tok0 + t * tokens, q_full);
-      }
-      ++items;
-      for (int b = blk; b < blk + take; ++b) {
-        const int next = b + 1 < blk + take ? page_of(b + 1) : 0;
-        const bool want = wanted(b);
-        if (want && (uint32_t)page >= (uint32_t)a.n_pages) {     // never followed: page 0 instead, and reported
-          atomicOr(a.status, kStatBadIndex);
-          page = 0;
-        }
-        const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, want)) * (uint32_t)(box_rows * 128);
-        const int y = ((e.b0 + b) * kTileKeys + bx * box_rows) & (page_tokens - 1);
-#pragma unroll
-        for (int v = 0; v < 2; ++v, ++it) {
-          const int s = it % Cfg::kStages;
-          mbar_wait(empty_bar(s), ((it / Cfg::kStages) & 1u) ^ 1u, s_abort, a.status);
-          if (*s_abort) break;
-          if (lane == 0) mbar_expect_tx(full_bar(s), bytes);
-          __syncwarp();
-          if (want)
-            tma_load_3d(ring + s * Cfg::kTile + ch * 16384 + bx * box_rows * 128, &tm, ch * 64, y, (page * 2 + v) * a.n_kv + head,
-                        full_bar(s));
-        }
+  if (warp >= 8) {
+    w.k = uniform(w.k); w.head = uniform(w.head); w.blk = uniform(w.blk);
+    uint32_t rs = 0, rph = 0;                 // next entry of the ring and its phase
+    auto step = [](uint32_t &s, uint32_t &ph) { if (++s == Cfg::kStages) { s = 0; ph ^= 1u; } };
+    uint32_t items = 0;
+    if (warp == 9) {
+      // ------------------------------ loads ------------------------------
+      const int page_tokens = 1 << a.page_shift;
+      const int box_rows = min(page_tokens, kDecKeys), boxes = kTileKeys / box_rows;
+      for (; w.load(a.w.tile, hdr.n_tile, a.n_kv, kTileCost, u_end) && !*s_abort; w.next(a.n_kv)) {
+        AttnEntry e = w.e;
+        e.n_tok = uniform(e.n_tok); e.pos0 = uniform(e.pos0); e.b0 = uniform(e.b0); e.tok0 = uniform(e.tok0);
+        const int take = uniform(w.take), blk = w.blk, head = w.head;
+        const int hi = max(0, e.pos0 + e.n_tok), lo = a.window > 0 ? max(0, e.pos0 - a.window + 1) : 0;
+        const int32_t *row = a.table + (long long)e.req * a.table_stride;
+        // lane i holds the page of box i of a block; boxes first .. last-1 of a block are loaded
+        auto page_of = [&](int b) -> int {
+          const int key = (e.b0 + b) * kTileKeys + lane * box_rows;
+          if (lane >= boxes || key >= hi || key + box_rows <= lo) return 0;
+          int page = row[key >> a.page_shift];
+          if ((uint32_t)page >= (uint32_t)a.n_pages) {     // never followed: page 0 instead, and reported
+            atomicOr(a.status, kStatBadIndex);
+            page = 0;
+          }
+          return page;
+        };
+        int page = page_of(blk);
+        wait_phase(q_empty, (items & 1u) ^ 1u, limit, s_abort, a.status);
         if (*s_abort) break;
-        page = next;
-      }
-      left -= take;
-      blk = 0;
-      if (++head == a.n_kv) { head = 0; ++k; }
-    }
-  } else if (warp == 8) {
-    // ------------------------------ tensor core ------------------------------
-    constexpr uint32_t type = BF16 ? (1u << 7) | (1u << 10) : 0u;
-    constexpr uint32_t idesc_qk = (1u << 4) | type | ((uint32_t)(kTileKeys >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);
-    constexpr uint32_t idesc_pv = (1u << 4) | type | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);
-    uint32_t it = 0, items = 0, np[2] = {0, 0}, no[2] = {0, 0};
-    while (left > 0) {
-      const AttnEntry e = a.w.tile[k];
-      const int take = min(left, e.nb - blk);
-      const int hi = max(0, e.pos0 + e.n_tok), lo = a.window > 0 ? max(0, e.pos0 - a.window + 1) : 0;
-      const TileSpan sp[2] = {tile_span(e, 0, tokens, a.window), tile_span(e, 1, tokens, a.window)};
-      bool fresh[2] = {true, true};
-      mbar_wait(q_full, items & 1u, s_abort, a.status);
-      ++items;
-      for (int j = 0; j <= take; ++j) {
-        // K of block j is ring entry it + 2j, V of block j-1 entry it + 2j - 1
-        const uint32_t ik = it + 2 * j, iv = ik - 1;
-        const int kb = e.b0 + blk + j;
-        const int sk = ik % Cfg::kStages, sv = iv % Cfg::kStages;
-        const uint32_t kt = ring + sk * Cfg::kTile, vt = ring + sv * Cfg::kTile;
-        bool ok = true;
-        if (j > 0) {
-          ok = mbar_wait(full_bar(sv), (iv / Cfg::kStages) & 1u, s_abort, a.status);
-          const int first = (kb - 1) * kTileKeys;
-          if (ok && (first + kTileKeys > hi || first < lo)) {
-            // values no row attends to may be anything: their weight is 0, so they have to be finite
-            for (int i = lane; i < kTileKeys * Cfg::kChunks * 8; i += 32) {
-              const int r = (i >> 3) % kTileKeys, c = (i >> 3) / kTileKeys;
-              if (first + r >= hi || first + r < lo)
-                asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(vt + c * 16384 + r * 128 + (i & 7) * 16), "r"(0u) : "memory");
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-          }
-        }
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (j > 0 && sp[t].active(kb - 1)) {
-            if (fresh[t]) mbar_wait(o_empty(t), (no[t] & 1u) ^ 1u, s_abort, a.status);
-            ok = mbar_wait(p_full(t), np[t] & 1u, s_abort, a.status) && ok;
-            ++np[t];
-            tc_fence_after();
-            if (lane == 0 && ok) {
-              const uint64_t dv = umma_desc(vt, 16384, 1024);      // (an address step is its 16-byte count in the low bits)
-#pragma unroll
-              for (int kk = 0; kk < kTileKeys / 16; ++kk)
-                umma_ts(tm_o + t * D, tm_s + t * 128 + kk * 8, dv + kk * (2048 >> 4), idesc_pv, (fresh[t] && kk == 0) ? 0u : 1u);
-            }
-            fresh[t] = false;
-            if (lane == 0 && (j == take || !sp[t].active(kb))) umma_commit(o_full(t));
-            if (j == take || !sp[t].active(kb)) ++no[t];
-          }
-          if (j < take && sp[t].active(kb)) {
-            ok = mbar_wait(full_bar(sk), (ik / Cfg::kStages) & 1u, s_abort, a.status) && ok;
-            tc_fence_after();
-            if (lane == 0) {
-              if (ok) {
-                const uint64_t dq = umma_desc(q_smem + t * Cfg::kTile, 16, 1024), dk = umma_desc(kt, 16, 1024);
-#pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk)
-                  umma_ss(tm_s + t * 128, dq + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16, dk + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16,
-                          idesc_qk, kk != 0 ? 1u : 0u);
-              }
-              umma_commit(s_full(t));
-            }
-          }
-        }
-        if (lane == 0) {
-          if (j > 0) umma_commit(empty_bar(sv));
-          if (j < take) {
-            // a block that no tile attends to is still waited for: its copies have to land before the stage is reused
-            if (!sp[0].active(kb) && !sp[1].active(kb)) mbar_wait(full_bar(sk), (ik / Cfg::kStages) & 1u, s_abort, a.status);
-            umma_commit(empty_bar(sk));
-          }
-          if (j == take - 1) umma_commit(q_empty);
+        ++items;
+        if (elect_one()) {
+          const int n_tiles = e.n_tok > tokens ? 2 : 1;
+          mbar_expect_tx(q_full, (uint32_t)(n_tiles * Cfg::kChunks * tokens * a.group * 128));
+          for (int t = 0; t < n_tiles; ++t)
+            for (int c = 0; c < Cfg::kChunks; ++c)
+              tma_load_4d(q_smem + t * Cfg::kTile + c * 16384, &tm_q, c * 64, 0, head, e.tok0 + t * tokens, q_full);
         }
         __syncwarp();
+        for (int b = blk; b < blk + take; ++b) {
+          const int next = b + 1 < blk + take ? page_of(b + 1) : 0;
+          const int key0 = (e.b0 + b) * kTileKeys;
+          const int first = max(0, lo - key0) / box_rows, last = min(boxes, (max(0, hi - key0) + box_rows - 1) / box_rows);
+          const uint32_t bytes = (uint32_t)(max(0, last - first) * box_rows * D * 2);
+          for (int v = 0; v < 2; ++v) {
+            wait_phase(empty_bar(rs), rph ^ 1u, limit, s_abort, a.status);
+            if (*s_abort) break;
+            if (elect_one()) mbar_expect_tx(full_bar(rs), bytes);
+            __syncwarp();
+            const uint32_t dst = ring + rs * Cfg::kTile;
+            for (int i = first; i < last; ++i) {
+              const int z = (__shfl_sync(0xffffffffu, page, i) * 2 + v) * a.n_kv + head, y = (key0 + i * box_rows) & (page_tokens - 1);
+              if (elect_one()) {
+#pragma unroll
+                for (int c = 0; c < Cfg::kChunks; ++c)
+                  tma_load_3d(dst + c * 16384 + i * box_rows * 128, &tm, c * 64, y, z, full_bar(rs));
+              }
+              __syncwarp();
+            }
+            step(rs, rph);
+          }
+          if (*s_abort) break;
+          page = next;
+        }
       }
-      it += 2 * take;
-      left -= take;
-      blk = 0;
-      if (++head == a.n_kv) { head = 0; ++k; }
+    } else {
+      // ------------------------------ tensor core ------------------------------
+      constexpr uint32_t type = BF16 ? (1u << 7) | (1u << 10) : 0u;
+      constexpr uint32_t idesc_qk = (1u << 4) | type | ((uint32_t)(kTileKeys >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);
+      constexpr uint32_t idesc_pv = (1u << 4) | type | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);
+      // (little code, the same for both tiles and both halves: what this warp runs is not in the instruction cache for long
+      // beside the softmax warps)
+      uint32_t cp0 = 0, cp1 = 0, no0 = 0, no1 = 0; // halves of weights consumed, items so far
+      uint32_t vs = 0, vph = 0;                    // ring entry of V of the block before; rs is K of the present one
+      const uint64_t dq = umma_desc(q_smem, 16, 1024);
+      for (; w.load(a.w.tile, hdr.n_tile, a.n_kv, kTileCost, u_end); w.next(a.n_kv)) {
+        AttnEntry e = w.e;
+        e.n_tok = uniform(e.n_tok); e.pos0 = uniform(e.pos0); e.b0 = uniform(e.b0);
+        const int take = uniform(w.take), kb0 = e.b0 + w.blk;
+        const int hi = max(0, e.pos0 + e.n_tok), lo = a.window > 0 ? max(0, e.pos0 - a.window + 1) : 0;
+        int h00, h01, h10, h11;
+        tile_span(e, 0, tokens, a.window).halves(kb0, kb0 + take, &h00, &h01);
+        tile_span(e, 1, tokens, a.window).halves(kb0, kb0 + take, &h10, &h11);
+        const int hf = max(h00, h10), hl = min(h01, h11);    // halves in use by both tiles, the first one of neither among them
+        wait_phase(q_full, items & 1u, limit, s_abort, a.status);
+        ++items;
+#pragma unroll 1
+        for (int j = 0; j <= take; ++j) {
+          const int kb = kb0 + j;
+          bool ok = true;
+          const uint32_t vt = ring + vs * Cfg::kTile;
+          if (j < take) ok = wait_phase(full_bar(rs), rph, limit, s_abort, a.status);
+          if (j > 0) {
+            ok = wait_phase(full_bar(vs), vph, limit, s_abort, a.status) && ok;
+            const int first = (kb - 1) * kTileKeys;
+            if (ok && (first + kTileKeys > hi || first < lo)) {
+              // values no row attends to may be anything: their weight is 0, so they have to be finite
+#pragma unroll 1
+              for (int i = lane; i < kTileKeys * Cfg::kChunks * 8; i += 32) {
+                const int r = (i >> 3) % kTileKeys, c = (i >> 3) / kTileKeys;
+                if (first + r >= hi || first + r < lo)
+                  asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(vt + c * 16384 + r * 128 + (i & 7) * 16), "r"(0u) : "memory");
+              }
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+            }
+          }
+          tc_fence_after();
+          const uint64_t dv = umma_desc(vt, 16384, 1024), dk = umma_desc(ring + rs * Cfg::kTile, 16, 1024);
+          if (j > 0 && j < take && 2 * kb - 2 > hf && 2 * kb + 2 <= hl) {
+            // every half of both blocks in use by both tiles
+            const uint32_t ppa = (cp0 >> 1) & 1u, ppb = (cp1 >> 1) & 1u;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              const uint32_t cp = t ? cp1 : cp0, ph = t ? ppb : ppa;
+#pragma unroll
+              for (int half = 0; half < 2; ++half) {
+                ok = wait_phase(p_full(t, (cp + half) & 1u), half && (cp & 1u) ? ph ^ 1u : ph, limit, s_abort, a.status) && ok;
+                tc_fence_after();
+                if (elect_one()) {
+                  if (ok)
+#pragma unroll
+                    for (int kk = half * 4; kk < half * 4 + 4; ++kk)
+                      umma_ts(tm_o + t * D, tm_s + t * 128 + kk * 8, dv + kk * (2048 >> 4), idesc_pv, 1u);
+                  umma_commit(pv_done(t, cp + half));
+                  if (half == 1) {
+                    if (ok)
+#pragma unroll
+                      for (int kk = 0; kk < D / 16; ++kk)
+                        umma_bf16(tm_s + t * 128, dq + (t * Cfg::kTile + (kk >> 2) * 16384 + (kk & 3) * 32) / 16,
+                                  dk + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16, idesc_qk, kk != 0 ? 1u : 0u);
+                    umma_commit(s_full(t));
+                    if (t == 1) {
+                      umma_commit(empty_bar(vs));
+                      umma_commit(empty_bar(rs));
+                      if (j == take - 1) umma_commit(q_empty);
+                    }
+                  }
+                }
+                __syncwarp();
+              }
+            }
+            cp0 += 2; cp1 += 2;
+          } else {
+#pragma unroll 1
+          for (int t = 0; t < 2; ++t) {
+            const int h0 = t ? h10 : h00, h1 = t ? h11 : h01;
+            const int hb = min(h1, 2 * kb);
+#pragma unroll 1
+            for (int h = max(h0, 2 * kb - 2); h < hb; ++h) {
+              const uint32_t cp = t ? cp1 : cp0;
+              if (h == h0) wait_phase(o_empty(t), ((t ? no1 : no0) & 1u) ^ 1u, limit, s_abort, a.status);
+              ok = wait_phase(p_full(t, cp & 1u), (cp >> 1) & 1u, limit, s_abort, a.status) && ok;
+              tc_fence_after();
+              if (elect_one()) {
+                if (ok) {
+                  const uint32_t p = tm_s + t * 128 + (h & 1) * 32, o = tm_o + t * D;
+                  const uint64_t d = dv + (h & 1) * (8192 >> 4);
+                  umma_ts(o, p, d, idesc_pv, h == h0 ? 0u : 1u);
+#pragma unroll
+                  for (int kk = 1; kk < 4; ++kk) umma_ts(o, p + kk * 8, d + kk * (2048 >> 4), idesc_pv, 1u);
+                }
+                umma_commit(pv_done(t, cp));
+              }
+              __syncwarp();
+              cp0 += 1 - t; cp1 += t;
+            }
+            if (elect_one()) {
+              if (j < take && 2 * kb < h1 && 2 * kb + 2 > h0) {
+                if (ok) {
+                  const uint32_t ds = tm_s + t * 128;
+                  const uint64_t d = dq + t * (Cfg::kTile >> 4);
+#pragma unroll
+                  for (int kk = 0; kk < D / 16; ++kk)
+                    umma_bf16(ds, d + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16, dk + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16, idesc_qk,
+                              kk != 0 ? 1u : 0u);
+                }
+                umma_commit(s_full(t));
+              }
+              if (t == 1) {
+                if (j > 0) umma_commit(empty_bar(vs));
+                if (j < take) umma_commit(empty_bar(rs));
+                if (j == take - 1) umma_commit(q_empty);
+              }
+            }
+            __syncwarp();
+          }
+          }
+          if (j < take) {
+            step(rs, rph);
+            vs = rs; vph = rph;
+            step(rs, rph);
+          }
+        }
+        no0 += h01 > h00 ? 1u : 0u;
+        no1 += h11 > h10 ? 1u : 0u;
+      }
     }
   } else {
     // ------------------------------ softmax ------------------------------
     const int t = warp >> 2, row = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts = tm_s + t * 128 + lanes, to = tm_o + t * D + lanes;
+    const uint32_t to = tm_o + t * D + lanes;
     const int tok = row / a.group, hq_in = row - tok * a.group;
     const float sl2 = fabsf(a.scale_log2);
     const bool negate = a.scale_log2 < 0.f;
-    uint32_t ns = 0, no = 0;
-    while (left > 0) {
-      const AttnEntry e = a.w.tile[k];
-      const int take = min(left, e.nb - blk);
+    uint32_t cs = 0, cb = 0;                               // halves and blocks so far
+    const uint32_t ts = tm_s + t * 128 + lanes;
+    for (; w.load(a.w.tile, hdr.n_tile, a.n_kv, kTileCost, u_end); w.next(a.n_kv)) {
+      const AttnEntry &e = w.e;
+      const int take = w.take, blk = w.blk, head = w.head;
       const TileSpan sp = tile_span(e, t, tokens, a.window);
       const bool valid = tok < sp.n;                       // (tok < tokens holds for rows below tokens * group)
       const int pos = valid ? sp.pos0 + tok : -1;
-      float m = -INFINITY, l = 0.f;
-      bool any = false;
-      for (int b = blk; b < blk + take; ++b) {
-        const int kb = e.b0 + b;
-        if (!sp.active(kb)) continue;
-        const bool ok = mbar_wait(s_full(t), ns & 1u, s_abort, a.status);
-        ++ns;
-        tc_fence_after();
-        uint32_t s[4][32];
+      int h0, h1;
+      sp.halves(e.b0 + blk, e.b0 + blk + take, &h0, &h1);
+      // halves in which every row of the tile attends to every key, after the first one
+      int f0 = h0 + 1, f1 = negate ? h0 : min(h1, (sp.pos0 + 1) / kTileHalf);
+      if (a.window > 0) f0 = max(f0, (sp.pos0 + sp.n - 1 - a.window + kTileHalf) / kTileHalf);
+      float m = valid ? -INFINITY : 0.f, l = 0.f;          // reference (log2 units) and sum of the row
+      uint32_t x[2][32], p[2][16];
+      float sum;
+      auto weights = [&](float ref) {
+        const uint64_t sl2_2 = f2(sl2, sl2), ref_2 = f2(-ref, -ref);
+        uint64_t acc[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32(ts + c * 32, s[c]);
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float p0, p1;
+            f2_split(fma2(f2(__uint_as_float(x[c][2 * i]), __uint_as_float(x[c][2 * i + 1])), sl2_2, ref_2), p0, p1);
+            p0 = ex2(p0);
+            p1 = ex2(p1);
+            acc[i & 3] = add2(acc[i & 3], f2(p0, p1));
+            p[c][i] = pack_pair<BF16>(p0, p1);
+          }
+        float l0, l1;
+        f2_split(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])), l0, l1);
+        sum = l0 + l1;
+      };
+#pragma unroll 1
+      for (int h = h0; h < h1; ++h, ++cs) {
+        if (h == h0 || (h & 1) == 0) {
+          wait_phase(s_full(t), cb & 1u, limit, s_abort, a.status);
+          tc_fence_after();
+          ++cb;
+        }
+        const uint32_t th = ts + (h & 1) * kTileHalf;
+        tmem_ld32(th, x[0]);
+        tmem_ld32(th + 32, x[1]);
         tmem_ld_wait();
-        if (negate) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int i = 0; i < 32; ++i) s[c][i] ^= 0x80000000u;
+        bool done = false;
+        if (h >= f0 && h < f1) {
+          weights(m);
+          done = __all_sync(0xffffffffu, sum <= 256.f);    // (false too for a row without a reference: its sum is not a number)
         }
-        const int first = kb * kTileKeys;
-        if (first + kTileKeys - 1 > sp.pos0 || (a.window > 0 && first <= sp.pos0 + sp.n - 1 - a.window)) {
-          const int c_hi = pos - first, c_lo = a.window > 0 ? pos - a.window + 1 - first : -1;
+        if (!done) {
+          const int first = h * kTileHalf;
+          if (negate) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
+            for (int i = 0; i < 64; ++i) x[i >> 5][i & 31] ^= 0x80000000u;
+          }
+          if (!(h >= f0 && h < f1)) {
+            const int c_hi = pos - first, c_lo = a.window > 0 ? pos - a.window + 1 - first : -1;
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (c * 32 + i > c_hi || c * 32 + i < c_lo) s[c][i] = 0xff800000u;
-        }
-        float mx[4];
+            for (int i = 0; i < 64; ++i)
+              if (i > c_hi || i < c_lo) x[i >> 5][i & 31] = 0xff800000u;
+          }
+          float mx[8];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          mx[c] = __uint_as_float(s[c][0]);
+          for (int i = 0; i < 8; ++i) mx[i] = fmaxf(__uint_as_float(x[0][i]), __uint_as_float(x[0][8 + i]));
 #pragma unroll
-          for (int i = 1; i < 32; ++i) mx[c] = fmaxf(mx[c], __uint_as_float(s[c][i]));
-        }
-        const float bm = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2;
-        // keep the old reference while the maximum is at most 2^8 above it
-        const bool grow = bm > m + 8.f;
-        if (any) {
-          if (__any_sync(0xffffffffu, grow)) {
+          for (int c = 16; c < 64; c += 16)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) mx[i] = max3(mx[i], __uint_as_float(x[c >> 5][(c & 31) + i]), __uint_as_float(x[c >> 5][(c & 31) + 8 + i]));
+          const float bm = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * sl2;
+          const bool grow = bm > m + 2.f;
+          if (h > h0 && __any_sync(0xffffffffu, grow)) {
+            // the product of the half before has to be in O (this one's is not asked for yet)
+            wait_phase(pv_done(t, cs - 1), ((cs - 1) >> 1) & 1u, limit, s_abort, a.status);
+            tc_fence_after();
             const float f = grow ? ex2(m - bm) : 1.f;
             l *= f;
 #pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-              uint32_t o[32];
-              tmem_ld32(to + c, o);
+            for (int c = 0; c < D; c += 16) {
+              uint32_t o[16];
+              tmem_ld16(to + c, o);
               tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-              tmem_st32(to + c, o);
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              tmem_st16(to + c, o);
             }
-            if (grow) m = bm;
           }
-        } else if (bm > m) {
-          m = bm;
+          if (grow) m = bm;
+          weights(m == -INFINITY ? 0.f : m);               // (every score -infinity: weights of 0)
         }
-        any = true;
-        const float base = m == -INFINITY ? 0.f : m;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-          uint32_t p[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float p0 = ex2(fmaf(__uint_as_float(s[q4][2 * i]), sl2, -base));
-            const float p1 = ex2(fmaf(__uint_as_float(s[q4][2 * i + 1]), sl2, -base));
-            sum[(2 * i) & 2] += p0;
-            sum[((2 * i) & 2) + 1] += p1;
-            p[i] = pack_pair<BF16>(p0, p1);
-          }
-          tmem_st16(ts + q4 * 16, p);
-        }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        l += sum;
+        tmem_st16(ts + (h & 1) * 32, p[0]);
+        tmem_st16(ts + (h & 1) * 32 + 16, p[1]);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full(t));
-        (void)ok;
+        if (lane == 0) mbar_arrive(p_full(t, cs & 1u));
       }
+      const bool any = h1 > h0;
 
       // ------------------------------ result of the item ------------------------------
       if (sp.n > 0) {
         if (any) {
-          mbar_wait(o_full(t), no & 1u, s_abort, a.status);
-          ++no;
+          wait_phase(pv_done(t, cs - 1), ((cs - 1) >> 1) & 1u, limit, s_abort, a.status);
           tc_fence_after();
         }
-        const int u0 = e.unit0 * a.n_kv + head * e.nb;
-        const int c_first = u0 / hdr.tile_quota, c_last = (u0 + e.nb - 1) / hdr.tile_quota;
+        const int c_first = w.u / hdr.tile_quota, c_last = (w.u + e.nb - 1) / hdr.tile_quota;
         const long long tg = e.tok0 + t * tokens + tok;
         const int hq = head * a.group + hq_in;
-        uint16_t *dst = a.out + tg * a.out_stride + hq * D;
-        auto store = [&](int c, const uint32_t (&o)[32], float inv) {
-          uint4 *d4 = reinterpret_cast<uint4 *>(dst + c);
+        const long long dst = tg * a.out_stride + hq * D;     // this thread's row
+        unsigned char *stage = s_stage + warp * 4096;         // this warp's 32 rows x 64 columns
+        // 64 columns of the rows, one a thread, to memory: through shared memory (16-byte chunks swizzled by the row), so that
+        // eight lanes write the 128 bytes of a row
+        auto emit = [&](int c, const uint32_t (&o)[2][32], float inv) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t w[4];
+          for (int i = 0; i < 8; ++i) {
+            uint32_t v[4];
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-              w[x] = pack_pair<BF16>(__uint_as_float(o[i * 8 + 2 * x]) * inv, __uint_as_float(o[i * 8 + 2 * x + 1]) * inv);
-            d4[i] = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int z = 0; z < 4; ++z)
+              v[z] = pack_pair<BF16>(__uint_as_float(o[i >> 2][(i & 3) * 8 + 2 * z]) * inv, __uint_as_float(o[i >> 2][(i & 3) * 8 + 2 * z + 1]) * inv);
+            *reinterpret_cast<uint4 *>(stage + lane * 128 + ((i ^ (lane & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+          }
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = i * 4 + (lane >> 3), z = lane & 7;
+            const uint4 v = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((z ^ (r & 7)) << 4));
+            const long long d = __shfl_sync(0xffffffffu, dst, r);
+            if (__shfl_sync(0xffffffffu, valid ? 1 : 0, r)) *reinterpret_cast<uint4 *>(a.out + d + c + z * 8) = v;
+          }
+          __syncwarp();
+        };
+        auto load_o = [&](int c, uint32_t (&o)[2][32]) {
+          if (any) {
+            tmem_ld32(to + c, o[0]);
+            tmem_ld32(to + c + 32, o[1]);
+            tmem_ld_wait();
+          } else {
+#pragma unroll
+            for (int i = 0; i < 64; ++i) o[i >> 5][i & 31] = 0u;
           }
         };
         auto store_lse = [&](float mm, float ll) {
           if (a.lse && valid) a.lse[tg * a.n_q + hq] = ll > 0.f ? (mm + log2f(ll)) * 0.693147180559945f : -INFINITY;
         };
-        if (c_first == c_last) {
-          const float inv = l > 0.f ? 1.f / l : 0.f;
+        const bool whole = c_first == c_last;
+        float *part = a.part + (size_t)((blockIdx.x * 2 + ((int)blockIdx.x == c_first ? 1 : 0)) * 2 + t) * Cfg::kPart;
+        const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll 1
-          for (int c = 0; c < D; c += 32) {
-            uint32_t o[32];
-            if (any) {
-              tmem_ld32(to + c, o);
-              tmem_ld_wait();
-            } else {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = 0u;
-            }
-            if (valid) store(c, o, inv);
+        for (int c = 0; c < D; c += 64) {
+          uint32_t (&o)[2][32] = x;
+          load_o(c, o);
+          if (any && c + 64 == D) {                           // O_t is free
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(o_empty(t));
           }
+          if (whole) {
+            emit(c, o, inv);
+          } else if (valid) {
+#pragma unroll
+            for (int i = 0; i < 64; ++i) part[256 + (c + i) * 128 + row] = __uint_as_float(o[i >> 5][i & 31]);
+          }
+        }
+        if (whole) {
           store_lse(m, l);
         } else {
-          float *part = a.part + (size_t)((blockIdx.x * 2 + ((int)blockIdx.x == c_first ? 1 : 0)) * 2 + t) * Cfg::kPart;
           part[row] = m;
           part[128 + row] = l;
-#pragma unroll 1
-          for (int c = 0; c < D; c += 32) {
-            uint32_t o[32];
-            if (any) {
-              tmem_ld32(to + c, o);
-              tmem_ld_wait();
-            } else {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = 0u;
-            }
-#pragma unroll
-            for (int i = 0; i < 32; ++i) part[256 + (c + i) * 128 + row] = __uint_as_float(o[i]);
-          }
           __threadfence();
           named_sync(1 + t, 128);
           if (row == 0) {
-            uint32_t *cnt = a.arrive + ((size_t)k * a.n_kv + head) * 2 + t;
+            uint32_t *cnt = a.arrive + ((size_t)w.k * a.n_kv + head) * 2 + t;
             const bool last = atomicAdd(cnt, 1u) == (uint32_t)(c_last - c_first);
             if (last) *cnt = 0u;
             s_last[t] = last;
@@ -422,44 +569,37 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
           }
           named_sync(1 + t, 128);
           if (s_last[t]) {
+            auto part_of = [&](int c) { return a.part + (size_t)((c * 2 + (c == c_first ? 1 : 0)) * 2 + t) * Cfg::kPart; };
             float mm = -INFINITY, ll = 0.f;
+#pragma unroll 4
             for (int c = c_first; c <= c_last; ++c) {
-              const float *pc = a.part + (size_t)((c * 2 + (c == c_first ? 1 : 0)) * 2 + t) * Cfg::kPart;
-              const float mc = __ldcg(pc + row), lc = __ldcg(pc + 128 + row);
+              const float mc = __ldcg(part_of(c) + row), lc = __ldcg(part_of(c) + 128 + row);
               const float mn = fmaxf(mm, mc), bm = mn == -INFINITY ? 0.f : mn;
               ll = ll * ex2(mm - bm) + lc * ex2(mc - bm);
               mm = mn;
             }
-            const float bm = mm == -INFINITY ? 0.f : mm, inv = ll > 0.f ? 1.f / ll : 0.f;
+            const float bm = mm == -INFINITY ? 0.f : mm, inv_all = ll > 0.f ? 1.f / ll : 0.f;
 #pragma unroll 1
-            for (int c0 = 0; c0 < D; c0 += 32) {
-              float acc[32];
+            for (int c0 = 0; c0 < D; c0 += 64) {
+              uint32_t (&o)[2][32] = x;
 #pragma unroll
-              for (int i = 0; i < 32; ++i) acc[i] = 0.f;
-              for (int c = c_first; c <= c_last; ++c) {
-                const float *pc = a.part + (size_t)((c * 2 + (c == c_first ? 1 : 0)) * 2 + t) * Cfg::kPart;
-                const float f = ex2(__ldcg(pc + row) - bm);
+              for (int i = 0; i < 64; ++i) o[i >> 5][i & 31] = 0u;
+              if (valid)
+#pragma unroll 1
+                for (int c = c_first; c <= c_last; ++c) {
+                  const float *pc = part_of(c);
+                  const float f = ex2(__ldcg(pc + row) - bm);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) acc[i] = fmaf(f, __ldcg(pc + 256 + (c0 + i) * 128 + row), acc[i]);
-              }
-              uint32_t o[32];
-#pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(acc[i]);
-              if (valid) store(c0, o, inv);
+                  for (int i = 0; i < 64; ++i)
+                    o[i >> 5][i & 31] = __float_as_uint(fmaf(f, __ldcg(pc + 256 + (c0 + i) * 128 + row), __uint_as_float(o[i >> 5][i & 31])));
+                }
+              emit(c0, o, inv_all);
             }
             store_lse(mm, ll);
           }
           named_sync(1 + t, 128);        // s_last is free again
         }
-        if (any) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(o_empty(t));
-        }
       }
-      left -= take;
-      blk = 0;
-      if (++head == a.n_kv) { head = 0; ++k; }
     }
   }
   abort_drain(s_abort);
