@@ -107,6 +107,7 @@ ft_status_t ft_attn_qk_rope(ft_attn_t *h, int T, const void *q, int64_t q_stride
  * out = sum_j softmax_j(scale * q.k_j) v_j, lse = log(sum_j exp(scale * q.k_j)).  A row that attends to nothing gets
  * zeros and lse = -infinity.  Rows of no request are not written.
  *   q, out: DEVICE [T][Hq][D], strides in elements from token to token, 16-byte aligned, strides % 8 == 0
+ *           and <= 2^23
  *   lse   : DEVICE float [T][Hq] or NULL
  * FT_ERR_STATE before the first slots/plan call. */
 ft_status_t ft_attn_forward(ft_attn_t *h, const void *q, int64_t q_stride, const void *kv_cache, const int32_t *table,

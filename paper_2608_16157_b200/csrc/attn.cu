@@ -23,8 +23,7 @@ struct ft_attn {
   AttnGeom geom;
   float *part = nullptr;           // partial results of work items that several CTAs share: streaming kernel, tiled kernel
   size_t part_tile = 0;            // floats before the second
-  uint32_t *arrive = nullptr;      // their arrival counters, in the same order
-  size_t arrive_tile = 0;
+  uint32_t *arrive = nullptr;      // arrival counters of the streaming kernel's
   size_t arrive_bytes = 0;
   void *encode = nullptr;          // cuTensorMapEncodeTiled
   bool planned = false;
@@ -140,9 +139,9 @@ ft_status_t launch_forward(ft_attn *h, AttnFwdArgs a, const void *cache, cudaStr
   if (h->max_new * h->geom.group > kDecRows) {
     if (!make_query_map(h, &tm_q, a.q, a.q_stride)) return FT_ERR_CUDA;
     a.part = h->part + h->part_tile;
-    a.arrive = h->arrive + h->arrive_tile;
     attn_tile_kernel<D, BF16><<<h->geom.tile_grid, kTileThreads, TileCfg<D>::kSmem, st>>>(tm_q, tm, a);
-    h->launches += 1;
+    attn_join_kernel<D, BF16><<<dim3(h->geom.tile_grid - 1, 2 * (D / 16)), 128, 0, st>>>(a);
+    h->launches += 2;
     FA_CUDA(cudaGetLastError());
   }
   return FT_OK;
@@ -162,7 +161,7 @@ ft_status_t allocate(ft_attn *h) {
   g.tile_cap = c.max_tokens / g.tile_tokens + c.max_requests;
   auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
   const size_t n_dec = up(sizeof(AttnEntry) * (size_t)c.max_requests), n_tile = up(sizeof(AttnEntry) * (size_t)g.tile_cap);
-  const size_t n_start = up(sizeof(int4) * kAttnMaxGrid), total = 256 + n_dec + n_tile + 2 * n_start;
+  const size_t n_start = up(sizeof(AttnStart) * kAttnMaxGrid), total = 256 + n_dec + n_tile + 2 * n_start;
   FA_CUDA(cudaMalloc(&h->work_mem, total));
   FA_CUDA(cudaMemset(h->work_mem, 0, total));
   FA_CUDA(cudaMalloc(&h->status_dev, 256));
@@ -171,13 +170,12 @@ ft_status_t allocate(ft_attn *h) {
   h->work.hdr = reinterpret_cast<AttnPlanHdr *>(b); b += 256;
   h->work.dec = reinterpret_cast<AttnEntry *>(b); b += n_dec;
   h->work.tile = reinterpret_cast<AttnEntry *>(b); b += n_tile;
-  h->work.dec_start = reinterpret_cast<int4 *>(b); b += n_start;
-  h->work.tile_start = reinterpret_cast<int4 *>(b);
+  h->work.dec_start = reinterpret_cast<AttnStart *>(b); b += n_start;
+  h->work.tile_start = reinterpret_cast<AttnStart *>(b);
   h->part_tile = (size_t)g.dec_grid * 2 * (c.head_dim == 128 ? StreamCfg<128>::kPart : StreamCfg<64>::kPart);
   const size_t part = h->part_tile + (size_t)g.tile_grid * 4 * (c.head_dim == 128 ? TileCfg<128>::kPart : TileCfg<64>::kPart);
   FA_CUDA(cudaMalloc(&h->part, part * sizeof(float)));
-  h->arrive_tile = (size_t)c.max_requests * c.n_kv_heads;
-  h->arrive_bytes = (h->arrive_tile + (size_t)g.tile_cap * c.n_kv_heads * 2) * sizeof(uint32_t);
+  h->arrive_bytes = (size_t)c.max_requests * c.n_kv_heads * sizeof(uint32_t);
   FA_CUDA(cudaMalloc(&h->arrive, h->arrive_bytes));
   FA_CUDA(cudaMemset(h->arrive, 0, h->arrive_bytes));
   FA_CUDA((allow_smem<64, true>()));
@@ -339,6 +337,7 @@ ft_status_t ft_attn_forward(ft_attn_t *h, const void *q, int64_t q_stride, const
   const int D = c.head_dim;
   if (!q || !kv_cache || !table || !out) return FT_ERR_INVALID_ARG;
   if (((uintptr_t)q | (uintptr_t)kv_cache | (uintptr_t)out) & 15) return FT_ERR_INVALID_ARG;
+  if (q_stride > (1 << 23) || out_stride > (1 << 23)) return FT_ERR_INVALID_ARG;
   if (q_stride < (int64_t)c.n_q_heads * D || out_stride < (int64_t)c.n_q_heads * D || ((q_stride | out_stride) & 7) ||
       table_stride < c.max_pages || !(scale == scale))
     return FT_ERR_INVALID_ARG;

@@ -29,6 +29,11 @@ struct __align__(16) AttnEntry {
   int32_t req, tok0, n_tok, pos0;   // request, first packed row, rows, position of the first row
   int32_t b0, nb, unit0, pad;
 };
+// Where a CTA's share begins: the first block at or behind its position, and that entry.
+struct __align__(16) AttnStart {
+  int32_t k, head, blk, pad;
+  AttnEntry e;
+};
 struct AttnPlanHdr {
   int32_t n_req, T;
   int32_t n_dec, dec_units, dec_quota;      // (units times key/value heads)
@@ -37,7 +42,7 @@ struct AttnPlanHdr {
 struct AttnWork {   // device pointers of a handle's work partition
   AttnPlanHdr *hdr;
   AttnEntry *dec, *tile;
-  int4 *dec_start, *tile_start;             // per CTA: entry, head, block of its first unit
+  AttnStart *dec_start, *tile_start;        // per CTA
 };
 struct AttnGeom {
   int32_t group, n_kv, window, tile_tokens;   // tile_tokens: rows of a request per work item of the tiled kernel
@@ -94,32 +99,38 @@ __device__ __forceinline__ int count_le(const int32_t *a, int n, int v) {
   return lo;
 }
 
-// The first block at or behind position u in a list of `n` entries: entry, head, block.
-__device__ __forceinline__ int4 locate_unit(const AttnEntry *e, int n, int n_kv, int cost, int u) {
+// The first block at or behind position u in a list of `n` entries.
+__device__ __forceinline__ AttnStart locate_unit(const AttnEntry *e, int n, int n_kv, int cost, int u) {
   int lo = 0, hi = n;                     // largest entry with unit0 * n_kv <= u
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (e[mid].unit0 * n_kv <= u) lo = mid; else hi = mid;
   }
-  const int rest = u - e[lo].unit0 * n_kv, w = e[lo].nb + cost;
-  return make_int4(lo, rest / w, max(0, rest % w - cost), 0);
+  AttnStart s;
+  s.e = e[lo];
+  const int rest = u - s.e.unit0 * n_kv, w = s.e.nb + cost;
+  s.k = lo; s.head = rest / w; s.blk = max(0, rest % w - cost); s.pad = 0;
+  return s;
 }
 
 // A CTA's walk over its share: `take` blocks from block `blk` of (entry k, head).
 struct WorkWalk {
   int k, head, blk, take, u;              // u: position of the item's first block
   AttnEntry e;
+  bool have;                              // e is entry k
+  __device__ __forceinline__ void start(const AttnStart &s) { k = s.k; head = s.head; blk = s.blk; e = s.e; have = true; }
   // false: the share is done
   __device__ __forceinline__ bool load(const AttnEntry *list, int n, int n_kv, int cost, int end) {
     if (k >= n) return false;
-    e = list[k];
+    if (!have) e = list[k];
+    have = true;
     u = e.unit0 * n_kv + head * (e.nb + cost) + cost;
     take = min(e.nb, end - u) - blk;
     return take > 0;
   }
   __device__ __forceinline__ void next(int n_kv) {
     blk = 0;
-    if (++head == n_kv) { head = 0; ++k; }
+    if (++head == n_kv) { head = 0; ++k; have = false; }
   }
 };
 

@@ -84,10 +84,10 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
   auto empty_bar = [&](int s) { return bars + 8u * (Cfg::kStages + s); };
 
   const AttnPlanHdr hdr = *a.w.hdr;
+  const AttnStart st = a.w.dec_start[blockIdx.x];     // (stale beyond the shares in use: not looked at)
   const long long u_first = (long long)blockIdx.x * hdr.dec_quota;
   if (u_first >= hdr.dec_units) return;
   const int u_end = (int)min(u_first + hdr.dec_quota, (long long)hdr.dec_units);
-  const int4 st = a.w.dec_start[blockIdx.x];
   if (tid == 0) {
     for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), kStreamWarps); }
     *s_abort = 0;
@@ -99,7 +99,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
   const int page_tokens = 1 << a.page_shift;
   const int box_rows = min(page_tokens, kDecKeys), boxes = kDecKeys / box_rows;   // boxes of a block along its keys
   WorkWalk w;
-  w.k = st.x; w.head = st.y; w.blk = st.z;
+  w.start(st);
   uint32_t it = 0;      // blocks of this CTA so far
 
   if (warp == kStreamWarps) {

@@ -4,7 +4,8 @@
 //
 // A work item is up to 256 query rows (tokens x heads of the group: the keys of a head are read once for all of them) of a
 // request, as two tiles of 128 rows; its key blocks of 128 are its work units, cut into equal shares, one CTA per SM (the
-// work partition of attn_plan.cuh).  Roles of the warps:
+// work partition of attn_plan.cuh).  An item with at most 128 rows (short chunks, drafts, single tokens of wide groups: bound by
+// HBM) uses both tiles on the same rows, one for the even and one for the odd blocks, and joins them at its end.  Roles of the warps:
 //   warp 9     brings Q (4-D TMA boxes: D, heads of the group, head, tokens) and the pages of K and V (128-byte swizzle)
 //   warp 8     issues tcgen05.mma: S_t = Q_t K^T into tensor memory, O_t += P_t V with P_t read from there
 //   warps 0-3, 4-7   softmax of tile 0 and 1: a thread owns a row, so maximum and sum need no exchange
@@ -54,7 +55,7 @@ __device__ __forceinline__ int uniform(int v) { return __reduce_max_sync(0xfffff
 __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, uint32_t limit, volatile int *abort_flag, uint32_t *status) {
   for (uint32_t i = 0; i <= limit; ++i) {
     if (mbar_try_wait(bar, parity)) return true;
-    if ((i & 255u) == 255u && *abort_flag) return false;
+    if (__builtin_expect((i & 255u) == 255u, 0) && *abort_flag) return false;
   }
   *abort_flag = 1;
   atomicOr(status, kStatTimeout);
@@ -111,6 +112,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
+// The half blocks a tile takes of the item's range [h0, h1): all, or with `keys` those of the blocks of its parity.
+__device__ __forceinline__ int first_half(bool keys, int t, int h0) { return keys && ((h0 >> 1) & 1) != t ? 2 * ((h0 >> 1) + 1) : h0; }
+__device__ __forceinline__ int next_half(bool keys, int h) { return keys && (h & 1) ? h + 3 : h + 1; }
+
 // What a tile of a work item covers.
 struct TileSpan {
   int n, lo, hi, pos0;       // rows' tokens, keys [lo, hi) some row attends to, position of the first token
@@ -140,7 +145,6 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   uint64_t *s_bar = reinterpret_cast<uint64_t *>(s_stage + Cfg::kStage);
   uint32_t *s_tmem = reinterpret_cast<uint32_t *>(s_bar + Cfg::kBars);
   volatile int *s_abort = reinterpret_cast<volatile int *>(s_tmem + 1);
-  volatile int *s_last = s_abort + 1;                        // [2]
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t q_smem = smem_u32(smem), ring = q_smem + 2 * Cfg::kTile, bars = smem_u32(s_bar);
   auto full_bar = [&](int s) { return bars + 8u * s; };
@@ -154,10 +158,10 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
 
   const uint32_t limit = g_wait_polls;
   const AttnPlanHdr hdr = *a.w.hdr;
+  const AttnStart st = a.w.tile_start[blockIdx.x];     // (stale beyond the shares in use: not looked at)
   const long long u_first = (long long)blockIdx.x * hdr.tile_quota;
   if (u_first >= hdr.tile_units) return;
   const int u_end = (int)min(u_first + hdr.tile_quota, (long long)hdr.tile_units);
-  const int4 st = a.w.tile_start[blockIdx.x];
   if (tid == 0) {
     for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     mbar_init(q_full, 1);
@@ -182,7 +186,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   const uint32_t tm_s = tmem, tm_o = tmem + 256;             // S_t (and P_t) at 128 t, O_t at 256 + D t
   const int tokens = kTileRows / a.group;                    // tokens of a tile
   WorkWalk w;
-  w.k = st.x; w.head = st.y; w.blk = st.z;
+  w.start(st);
 
   if (warp >= 8) {
     w.k = uniform(w.k); w.head = uniform(w.head); w.blk = uniform(w.blk);
@@ -202,50 +206,55 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         // lane i holds the page of box i of a block; boxes first .. last-1 of a block are loaded
         auto page_of = [&](int b) -> int {
           const int key = (e.b0 + b) * kTileKeys + lane * box_rows;
-          if (lane >= boxes || key >= hi || key + box_rows <= lo) return 0;
-          int page = row[key >> a.page_shift];
-          if ((uint32_t)page >= (uint32_t)a.n_pages) {     // never followed: page 0 instead, and reported
+          return lane < boxes && key < hi && key + box_rows > lo ? row[key >> a.page_shift] : 0;
+        };
+        auto checked = [&](int page) -> int {              // never followed out of the pool: page 0 instead, and reported
+          if (__builtin_expect((uint32_t)page >= (uint32_t)a.n_pages, 0)) {
             atomicOr(a.status, kStatBadIndex);
             page = 0;
           }
           return page;
         };
-        int page = page_of(blk);
+        const bool keys = e.n_tok <= tokens;
+        const int lag = keys ? 2 : 1;             // V of a block comes behind K of the `lag`-th block after it: the order of use
+        int page = page_of(blk), page1 = 0, page2 = 0;
         wait_phase(q_empty, (items & 1u) ^ 1u, limit, s_abort, a.status);
         if (*s_abort) break;
         ++items;
         if (elect_one()) {
-          const int n_tiles = e.n_tok > tokens ? 2 : 1;
+          const int n_tiles = keys ? 1 : 2;
           mbar_expect_tx(q_full, (uint32_t)(n_tiles * Cfg::kChunks * tokens * a.group * 128));
           for (int t = 0; t < n_tiles; ++t)
             for (int c = 0; c < Cfg::kChunks; ++c)
               tma_load_4d(q_smem + t * Cfg::kTile + c * 16384, &tm_q, c * 64, 0, head, e.tok0 + t * tokens, q_full);
         }
         __syncwarp();
-        for (int b = blk; b < blk + take; ++b) {
-          const int next = b + 1 < blk + take ? page_of(b + 1) : 0;
+        auto load_tile = [&](int b, int pages, int v) {
+          wait_phase(empty_bar(rs), rph ^ 1u, limit, s_abort, a.status);
+          if (*s_abort) return;
           const int key0 = (e.b0 + b) * kTileKeys;
           const int first = max(0, lo - key0) / box_rows, last = min(boxes, (max(0, hi - key0) + box_rows - 1) / box_rows);
-          const uint32_t bytes = (uint32_t)(max(0, last - first) * box_rows * D * 2);
-          for (int v = 0; v < 2; ++v) {
-            wait_phase(empty_bar(rs), rph ^ 1u, limit, s_abort, a.status);
-            if (*s_abort) break;
-            if (elect_one()) mbar_expect_tx(full_bar(rs), bytes);
-            __syncwarp();
-            const uint32_t dst = ring + rs * Cfg::kTile;
-            for (int i = first; i < last; ++i) {
-              const int z = (__shfl_sync(0xffffffffu, page, i) * 2 + v) * a.n_kv + head, y = (key0 + i * box_rows) & (page_tokens - 1);
-              if (elect_one()) {
+          if (elect_one()) mbar_expect_tx(full_bar(rs), (uint32_t)(max(0, last - first) * box_rows * D * 2));
+          __syncwarp();
+          const uint32_t dst = ring + rs * Cfg::kTile;
+          for (int i = first; i < last; ++i) {
+            const int z = (__shfl_sync(0xffffffffu, pages, i) * 2 + v) * a.n_kv + head, y = (key0 + i * box_rows) & (page_tokens - 1);
+            if (elect_one()) {
 #pragma unroll
-                for (int c = 0; c < Cfg::kChunks; ++c)
-                  tma_load_3d(dst + c * 16384 + i * box_rows * 128, &tm, c * 64, y, z, full_bar(rs));
-              }
-              __syncwarp();
+              for (int c = 0; c < Cfg::kChunks; ++c)
+                tma_load_3d(dst + c * 16384 + i * box_rows * 128, &tm, c * 64, y, z, full_bar(rs));
             }
-            step(rs, rph);
+            __syncwarp();
           }
-          if (*s_abort) break;
-          page = next;
+          step(rs, rph);
+        };
+#pragma unroll 1
+        for (int i = 0; i < take + lag && !*s_abort; ++i) {
+          const int next = i + 1 < take ? page_of(blk + i + 1) : 0;     // (used, and waited for, a step later)
+          page = checked(page);
+          if (i >= lag) load_tile(blk + i - lag, keys ? page2 : page1, 1);
+          if (i < take) load_tile(blk + i, page, 0);
+          page2 = page1; page1 = page; page = next;
         }
       }
     } else {
@@ -256,29 +265,39 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       // (little code, the same for both tiles and both halves: what this warp runs is not in the instruction cache for long
       // beside the softmax warps)
       uint32_t cp0 = 0, cp1 = 0, no0 = 0, no1 = 0; // halves of weights consumed, items so far
-      uint32_t vs = 0, vph = 0;                    // ring entry of V of the block before; rs is K of the present one
       const uint64_t dq = umma_desc(q_smem, 16, 1024);
       for (; w.load(a.w.tile, hdr.n_tile, a.n_kv, kTileCost, u_end); w.next(a.n_kv)) {
         AttnEntry e = w.e;
         e.n_tok = uniform(e.n_tok); e.pos0 = uniform(e.pos0); e.b0 = uniform(e.b0);
         const int take = uniform(w.take), kb0 = e.b0 + w.blk;
         const int hi = max(0, e.pos0 + e.n_tok), lo = a.window > 0 ? max(0, e.pos0 - a.window + 1) : 0;
+        const bool keys = e.n_tok <= tokens;
+        const int lag = keys ? 2 : 1;
         int h00, h01, h10, h11;
         tile_span(e, 0, tokens, a.window).halves(kb0, kb0 + take, &h00, &h01);
-        tile_span(e, 1, tokens, a.window).halves(kb0, kb0 + take, &h10, &h11);
-        const int hf = max(h00, h10), hl = min(h01, h11);    // halves in use by both tiles, the first one of neither among them
+        tile_span(e, keys ? 0 : 1, tokens, a.window).halves(kb0, kb0 + take, &h10, &h11);
+        h00 = first_half(keys, 0, h00);
+        h10 = first_half(keys, 1, h10);
+        // halves in use by both tiles, the first one of neither among them
+        const int hf = max(h00, h10), hl = keys ? 0 : min(h01, h11);
         wait_phase(q_full, items & 1u, limit, s_abort, a.status);
         ++items;
+        // step j: P V of block j - lag, Q K^T of block j; the ring holds V and K in this order
 #pragma unroll 1
-        for (int j = 0; j <= take; ++j) {
-          const int kb = kb0 + j;
+        for (int j = 0; j < take + lag; ++j) {
+          const int kb = kb0 + j, kv = kb - lag;
+          const bool has_v = j >= lag, has_k = j < take;
           bool ok = true;
+          const uint32_t vs = rs, vph = rph;
+          if (has_v) step(rs, rph);
+          const uint32_t ks = rs, kph = rph;
+          if (has_k) step(rs, rph);
           const uint32_t vt = ring + vs * Cfg::kTile;
-          if (j < take) ok = wait_phase(full_bar(rs), rph, limit, s_abort, a.status);
-          if (j > 0) {
+          if (has_k) ok = wait_phase(full_bar(ks), kph, limit, s_abort, a.status);
+          if (has_v) {
             ok = wait_phase(full_bar(vs), vph, limit, s_abort, a.status) && ok;
-            const int first = (kb - 1) * kTileKeys;
-            if (ok && (first + kTileKeys > hi || first < lo)) {
+            const int first = kv * kTileKeys;
+            if (__builtin_expect(ok && (first + kTileKeys > hi || first < lo), 0)) {
               // values no row attends to may be anything: their weight is 0, so they have to be finite
 #pragma unroll 1
               for (int i = lane; i < kTileKeys * Cfg::kChunks * 8; i += 32) {
@@ -291,8 +310,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             }
           }
           tc_fence_after();
-          const uint64_t dv = umma_desc(vt, 16384, 1024), dk = umma_desc(ring + rs * Cfg::kTile, 16, 1024);
-          if (j > 0 && j < take && 2 * kb - 2 > hf && 2 * kb + 2 <= hl) {
+          const uint64_t dv = umma_desc(vt, 16384, 1024), dk = umma_desc(ring + ks * Cfg::kTile, 16, 1024);
+          if (has_v && has_k && 2 * kb - 2 > hf && 2 * kb + 2 <= hl) {
             // every half of both blocks in use by both tiles
             const uint32_t ppa = (cp0 >> 1) & 1u, ppb = (cp1 >> 1) & 1u;
 #pragma unroll
@@ -317,7 +336,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                     umma_commit(s_full(t));
                     if (t == 1) {
                       umma_commit(empty_bar(vs));
-                      umma_commit(empty_bar(rs));
+                      umma_commit(empty_bar(ks));
                       if (j == take - 1) umma_commit(q_empty);
                     }
                   }
@@ -328,11 +347,11 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             cp0 += 2; cp1 += 2;
           } else {
 #pragma unroll 1
-          for (int t = 0; t < 2; ++t) {
+          for (int t = keys ? kb & 1 : 0; t < (keys ? (kb & 1) + 1 : 2); ++t) {
             const int h0 = t ? h10 : h00, h1 = t ? h11 : h01;
-            const int hb = min(h1, 2 * kb);
+            const int hb = has_v ? min(h1, 2 * kv + 2) : h0;
 #pragma unroll 1
-            for (int h = max(h0, 2 * kb - 2); h < hb; ++h) {
+            for (int h = max(h0, 2 * kv); h < hb; ++h) {
               const uint32_t cp = t ? cp1 : cp0;
               if (h == h0) wait_phase(o_empty(t), ((t ? no1 : no0) & 1u) ^ 1u, limit, s_abort, a.status);
               ok = wait_phase(p_full(t, cp & 1u), (cp >> 1) & 1u, limit, s_abort, a.status) && ok;
@@ -351,10 +370,10 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
               cp0 += 1 - t; cp1 += t;
             }
             if (elect_one()) {
-              if (j < take && 2 * kb < h1 && 2 * kb + 2 > h0) {
+              if (has_k && 2 * kb < h1 && 2 * kb + 2 > h0) {
                 if (ok) {
                   const uint32_t ds = tm_s + t * 128;
-                  const uint64_t d = dq + t * (Cfg::kTile >> 4);
+                  const uint64_t d = dq + (keys ? 0 : t) * (Cfg::kTile >> 4);
 #pragma unroll
                   for (int kk = 0; kk < D / 16; ++kk)
                     umma_bf16(ds, d + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16, dk + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16, idesc_qk,
@@ -362,19 +381,14 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 }
                 umma_commit(s_full(t));
               }
-              if (t == 1) {
-                if (j > 0) umma_commit(empty_bar(vs));
-                if (j < take) umma_commit(empty_bar(rs));
+              if (keys || t == 1) {
+                if (has_v) umma_commit(empty_bar(vs));
+                if (has_k) umma_commit(empty_bar(ks));
                 if (j == take - 1) umma_commit(q_empty);
               }
             }
             __syncwarp();
           }
-          }
-          if (j < take) {
-            step(rs, rph);
-            vs = rs; vph = rph;
-            step(rs, rph);
           }
         }
         no0 += h01 > h00 ? 1u : 0u;
@@ -394,11 +408,13 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     for (; w.load(a.w.tile, hdr.n_tile, a.n_kv, kTileCost, u_end); w.next(a.n_kv)) {
       const AttnEntry &e = w.e;
       const int take = w.take, blk = w.blk, head = w.head;
-      const TileSpan sp = tile_span(e, t, tokens, a.window);
+      const bool keys = e.n_tok <= tokens;
+      const TileSpan sp = tile_span(e, keys ? 0 : t, tokens, a.window);
       const bool valid = tok < sp.n;                       // (tok < tokens holds for rows below tokens * group)
       const int pos = valid ? sp.pos0 + tok : -1;
       int h0, h1;
       sp.halves(e.b0 + blk, e.b0 + blk + take, &h0, &h1);
+      h0 = first_half(keys, t, h0);
       // halves in which every row of the tile attends to every key, after the first one
       int f0 = h0 + 1, f1 = negate ? h0 : min(h1, (sp.pos0 + 1) / kTileHalf);
       if (a.window > 0) f0 = max(f0, (sp.pos0 + sp.n - 1 - a.window + kTileHalf) / kTileHalf);
@@ -424,7 +440,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         sum = l0 + l1;
       };
 #pragma unroll 1
-      for (int h = h0; h < h1; ++h, ++cs) {
+      for (int h = h0; h < h1; h = next_half(keys, h), ++cs) {
         if (h == h0 || (h & 1) == 0) {
           wait_phase(s_full(t), cb & 1u, limit, s_abort, a.status);
           tc_fence_after();
@@ -434,12 +450,12 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         tmem_ld32(th, x[0]);
         tmem_ld32(th + 32, x[1]);
         tmem_ld_wait();
-        bool done = false;
+        bool over = true;
         if (h >= f0 && h < f1) {
           weights(m);
-          done = __all_sync(0xffffffffu, sum <= 256.f);    // (false too for a row without a reference: its sum is not a number)
+          over = !(sum <= 256.f);                          // (true too for a row without a reference: its sum is not a number)
         }
-        if (!done) {
+        if (__builtin_expect(__any_sync(0xffffffffu, over), 0)) {
           const int first = h * kTileHalf;
           if (negate) {
 #pragma unroll
@@ -459,7 +475,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
 #pragma unroll
             for (int i = 0; i < 8; ++i) mx[i] = max3(mx[i], __uint_as_float(x[c >> 5][(c & 31) + i]), __uint_as_float(x[c >> 5][(c & 31) + 8 + i]));
           const float bm = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * sl2;
-          const bool grow = bm > m + 2.f;
+          const bool grow = bm > m + 8.f || (over && bm > m && h >= f0 && h < f1);
           if (h > h0 && __any_sync(0xffffffffu, grow)) {
             // the product of the half before has to be in O (this one's is not asked for yet)
             wait_phase(pv_done(t, cs - 1), ((cs - 1) >> 1) & 1u, limit, s_abort, a.status);
@@ -495,10 +511,15 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
           wait_phase(pv_done(t, cs - 1), ((cs - 1) >> 1) & 1u, limit, s_abort, a.status);
           tc_fence_after();
         }
-        const int c_first = w.u / hdr.tile_quota, c_last = (w.u + e.nb - 1) / hdr.tile_quota;
-        const long long tg = e.tok0 + t * tokens + tok;
+        const int tok_base = e.tok0 + (keys ? 0 : t) * tokens;
+        const long long tg = tok_base + tok;
         const int hq = head * a.group + hq_in;
-        const long long dst = tg * a.out_stride + hq * D;     // this thread's row
+        // this thread's row relative to the tile's first, -1 where there is none; the rows it writes in `emit`
+        const int dst = valid ? tok * (int)a.out_stride + hq_in * D : -1;
+        uint16_t *out = a.out + (long long)tok_base * a.out_stride + (long long)head * a.group * D + (lane & 7) * 8;
+        int rows[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rows[i] = __shfl_sync(0xffffffffu, dst, i * 4 + (lane >> 3));
         unsigned char *stage = s_stage + warp * 4096;         // this warp's 32 rows x 64 columns
         // 64 columns of the rows, one a thread, to memory: through shared memory (16-byte chunks swizzled by the row), so that
         // eight lanes write the 128 bytes of a row
@@ -514,90 +535,91 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
           __syncwarp();
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const int r = i * 4 + (lane >> 3), z = lane & 7;
-            const uint4 v = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((z ^ (r & 7)) << 4));
-            const long long d = __shfl_sync(0xffffffffu, dst, r);
-            if (__shfl_sync(0xffffffffu, valid ? 1 : 0, r)) *reinterpret_cast<uint4 *>(a.out + d + c + z * 8) = v;
+            const int r = i * 4 + (lane >> 3);
+            const uint4 v = *reinterpret_cast<const uint4 *>(stage + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+            if (rows[i] >= 0) *reinterpret_cast<uint4 *>(out + rows[i] + c) = v;
           }
           __syncwarp();
-        };
-        auto load_o = [&](int c, uint32_t (&o)[2][32]) {
-          if (any) {
-            tmem_ld32(to + c, o[0]);
-            tmem_ld32(to + c + 32, o[1]);
-            tmem_ld_wait();
-          } else {
-#pragma unroll
-            for (int i = 0; i < 64; ++i) o[i >> 5][i & 31] = 0u;
-          }
         };
         auto store_lse = [&](float mm, float ll) {
           if (a.lse && valid) a.lse[tg * a.n_q + hq] = ll > 0.f ? (mm + log2f(ll)) * 0.693147180559945f : -INFINITY;
         };
-        const bool whole = c_first == c_last;
-        float *part = a.part + (size_t)((blockIdx.x * 2 + ((int)blockIdx.x == c_first ? 1 : 0)) * 2 + t) * Cfg::kPart;
+        const bool whole = take == e.nb;
+        // (an item that began in the share before leaves its part in the CTA's first place, one that goes on in its second)
+        float *part = a.part + (size_t)((blockIdx.x * 2 + (blk == 0 ? 1 : 0)) * 2 + (keys ? 0 : t)) * Cfg::kPart;
+        float f_own = 1.f, f_other = 0.f;
+        bool any_other = false;
+        if (keys) {
+          // the other tile has the same rows: its reference and sum through shared memory, its O from tensor memory
+          float2 *ml = reinterpret_cast<float2 *>(stage);
+          ml[lane] = make_float2(m, l);
+          if (lane == 0) ml[32].x = any ? 1.f : 0.f;
+          tc_fence_before();
+          named_sync(1, 256);
+          tc_fence_after();
+          const float2 *other = reinterpret_cast<const float2 *>(s_stage + (warp ^ 4) * 4096);
+          const float mo = other[lane].x, lo_sum = other[lane].y;
+          any_other = other[32].x != 0.f;
+          named_sync(1, 256);
+          const float mj = fmaxf(m, mo), bm = mj == -INFINITY ? 0.f : mj;
+          f_own = ex2(m - bm);
+          f_other = ex2(mo - bm);
+          l = l * f_own + lo_sum * f_other;
+          m = mj;
+        }
         const float inv = l > 0.f ? 1.f / l : 0.f;
+        const uint32_t other_o = tm_o + (1 - t) * D + lanes;
+        // with `keys` the tiles share the columns out (D = 64: tile 0 takes them)
+        const int c_begin = keys ? t * 64 : 0, c_end = keys ? min(D, (t + 1) * 64) : D;
 #pragma unroll 1
-        for (int c = 0; c < D; c += 64) {
-          uint32_t (&o)[2][32] = x;
-          load_o(c, o);
-          if (any && c + 64 == D) {                           // O_t is free
+        for (int c = c_begin; c < c_end; c += 64) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (any) {
+              tmem_ld32(to + c + i * 32, x[i]);
+              tmem_ld_wait();
+            } else {
+#pragma unroll
+              for (int z = 0; z < 32; ++z) x[i][z] = 0u;
+            }
+            if (keys) {
+              uint32_t y[32];
+              if (any_other) {
+                tmem_ld32(other_o + c + i * 32, y);
+                tmem_ld_wait();
+              } else {
+#pragma unroll
+                for (int z = 0; z < 32; ++z) y[z] = 0u;
+              }
+#pragma unroll
+              for (int z = 0; z < 32; ++z)
+                x[i][z] = __float_as_uint(__uint_as_float(x[i][z]) * f_own + __uint_as_float(y[z]) * f_other);
+            }
+          }
+          if (!keys && any && c + 64 == D) {                  // O_t is free
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(o_empty(t));
           }
           if (whole) {
-            emit(c, o, inv);
+            emit(c, x, inv);
           } else if (valid) {
 #pragma unroll
-            for (int i = 0; i < 64; ++i) part[256 + (c + i) * 128 + row] = __uint_as_float(o[i >> 5][i & 31]);
+            for (int i = 0; i < 64; ++i) part[256 + (c + i) * 128 + row] = __uint_as_float(x[i >> 5][i & 31]);
           }
         }
-        if (whole) {
-          store_lse(m, l);
-        } else {
-          part[row] = m;
-          part[128 + row] = l;
-          __threadfence();
-          named_sync(1 + t, 128);
-          if (row == 0) {
-            uint32_t *cnt = a.arrive + ((size_t)w.k * a.n_kv + head) * 2 + t;
-            const bool last = atomicAdd(cnt, 1u) == (uint32_t)(c_last - c_first);
-            if (last) *cnt = 0u;
-            s_last[t] = last;
-            __threadfence();
+        if (keys) {                                           // both have read both
+          tc_fence_before();
+          named_sync(1, 256);
+          if (any && lane == 0) mbar_arrive(o_empty(t));
+        }
+        if (!keys || t == 0) {
+          if (whole) {
+            store_lse(m, l);
+          } else {
+            part[row] = m;
+            part[128 + row] = l;
           }
-          named_sync(1 + t, 128);
-          if (s_last[t]) {
-            auto part_of = [&](int c) { return a.part + (size_t)((c * 2 + (c == c_first ? 1 : 0)) * 2 + t) * Cfg::kPart; };
-            float mm = -INFINITY, ll = 0.f;
-#pragma unroll 4
-            for (int c = c_first; c <= c_last; ++c) {
-              const float mc = __ldcg(part_of(c) + row), lc = __ldcg(part_of(c) + 128 + row);
-              const float mn = fmaxf(mm, mc), bm = mn == -INFINITY ? 0.f : mn;
-              ll = ll * ex2(mm - bm) + lc * ex2(mc - bm);
-              mm = mn;
-            }
-            const float bm = mm == -INFINITY ? 0.f : mm, inv_all = ll > 0.f ? 1.f / ll : 0.f;
-#pragma unroll 1
-            for (int c0 = 0; c0 < D; c0 += 64) {
-              uint32_t (&o)[2][32] = x;
-#pragma unroll
-              for (int i = 0; i < 64; ++i) o[i >> 5][i & 31] = 0u;
-              if (valid)
-#pragma unroll 1
-                for (int c = c_first; c <= c_last; ++c) {
-                  const float *pc = part_of(c);
-                  const float f = ex2(__ldcg(pc + row) - bm);
-#pragma unroll
-                  for (int i = 0; i < 64; ++i)
-                    o[i >> 5][i & 31] = __float_as_uint(fmaf(f, __ldcg(pc + 256 + (c0 + i) * 128 + row), __uint_as_float(o[i >> 5][i & 31])));
-                }
-              emit(c0, o, inv_all);
-            }
-            store_lse(mm, ll);
-          }
-          named_sync(1 + t, 128);        // s_last is free again
         }
       }
     }
@@ -609,6 +631,57 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
+}
+
+// Joins the parts of the items that several CTAs of the tiled kernel shared, in the order of the CTAs:
+//   m = max_c m_c, out = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c.
+// Block (c, y): the item that began in CTA c - 1 and goes on in CTA c (none, mostly), tile y / (D/16), 16 of its columns;
+// a thread owns a row, so the parts, kept by column, are read in whole lines.  A launch of its own: one CTA joining an item
+// that all 148 share (19 MB of parts) took 60 us and more.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(128) attn_join_kernel(const AttnFwdArgs a) {
+  using Cfg = TileCfg<D>;
+  const AttnPlanHdr hdr = *a.w.hdr;
+  const int c = blockIdx.x + 1, t = blockIdx.y / (D / 16), c0 = (blockIdx.y % (D / 16)) * 16, row = threadIdx.x;
+  if ((long long)c * hdr.tile_quota >= hdr.tile_units) return;
+  const AttnStart st = a.w.tile_start[c];
+  const AttnEntry &e = st.e;
+  const int u = e.unit0 * a.n_kv + st.head * (e.nb + kTileCost) + kTileCost;
+  if (st.blk == 0 || u / hdr.tile_quota != c - 1) return;
+  const int tokens = kTileRows / a.group, tok = row / a.group;
+  const int last = (u + e.nb - 1) / hdr.tile_quota;
+  if (tok >= min(tokens, e.n_tok - t * tokens)) return;
+  auto part_of = [&](int i) { return a.part + (size_t)((i * 2 + (i == c - 1 ? 1 : 0)) * 2 + t) * Cfg::kPart; };
+  float mm = -INFINITY, ll = 0.f;
+#pragma unroll 4
+  for (int i = c - 1; i <= last; ++i) {
+    const float mc = part_of(i)[row], lc = part_of(i)[128 + row];
+    const float mn = fmaxf(mm, mc), bm = mn == -INFINITY ? 0.f : mn;
+    ll = ll * ex2(mm - bm) + lc * ex2(mc - bm);
+    mm = mn;
+  }
+  const float bm = mm == -INFINITY ? 0.f : mm, inv = ll > 0.f ? 1.f / ll : 0.f;
+  float acc[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+#pragma unroll 2
+  for (int i = c - 1; i <= last; ++i) {
+    const float *pc = part_of(i);
+    const float f = ex2(pc[row] - bm);
+#pragma unroll
+    for (int x = 0; x < 16; ++x) acc[x] = fmaf(f, pc[256 + (c0 + x) * 128 + row], acc[x]);
+  }
+  const long long tg = e.tok0 + t * tokens + tok;
+  const int hq = st.head * a.group + row - tok * a.group;
+  uint4 *dst = reinterpret_cast<uint4 *>(a.out + tg * a.out_stride + hq * D + c0);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t v[4];
+#pragma unroll
+    for (int z = 0; z < 4; ++z) v[z] = pack_pair<BF16>(acc[i * 8 + 2 * z] * inv, acc[i * 8 + 2 * z + 1] * inv);
+    dst[i] = make_uint4(v[0], v[1], v[2], v[3]);
+  }
+  if (a.lse && c0 == 0) a.lse[tg * a.n_q + hq] = ll > 0.f ? (mm + log2f(ll)) * 0.693147180559945f : -INFINITY;
 }
 
 }  // namespace ftmoe
