@@ -102,8 +102,10 @@ class FtAttn:
         self.cfg = cfg
         self._h = C.c_void_p()
         _check(self._lib.ft_attn_create(C.byref(cfg), C.byref(self._h)), "ft_attn_create")
-        self._device = torch.device("cuda", cfg.device)
+        self._index, self._device = cfg.device, torch.device("cuda", cfg.device)
         self._dtype = torch.bfloat16 if cfg.dtype == FT_ATTN_BF16 else torch.float16
+        self._max_pages, self._n_pages, self._hq, self._hkv, self._d = cfg.max_pages, cfg.n_pages, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
+        self._n_req = self._rows = None
         self._cache_shape = (cfg.n_pages, 2, cfg.n_kv_heads, cfg.page_tokens, cfg.head_dim)
 
     def destroy(self):
@@ -120,19 +122,19 @@ class FtAttn:
     # ---- checks ---------------------------------------------------------------------
     def _stream(self, s):
         if s is None:
-            return torch.cuda.current_stream(self._device).cuda_stream
+            return torch._C._cuda_getCurrentRawStream(self._index)     # (torch.cuda.current_stream builds an object: 1 us)
         return s if isinstance(s, int) else s.cuda_stream
 
     def _vec(self, where, name, t, n, dtype=torch.int32):
         """Address of a contiguous device vector of at least n elements."""
-        if t.dtype != dtype or t.device != self._device or not t.is_contiguous() or t.numel() < n:
+        if t.dtype is not dtype or t.get_device() != self._index or not t.is_contiguous() or t.numel() < n:
             raise FtAttnError(FT_ERR_INVALID_ARG, where, f"{name}: contiguous {dtype} tensor of >= {n} elements on {self._device}")
         return t.data_ptr()
 
     def _heads(self, where, name, t, rows, heads):
         """(address, row stride) of a [rows, heads, D] tensor whose heads are contiguous."""
-        d = self.cfg.head_dim
-        if t.dtype != self._dtype or t.device != self._device or t.shape != (rows, heads, d):
+        d = self._d
+        if t.dtype is not self._dtype or t.get_device() != self._index or t.shape != (rows, heads, d):
             raise FtAttnError(FT_ERR_INVALID_ARG, where, f"{name}: {self._dtype} [{rows}, {heads}, {d}] on {self._device}")
         s = t.stride()
         if s[2] != 1 or (s[1] != d and heads > 1):
@@ -140,15 +142,16 @@ class FtAttn:
         return t.data_ptr(), (s[0] if rows > 1 else heads * d)
 
     def _cache(self, where, t):
-        if t.dtype != self._dtype or t.device != self._device or t.shape != self._cache_shape or not t.is_contiguous():
+        if t.dtype is not self._dtype or t.get_device() != self._index or t.shape != self._cache_shape or not t.is_contiguous():
             raise FtAttnError(FT_ERR_INVALID_ARG, where, f"kv_cache: contiguous {self._dtype} {list(self._cache_shape)} on {self._device}")
         return t.data_ptr()
 
     def _table(self, where, t, n_req):
-        if (t.dtype != torch.int32 or t.device != self._device or t.dim() != 2 or t.shape[0] < n_req or
-                t.shape[1] != self.cfg.max_pages or (t.shape[1] > 1 and t.stride(1) != 1)):
-            raise FtAttnError(FT_ERR_INVALID_ARG, where, f"table: torch.int32 [>= {n_req}, {self.cfg.max_pages}] on {self._device}")
-        return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+        shape, stride = t.shape, t.stride()
+        if (t.dtype is not torch.int32 or t.get_device() != self._index or len(shape) != 2 or shape[0] < n_req or
+                shape[1] != self._max_pages or (shape[1] > 1 and stride[1] != 1)):
+            raise FtAttnError(FT_ERR_INVALID_ARG, where, f"table: torch.int32 [>= {n_req}, {self._max_pages}] on {self._device}")
+        return t.data_ptr(), (stride[0] if shape[0] > 1 else shape[1])
 
     # ---- the operators --------------------------------------------------------------
     def slots(self, new_len, ctx_len, table, free_pages, n_free, max_new, *, q_start, kv_len, n_free_out, admitted, position, slot,
@@ -161,7 +164,7 @@ class FtAttn:
         v = self._vec
         _check(self._lib.ft_attn_slots(
             self._h, r, t, max_new, v(w, "new_len", new_len, r), v(w, "ctx_len", ctx_len, r), tab, stride,
-            v(w, "free_pages", free_pages, self.cfg.n_pages), v(w, "n_free", n_free, 1), v(w, "q_start", q_start, r + 1),
+            v(w, "free_pages", free_pages, self._n_pages), v(w, "n_free", n_free, 1), v(w, "q_start", q_start, r + 1),
             v(w, "kv_len", kv_len, r), v(w, "n_free_out", n_free_out, 1), v(w, "admitted", admitted, r),
             v(w, "position", position, t), v(w, "slot", slot, t), self._stream(stream)), w)
         self._n_req = r
@@ -181,20 +184,19 @@ class FtAttn:
         """Norm of the query and key heads, rotation, cache write (``ft_attn_qk_rope``).  ``cos_sin`` is float32
         ``[max_pos, rot_dim]`` (cosines, then sines) or None for no rotation; ``w_q`` / ``w_k`` None for no norm."""
         w = "ft_attn_qk_rope"
-        c = self.cfg
         t = q.shape[0]
-        qp, qs = self._heads(w, "q", q, t, c.n_q_heads)
-        kp, ks = self._heads(w, "k", k, t, c.n_kv_heads)
-        vp, vs = self._heads(w, "v", v, t, c.n_kv_heads)
-        op, os_ = self._heads(w, "q_out", q_out, t, c.n_q_heads)
+        qp, qs = self._heads(w, "q", q, t, self._hq)
+        kp, ks = self._heads(w, "k", k, t, self._hkv)
+        vp, vs = self._heads(w, "v", v, t, self._hkv)
+        op, os_ = self._heads(w, "q_out", q_out, t, self._hq)
         csp, max_pos, rot = None, 0, 0
         if cos_sin is not None:
             if cos_sin.dim() != 2:
                 raise FtAttnError(FT_ERR_INVALID_ARG, w, "cos_sin: [max_pos, rot_dim]")
             max_pos, rot = cos_sin.shape
             csp = self._vec(w, "cos_sin", cos_sin, 1, torch.float32)
-        wq = None if w_q is None else self._vec(w, "w_q", w_q, c.head_dim, self._dtype)
-        wk = None if w_k is None else self._vec(w, "w_k", w_k, c.head_dim, self._dtype)
+        wq = None if w_q is None else self._vec(w, "w_q", w_q, self._d, self._dtype)
+        wk = None if w_k is None else self._vec(w, "w_k", w_k, self._d, self._dtype)
         _check(self._lib.ft_attn_qk_rope(self._h, t, qp, qs, kp, ks, vp, vs, wq, wk, eps, csp, max_pos, rot, 1 if interleaved else 0,
                                          self._vec(w, "position", position, t), self._vec(w, "slot", slot, t), op, os_,
                                          self._cache(w, kv_cache), self._stream(stream)), w)
@@ -203,16 +205,15 @@ class FtAttn:
         """Causal attention of the planned step's rows over the cache (``ft_attn_forward``); ``scale`` defaults to
         ``head_dim ** -0.5``, ``lse`` is float32 ``[T, n_q_heads]``."""
         w = "ft_attn_forward"
-        c = self.cfg
-        t = getattr(self, "_rows", None)
+        t = self._rows
         if t is None:
             raise FtAttnError(_b.FT_ERR_STATE, w)
-        qp, qs = self._heads(w, "q", q, t, c.n_q_heads)
-        op, os_ = self._heads(w, "out", out, t, c.n_q_heads)
+        qp, qs = self._heads(w, "q", q, t, self._hq)
+        op, os_ = self._heads(w, "out", out, t, self._hq)
         tab, stride = self._table(w, table, self._n_req)
-        lp = None if lse is None else self._vec(w, "lse", lse, t * c.n_q_heads, torch.float32)
+        lp = None if lse is None else self._vec(w, "lse", lse, t * self._hq, torch.float32)
         _check(self._lib.ft_attn_forward(self._h, qp, qs, self._cache(w, kv_cache), tab, stride, op, os_, lp,
-                                         c.head_dim ** -0.5 if scale is None else scale, self._stream(stream)), w)
+                                         self._d ** -0.5 if scale is None else scale, self._stream(stream)), w)
 
     def sync_status(self):
         return int(self._lib.ft_attn_sync_status(self._h))

@@ -147,6 +147,19 @@ ft_status_t launch_forward(ft_attn *h, AttnFwdArgs a, const void *cache, cudaStr
   return FT_OK;
 }
 
+template <int D, bool BF16>
+void launch_rope(const ft_attn *h, RopeArgs &a, bool wide, cudaStream_t st) {
+  const int heads = a.n_q + 2 * a.n_kv, lanes = wide ? D / 16 : D / 8;
+  // one head per lane group while that does not fill the GPU (2048 threads an SM), more, up to 8, where it fills it several
+  // times over: the token's cosines and sines are read once per group
+  const long long fill = (long long)a.T * heads * lanes / ((long long)h->sm_count * 2048);
+  a.heads_per_group = fill < 1 ? 1 : fill > 8 ? 8 : (int)fill;
+  const int parts = (heads + a.heads_per_group - 1) / a.heads_per_group;
+  const unsigned grid = (unsigned)(((long long)a.T * parts * lanes + 255) / 256);
+  if (wide) attn_rope_kernel<D, BF16, 8><<<grid, 256, 0, st>>>(a);
+  else attn_rope_kernel<D, BF16, 4><<<grid, 256, 0, st>>>(a);
+}
+
 ft_status_t allocate(ft_attn *h) {
   const ft_attn_config_t &c = h->cfg;
   FA_CUDA(cudaDeviceGetAttribute(&h->sm_count, cudaDevAttrMultiProcessorCount, c.device));
@@ -312,17 +325,13 @@ ft_status_t ft_attn_qk_rope(ft_attn_t *h, int T, const void *q, int64_t q_stride
   a.eps = eps; a.cos_sin = cos_sin; a.position = position; a.slot = slot;
   a.q_out = static_cast<uint16_t *>(q_out); a.cache = static_cast<uint16_t *>(kv_cache);
   a.status = h->status_dev;
-  a.heads_per_group = 4;
-  const int heads = a.n_q + 2 * a.n_kv, parts = (heads + a.heads_per_group - 1) / a.heads_per_group;
-  const long long threads = (long long)T * parts * (D / 8);
-  const unsigned grid = (unsigned)((threads + 255) / 256);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool bf = c.dtype == FT_ATTN_BF16;
-  if (D == 128) {
-    if (bf) attn_rope_kernel<128, true><<<grid, 256, 0, st>>>(a); else attn_rope_kernel<128, false><<<grid, 256, 0, st>>>(a);
-  } else {
-    if (bf) attn_rope_kernel<64, true><<<grid, 256, 0, st>>>(a); else attn_rope_kernel<64, false><<<grid, 256, 0, st>>>(a);
-  }
+  // 16-byte accesses where every address and the halves of the rotated part allow them
+  const bool wide = !(((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)w_q | (uintptr_t)w_k | (uintptr_t)q_out) & 15) &&
+                    !((q_stride | k_stride | v_stride | q_out_stride) & 7) && rot_dim % 16 == 0;
+  if (D == 128) bf ? launch_rope<128, true>(h, a, wide, st) : launch_rope<128, false>(h, a, wide, st);
+  else bf ? launch_rope<64, true>(h, a, wide, st) : launch_rope<64, false>(h, a, wide, st);
   h->launches += 1;
   FA_CUDA(cudaGetLastError());
   return FT_OK;

@@ -2,10 +2,10 @@
 // one pass.  Bound: HBM (each of the T x (Hq + 2 Hkv) x D elements is read once and written once) for many tokens,
 // latency for few.
 //   y = x * rsqrt(mean(x^2) + eps) * w;  (a, b) -> (a cos - b sin, b cos + a sin)
-// D/8 lanes share a head; a lane owns 8 elements such that both members of a rotated pair are its own (no exchange but
-// the sum of squares): 4 pairs (i, i + rot/2) as two 8-byte accesses D/16 lanes wide, or 8 neighbouring elements when
-// pairs are interleaved.  A lane group keeps the cosines and sines of its token in registers and walks over
-// `heads_per_group` heads, so that the table costs 1/heads_per_group of a read per head.
+// D/(2V) lanes share a head; a lane owns 2V elements such that both members of a rotated pair are its own (no exchange but
+// the sum of squares): V pairs (i, i + rot/2), or 2V neighbouring elements when pairs are interleaved.  V = 8 (16-byte
+// accesses) where alignment and rot allow it, else 4.  A lane group keeps the cosines and sines of its token in registers and
+// walks over `heads_per_group` heads, kUnroll of them in flight.
 #pragma once
 #include "common.cuh"
 
@@ -23,14 +23,14 @@ struct RopeArgs {
 };
 
 template <bool BF16>
-__device__ __forceinline__ void unpack4(uint2 v, float (&f)[4]) {
+__device__ __forceinline__ void unpack2(uint32_t v, float &a, float &b) {
   if (BF16) {
-    f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
-    f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
+    a = __uint_as_float(v << 16);
+    b = __uint_as_float(v & 0xffff0000u);
   } else {
-    const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&v.x));
-    const float2 b = __half22float2(*reinterpret_cast<const __half2 *>(&v.y));
-    f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&v));
+    a = f.x;
+    b = f.y;
   }
 }
 template <bool BF16>
@@ -43,72 +43,47 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
   return *reinterpret_cast<const uint32_t *>(&v);
 }
 
-template <int D, bool BF16>
+// V 16-bit elements as V/2 words; not through the read-only path, since the result may go where the input is.
+template <int V>
+__device__ __forceinline__ void load_elems(const uint16_t *p, uint32_t (&r)[V / 2]) {
+  if constexpr (V == 8)
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p));
+  else
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "l"(p));
+}
+template <int V>
+__device__ __forceinline__ void store_elems(uint16_t *p, const uint32_t (&r)[V / 2]) {
+  if constexpr (V == 8)
+    *reinterpret_cast<uint4 *>(p) = make_uint4(r[0], r[1], r[2], r[3]);
+  else
+    *reinterpret_cast<uint2 *>(p) = make_uint2(r[0], r[1]);
+}
+
+template <int D, bool BF16, int V>
 __global__ void __launch_bounds__(256) attn_rope_kernel(const RopeArgs a) {
-  constexpr int L = D / 8, kUnroll = 4;                // lanes per head; heads in flight per lane
+  constexpr int L = D / (2 * V), kUnroll = V == 8 ? 4 : 8;   // lanes per head; heads in flight per lane
   const int lane_in = threadIdx.x % L;
   const int heads = a.n_q + 2 * a.n_kv, parts = (heads + a.heads_per_group - 1) / a.heads_per_group;
   const long long group = ((long long)blockIdx.x * blockDim.x + threadIdx.x) / L;
   const int t = (int)(group / parts), part = (int)(group - (long long)t * parts);
   if (t >= a.T) return;
-  const uint32_t mask = ((L == 32 ? 0u : (1u << L)) - 1u) << ((threadIdx.x & 31) / L * L);
+  const uint32_t mask = ((1u << L) - 1u) << ((threadIdx.x & 31) / L * L);
 
-  // the lane's elements: off0 .. off0+3 and off1 .. off1+3
-  int off0, off1;
-  float c[4], s[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { c[i] = 1.f; s[i] = 0.f; }
-  int pos = a.position[t];
-  if (pos >= a.max_pos && a.rot_half > 0) {
-    if (lane_in == 0) atomicOr(a.status, kStatBadIndex);
-    pos = -1;
-  }
+  // the lane's elements: off0 .. off0+V-1 and off1 .. off1+V-1; its pairs from `pair` on (none: not rotated)
+  int off0, off1, pair;
   if (a.interleaved) {
-    off0 = lane_in * 8;
-    off1 = off0 + 4;
-    if (off0 < 2 * a.rot_half && pos >= 0) {           // pairs 4*lane .. 4*lane+3
-      const float4 cc = *reinterpret_cast<const float4 *>(a.cos_sin + (long long)pos * 2 * a.rot_half + lane_in * 4);
-      const float4 ss = *reinterpret_cast<const float4 *>(a.cos_sin + (long long)pos * 2 * a.rot_half + a.rot_half + lane_in * 4);
-      c[0] = cc.x; c[1] = cc.y; c[2] = cc.z; c[3] = cc.w;
-      s[0] = ss.x; s[1] = ss.y; s[2] = ss.z; s[3] = ss.w;
-    }
+    off0 = lane_in * 2 * V;
+    off1 = off0 + V;
+    pair = off0 < 2 * a.rot_half ? lane_in * V : -1;
   } else {
-    const int i = lane_in * 4;
-    if (i < a.rot_half) {
-      off0 = i;
-      off1 = i + a.rot_half;
-      if (pos >= 0) {
-        const float4 cc = *reinterpret_cast<const float4 *>(a.cos_sin + (long long)pos * 2 * a.rot_half + i);
-        const float4 ss = *reinterpret_cast<const float4 *>(a.cos_sin + (long long)pos * 2 * a.rot_half + a.rot_half + i);
-        c[0] = cc.x; c[1] = cc.y; c[2] = cc.z; c[3] = cc.w;
-        s[0] = ss.x; s[1] = ss.y; s[2] = ss.z; s[3] = ss.w;
-      }
-    } else {                                           // what is not rotated: the halves of [rot, D)
-      off0 = i + a.rot_half;
-      off1 = i + D / 2;
-    }
+    const int i = lane_in * V;
+    pair = i < a.rot_half ? i : -1;
+    off0 = pair >= 0 ? i : i + a.rot_half;            // what is not rotated: the halves of [rot, D)
+    off1 = pair >= 0 ? i + a.rot_half : i + D / 2;
   }
-  const int sl = a.slot[t];
-  const bool store_kv = sl >= 0 && sl < (a.n_pages << a.page_shift) && pos >= 0;
-  if (sl >= 0 && !(sl < (a.n_pages << a.page_shift)) && lane_in == 0) atomicOr(a.status, kStatBadIndex);
-  const long long page = sl >> a.page_shift, row = sl & ((1 << a.page_shift) - 1);
-
-  float wq[8], wk[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) { wq[i] = 1.f; wk[i] = 1.f; }
-  auto load_w = [&](const uint16_t *w, float (&f)[8]) {
-    float x0[4], x1[4];
-    unpack4<BF16>(*reinterpret_cast<const uint2 *>(w + off0), x0);
-    unpack4<BF16>(*reinterpret_cast<const uint2 *>(w + off1), x1);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { f[i] = x0[i]; f[4 + i] = x1[i]; }
-  };
-  if (a.w_q) load_w(a.w_q, wq);
-  if (a.w_k) load_w(a.w_k, wk);
-
-  const int h_end = min(heads, (part + 1) * a.heads_per_group);
-  for (int h0 = part * a.heads_per_group; h0 < h_end; h0 += kUnroll) {
-    uint2 r0[kUnroll], r1[kUnroll];
+  const int h_begin = part * a.heads_per_group, h_end = min(heads, h_begin + a.heads_per_group);
+  uint32_t r0[kUnroll][V / 2], r1[kUnroll][V / 2];
+  auto load = [&](int h0) {
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int h = h0 + u;
@@ -116,58 +91,101 @@ __global__ void __launch_bounds__(256) attn_rope_kernel(const RopeArgs a) {
       const uint16_t *src = h < a.n_q ? a.q + t * a.q_stride + h * D
                             : h < a.n_q + a.n_kv ? a.k + t * a.k_stride + (h - a.n_q) * D
                                                  : a.v + t * a.v_stride + (h - a.n_q - a.n_kv) * D;
-      r0[u] = *reinterpret_cast<const uint2 *>(src + off0);
-      r1[u] = *reinterpret_cast<const uint2 *>(src + off1);
+      load_elems<V>(src + off0, r0[u]);
+      load_elems<V>(src + off1, r1[u]);
     }
+  };
+  load(h_begin);
+
+  int pos = a.position[t];
+  const int sl = a.slot[t];
+  if (pos >= a.max_pos && a.rot_half > 0) {
+    if (lane_in == 0) atomicOr(a.status, kStatBadIndex);
+    pos = -1;
+  }
+  const bool store_kv = sl >= 0 && sl < (a.n_pages << a.page_shift) && pos >= 0;
+  if (sl >= (a.n_pages << a.page_shift) && lane_in == 0) atomicOr(a.status, kStatBadIndex);
+  const long long page = sl >> a.page_shift, row = sl & ((1 << a.page_shift) - 1);
+  float c[V], s[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) { c[i] = 1.f; s[i] = 0.f; }
+  if (pair >= 0 && pos >= 0) {
+    const float4 *cp = reinterpret_cast<const float4 *>(a.cos_sin + (long long)pos * 2 * a.rot_half + pair);
+    const float4 *sp = reinterpret_cast<const float4 *>(a.cos_sin + (long long)pos * 2 * a.rot_half + a.rot_half + pair);
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) {
+      const float4 cc = cp[i], ss = sp[i];
+      c[4 * i] = cc.x; c[4 * i + 1] = cc.y; c[4 * i + 2] = cc.z; c[4 * i + 3] = cc.w;
+      s[4 * i] = ss.x; s[4 * i + 1] = ss.y; s[4 * i + 2] = ss.z; s[4 * i + 3] = ss.w;
+    }
+  }
+  uint32_t wq0[V / 2], wq1[V / 2], wk0[V / 2], wk1[V / 2];     // (packed: read where they are used)
+  if (a.w_q) { load_elems<V>(a.w_q + off0, wq0); load_elems<V>(a.w_q + off1, wq1); }
+  if (a.w_k) { load_elems<V>(a.w_k + off0, wk0); load_elems<V>(a.w_k + off1, wk1); }
+
+  for (int h0 = h_begin; h0 < h_end; h0 += kUnroll) {
+    if (h0 > h_begin) load(h0);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int h = h0 + u;
       if (h >= h_end) break;
-      uint2 o0 = r0[u], o1 = r1[u];
       const bool is_q = h < a.n_q, is_v = h >= a.n_q + a.n_kv;
       if (!is_v) {
-        float x[8], x0[4], x1[4];
-        unpack4<BF16>(o0, x0);
-        unpack4<BF16>(o1, x1);
+        float x[2 * V], y[2 * V];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { x[i] = x0[i]; x[4 + i] = x1[i]; }
+        for (int i = 0; i < V / 2; ++i) {
+          unpack2<BF16>(r0[u][i], x[2 * i], x[2 * i + 1]);
+          unpack2<BF16>(r1[u][i], x[V + 2 * i], x[V + 2 * i + 1]);
+        }
         if (is_q ? a.w_q != nullptr : a.w_k != nullptr) {
           float sum = 0.f;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
+          for (int i = 0; i < 2 * V; ++i) sum = fmaf(x[i], x[i], sum);
 #pragma unroll
           for (int o = L / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(mask, sum, o);
           const float inv = rsqrtf(sum * (1.f / D) + a.eps);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = x[i] * inv * (is_q ? wq[i] : wk[i]);
+          for (int i = 0; i < V / 2; ++i) {
+            float w0, w1, w2, w3;
+            unpack2<BF16>(is_q ? wq0[i] : wk0[i], w0, w1);
+            unpack2<BF16>(is_q ? wq1[i] : wk1[i], w2, w3);
+            x[2 * i] *= inv * w0; x[2 * i + 1] *= inv * w1;
+            x[V + 2 * i] *= inv * w2; x[V + 2 * i + 1] *= inv * w3;
+          }
         }
-        float y[8];
         if (a.interleaved) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < V; ++i) {
             y[2 * i] = x[2 * i] * c[i] - x[2 * i + 1] * s[i];
             y[2 * i + 1] = x[2 * i + 1] * c[i] + x[2 * i] * s[i];
           }
         } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            y[i] = x[i] * c[i] - x[4 + i] * s[i];
-            y[4 + i] = x[4 + i] * c[i] + x[i] * s[i];
+          for (int i = 0; i < V; ++i) {
+            y[i] = x[i] * c[i] - x[V + i] * s[i];
+            y[V + i] = x[V + i] * c[i] + x[i] * s[i];
           }
         }
-        o0 = make_uint2(pack_pair<BF16>(y[0], y[1]), pack_pair<BF16>(y[2], y[3]));
-        o1 = make_uint2(pack_pair<BF16>(y[4], y[5]), pack_pair<BF16>(y[6], y[7]));
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+          r0[u][i] = pack_pair<BF16>(y[2 * i], y[2 * i + 1]);
+          r1[u][i] = pack_pair<BF16>(y[V + 2 * i], y[V + 2 * i + 1]);
+        }
       }
+      uint16_t *dst = nullptr;
       if (is_q) {
-        if (pos < 0) { o0 = make_uint2(0u, 0u); o1 = o0; }
-        uint16_t *dst = a.q_out + t * a.out_stride + h * D;
-        *reinterpret_cast<uint2 *>(dst + off0) = o0;
-        *reinterpret_cast<uint2 *>(dst + off1) = o1;
+        dst = a.q_out + t * a.out_stride + h * D;
+        if (pos < 0) {
+#pragma unroll
+          for (int i = 0; i < V / 2; ++i) r0[u][i] = r1[u][i] = 0u;
+        }
       } else if (store_kv) {
-        const int hk = h - a.n_q;            // keys 0 .. n_kv-1, values n_kv .. 2 n_kv-1: the cache's order
-        uint16_t *dst = a.cache + (((page * 2 * a.n_kv + hk) << a.page_shift) + row) * D;
-        *reinterpret_cast<uint2 *>(dst + off0) = o0;
-        *reinterpret_cast<uint2 *>(dst + off1) = o1;
+        // keys 0 .. n_kv-1, values n_kv .. 2 n_kv-1: the cache's order
+        dst = a.cache + (((page * 2 * a.n_kv + h - a.n_q) << a.page_shift) + row) * D;
+      }
+      if (dst) {
+        store_elems<V>(dst + off0, r0[u]);
+        store_elems<V>(dst + off1, r1[u]);
       }
     }
   }
