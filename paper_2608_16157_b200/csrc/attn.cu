@@ -122,6 +122,7 @@ bool make_query_map(const ft_attn *h, CUtensorMap *tm, const void *q, int64_t q_
 template <int D, bool BF16>
 cudaError_t allow_smem() {
   cudaError_t e = cudaFuncSetAttribute(attn_stream_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, StreamCfg<D>::kSmem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_rope_stream_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 / kRopeBlocks - 1024);
   if (e == cudaSuccess)
     e = cudaFuncSetAttribute(attn_tile_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, TileCfg<D>::kSmem);
   return e;
@@ -154,6 +155,14 @@ void launch_rope(const ft_attn *h, RopeArgs &a, bool wide, cudaStream_t st) {
   // times over: the token's cosines and sines are read once per group
   const long long fill = (long long)a.T * heads * lanes / ((long long)h->sm_count * 2048);
   a.heads_per_group = fill < 1 ? 1 : fill > 8 ? 8 : (int)fill;
+  // many tokens: resident blocks (kRopeBlocks an SM), a lane group for every head or every second, third, ... one
+  const int stage = rope_stage_bytes(heads, D, 2 * a.rot_half), smem = kRopeStages * stage + 2 * kRopeStages * 8 + 16;
+  if (wide && fill >= 1 && smem <= 232448 / kRopeBlocks - 1024) {
+    const int passes = (heads * lanes + 511) / 512, consumers = ((heads + passes - 1) / passes * lanes + 31) / 32 * 32;
+    const long long blocks = (long long)h->sm_count * kRopeBlocks;
+    attn_rope_stream_kernel<D, BF16><<<(unsigned)(a.T < blocks ? a.T : blocks), consumers + 32, smem, st>>>(a);
+    return;
+  }
   const int parts = (heads + a.heads_per_group - 1) / a.heads_per_group;
   const unsigned grid = (unsigned)(((long long)a.T * parts * lanes + 255) / 256);
   if (wide) attn_rope_kernel<D, BF16, 8><<<grid, 256, 0, st>>>(a);

@@ -4,9 +4,13 @@
 //   y = x * rsqrt(mean(x^2) + eps) * w;  (a, b) -> (a cos - b sin, b cos + a sin)
 // D/(2V) lanes share a head; a lane owns 2V elements such that both members of a rotated pair are its own (no exchange but
 // the sum of squares): V pairs (i, i + rot/2), or 2V neighbouring elements when pairs are interleaved.  V = 8 (16-byte
-// accesses) where alignment and rot allow it, else 4.  A lane group keeps the cosines and sines of its token in registers and
-// walks over `heads_per_group` heads, kUnroll of them in flight.
+// accesses) where alignment and rot allow it, else 4.
+// Two forms.  Few tokens: a lane group keeps the cosines and sines of its token in registers and walks over
+// `heads_per_group` heads.  Many tokens: resident blocks, to whose shared memory a producer warp brings whole tokens and their
+// table rows with bulk copies, several tokens ahead (the position is only known after a load, the table row after another:
+// held in registers meanwhile, the data of too few tokens is on its way: 84 us against a copy's 55 us for 16384 tokens).
 #pragma once
+#include "async.cuh"
 #include "common.cuh"
 
 namespace ftmoe {
@@ -21,6 +25,29 @@ struct RopeArgs {
   uint16_t *q_out, *cache;
   uint32_t *status;
 };
+
+// Two floats in a register pair: one instruction for both.
+__device__ __forceinline__ uint64_t f2(float lo, float hi) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+  return v;
+}
+__device__ __forceinline__ void f2_split(uint64_t v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 
 template <bool BF16>
 __device__ __forceinline__ void unpack2(uint32_t v, float &a, float &b) {
@@ -189,6 +216,174 @@ __global__ void __launch_bounds__(256) attn_rope_kernel(const RopeArgs a) {
       }
     }
   }
+}
+
+// The form for many tokens.  Dynamic shared memory: stages of [q row | k row | v row | table row], then the barriers.
+constexpr int kRopeStages = 5, kRopeBlocks = 2;    // tokens ahead in a block, blocks an SM
+__host__ __device__ inline int rope_stage_bytes(int heads, int D, int rot) { return (heads * D * 2 + rot * 4 + 127) / 128 * 128; }
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(544) attn_rope_stream_kernel(const RopeArgs a) {
+  constexpr int V = 8, L = D / (2 * V);
+  extern __shared__ __align__(128) unsigned char smem[];
+  const int heads = a.n_q + 2 * a.n_kv, stage = rope_stage_bytes(heads, D, 2 * a.rot_half);
+  uint64_t *s_bar = reinterpret_cast<uint64_t *>(smem + kRopeStages * stage);
+  volatile int *s_abort = reinterpret_cast<volatile int *>(s_bar + 2 * kRopeStages);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, consumers = blockDim.x - 32;
+  const uint32_t base = smem_u32(smem), bars = smem_u32(s_bar);
+  auto full_bar = [&](int s) { return bars + 8u * s; };
+  auto empty_bar = [&](int s) { return bars + 8u * (kRopeStages + s); };
+  if (tid == 0) {
+    for (int s = 0; s < kRopeStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), consumers / 32); }
+    *s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  __syncthreads();
+  const int q_bytes = a.n_q * D * 2, kv_bytes = a.n_kv * D * 2, step = gridDim.x;
+  int s = 0;
+  uint32_t ph = 0;
+  auto advance = [&]() { if (++s == kRopeStages) { s = 0; ph ^= 1u; } };
+
+  if (warp == consumers / 32) {
+    // ------------------------------ producer: positions 32 tokens at a time ------------------------------
+    for (int t0 = blockIdx.x; t0 < a.T && !*s_abort; t0 += 32 * step) {
+      const int pos = t0 + lane * step < a.T ? a.position[t0 + lane * step] : -1;
+      for (int i = 0; i < 32 && t0 + i * step < a.T; ++i) {
+        const long long t = t0 + i * step;
+        const int p = __shfl_sync(0xffffffffu, pos, i);
+        const bool table = a.rot_half > 0 && p >= 0 && p < a.max_pos;
+        mbar_wait(empty_bar(s), ph ^ 1u, s_abort, a.status);
+        if (*s_abort) break;
+        if (lane == 0) {
+          const uint32_t dst = base + s * stage;
+          mbar_expect_tx(full_bar(s), q_bytes + 2 * kv_bytes + (table ? 8 * a.rot_half : 0));
+          bulk_g2s(dst, a.q + t * a.q_stride, q_bytes, full_bar(s));
+          bulk_g2s(dst + q_bytes, a.k + t * a.k_stride, kv_bytes, full_bar(s));
+          bulk_g2s(dst + q_bytes + kv_bytes, a.v + t * a.v_stride, kv_bytes, full_bar(s));
+          if (table) bulk_g2s(dst + q_bytes + 2 * kv_bytes, a.cos_sin + (long long)p * 2 * a.rot_half, 8 * a.rot_half, full_bar(s));
+        }
+        __syncwarp();
+        advance();
+      }
+    }
+    abort_drain(s_abort);
+    return;
+  }
+
+  // ------------------------------ consumers: one head's lane group each, some more than one head ------------------------------
+  const int lane_in = tid % L, groups = consumers / L;
+  const uint32_t mask = ((1u << L) - 1u) << (lane / L * L);
+  int off0, off1, pair;
+  if (a.interleaved) {
+    off0 = lane_in * 2 * V;
+    off1 = off0 + V;
+    pair = off0 < 2 * a.rot_half ? lane_in * V : -1;
+  } else {
+    const int i = lane_in * V;
+    pair = i < a.rot_half ? i : -1;
+    off0 = pair >= 0 ? i : i + a.rot_half;
+    off1 = pair >= 0 ? i + a.rot_half : i + D / 2;
+  }
+  uint32_t w0[V / 2], w1[V / 2];               // norm weights of the head at hand
+  const uint16_t *w_now = nullptr;
+  int pos_next = blockIdx.x < a.T ? a.position[blockIdx.x] : 0, slot_next = blockIdx.x < a.T ? a.slot[blockIdx.x] : 0;
+  for (long long t = blockIdx.x; t < a.T; t += step) {
+    int pos = pos_next;
+    const int sl = slot_next;
+    if (t + step < a.T) { pos_next = a.position[t + step]; slot_next = a.slot[t + step]; }
+    if (pos >= a.max_pos && a.rot_half > 0) {
+      if (tid == 0) atomicOr(a.status, kStatBadIndex);
+      pos = -1;
+    }
+    const bool store_kv = sl >= 0 && sl < (a.n_pages << a.page_shift) && pos >= 0;
+    if (sl >= (a.n_pages << a.page_shift) && tid == 0) atomicOr(a.status, kStatBadIndex);
+    const long long page = sl >> a.page_shift, row = sl & ((1 << a.page_shift) - 1);
+    const bool ok = mbar_wait(full_bar(s), ph, s_abort, a.status);
+    const unsigned char *st = smem + s * stage;
+    if (ok)
+      for (int h = tid / L; h < heads; h += groups) {
+        const bool is_q = h < a.n_q, is_v = h >= a.n_q + a.n_kv;
+        uint16_t *dst = nullptr;
+        if (is_q) dst = a.q_out + t * a.out_stride + h * D;
+        else if (store_kv) dst = a.cache + (((page * 2 * a.n_kv + h - a.n_q) << a.page_shift) + row) * D;
+        if (!dst) continue;                    // (the same for the lanes of the group)
+        const uint16_t *src = reinterpret_cast<const uint16_t *>(st) + h * D;
+        uint4 v0 = *reinterpret_cast<const uint4 *>(src + off0), v1 = *reinterpret_cast<const uint4 *>(src + off1);
+        if (!is_v) {
+          uint32_t r0[4] = {v0.x, v0.y, v0.z, v0.w}, r1[4] = {v1.x, v1.y, v1.z, v1.w};
+          uint64_t x0[4], x1[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float p, q;
+            unpack2<BF16>(r0[i], p, q);
+            x0[i] = f2(p, q);
+            unpack2<BF16>(r1[i], p, q);
+            x1[i] = f2(p, q);
+          }
+          const uint16_t *w = is_q ? a.w_q : a.w_k;
+          if (w) {
+            if (w != w_now) { load_elems<V>(w + off0, w0); load_elems<V>(w + off1, w1); w_now = w; }
+            uint64_t acc0 = 0, acc1 = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { acc0 = fma2(x0[i], x0[i], acc0); acc1 = fma2(x1[i], x1[i], acc1); }
+            float p, q;
+            f2_split(add2(acc0, acc1), p, q);
+            float sum = p + q;
+#pragma unroll
+            for (int o = L / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(mask, sum, o);
+            const float inv = rsqrtf(sum * (1.f / D) + a.eps);
+            const uint64_t inv2 = f2(inv, inv);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              unpack2<BF16>(w0[i], p, q);
+              x0[i] = mul2(x0[i], mul2(inv2, f2(p, q)));
+              unpack2<BF16>(w1[i], p, q);
+              x1[i] = mul2(x1[i], mul2(inv2, f2(p, q)));
+            }
+          }
+          if (pair >= 0 && pos >= 0) {
+            const float *cp = reinterpret_cast<const float *>(st + q_bytes + 2 * kv_bytes) + pair, *sp = cp + a.rot_half;
+            if (a.interleaved) {
+              // a register pair is (a, b) of one pair: (a, b) cos + (b, a) (-sin, sin)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                float p, q;
+                f2_split(x0[i], p, q);
+                x0[i] = f2(p * cp[i] - q * sp[i], q * cp[i] + p * sp[i]);
+                f2_split(x1[i], p, q);
+                x1[i] = f2(p * cp[4 + i] - q * sp[4 + i], q * cp[4 + i] + p * sp[4 + i]);
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const ulonglong2 c = *reinterpret_cast<const ulonglong2 *>(cp + 4 * i), z = *reinterpret_cast<const ulonglong2 *>(sp + 4 * i);
+                const uint64_t sign = 0x8000000080000000ull;
+                const uint64_t a0 = fma2(x0[2 * i], c.x, mul2(x1[2 * i], z.x) ^ sign), b0 = fma2(x0[2 * i], z.x, mul2(x1[2 * i], c.x));
+                const uint64_t a1 = fma2(x0[2 * i + 1], c.y, mul2(x1[2 * i + 1], z.y) ^ sign), b1 = fma2(x0[2 * i + 1], z.y, mul2(x1[2 * i + 1], c.y));
+                x0[2 * i] = a0; x1[2 * i] = b0; x0[2 * i + 1] = a1; x1[2 * i + 1] = b1;
+              }
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float p, q;
+            f2_split(x0[i], p, q);
+            r0[i] = pack_pair<BF16>(p, q);
+            f2_split(x1[i], p, q);
+            r1[i] = pack_pair<BF16>(p, q);
+          }
+          v0 = pos < 0 ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(r0[0], r0[1], r0[2], r0[3]);
+          v1 = pos < 0 ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(r1[0], r1[1], r1[2], r1[3]);
+        }
+        *reinterpret_cast<uint4 *>(dst + off0) = v0;
+        *reinterpret_cast<uint4 *>(dst + off1) = v1;
+      }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(empty_bar(s));
+    advance();
+  }
+  abort_drain(s_abort);
 }
 
 }  // namespace ftmoe

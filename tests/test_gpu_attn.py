@@ -148,6 +148,47 @@ def test_qk_rope(dtype, hq, hkv, d, rot, inter, norm):
         h.destroy()
 
 
+@pytest.mark.parametrize("dtype,hq,hkv,d,rot,inter,norm,t", [
+    ("bf16", 32, 4, 128, 128, False, True, 1003), ("fp16", 64, 8, 64, 32, True, True, 1500), ("bf16", 3, 1, 64, 64, False, False, 15200),
+    ("fp16", 96, 8, 128, 48, False, True, 700), ("bf16", 8, 8, 128, 0, False, True, 1700)])
+def test_qk_rope_many_tokens(dtype, hq, hkv, d, rot, inter, norm, t):
+    """Enough tokens for the kernel that brings whole tokens to shared memory; rows with padding between them."""
+    dt, page = R.DT[dtype], 64
+    g = torch.Generator().manual_seed(t)
+    n_pages = R.ceil_div(t, page) + 2
+    qkv = torch.randn(t, (hq + 2 * hkv) * d + 16, generator=g).to(dt)
+    cs = torch.randn(300, rot, generator=g) if rot else None
+    pos = torch.randint(0, 300, (t,), generator=g, dtype=torch.int32)
+    slot = torch.randperm(n_pages * page, generator=g)[:t].to(torch.int32)
+    pos[::7], slot[::7], slot[3::11] = -1, -1, -1
+    w_q = (1 + 0.5 * torch.randn(d, generator=g)).to(dt) if norm else None
+    w_k = (1 + 0.5 * torch.randn(d, generator=g)).to(dt) if norm else None
+    cut = lambda x: (x[:, :hq * d].unflatten(1, (hq, d)), x[:, hq * d:(hq + hkv) * d].unflatten(1, (hkv, d)),
+                     x[:, (hq + hkv) * d:(hq + 2 * hkv) * d].unflatten(1, (hkv, d)))
+    dev = lambda x: None if x is None else x.to(DEV)
+    h = A.FtAttn(A.make_config(n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_tokens=page, n_pages=n_pages, max_requests=1, max_tokens=t,
+                               max_pages=4, dtype=dtype))
+    qd, kd, vd = cut(dev(qkv))
+    out, cache = torch.full((t, hq, d), 7.0, dtype=dt, device=DEV), torch.full((n_pages, 2, hkv, page, d), 3.0, dtype=dt, device=DEV)
+    h.qk_rope(qd, kd, vd, out, cache, dev(pos), dev(slot), dev(cs), w_q=dev(w_q), w_k=dev(w_k), eps=1e-5, interleaved=inter)
+    assert h.sync_status() == 0
+    q, k, v = cut(qkv)
+    yq, mq = R.norm_rope(q, w_q, cs, pos, 1e-5, inter)
+    yk, mk = R.norm_rope(k, w_k, cs, pos, 1e-5, inter)
+    bound = lambda y, m: R.UNIT[dtype] * y.abs() + 2.0 ** -20 * m + (2.0 ** -25 if dtype == "fp16" else 1e-38)
+    want = yq * (pos >= 0)[:, None, None]
+    assert ((out.double().cpu() - want).abs() <= bound(yq, mq)).all()
+    gc = cache.cpu().permute(0, 3, 1, 2, 4).reshape(n_pages * page, 2, hkv, d)
+    kept = slot >= 0
+    rows = gc[slot[kept].long()]
+    assert ((rows[:, 0].double() - yk[kept]).abs() <= bound(yk[kept], mk[kept])).all()
+    assert torch.equal(rows[:, 1], v[kept])
+    other = torch.ones(n_pages * page, dtype=torch.bool)
+    other[slot[kept].long()] = False
+    assert (gc[other] == 3.0).all()
+    h.destroy()
+
+
 def test_qk_rope_bad_indices_are_latched_and_skipped():
     hq, hkv, d, page, n_pages = 4, 2, 64, 16, 3
     h = A.FtAttn(A.make_config(n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_tokens=page, n_pages=n_pages, max_requests=1, max_tokens=8, max_pages=4))
