@@ -222,9 +222,12 @@ ft_status_t launch_slots(ft_attn *h, AttnSlotsArgs &a, cudaStream_t st) {
   a.w = h->work;
   a.g = h->geom;
   a.status = h->status_dev;
-  // block 0 keeps the requests and the work partition; the others share the tokens and pages, 2048 tokens each
-  const int grid = a.own_tables ? 1 : 2 + (a.T - 1) / 2048;
-  if (a.n_req <= 256) attn_slots_kernel<256><<<grid, 256, 0, st>>>(a);
+  // block 0 keeps the requests and the work partition; the others share the tokens and pages, a token a thread while there are
+  // SMs for that (a token waits for two loads, one after the other)
+  const int threads = a.n_req <= 256 ? 256 : 1024;
+  const int blocks = 1 + (a.T > 1 ? a.T - 1 : 0) / threads;
+  const int grid = a.own_tables ? 1 : 1 + (blocks < h->sm_count - 1 ? blocks : h->sm_count - 1);
+  if (threads == 256) attn_slots_kernel<256><<<grid, 256, 0, st>>>(a);
   else attn_slots_kernel<1024><<<grid, 1024, 0, st>>>(a);
   h->launches += 1;
   FA_CUDA(cudaGetLastError());

@@ -13,6 +13,7 @@
 namespace ftmoe {
 
 constexpr int kAttnMaxRequests = 1024;
+constexpr int kUnitCache = 2048;       // entries whose positions a work partition keeps in shared memory while it is made
 constexpr int kAttnMaxGrid = 512;      // CTAs a work partition can address
 constexpr int kDecRows = 16;           // query rows (tokens x heads of a group) the streaming kernel takes
 constexpr int kDecKeys = 64;           // keys of one of its work units
@@ -99,12 +100,13 @@ __device__ __forceinline__ int count_le(const int32_t *a, int n, int v) {
   return lo;
 }
 
-// The first block at or behind position u in a list of `n` entries.
-__device__ __forceinline__ AttnStart locate_unit(const AttnEntry *e, int n, int n_kv, int cost, int u) {
+// The first block at or behind position u in a list of `n` entries, whose unit0 are also in `units` as far as that goes (null:
+// too many).
+__device__ __forceinline__ AttnStart locate_unit(const AttnEntry *e, const int32_t *units, int n, int n_kv, int cost, int u) {
   int lo = 0, hi = n;                     // largest entry with unit0 * n_kv <= u
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (e[mid].unit0 * n_kv <= u) lo = mid; else hi = mid;
+    if ((units ? units[mid] : e[mid].unit0) * n_kv <= u) lo = mid; else hi = mid;
   }
   AttnStart s;
   s.e = e[lo];
@@ -146,7 +148,7 @@ __device__ __forceinline__ void block_range(int pos0, int n, int window, int key
 // The work partition, by one block; thread r owns request r (n rows from packed row tok0, kv cached tokens).
 template <int NT>
 __device__ void build_work(const AttnSlotsArgs &a, int n, int tok0, int kv, unsigned long long *s_warp, int32_t *s_tile,
-                           const int32_t *s_q, const int32_t *s_kv) {
+                           const int32_t *s_q, const int32_t *s_kv, int32_t *s_dec, int32_t *s_unit) {
   const int tid = threadIdx.x;
   const AttnGeom &g = a.g;
   const bool dec = n > 0 && n * g.group <= kDecRows;
@@ -161,6 +163,7 @@ __device__ void build_work(const AttnSlotsArgs &a, int n, int tok0, int kv, unsi
     e.req = tid; e.tok0 = tok0; e.n_tok = n; e.pos0 = kv - n; e.b0 = b0; e.nb = nb;
     e.unit0 = (int)(inc >> 32) - w; e.pad = 0;
     a.w.dec[(uint32_t)inc - 1] = e;
+    s_dec[(uint32_t)inc - 1] = e.unit0;
   }
   const int tiles = (n > 0 && !dec) ? (n + g.tile_tokens - 1) / g.tile_tokens : 0;
   const unsigned long long tinc = block_scan<NT>((unsigned long long)tiles, s_warp, &tot);
@@ -182,6 +185,7 @@ __device__ void build_work(const AttnSlotsArgs &a, int n, int tok0, int kv, unsi
     if (t < n_tile) {
       e.unit0 = carry + (int)ui - w;
       a.w.tile[t] = e;
+      if (t < kUnitCache) s_unit[t] = e.unit0;
     }
     carry += (int)tot;
   }
@@ -197,16 +201,16 @@ __device__ void build_work(const AttnSlotsArgs &a, int n, int tok0, int kv, unsi
   }
   __syncthreads();
   for (int c = tid; c < g.dec_grid; c += NT)
-    if ((long long)c * dec_quota < dec_units) a.w.dec_start[c] = locate_unit(a.w.dec, n_dec, g.n_kv, kDecCost, c * dec_quota);
+    if ((long long)c * dec_quota < dec_units) a.w.dec_start[c] = locate_unit(a.w.dec, s_dec, n_dec, g.n_kv, kDecCost, c * dec_quota);
   for (int c = tid; c < g.tile_grid; c += NT)
-    if ((long long)c * tile_quota < tile_units) a.w.tile_start[c] = locate_unit(a.w.tile, n_tile, g.n_kv, kTileCost, c * tile_quota);
+    if ((long long)c * tile_quota < tile_units) a.w.tile_start[c] = locate_unit(a.w.tile, n_tile <= kUnitCache ? s_unit : nullptr, n_tile, g.n_kv, kTileCost, c * tile_quota);
 }
 
 // NT >= n_req: 256 threads for up to 256 requests, 1024 above.
 template <int NT>
 __global__ void __launch_bounds__(NT) attn_slots_kernel(const AttnSlotsArgs a) {
   __shared__ unsigned long long s_warp[NT / 32];
-  __shared__ int32_t s_q[NT + 1], s_ctx[NT], s_held[NT], s_freed[NT], s_need[NT], s_kv[NT], s_adm[NT];
+  __shared__ int32_t s_q[NT + 1], s_ctx[NT], s_held[NT], s_freed[NT], s_need[NT], s_kv[NT], s_adm[NT], s_unit[kUnitCache];
   const int tid = threadIdx.x, r = tid;
   unsigned long long tot;
 
@@ -225,7 +229,7 @@ __global__ void __launch_bounds__(NT) attn_slots_kernel(const AttnSlotsArgs a) {
       s_kv[r] = kv;
       if (r == a.n_req - 1) s_q[a.n_req] = q1;
     }
-    build_work<NT>(a, n, q0, kv, s_warp, s_freed, s_q, s_kv);
+    build_work<NT>(a, n, q0, kv, s_warp, s_freed, s_q, s_kv, s_need, s_unit);
     return;
   }
 
@@ -274,7 +278,7 @@ __global__ void __launch_bounds__(NT) attn_slots_kernel(const AttnSlotsArgs a) {
     }
     if (r == 0) *a.n_free_out = avail - taken;
     // (a request that is not admitted keeps its rows, which attend to nothing; rows past T do not exist)
-    build_work<NT>(a, q1 > a.T ? 0 : n, q0, adm ? kv : 0, s_warp, s_freed, s_q, s_kv);
+    build_work<NT>(a, q1 > a.T ? 0 : n, q0, adm ? kv : 0, s_warp, s_freed, s_q, s_kv, s_need, s_unit);
     return;
   }
 
