@@ -119,6 +119,17 @@ bool make_query_map(const ft_attn *h, CUtensorMap *tm, const void *q, int64_t q_
   return make_map(h, tm, q, 4, dims, strides, box);
 }
 
+// The same cache as [(page, keys or values, head)][keys, values][chunk of 64 elements][tokens of the page][64 elements]: from the
+// place of a head's keys, a box is the keys and values of up to 64 tokens.
+bool make_page_map(const ft_attn *h, CUtensorMap *tm, const void *cache) {
+  const ft_attn_config_t &c = h->cfg;
+  const cuuint64_t D = c.head_dim, page = (cuuint64_t)c.page_tokens * D;
+  const cuuint64_t dims[5] = {64, (cuuint64_t)c.page_tokens, D / 64, 2, (cuuint64_t)c.n_pages * 2 * c.n_kv_heads - c.n_kv_heads};
+  const cuuint64_t strides[4] = {D, 64, page * c.n_kv_heads, page};
+  const cuuint32_t box[5] = {64, (cuuint32_t)(c.page_tokens < kDecKeys ? c.page_tokens : kDecKeys), (cuuint32_t)(D / 64), 2, 1};
+  return make_map(h, tm, cache, 5, dims, strides, box);
+}
+
 template <int D, bool BF16>
 cudaError_t allow_smem() {
   cudaError_t e = cudaFuncSetAttribute(attn_stream_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, StreamCfg<D>::kSmem);
@@ -131,14 +142,14 @@ cudaError_t allow_smem() {
 template <int D, bool BF16>
 ft_status_t launch_forward(ft_attn *h, AttnFwdArgs a, const void *cache, cudaStream_t st) {
   CUtensorMap tm, tm_q;
-  if (!make_cache_map(h, &tm, cache)) return FT_ERR_CUDA;
+  if (!make_page_map(h, &tm, cache)) return FT_ERR_CUDA;
   a.part = h->part;
   a.arrive = h->arrive;
   attn_stream_kernel<D, BF16><<<h->geom.dec_grid, kStreamThreads, StreamCfg<D>::kSmem, st>>>(tm, a);
   h->launches += 1;
   FA_CUDA(cudaGetLastError());
   if (h->max_new * h->geom.group > kDecRows) {
-    if (!make_query_map(h, &tm_q, a.q, a.q_stride)) return FT_ERR_CUDA;
+    if (!make_query_map(h, &tm_q, a.q, a.q_stride) || !make_cache_map(h, &tm, cache)) return FT_ERR_CUDA;
     a.part = h->part + h->part_tile;
     attn_tile_kernel<D, BF16><<<h->geom.tile_grid, kTileThreads, TileCfg<D>::kSmem, st>>>(tm_q, tm, a);
     attn_join_kernel<D, BF16><<<dim3(h->geom.tile_grid - 1, 2 * (D / 16)), 128, 0, st>>>(a);

@@ -65,6 +65,17 @@ __device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
                : "r"(addr));
 }
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *tm, int x, int y, int z, int v, int w, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+      "l"(tm), "r"(x), "r"(y), "r"(z), "r"(v), "r"(w), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(p));
+  return p != 0;
+}
 __device__ __forceinline__ void named_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 
 template <int D, bool BF16>
@@ -104,39 +115,36 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
 
   if (warp == kStreamWarps) {
     // ------------------------------ producer ------------------------------
-    // lane -> (box along the keys, 64-element chunk of D, keys or values)
-    constexpr int kChunks = D / 64;
-    const int per_box = 2 * kChunks;
-    const int bx = lane / per_box, ch = (lane % per_box) >> 1, is_v = lane & 1;
-    const bool owner = bx < boxes;
+    // one 5-D box per page (or 64 tokens of one): 64 elements, tokens, 64-element chunks of D, keys and values
     for (; w.load(a.w.dec, hdr.n_dec, a.n_kv, kDecCost, u_end); w.next(a.n_kv)) {
       const AttnEntry &e = w.e;
       const int blk = w.blk, take = w.take, head = w.head;
       const int hi = max(0, e.pos0 + e.n_tok), lo = a.window > 0 ? max(0, e.pos0 - a.window + 1) : 0;
       const int32_t *row = a.table + (long long)e.req * a.table_stride;
-      auto page_of = [&](int b) -> int {       // page of this lane's box of block b, -1: nothing to load
-        const int key = (e.b0 + b) * kDecKeys + bx * box_rows;
-        if (!owner || key >= hi || key + box_rows <= lo) return -1;
-        return row[key >> a.page_shift];
+      auto page_of = [&](int b) -> int {       // page of box `lane` of block b
+        const int key = (e.b0 + b) * kDecKeys + lane * box_rows;
+        return lane < boxes && key < hi && key + box_rows > lo ? row[key >> a.page_shift] : 0;
       };
       int page = page_of(blk);
       for (int b = blk; b < blk + take; ++b, ++it) {
-        const int next = b + 1 < blk + take ? page_of(b + 1) : -1;
-        const int key = (e.b0 + b) * kDecKeys + bx * box_rows;
-        const bool want = owner && key < hi && key + box_rows > lo;
-        if (want && (uint32_t)page >= (uint32_t)a.n_pages) {     // never followed: page 0 instead, and reported
+        const int next = b + 1 < blk + take ? page_of(b + 1) : 0;      // (used, and waited for, a step later)
+        if ((uint32_t)page >= (uint32_t)a.n_pages) {                   // never followed: page 0 instead, and reported
           atomicOr(a.status, kStatBadIndex);
           page = 0;
         }
+        const int key0 = (e.b0 + b) * kDecKeys;
+        const int first = max(0, lo - key0) / box_rows, last = min(boxes, (max(0, hi - key0) + box_rows - 1) / box_rows);
         const int s = it % Cfg::kStages;
         mbar_wait(empty_bar(s), ((it / Cfg::kStages) & 1u) ^ 1u, s_abort, a.status);
         if (*s_abort) break;
-        const uint32_t n = __popc(__ballot_sync(0xffffffffu, want));
-        if (lane == 0) mbar_expect_tx(full_bar(s), n * (uint32_t)(box_rows * 128));
+        if (elect_one()) mbar_expect_tx(full_bar(s), (uint32_t)(max(0, last - first) * box_rows * D * 4));
         __syncwarp();
-        if (want)
-          tma_load_3d(ring + s * Cfg::kStage + is_v * Cfg::kHalf + ch * (kDecKeys * 128) + bx * box_rows * 128, &tm, ch * 64,
-                      key & (page_tokens - 1), (page * 2 + is_v) * a.n_kv + head, full_bar(s));
+        for (int i = first; i < last; ++i) {
+          const int z = __shfl_sync(0xffffffffu, page, i) * 2 * a.n_kv + head;
+          if (elect_one())
+            tma_load_5d(ring + s * Cfg::kStage + i * box_rows * D * 4, &tm, 0, (key0 + i * box_rows) & (page_tokens - 1), 0, 0, z, full_bar(s));
+          __syncwarp();
+        }
         page = next;
       }
       if (*s_abort) break;
@@ -148,7 +156,9 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
 
   // ------------------------------ consumers ------------------------------
   const int g = lane >> 2, t4 = lane & 3;
-  const int key0 = warp * 16;                   // this warp's keys of a block
+  // this warp's 16 keys of a block: in box key0 / box_rows, whose parts are [keys, values][chunk of D][token][64 elements]
+  const int key0 = warp * 16, chunk = box_rows * 128;
+  const uint32_t my_keys = (key0 / box_rows) * (box_rows * D * 4) + (key0 % box_rows) * 128, my_values = my_keys + box_rows * D * 2;
   for (; w.load(a.w.dec, hdr.n_dec, a.n_kv, kDecCost, u_end); w.next(a.n_kv)) {
     const AttnEntry &e = w.e;
     const int blk = w.blk, take = w.take, head = w.head;
@@ -182,7 +192,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
     for (int b = blk; b < blk + take; ++b, ++it) {
       const int s = it % Cfg::kStages;
       const bool ok = mbar_wait(full_bar(s), (it / Cfg::kStages) & 1u, s_abort, a.status);
-      const uint32_t kt = ring + s * Cfg::kStage, vt = kt + Cfg::kHalf;
+      const uint32_t kt = ring + s * Cfg::kStage + my_keys, vt = ring + s * Cfg::kStage + my_values;
       const int base = (e.b0 + b) * kDecKeys + key0;                    // position of this warp's first key
       if (ok && base < hi && base + 16 > lo) {
         const bool edge = base + 16 > hi || base < lo;
@@ -191,7 +201,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
           for (int i = lane; i < 16 * (D / 8); i += 32) {
             const int r = i / (D / 8), c = i % (D / 8), key = base + r;
             if (key >= hi || key < lo)
-              asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(vt + (c >> 3) * (kDecKeys * 128) + (key0 + r) * 128 +
+              asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(vt + (c >> 3) * chunk + r * 128 +
                                                                         (((c & 7) ^ (r & 7)) << 4)),
                            "r"(0u)
                            : "memory");
@@ -210,11 +220,11 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
         {
           // matrices of an ldmatrix: (keys 0-7, d 0-7), (keys 0-7, d 8-15), (keys 8-15, d 0-7), (keys 8-15, d 8-15)
           const int r = (lane & 7) + ((lane >> 4) << 3), cj = (lane >> 3) & 1;
-          const uint32_t ra = kt + (key0 + r) * 128;
+          const uint32_t ra = kt + r * 128;
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
             uint32_t bm[4];
-            ldmatrix_x4(bm, ra + (kk >> 2) * (kDecKeys * 128) + ((((kk & 3) * 2 + cj) ^ (r & 7)) << 4));
+            ldmatrix_x4(bm, ra + (kk >> 2) * chunk + ((((kk & 3) * 2 + cj) ^ (r & 7)) << 4));
             mma_16<BF16>(sc[0][kk & 1], q[kk], bm[0], bm[1]);
             mma_16<BF16>(sc[1][kk & 1], q[kk], bm[2], bm[3]);
           }
@@ -256,11 +266,11 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
         {
           // matrices: (keys 0-7, d 0-7), (keys 8-15, d 0-7), (keys 0-7, d 8-15), (keys 8-15, d 8-15), transposed
           const int r = lane & 15, cj = lane >> 4;
-          const uint32_t ra = vt + (key0 + r) * 128;
+          const uint32_t ra = vt + r * 128;
 #pragma unroll
           for (int nn = 0; nn < D / 16; ++nn) {
             uint32_t bm[4];
-            ldmatrix_x4_trans(bm, ra + (nn >> 2) * (kDecKeys * 128) + ((((nn & 3) * 2 + cj) ^ (r & 7)) << 4));
+            ldmatrix_x4_trans(bm, ra + (nn >> 2) * chunk + ((((nn & 3) * 2 + cj) ^ (r & 7)) << 4));
             mma_16<BF16>(o[2 * nn], pa, bm[0], bm[1]);
             mma_16<BF16>(o[2 * nn + 1], pa, bm[2], bm[3]);
           }
