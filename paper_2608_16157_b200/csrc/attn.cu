@@ -145,7 +145,7 @@ ft_status_t launch_forward(ft_attn *h, AttnFwdArgs a, const void *cache, cudaStr
   if (!make_page_map(h, &tm, cache)) return FT_ERR_CUDA;
   a.part = h->part;
   a.arrive = h->arrive;
-  attn_stream_kernel<D, BF16><<<h->geom.dec_grid, kStreamThreads, StreamCfg<D>::kSmem, st>>>(tm, a);
+  attn_stream_kernel<D, BF16><<<h->geom.dec_grid, StreamCfg<D>::kThreads, StreamCfg<D>::kSmem, st>>>(tm, a);
   h->launches += 1;
   FA_CUDA(cudaGetLastError());
   if (h->max_new * h->geom.group > kDecRows) {
@@ -189,7 +189,7 @@ ft_status_t allocate(ft_attn *h) {
   g.window = c.window;
   g.tile_tokens = 2 * (kTileRows / g.group);
   g.dec_grid = g.tile_grid = h->sm_count < kAttnMaxGrid ? h->sm_count : kAttnMaxGrid;
-  g.dec_min_quota = 1;
+  g.dec_min_quota = 2;      // one block and its cost (one request of 1000 tokens: 9.1 us with 1, 8.5 with 2, 9.8 with 3)
   g.tile_min_quota = 1;
   g.tile_cap = c.max_tokens / g.tile_tokens + c.max_requests;
   auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };

@@ -3,8 +3,8 @@
 //
 // The key blocks (64 keys) of all requests and key/value heads form one flat list that is cut into equal shares, one
 // CTA per SM (the work partition of attn_plan.cuh), so the cache streams at an even rate whatever the lengths are.  A
-// producer warp brings a block's pages with TMA tile loads (128-byte swizzle) into a ring of 160 KB; the four consumer
-// warps take 16 keys each of every block: S = Q K^T and O += P V with mma.sync m16n8k16 (the rows on M), the running maximum
+// producer warp brings a block's pages with TMA tile loads (128-byte swizzle) into a ring of 160 KB; the consumer
+// warps take 16 keys each of a block: S = Q K^T and O += P V with mma.sync m16n8k16 (the rows on M), the running maximum
 // m and sum l of every row per warp:
 //   m' = max(m, max_j s_j),  l' = l 2^(m-m') + sum_j 2^(s_j-m'),  O' = O 2^(m-m') + sum_j 2^(s_j-m') v_j,  s in units of log2
 // P is rounded to the values' type for the second product (relative 2^-9 of each weight on average, below the rounding of
@@ -35,14 +35,17 @@ struct AttnFwdArgs {
   uint32_t *status;
 };
 
-constexpr int kStreamWarps = 4, kStreamThreads = (kStreamWarps + 1) * 32;
 template <int D> struct StreamCfg {
+  // four warps share a block's keys; with D = 64, where a block is half the bytes but nearly the same chain of latencies, two such
+  // groups take the blocks in turn (one group: 850 clocks a block where HBM gives one in 700)
+  static constexpr int kGroups = D == 128 ? 1 : 2;
+  static constexpr int kWarps = 4 * kGroups, kConsumers = kWarps * 32, kThreads = kConsumers + 32;
   static constexpr int kHalf = kDecKeys * D * 2;            // bytes of the keys (or values) of a block
   static constexpr int kStage = 2 * kHalf;
   static constexpr int kStages = D == 128 ? 5 : 10;
   static constexpr int kRow = D + 8;                        // floats per row of the join buffer (bank-conflict free)
-  static constexpr int kJoin = kStreamWarps * kDecRows * kRow * 4;
-  static constexpr int kSmem = 1024 + kStages * kStage + kJoin + kStreamWarps * kDecRows * 8 + 2 * kStages * 8 + 64;
+  static constexpr int kJoin = kWarps * kDecRows * kRow * 4;
+  static constexpr int kSmem = 1024 + kStages * kStage + kJoin + kWarps * kDecRows * 8 + 2 * kStages * 8 + 64;
   static constexpr int kPart = kDecRows * (D + 2);          // floats of one partial result: m[16], l[16], O[16][D]
 };
 
@@ -79,14 +82,14 @@ __device__ __forceinline__ bool elect_one() {
 __device__ __forceinline__ void named_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kStreamThreads, 1)
+__global__ void __launch_bounds__(StreamCfg<D>::kThreads, 1)
 attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) {
   using Cfg = StreamCfg<D>;
   extern __shared__ unsigned char smem_raw[];
   unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   float *s_join = reinterpret_cast<float *>(smem + Cfg::kStages * Cfg::kStage);
   float *s_ml = s_join + Cfg::kJoin / 4;                                  // [warp][16][m, l]
-  uint64_t *s_bar = reinterpret_cast<uint64_t *>(s_ml + kStreamWarps * kDecRows * 2);
+  uint64_t *s_bar = reinterpret_cast<uint64_t *>(s_ml + Cfg::kWarps * kDecRows * 2);
   volatile int *s_abort = reinterpret_cast<volatile int *>(s_bar + 2 * Cfg::kStages);
   volatile int *s_last = s_abort + 1;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -100,7 +103,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
   if (u_first >= hdr.dec_units) return;
   const int u_end = (int)min(u_first + hdr.dec_quota, (long long)hdr.dec_units);
   if (tid == 0) {
-    for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), kStreamWarps); }
+    for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 4); }
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -113,7 +116,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
   w.start(st);
   uint32_t it = 0;      // blocks of this CTA so far
 
-  if (warp == kStreamWarps) {
+  if (warp == Cfg::kWarps) {
     // ------------------------------ producer ------------------------------
     // one 5-D box per page (or 64 tokens of one): 64 elements, tokens, 64-element chunks of D, keys and values
     for (; w.load(a.w.dec, hdr.n_dec, a.n_kv, kDecCost, u_end); w.next(a.n_kv)) {
@@ -121,16 +124,22 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
       const int blk = w.blk, take = w.take, head = w.head;
       const int hi = max(0, e.pos0 + e.n_tok), lo = a.window > 0 ? max(0, e.pos0 - a.window + 1) : 0;
       const int32_t *row = a.table + (long long)e.req * a.table_stride;
-      auto page_of = [&](int b) -> int {       // page of box `lane` of block b
+      // the lanes hold the pages of the boxes of 32 / boxes blocks at a time, the next ones on their way
+      const int per = 32 / boxes;
+      auto pages_of = [&](int b) -> int {
         const int key = (e.b0 + b) * kDecKeys + lane * box_rows;
-        return lane < boxes && key < hi && key + box_rows > lo ? row[key >> a.page_shift] : 0;
+        return key < hi && key + box_rows > lo ? row[key >> a.page_shift] : 0;
       };
-      int page = page_of(blk);
-      for (int b = blk; b < blk + take; ++b, ++it) {
-        const int next = b + 1 < blk + take ? page_of(b + 1) : 0;      // (used, and waited for, a step later)
-        if ((uint32_t)page >= (uint32_t)a.n_pages) {                   // never followed: page 0 instead, and reported
-          atomicOr(a.status, kStatBadIndex);
-          page = 0;
+      int pages = 0, next = pages_of(blk), i0 = 0;
+      for (int b = blk; b < blk + take; ++b, ++it, i0 += boxes) {
+        if ((b - blk) % per == 0) {
+          pages = next;
+          i0 = 0;
+          if (b + per < blk + take) next = pages_of(b + per);
+          if ((uint32_t)pages >= (uint32_t)a.n_pages) {                // never followed: page 0 instead, and reported
+            atomicOr(a.status, kStatBadIndex);
+            pages = 0;
+          }
         }
         const int key0 = (e.b0 + b) * kDecKeys;
         const int first = max(0, lo - key0) / box_rows, last = min(boxes, (max(0, hi - key0) + box_rows - 1) / box_rows);
@@ -140,12 +149,11 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
         if (elect_one()) mbar_expect_tx(full_bar(s), (uint32_t)(max(0, last - first) * box_rows * D * 4));
         __syncwarp();
         for (int i = first; i < last; ++i) {
-          const int z = __shfl_sync(0xffffffffu, page, i) * 2 * a.n_kv + head;
+          const int z = __shfl_sync(0xffffffffu, pages, i0 + i) * 2 * a.n_kv + head;
           if (elect_one())
             tma_load_5d(ring + s * Cfg::kStage + i * box_rows * D * 4, &tm, 0, (key0 + i * box_rows) & (page_tokens - 1), 0, 0, z, full_bar(s));
           __syncwarp();
         }
-        page = next;
       }
       if (*s_abort) break;
     }
@@ -157,7 +165,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
   // ------------------------------ consumers ------------------------------
   const int g = lane >> 2, t4 = lane & 3;
   // this warp's 16 keys of a block: in box key0 / box_rows, whose parts are [keys, values][chunk of D][token][64 elements]
-  const int key0 = warp * 16, chunk = box_rows * 128;
+  const int key0 = (warp & 3) * 16, chunk = box_rows * 128;
   const uint32_t my_keys = (key0 / box_rows) * (box_rows * D * 4) + (key0 % box_rows) * 128, my_values = my_keys + box_rows * D * 2;
   for (; w.load(a.w.dec, hdr.n_dec, a.n_kv, kDecCost, u_end); w.next(a.n_kv)) {
     const AttnEntry &e = w.e;
@@ -190,6 +198,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
       for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
 
     for (int b = blk; b < blk + take; ++b, ++it) {
+      if (Cfg::kGroups > 1 && (it & 1u) != (uint32_t)(warp >> 2)) continue;
       const int s = it % Cfg::kStages;
       const bool ok = mbar_wait(full_bar(s), (it / Cfg::kStages) & 1u, s_abort, a.status);
       const uint32_t kt = ring + s * Cfg::kStage + my_keys, vt = ring + s * Cfg::kStage + my_values;
@@ -294,10 +303,10 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) *reinterpret_cast<float2 *>(dst + i * 8) = make_float2(o[i][2 * h2], o[i][2 * h2 + 1]);
     }
-    named_sync(1, kStreamWarps * 32);
+    named_sync(1, Cfg::kConsumers);
     const int c_first = w.u / hdr.dec_quota, c_last = (w.u + e.nb - 1) / hdr.dec_quota;
     const bool whole = c_first == c_last;
-    constexpr int kCols = D / 4;                       // a thread owns 4 columns of every (128 / kCols)-th row
+    constexpr int kCols = D / 4;                       // a thread owns 4 columns of every (kConsumers / kCols)-th row
     const int col = (tid % kCols) * 4, row0 = tid / kCols;
     auto write_row = [&](int r, float mm, float ll, float4 v) {
       const float inv = ll > 0.f ? 1.f / ll : 0.f;
@@ -308,14 +317,14 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
       if (a.lse && col == 0) a.lse[t * a.n_q + hq] = ll > 0.f ? (mm + log2f(ll)) * 0.693147180559945f : -INFINITY;
     };
     float *part = a.part + (size_t)(blockIdx.x * 2 + (blockIdx.x == c_first ? 1 : 0)) * Cfg::kPart;
-    for (int r = row0; r < rows; r += kStreamWarps * 32 / kCols) {
+    for (int r = row0; r < rows; r += Cfg::kConsumers / kCols) {
       float mm = -INFINITY, ll = 0.f;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int i = 0; i < kStreamWarps; ++i) mm = fmaxf(mm, s_ml[(i * kDecRows + r) * 2]);
+      for (int i = 0; i < Cfg::kWarps; ++i) mm = fmaxf(mm, s_ml[(i * kDecRows + r) * 2]);
       const float bm = mm == -INFINITY ? 0.f : mm;
 #pragma unroll
-      for (int i = 0; i < kStreamWarps; ++i) {
+      for (int i = 0; i < Cfg::kWarps; ++i) {
         const float f = ex2(s_ml[(i * kDecRows + r) * 2] - bm);
         const float4 x = *reinterpret_cast<const float4 *>(s_join + (i * kDecRows + r) * Cfg::kRow + col);
         ll = fmaf(f, s_ml[(i * kDecRows + r) * 2 + 1], ll);
@@ -330,7 +339,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
     }
     if (!whole) {
       __threadfence();
-      named_sync(1, kStreamWarps * 32);
+      named_sync(1, Cfg::kConsumers);
       if (tid == 0) {
         uint32_t *cnt = a.arrive + (size_t)w.k * a.n_kv + head;
         const uint32_t n = (uint32_t)(c_last - c_first + 1);
@@ -339,27 +348,48 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
         *s_last = last;
         __threadfence();
       }
-      named_sync(1, kStreamWarps * 32);
+      named_sync(1, Cfg::kConsumers);
       if (*s_last) {
-        for (int r = row0; r < rows; r += kStreamWarps * 32 / kCols) {
-          float mm = -INFINITY, ll = 0.f;
-          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-          for (int c = c_first; c <= c_last; ++c) {
-            const float *pc = a.part + (size_t)(c * 2 + (c == c_first ? 1 : 0)) * Cfg::kPart;
-            const float mc = __ldcg(pc + r), lc = __ldcg(pc + kDecRows + r);
-            const float4 x = __ldcg(reinterpret_cast<const float4 *>(pc + 2 * kDecRows + r * D + col));
-            const float mn = fmaxf(mm, mc), bm = mn == -INFINITY ? 0.f : mn;
-            const float f0 = ex2(mm - bm), f1 = ex2(mc - bm);
-            ll = ll * f0 + lc * f1;
-            v.x = v.x * f0 + x.x * f1; v.y = v.y * f0 + x.y * f1; v.z = v.z * f0 + x.z * f1; v.w = v.w * f0 + x.w * f1;
-            mm = mn;
-          }
-          write_row(r, mm, ll, v);
+        // all of a thread's rows and four parts at a time: what costs here is one load waiting for another
+        constexpr int kStep = Cfg::kConsumers / kCols, kMine = kDecRows / kStep;
+        float mm[kMine], ll[kMine];
+        float4 v[kMine];
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) { mm[i] = -INFINITY; ll[i] = 0.f; v[i] = make_float4(0.f, 0.f, 0.f, 0.f); }
+        for (int c0 = c_first; c0 <= c_last; c0 += 4) {
+          float mc[4][kMine], lc[4][kMine];
+          float4 x[4][kMine];
+#pragma unroll
+          for (int z = 0; z < 4; ++z)
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+              const int c = c0 + z, r = row0 + i * kStep;
+              mc[z][i] = -INFINITY; lc[z][i] = 0.f; x[z][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (c <= c_last && r < rows) {
+                const float *pc = a.part + (size_t)(c * 2 + (c == c_first ? 1 : 0)) * Cfg::kPart;
+                mc[z][i] = __ldcg(pc + r);
+                lc[z][i] = __ldcg(pc + kDecRows + r);
+                x[z][i] = __ldcg(reinterpret_cast<const float4 *>(pc + 2 * kDecRows + r * D + col));
+              }
+            }
+#pragma unroll
+          for (int z = 0; z < 4; ++z)
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+              const float mn = fmaxf(mm[i], mc[z][i]), bm = mn == -INFINITY ? 0.f : mn;
+              const float f0 = ex2(mm[i] - bm), f1 = ex2(mc[z][i] - bm);
+              ll[i] = ll[i] * f0 + lc[z][i] * f1;
+              v[i].x = v[i].x * f0 + x[z][i].x * f1; v[i].y = v[i].y * f0 + x[z][i].y * f1;
+              v[i].z = v[i].z * f0 + x[z][i].z * f1; v[i].w = v[i].w * f0 + x[z][i].w * f1;
+              mm[i] = mn;
+            }
         }
+#pragma unroll
+        for (int i = 0; i < kMine; ++i)
+          if (row0 + i * kStep < rows) write_row(row0 + i * kStep, mm[i], ll[i], v[i]);
       }
     }
-    named_sync(1, kStreamWarps * 32);      // the join buffer is free again
+    named_sync(1, Cfg::kConsumers);      // the join buffer is free again
   }
   abort_drain(s_abort);
 }
