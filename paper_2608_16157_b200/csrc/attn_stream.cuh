@@ -79,6 +79,17 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(p));
   return p != 0;
 }
+// Bounded wait without anything between the polls (limit: g_wait_polls, read once): a wait is on the critical path of every
+// block several times.  Returns false, after latching, if the phase never completes.
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, uint32_t limit, volatile int *abort_flag, uint32_t *status) {
+  for (uint32_t i = 0; i <= limit; ++i) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if (__builtin_expect((i & 255u) == 255u, 0) && *abort_flag) return false;
+  }
+  *abort_flag = 1;
+  atomicOr(status, kStatTimeout);
+  return false;
+}
 __device__ __forceinline__ void named_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 
 template <int D, bool BF16>
@@ -98,7 +109,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
   auto empty_bar = [&](int s) { return bars + 8u * (Cfg::kStages + s); };
 
   const AttnPlanHdr hdr = *a.w.hdr;
-  const AttnStart st = a.w.dec_start[blockIdx.x];     // (stale beyond the shares in use: not looked at)
+  const AttnStart start = a.w.dec_start[blockIdx.x];     // (stale beyond the shares in use: not looked at)
   const long long u_first = (long long)blockIdx.x * hdr.dec_quota;
   if (u_first >= hdr.dec_units) return;
   const int u_end = (int)min(u_first + hdr.dec_quota, (long long)hdr.dec_units);
@@ -111,10 +122,12 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
   __syncthreads();
 
   const int page_tokens = 1 << a.page_shift;
-  const int box_rows = min(page_tokens, kDecKeys), boxes = kDecKeys / box_rows;   // boxes of a block along its keys
+  const int box_shift = min(a.page_shift, 6), box_rows = 1 << box_shift, boxes = kDecKeys >> box_shift;   // boxes of a block
   WorkWalk w;
-  w.start(st);
-  uint32_t it = 0;      // blocks of this CTA so far
+  w.start(start);
+  int s = 0;            // stage of the next block and its phase
+  uint32_t ph = 0;
+  const uint32_t limit = g_wait_polls;
 
   if (warp == Cfg::kWarps) {
     // ------------------------------ producer ------------------------------
@@ -125,14 +138,14 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
       const int hi = max(0, e.pos0 + e.n_tok), lo = a.window > 0 ? max(0, e.pos0 - a.window + 1) : 0;
       const int32_t *row = a.table + (long long)e.req * a.table_stride;
       // the lanes hold the pages of the boxes of 32 / boxes blocks at a time, the next ones on their way
-      const int per = 32 / boxes;
+      const int per = 32 >> (6 - box_shift);
       auto pages_of = [&](int b) -> int {
         const int key = (e.b0 + b) * kDecKeys + lane * box_rows;
         return key < hi && key + box_rows > lo ? row[key >> a.page_shift] : 0;
       };
       int pages = 0, next = pages_of(blk), i0 = 0;
-      for (int b = blk; b < blk + take; ++b, ++it, i0 += boxes) {
-        if ((b - blk) % per == 0) {
+      for (int b = blk; b < blk + take; ++b, i0 += boxes) {
+        if (((b - blk) & (per - 1)) == 0) {
           pages = next;
           i0 = 0;
           if (b + per < blk + take) next = pages_of(b + per);
@@ -142,9 +155,8 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
           }
         }
         const int key0 = (e.b0 + b) * kDecKeys;
-        const int first = max(0, lo - key0) / box_rows, last = min(boxes, (max(0, hi - key0) + box_rows - 1) / box_rows);
-        const int s = it % Cfg::kStages;
-        mbar_wait(empty_bar(s), ((it / Cfg::kStages) & 1u) ^ 1u, s_abort, a.status);
+        const int first = max(0, lo - key0) >> box_shift, last = min(boxes, (max(0, hi - key0) + box_rows - 1) >> box_shift);
+        wait_phase(empty_bar(s), ph ^ 1u, limit, s_abort, a.status);
         if (*s_abort) break;
         if (elect_one()) mbar_expect_tx(full_bar(s), (uint32_t)(max(0, last - first) * box_rows * D * 4));
         __syncwarp();
@@ -154,6 +166,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
             tma_load_5d(ring + s * Cfg::kStage + i * box_rows * D * 4, &tm, 0, (key0 + i * box_rows) & (page_tokens - 1), 0, 0, z, full_bar(s));
           __syncwarp();
         }
+        if (++s == Cfg::kStages) { s = 0; ph ^= 1u; }
       }
       if (*s_abort) break;
     }
@@ -166,7 +179,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
   const int g = lane >> 2, t4 = lane & 3;
   // this warp's 16 keys of a block: in box key0 / box_rows, whose parts are [keys, values][chunk of D][token][64 elements]
   const int key0 = (warp & 3) * 16, chunk = box_rows * 128;
-  const uint32_t my_keys = (key0 / box_rows) * (box_rows * D * 4) + (key0 % box_rows) * 128, my_values = my_keys + box_rows * D * 2;
+  const uint32_t my_keys = (key0 >> box_shift) * (box_rows * D * 4) + (key0 & (box_rows - 1)) * 128, my_values = my_keys + box_rows * D * 2;
   for (; w.load(a.w.dec, hdr.n_dec, a.n_kv, kDecCost, u_end); w.next(a.n_kv)) {
     const AttnEntry &e = w.e;
     const int blk = w.blk, take = w.take, head = w.head;
@@ -197,11 +210,13 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
 
-    for (int b = blk; b < blk + take; ++b, ++it) {
-      if (Cfg::kGroups > 1 && (it & 1u) != (uint32_t)(warp >> 2)) continue;
-      const int s = it % Cfg::kStages;
-      const bool ok = mbar_wait(full_bar(s), (it / Cfg::kStages) & 1u, s_abort, a.status);
-      const uint32_t kt = ring + s * Cfg::kStage + my_keys, vt = ring + s * Cfg::kStage + my_values;
+    for (int b = blk; b < blk + take; ++b) {
+      const int st = s;
+      const uint32_t st_ph = ph;
+      if (++s == Cfg::kStages) { s = 0; ph ^= 1u; }
+      if (Cfg::kGroups > 1 && (st & 1) != (warp >> 2)) continue;     // (an even number of stages then)
+      const bool ok = wait_phase(full_bar(st), st_ph, limit, s_abort, a.status);
+      const uint32_t kt = ring + st * Cfg::kStage + my_keys, vt = ring + st * Cfg::kStage + my_values;
       const int base = (e.b0 + b) * kDecKeys + key0;                    // position of this warp's first key
       if (ok && base < hi && base + 16 > lo) {
         const bool edge = base + 16 > hi || base < lo;
@@ -286,7 +301,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
         }
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(empty_bar(s));
+      if (lane == 0) mbar_arrive(empty_bar(st));
     }
 
     // join the warps: (m, l) and O of every row

@@ -45,17 +45,6 @@ __device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a_tmem, uint64_t b,
 }
 // A value all lanes hold, in a uniform register.
 __device__ __forceinline__ int uniform(int v) { return __reduce_max_sync(0xffffffffu, v); }
-// Bounded wait without anything between the polls (limit: g_wait_polls, read once): a wait is on the critical path of every
-// block several times.  Returns false, after latching, if the phase never completes.
-__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, uint32_t limit, volatile int *abort_flag, uint32_t *status) {
-  for (uint32_t i = 0; i <= limit; ++i) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if (__builtin_expect((i & 255u) == 255u, 0) && *abort_flag) return false;
-  }
-  *abort_flag = 1;
-  atomicOr(status, kStatTimeout);
-  return false;
-}
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
@@ -175,7 +164,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     if (warp == 9) {
       // ------------------------------ loads ------------------------------
       const int page_tokens = 1 << a.page_shift;
-      const int box_rows = min(page_tokens, kDecKeys), boxes = kTileKeys / box_rows;
+      const int box_shift = min(a.page_shift, 6), box_rows = 1 << box_shift, boxes = kTileKeys >> box_shift;
       for (; w.load(a.w.tile, hdr.n_tile, a.n_kv, kTileCost, u_end) && !*s_abort; w.next(a.n_kv)) {
         AttnEntry e = w.e;
         e.n_tok = uniform(e.n_tok); e.pos0 = uniform(e.pos0); e.b0 = uniform(e.b0); e.tok0 = uniform(e.tok0);
@@ -212,7 +201,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
           wait_phase(empty_bar(rs), rph ^ 1u, limit, s_abort, a.status);
           if (*s_abort) return;
           const int key0 = (e.b0 + b) * kTileKeys;
-          const int first = max(0, lo - key0) / box_rows, last = min(boxes, (max(0, hi - key0) + box_rows - 1) / box_rows);
+          const int first = max(0, lo - key0) >> box_shift, last = min(boxes, (max(0, hi - key0) + box_rows - 1) >> box_shift);
           if (elect_one()) mbar_expect_tx(full_bar(rs), (uint32_t)(max(0, last - first) * box_rows * D * 2));
           __syncwarp();
           const uint32_t dst = ring + rs * Cfg::kTile;
