@@ -6,6 +6,7 @@
 
 #include <cstring>
 #include <new>
+#include <utility>
 
 #include "attn_plan.cuh"
 #include "attn_rope.cuh"
@@ -139,28 +140,43 @@ cudaError_t allow_smem() {
   return e;
 }
 
+// A launch the stream's next kernel may be scheduled beside: every kernel here waits for all before it (grid_wait) before it
+// touches global memory, so only launch latency and prologues overlap.
+template <typename... P, typename... Args>
+cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, Args &&...args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+
 template <int D, bool BF16>
 ft_status_t launch_forward(ft_attn *h, AttnFwdArgs a, const void *cache, cudaStream_t st) {
   CUtensorMap tm, tm_q;
   if (!make_page_map(h, &tm, cache)) return FT_ERR_CUDA;
   a.part = h->part;
   a.arrive = h->arrive;
-  attn_stream_kernel<D, BF16><<<h->geom.dec_grid, StreamCfg<D>::kThreads, StreamCfg<D>::kSmem, st>>>(tm, a);
+  FA_CUDA(launch(attn_stream_kernel<D, BF16>, h->geom.dec_grid, StreamCfg<D>::kThreads, StreamCfg<D>::kSmem, st, tm, a));
   h->launches += 1;
-  FA_CUDA(cudaGetLastError());
   if (h->max_new * h->geom.group > kDecRows) {
     if (!make_query_map(h, &tm_q, a.q, a.q_stride) || !make_cache_map(h, &tm, cache)) return FT_ERR_CUDA;
     a.part = h->part + h->part_tile;
-    attn_tile_kernel<D, BF16><<<h->geom.tile_grid, kTileThreads, TileCfg<D>::kSmem, st>>>(tm_q, tm, a);
-    attn_join_kernel<D, BF16><<<dim3(h->geom.tile_grid - 1, 2 * (D / 16)), 128, 0, st>>>(a);
+    FA_CUDA(launch(attn_tile_kernel<D, BF16>, h->geom.tile_grid, kTileThreads, TileCfg<D>::kSmem, st, tm_q, tm, a));
+    FA_CUDA(launch(attn_join_kernel<D, BF16>, dim3(h->geom.tile_grid - 1, 2 * (D / 16)), 128, 0, st, a));
     h->launches += 2;
-    FA_CUDA(cudaGetLastError());
   }
   return FT_OK;
 }
 
 template <int D, bool BF16>
-void launch_rope(const ft_attn *h, RopeArgs &a, bool wide, cudaStream_t st) {
+cudaError_t launch_rope(const ft_attn *h, RopeArgs &a, bool wide, cudaStream_t st) {
   const int heads = a.n_q + 2 * a.n_kv, lanes = wide ? D / 16 : D / 8;
   // one head per lane group while that does not fill the GPU (2048 threads an SM), more, up to 8, where it fills it several
   // times over: the token's cosines and sines are read once per group
@@ -171,13 +187,11 @@ void launch_rope(const ft_attn *h, RopeArgs &a, bool wide, cudaStream_t st) {
   if (wide && fill >= 1 && smem <= 232448 / kRopeBlocks - 1024) {
     const int passes = (heads * lanes + 511) / 512, consumers = ((heads + passes - 1) / passes * lanes + 31) / 32 * 32;
     const long long blocks = (long long)h->sm_count * kRopeBlocks;
-    attn_rope_stream_kernel<D, BF16><<<(unsigned)(a.T < blocks ? a.T : blocks), consumers + 32, smem, st>>>(a);
-    return;
+    return launch(attn_rope_stream_kernel<D, BF16>, (unsigned)(a.T < blocks ? a.T : blocks), consumers + 32, smem, st, a);
   }
   const int parts = (heads + a.heads_per_group - 1) / a.heads_per_group;
   const unsigned grid = (unsigned)(((long long)a.T * parts * lanes + 255) / 256);
-  if (wide) attn_rope_kernel<D, BF16, 8><<<grid, 256, 0, st>>>(a);
-  else attn_rope_kernel<D, BF16, 4><<<grid, 256, 0, st>>>(a);
+  return wide ? launch(attn_rope_kernel<D, BF16, 8>, grid, 256, 0, st, a) : launch(attn_rope_kernel<D, BF16, 4>, grid, 256, 0, st, a);
 }
 
 ft_status_t allocate(ft_attn *h) {
@@ -238,10 +252,8 @@ ft_status_t launch_slots(ft_attn *h, AttnSlotsArgs &a, cudaStream_t st) {
   const int threads = a.n_req <= 256 ? 256 : 1024;
   const int blocks = 1 + (a.T > 1 ? a.T - 1 : 0) / threads;
   const int grid = a.own_tables ? 1 : 1 + (blocks < h->sm_count - 1 ? blocks : h->sm_count - 1);
-  if (threads == 256) attn_slots_kernel<256><<<grid, 256, 0, st>>>(a);
-  else attn_slots_kernel<1024><<<grid, 1024, 0, st>>>(a);
+  FA_CUDA(threads == 256 ? launch(attn_slots_kernel<256>, grid, 256, 0, st, a) : launch(attn_slots_kernel<1024>, grid, 1024, 0, st, a));
   h->launches += 1;
-  FA_CUDA(cudaGetLastError());
   h->planned = true;
   h->n_req = a.n_req; h->T = a.T; h->max_new = a.max_new;
   return FT_OK;
@@ -353,10 +365,9 @@ ft_status_t ft_attn_qk_rope(ft_attn_t *h, int T, const void *q, int64_t q_stride
   // 16-byte accesses where every address and the halves of the rotated part allow them
   const bool wide = !(((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)w_q | (uintptr_t)w_k | (uintptr_t)q_out) & 15) &&
                     !((q_stride | k_stride | v_stride | q_out_stride) & 7) && rot_dim % 16 == 0;
-  if (D == 128) bf ? launch_rope<128, true>(h, a, wide, st) : launch_rope<128, false>(h, a, wide, st);
-  else bf ? launch_rope<64, true>(h, a, wide, st) : launch_rope<64, false>(h, a, wide, st);
+  FA_CUDA(D == 128 ? (bf ? launch_rope<128, true>(h, a, wide, st) : launch_rope<128, false>(h, a, wide, st))
+                   : (bf ? launch_rope<64, true>(h, a, wide, st) : launch_rope<64, false>(h, a, wide, st)));
   h->launches += 1;
-  FA_CUDA(cudaGetLastError());
   return FT_OK;
 }
 

@@ -8,7 +8,7 @@
 // released and the new pages.  Reads are of the step's old state alone: the stack below n_free, columns below held_r;
 // writes are of the stack from n_free up and columns from held_r up.
 #pragma once
-#include "common.cuh"
+#include "async.cuh"
 
 namespace ftmoe {
 
@@ -213,6 +213,8 @@ __global__ void __launch_bounds__(NT) attn_slots_kernel(const AttnSlotsArgs a) {
   __shared__ int32_t s_q[NT + 1], s_ctx[NT], s_held[NT], s_freed[NT], s_need[NT], s_kv[NT], s_adm[NT], s_unit[kUnitCache];
   const int tid = threadIdx.x, r = tid;
   unsigned long long tot;
+  grid_let_next();
+  grid_wait();
 
   if (a.own_tables) {                       // lengths given: one block, the work partition alone
     int n = 0, q0 = 0, kv = 0;

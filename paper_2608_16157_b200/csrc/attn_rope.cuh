@@ -89,6 +89,8 @@ __device__ __forceinline__ void store_elems(uint16_t *p, const uint32_t (&r)[V /
 template <int D, bool BF16, int V>
 __global__ void __launch_bounds__(256) attn_rope_kernel(const RopeArgs a) {
   constexpr int L = D / (2 * V), kUnroll = V == 8 ? 4 : 8;   // lanes per head; heads in flight per lane
+  grid_let_next();
+  grid_wait();
   const int lane_in = threadIdx.x % L;
   const int heads = a.n_q + 2 * a.n_kv, parts = (heads + a.heads_per_group - 1) / a.heads_per_group;
   const long long group = ((long long)blockIdx.x * blockDim.x + threadIdx.x) / L;
@@ -233,6 +235,7 @@ __global__ void __launch_bounds__(544) attn_rope_stream_kernel(const RopeArgs a)
   const uint32_t base = smem_u32(smem), bars = smem_u32(s_bar);
   auto full_bar = [&](int s) { return bars + 8u * s; };
   auto empty_bar = [&](int s) { return bars + 8u * (kRopeStages + s); };
+  grid_let_next();
   if (tid == 0) {
     for (int s = 0; s < kRopeStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), consumers / 32); }
     *s_abort = 0;
@@ -240,6 +243,7 @@ __global__ void __launch_bounds__(544) attn_rope_stream_kernel(const RopeArgs a)
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   __syncthreads();
+  grid_wait();
   const int q_bytes = a.n_q * D * 2, kv_bytes = a.n_kv * D * 2, step = gridDim.x;
   int s = 0;
   uint32_t ph = 0;

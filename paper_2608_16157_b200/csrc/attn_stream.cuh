@@ -108,11 +108,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
   auto full_bar = [&](int s) { return bars + 8u * s; };
   auto empty_bar = [&](int s) { return bars + 8u * (Cfg::kStages + s); };
 
-  const AttnPlanHdr hdr = *a.w.hdr;
-  const AttnStart start = a.w.dec_start[blockIdx.x];     // (stale beyond the shares in use: not looked at)
-  const long long u_first = (long long)blockIdx.x * hdr.dec_quota;
-  if (u_first >= hdr.dec_units) return;
-  const int u_end = (int)min(u_first + hdr.dec_quota, (long long)hdr.dec_units);
+  grid_let_next();
   if (tid == 0) {
     for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 4); }
     *s_abort = 0;
@@ -120,6 +116,12 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   __syncthreads();
+  grid_wait();
+  const AttnPlanHdr hdr = *a.w.hdr;
+  const AttnStart start = a.w.dec_start[blockIdx.x];     // (stale beyond the shares in use: not looked at)
+  const long long u_first = (long long)blockIdx.x * hdr.dec_quota;
+  if (u_first >= hdr.dec_units) return;
+  const int u_end = (int)min(u_first + hdr.dec_quota, (long long)hdr.dec_units);
 
   const int page_tokens = 1 << a.page_shift;
   const int box_shift = min(a.page_shift, 6), box_rows = 1 << box_shift, boxes = kDecKeys >> box_shift;   // boxes of a block
@@ -353,9 +355,9 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
       }
     }
     if (!whole) {
-      __threadfence();
       named_sync(1, Cfg::kConsumers);
       if (tid == 0) {
+        __threadfence();                   // (for the whole group: the barrier orders its stores before)
         uint32_t *cnt = a.arrive + (size_t)w.k * a.n_kv + head;
         const uint32_t n = (uint32_t)(c_last - c_first + 1);
         const bool last = atomicAdd(cnt, 1u) == n - 1;

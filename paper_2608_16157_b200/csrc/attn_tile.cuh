@@ -125,11 +125,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   auto o_empty = [&](int t) { return q_full + 112 + 8u * t; };
 
   const uint32_t limit = g_wait_polls;
-  const AttnPlanHdr hdr = *a.w.hdr;
-  const AttnStart st = a.w.tile_start[blockIdx.x];     // (stale beyond the shares in use: not looked at)
-  const long long u_first = (long long)blockIdx.x * hdr.tile_quota;
-  if (u_first >= hdr.tile_units) return;
-  const int u_end = (int)min(u_first + hdr.tile_quota, (long long)hdr.tile_units);
+  grid_let_next();
   if (tid == 0) {
     for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     mbar_init(q_full, 1);
@@ -151,6 +147,15 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
+  grid_wait();
+  const AttnPlanHdr hdr = *a.w.hdr;
+  const AttnStart st = a.w.tile_start[blockIdx.x];     // (stale beyond the shares in use: not looked at)
+  const long long u_first = (long long)blockIdx.x * hdr.tile_quota;
+  if (u_first >= hdr.tile_units) {
+    if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    return;
+  }
+  const int u_end = (int)min(u_first + hdr.tile_quota, (long long)hdr.tile_units);
   const uint32_t tm_s = tmem, tm_o = tmem + 256;             // S_t (and P_t) at 128 t, O_t at 256 + D t
   const int tokens = kTileRows / a.group;                    // tokens of a tile
   WorkWalk w;
@@ -609,6 +614,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
 template <int D, bool BF16>
 __global__ void __launch_bounds__(128) attn_join_kernel(const AttnFwdArgs a) {
   using Cfg = TileCfg<D>;
+  grid_let_next();
+  grid_wait();
   const AttnPlanHdr hdr = *a.w.hdr;
   const int c = blockIdx.x + 1, t = blockIdx.y / (D / 16), c0 = (blockIdx.y % (D / 16)) * 16, row = threadIdx.x;
   if ((long long)c * hdr.tile_quota >= hdr.tile_units) return;
