@@ -35,7 +35,7 @@ struct __align__(16) AttnStart {
   int32_t k, head, blk, pad;
   AttnEntry e;
 };
-struct AttnPlanHdr {
+struct __align__(16) AttnPlanHdr {
   int32_t n_req, T;
   int32_t n_dec, dec_units, dec_quota;      // (units times key/value heads)
   int32_t n_tile, tile_units, tile_quota;
@@ -115,6 +115,17 @@ __device__ __forceinline__ AttnStart locate_unit(const AttnEntry *e, const int32
   return s;
 }
 
+// A record of whole 16-byte words from L2.
+template <typename T>
+__device__ __forceinline__ void load_l2(T &out, const T *p) {
+  static_assert(sizeof(T) % 16 == 0, "whole words");
+#pragma unroll
+  for (size_t i = 0; i < sizeof(T) / 16; ++i) {
+    const int4 v = __ldcg(reinterpret_cast<const int4 *>(p) + i);
+    memcpy(reinterpret_cast<char *>(&out) + 16 * i, &v, 16);
+  }
+}
+
 // A CTA's walk over its share: `take` blocks from block `blk` of (entry k, head).
 struct WorkWalk {
   int k, head, blk, take, u;              // u: position of the item's first block
@@ -124,7 +135,7 @@ struct WorkWalk {
   // false: the share is done
   __device__ __forceinline__ bool load(const AttnEntry *list, int n, int n_kv, int cost, int end) {
     if (k >= n) return false;
-    if (!have) e = list[k];
+    if (!have) load_l2(e, list + k);
     have = true;
     u = e.unit0 * n_kv + head * (e.nb + cost) + cost;
     take = min(e.nb, end - u) - blk;

@@ -7,7 +7,8 @@
 // work partition of attn_plan.cuh).  An item with at most 128 rows (short chunks, drafts, single tokens of wide groups: bound by
 // HBM) uses both tiles on the same rows, one for the even and one for the odd blocks, and joins them at its end.  Roles of the warps:
 //   warp 9     brings Q (4-D TMA boxes: D, heads of the group, head, tokens) and the pages of K and V (128-byte swizzle)
-//   warp 8     issues tcgen05.mma: S_t = Q_t K^T into tensor memory, O_t += P_t V with P_t read from there
+//   warp 8     issues tcgen05.mma: S_t = Q_t K^T into tensor memory, O_t += P_t V with P_t read from there (warp 10: for the second
+//              tile of an item with at most 128 rows)
 //   warps 0-3, 4-7   softmax of tile 0 and 1: a thread owns a row, so maximum and sum need no exchange
 // While one tile is in its softmax the tensor pipe works for the other: one warp issues for both in turn, P_t V of block j and
 // then Q_t K^T of block j+1, which keeps the two out of step (two issuing warps fell into step: 4750 against 3870 clocks a
@@ -24,7 +25,7 @@
 
 namespace ftmoe {
 
-constexpr int kTileThreads = 320, kTileHalf = 64;    // keys of half a block
+constexpr int kTileThreads = 352, kTileHalf = 64;    // keys of half a block
 template <int D> struct TileCfg {
   static constexpr int kChunks = D / 64;                    // 64-element pieces of D: 128 rows x 128 bytes each
   static constexpr int kTile = 128 * D * 2;                 // bytes of 128 rows of Q, K or V
@@ -84,6 +85,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 __device__ __forceinline__ int first_half(bool keys, int t, int h0) { return keys && ((h0 >> 1) & 1) != t ? 2 * ((h0 >> 1) + 1) : h0; }
 __device__ __forceinline__ int next_half(bool keys, int h) { return keys && (h & 1) ? h + 3 : h + 1; }
 
+__device__ __forceinline__ int count_halves(bool keys, int t, int h0, int h1) {
+  auto below = [t](int h) { return 2 * (h >> 2) + max(0, min(2, (h & 3) - 2 * t)); };     // of the blocks of parity t
+  return keys ? max(0, below(h1) - below(h0)) : h1 - h0;
+}
+
 // What a tile of a work item covers.
 struct TileSpan {
   int n, lo, hi, pos0;       // rows' tokens, keys [lo, hi) some row attends to, position of the first token
@@ -129,7 +135,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   if (tid == 0) {
     for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     mbar_init(q_full, 1);
-    mbar_init(q_empty, 1);
+    mbar_init(q_empty, 2);
     for (int t = 0; t < 2; ++t) {
       mbar_init(s_full(t), 1);
       for (int i = 0; i < 2; ++i) { mbar_init(p_full(t, i), 4); mbar_init(pv_done(t, i), 1); }
@@ -147,12 +153,17 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
-  grid_wait();
-  const AttnPlanHdr hdr = *a.w.hdr;
-  const AttnStart st = a.w.tile_start[blockIdx.x];     // (stale beyond the shares in use: not looked at)
+  // The kernel before in the stream is the streaming kernel of the same call, which lets this one start only after its own wait:
+  // all before it is complete.  This one shares no output with it and starts on the SMs it leaves; it waits at its end, so that
+  // what follows has both behind it.
+  AttnPlanHdr hdr;
+  AttnStart st;                                        // (stale beyond the shares in use: not looked at)
+  load_l2(hdr, a.w.hdr);
+  load_l2(st, a.w.tile_start + blockIdx.x);
   const long long u_first = (long long)blockIdx.x * hdr.tile_quota;
   if (u_first >= hdr.tile_units) {
     if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    grid_wait();
     return;
   }
   const int u_end = (int)min(u_first + hdr.tile_quota, (long long)hdr.tile_units);
@@ -179,7 +190,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         // lane i holds the page of box i of a block; boxes first .. last-1 of a block are loaded
         auto page_of = [&](int b) -> int {
           const int key = (e.b0 + b) * kTileKeys + lane * box_rows;
-          return lane < boxes && key < hi && key + box_rows > lo ? row[key >> a.page_shift] : 0;
+          return lane < boxes && key < hi && key + box_rows > lo ? __ldcg(row + (key >> a.page_shift)) : 0;
         };
         auto checked = [&](int page) -> int {              // never followed out of the pool: page 0 instead, and reported
           if (__builtin_expect((uint32_t)page >= (uint32_t)a.n_pages, 0)) {
@@ -231,7 +242,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         }
       }
     } else {
-      // ------------------------------ tensor core ------------------------------
+      // ------------------------------ tensor core (warps 8 and 10) ------------------------------
+      const int mine = warp == 8 ? 0 : 1;
       constexpr uint32_t type = BF16 ? (1u << 7) | (1u << 10) : 0u;
       constexpr uint32_t idesc_qk = (1u << 4) | type | ((uint32_t)(kTileKeys >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);
       constexpr uint32_t idesc_pv = (1u << 4) | type | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);
@@ -253,8 +265,15 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         h10 = first_half(keys, 1, h10);
         // halves in use by both tiles, the first one of neither among them
         const int hf = max(h00, h10), hl = keys ? 0 : min(h01, h11);
+        const uint32_t base0 = cp0, base1 = cp1;
         wait_phase(q_full, items & 1u, limit, s_abort, a.status);
         ++items;
+        bool gave_q = false;
+        if (!keys && mine == 1) {                             // both tiles are the other warp's
+          const uint32_t to = rs + 2 * take;
+          rph ^= (to / Cfg::kStages) & 1u;
+          rs = to % Cfg::kStages;
+        } else
         // step j: P V of block j - lag, Q K^T of block j; the ring holds V and K in this order
 #pragma unroll 1
         for (int j = 0; j < take + lag; ++j) {
@@ -265,6 +284,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
           if (has_v) step(rs, rph);
           const uint32_t ks = rs, kph = rph;
           if (has_k) step(rs, rph);
+          if (keys && (kb & 1) != mine) continue;
+          const bool last_k = has_k && j + lag >= take;
           const uint32_t vt = ring + vs * Cfg::kTile;
           if (has_k) ok = wait_phase(full_bar(ks), kph, limit, s_abort, a.status);
           if (has_v) {
@@ -310,7 +331,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                     if (t == 1) {
                       umma_commit(empty_bar(vs));
                       umma_commit(empty_bar(ks));
-                      if (j == take - 1) umma_commit(q_empty);
+                      if (last_k) umma_commit(q_empty);
                     }
                   }
                 }
@@ -357,13 +378,20 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
               if (keys || t == 1) {
                 if (has_v) umma_commit(empty_bar(vs));
                 if (has_k) umma_commit(empty_bar(ks));
-                if (j == take - 1) umma_commit(q_empty);
+                if (last_k) umma_commit(q_empty);
               }
             }
             __syncwarp();
           }
           }
+          gave_q = gave_q || last_k;
         }
+        if (!gave_q) {
+          if (elect_one()) mbar_arrive(q_empty);
+          __syncwarp();
+        }
+        cp0 = base0 + count_halves(keys, 0, h00, h01);
+        cp1 = base1 + count_halves(keys, 1, h10, h11);
         no0 += h01 > h00 ? 1u : 0u;
         no1 += h11 > h10 ? 1u : 0u;
       }
@@ -604,6 +632,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
+  grid_wait();
 }
 
 // Joins the parts of the items that several CTAs of the tiled kernel shared, in the order of the CTAs:
