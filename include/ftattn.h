@@ -115,6 +115,14 @@ ft_status_t ft_attn_forward(ft_attn_t *h, const void *q, int64_t q_stride, const
 
 /* Waits for the device and returns (and clears) the latched device status. */
 ft_status_t ft_attn_sync_status(ft_attn_t *h);
+/* Test hook for the failure path of the bounded device-side waits, as ft_moe_debug_inject: withhold_mask names kernels whose
+ * first producer leaves out one copy, wait_polls is the poll limit of every wait from now on (0 = the default, 2^22).  The
+ * kernel then gives up, latches FT_ERR_TIMEOUT and runs to completion; ft_attn_sync_status reports it once and makes the
+ * handle usable again.  Per process and device; (0, 0) restores normal operation.  Waits for the device. */
+enum { FT_ATTN_DEBUG_WITHHOLD_STREAM = 1,   /* attention of requests with few rows */
+       FT_ATTN_DEBUG_WITHHOLD_TILE = 2,     /* attention of requests with many rows */
+       FT_ATTN_DEBUG_WITHHOLD_ROPE = 4 };   /* norm and rotation of many tokens */
+ft_status_t ft_attn_debug_inject(ft_attn_t *h, uint32_t withhold_mask, uint32_t wait_polls);
 /* Number of kernels this handle has launched since create. */
 ft_status_t ft_attn_launch_count(ft_attn_t *h, uint64_t *out);
 /* Text of the CUDA runtime error behind the most recent FT_ERR_CUDA / FT_ERR_OOM of a ft_attn_ call. */

@@ -26,7 +26,7 @@ DTYPES = {"bf16": (FT_ATTN_BF16, torch.bfloat16), "fp16": (FT_ATTN_FP16, torch.f
 # every symbol include/ftattn.h declares
 SYMBOLS = (
     "ft_attn_cache_bytes", "ft_attn_create", "ft_attn_destroy", "ft_attn_slots", "ft_attn_plan", "ft_attn_qk_rope",
-    "ft_attn_forward", "ft_attn_sync_status", "ft_attn_launch_count", "ft_attn_last_cuda_error",
+    "ft_attn_forward", "ft_attn_sync_status", "ft_attn_debug_inject", "ft_attn_launch_count", "ft_attn_last_cuda_error",
 )
 
 
@@ -57,6 +57,7 @@ def load():
         "ft_attn_qk_rope": (i32, [vp, i32, vp, i64, vp, i64, vp, i64, vp, vp, f32, vp, i32, i32, i32, vp, vp, vp, i64, vp, vp]),
         "ft_attn_forward": (i32, [vp, vp, i64, vp, vp, i64, vp, i64, vp, f32, vp]),
         "ft_attn_sync_status": (i32, [vp]),
+        "ft_attn_debug_inject": (i32, [vp, C.c_uint32, C.c_uint32]),
         "ft_attn_launch_count": (i32, [vp, C.POINTER(C.c_uint64)]),
         "ft_attn_last_cuda_error": (C.c_char_p, []),
     }
@@ -217,6 +218,9 @@ class FtAttn:
 
     def sync_status(self):
         return int(self._lib.ft_attn_sync_status(self._h))
+
+    def debug_inject(self, withhold_mask, wait_polls):
+        _check(self._lib.ft_attn_debug_inject(self._h, int(withhold_mask), int(wait_polls)), "ft_attn_debug_inject")
 
     def launch_count(self):
         n = C.c_uint64()

@@ -418,6 +418,18 @@ ft_status_t ft_attn_sync_status(ft_attn_t *h) {
   return (st & kStatBadIndex) ? FT_ERR_INVALID_ARG : FT_ERR_CUDA;
 }
 
+ft_status_t ft_attn_debug_inject(ft_attn_t *h, uint32_t withhold_mask, uint32_t wait_polls) {
+  if (!h) return FT_ERR_INVALID_ARG;
+  DeviceScope dev(h->cfg.device);
+  FA_CUDA(dev.err);
+  const uint32_t polls = wait_polls ? wait_polls : kDefaultWaitPolls;
+  FA_CUDA(cudaDeviceSynchronize());
+  FA_CUDA(cudaMemcpyToSymbol(g_debug_withhold, &withhold_mask, sizeof(withhold_mask)));
+  FA_CUDA(cudaMemcpyToSymbol(g_wait_polls, &polls, sizeof(polls)));
+  FA_CUDA(cudaDeviceSynchronize());
+  return FT_OK;
+}
+
 ft_status_t ft_attn_launch_count(ft_attn_t *h, uint64_t *out) {
   if (!h || !out) return FT_ERR_INVALID_ARG;
   *out = h->launches;

@@ -220,6 +220,7 @@ __global__ void __launch_bounds__(256) attn_rope_kernel(const RopeArgs a) {
   }
 }
 
+constexpr uint32_t kWithholdRope = 4u;   // ft_attn_debug_inject
 // The form for many tokens.  Dynamic shared memory: stages of [q row | k row | v row | table row], then the barriers.
 constexpr int kRopeStages = 5, kRopeBlocks = 2;    // tokens ahead in a block, blocks an SM
 __host__ __device__ inline int rope_stage_bytes(int heads, int D, int rot) { return (heads * D * 2 + rot * 4 + 127) / 128 * 128; }
@@ -251,6 +252,7 @@ __global__ void __launch_bounds__(544) attn_rope_stream_kernel(const RopeArgs a)
 
   if (warp == consumers / 32) {
     // ------------------------------ producer: positions 32 tokens at a time ------------------------------
+    bool withhold = blockIdx.x == 0 && (g_debug_withhold & kWithholdRope);
     for (int t0 = blockIdx.x; t0 < a.T && !*s_abort; t0 += 32 * step) {
       const int pos = t0 + lane * step < a.T ? a.position[t0 + lane * step] : -1;
       for (int i = 0; i < 32 && t0 + i * step < a.T; ++i) {
@@ -262,12 +264,13 @@ __global__ void __launch_bounds__(544) attn_rope_stream_kernel(const RopeArgs a)
         if (lane == 0) {
           const uint32_t dst = base + s * stage;
           mbar_expect_tx(full_bar(s), q_bytes + 2 * kv_bytes + (table ? 8 * a.rot_half : 0));
-          bulk_g2s(dst, a.q + t * a.q_stride, q_bytes, full_bar(s));
+          if (!withhold) bulk_g2s(dst, a.q + t * a.q_stride, q_bytes, full_bar(s));     // (withheld: test hook)
           bulk_g2s(dst + q_bytes, a.k + t * a.k_stride, kv_bytes, full_bar(s));
           bulk_g2s(dst + q_bytes + kv_bytes, a.v + t * a.v_stride, kv_bytes, full_bar(s));
           if (table) bulk_g2s(dst + q_bytes + 2 * kv_bytes, a.cos_sin + (long long)p * 2 * a.rot_half, 8 * a.rot_half, full_bar(s));
         }
         __syncwarp();
+        withhold = false;
         advance();
       }
     }

@@ -35,6 +35,7 @@ struct AttnFwdArgs {
   uint32_t *status;
 };
 
+constexpr uint32_t kWithholdAttnStream = 1u, kWithholdAttnTile = 2u;
 template <int D> struct StreamCfg {
   // four warps share a block's keys; with D = 64, where a block is half the bytes but nearly the same chain of latencies, two such
   // groups take the blocks in turn (one group: 850 clocks a block where HBM gives one in 700)
@@ -133,12 +134,14 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
 
   if (warp == Cfg::kWarps) {
     // ------------------------------ producer ------------------------------
+    const bool hook = g_debug_withhold & kWithholdAttnStream;
     // one 5-D box per page (or 64 tokens of one): 64 elements, tokens, 64-element chunks of D, keys and values
     for (; w.load(a.w.dec, hdr.n_dec, a.n_kv, kDecCost, u_end); w.next(a.n_kv)) {
       const AttnEntry &e = w.e;
       const int blk = w.blk, take = w.take, head = w.head;
       const int hi = max(0, e.pos0 + e.n_tok), lo = a.window > 0 ? max(0, e.pos0 - a.window + 1) : 0;
       const int32_t *row = a.table + (long long)e.req * a.table_stride;
+      bool withhold = hook && w.k == 0 && head == 0 && blk == 0;
       // the lanes hold the pages of the boxes of 32 / boxes blocks at a time, the next ones on their way
       const int per = 32 >> (6 - box_shift);
       auto pages_of = [&](int b) -> int {
@@ -162,7 +165,9 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
         if (*s_abort) break;
         if (elect_one()) mbar_expect_tx(full_bar(s), (uint32_t)(max(0, last - first) * box_rows * D * 4));
         __syncwarp();
-        for (int i = first; i < last; ++i) {
+        const bool skip = withhold;                                    // test hook: the block's copies never come
+        withhold = false;
+        for (int i = first; i < last && !skip; ++i) {
           const int z = __shfl_sync(0xffffffffu, pages, i0 + i) * 2 * a.n_kv + head;
           if (elect_one())
             tma_load_5d(ring + s * Cfg::kStage + i * box_rows * D * 4, &tm, 0, (key0 + i * box_rows) & (page_tokens - 1), 0, 0, z, full_bar(s));

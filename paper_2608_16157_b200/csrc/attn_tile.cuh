@@ -15,8 +15,8 @@
 // unit).  P overwrites its scores (tensor memory: 2 x (128 + D) columns) and is handed over in two halves of 64 keys.
 // No maximum is taken as a rule: a half block's weights are made with the row's present reference, and their sum tells
 // whether any exceeds 2^8; only then (and in a row's first half block) the maximum is taken, O rescaled in tensor memory and the
-// half repeated (the maximum is also taken where a mask is applied).  The result is the same, since weights and sum share one reference; 16-bit weights up to 2^8 have the same
-// relative rounding.
+// half repeated (the maximum is also taken where a mask is applied).  The result is the same, since weights and sum share one
+// reference; 16-bit weights up to 2^8 have the same relative rounding.
 // P is rounded to the values' type for the second product; scores, maxima, sums and O stay in 32 bits.
 #pragma once
 #include <type_traits>
@@ -31,7 +31,7 @@ template <int D> struct TileCfg {
   static constexpr int kTile = 128 * D * 2;                 // bytes of 128 rows of Q, K or V
   static constexpr int kStages = D == 128 ? 4 : 8;          // ring of K and V tiles
   static constexpr int kStage = 8 * 4096;                   // results on their way out
-  static constexpr int kBars = 2 * kStages + 2 + 14;
+  static constexpr int kBars = 2 * kStages + 2 + 14;         // (one place of them free)
   static constexpr int kSmem = 1024 + 2 * kTile + kStages * kTile + kStage + kBars * 8 + 64;
   static constexpr int kPart = 128 * (D + 2);               // floats of one tile's partial result: m[128], l[128], O[D][128]
 };
@@ -125,6 +125,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   auto empty_bar = [&](int s) { return bars + 8u * (Cfg::kStages + s); };
   const uint32_t q_full = bars + 8u * (2 * Cfg::kStages), q_empty = q_full + 8;
   auto s_full = [&](int t) { return q_full + 16 + 8u * t; };
+  const uint32_t handed = q_full + 32;
   auto p_full = [&](int t, uint32_t buf) { return q_full + 48 + 16u * t + 8u * buf; };
   // (by the parity of the half's number: a waiter knows the one before the last on each to be complete)
   auto pv_done = [&](int t, uint32_t i) { return q_full + 80 + 16u * t + 8u * (i & 1u); };
@@ -136,6 +137,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     mbar_init(q_full, 1);
     mbar_init(q_empty, 2);
+    mbar_init(handed, 2);
     for (int t = 0; t < 2; ++t) {
       mbar_init(s_full(t), 1);
       for (int i = 0; i < 2; ++i) { mbar_init(p_full(t, i), 4); mbar_init(pv_done(t, i), 1); }
@@ -179,6 +181,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     uint32_t items = 0;
     if (warp == 9) {
       // ------------------------------ loads ------------------------------
+      const bool hook = g_debug_withhold & kWithholdAttnTile;
       const int page_tokens = 1 << a.page_shift;
       const int box_shift = min(a.page_shift, 6), box_rows = 1 << box_shift, boxes = kTileKeys >> box_shift;
       for (; w.load(a.w.tile, hdr.n_tile, a.n_kv, kTileCost, u_end) && !*s_abort; w.next(a.n_kv)) {
@@ -200,6 +203,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
           return page;
         };
         const bool keys = e.n_tok <= tokens;
+        bool withhold = hook && w.k == 0 && head == 0 && blk == 0;
         const int lag = keys ? 2 : 1;             // V of a block comes behind K of the `lag`-th block after it: the order of use
         int page = page_of(blk), page1 = 0, page2 = 0;
         wait_phase(q_empty, (items & 1u) ^ 1u, limit, s_abort, a.status);
@@ -221,7 +225,9 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
           if (elect_one()) mbar_expect_tx(full_bar(rs), (uint32_t)(max(0, last - first) * box_rows * D * 2));
           __syncwarp();
           const uint32_t dst = ring + rs * Cfg::kTile;
-          for (int i = first; i < last; ++i) {
+          const bool skip = withhold;                      // test hook: the tile's copies never come
+          withhold = false;
+          for (int i = first; i < last && !skip; ++i) {
             const int z = (__shfl_sync(0xffffffffu, pages, i) * 2 + v) * a.n_kv + head, y = (key0 + i * box_rows) & (page_tokens - 1);
             if (elect_one()) {
 #pragma unroll
@@ -250,6 +256,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       // (little code, the same for both tiles and both halves: what this warp runs is not in the instruction cache for long
       // beside the softmax warps)
       uint32_t cp0 = 0, cp1 = 0, no0 = 0, no1 = 0; // halves of weights consumed, items so far
+      uint32_t switches = 0;
+      bool issued = false, keys_before = false;
       const uint64_t dq = umma_desc(q_smem, 16, 1024);
       for (; w.load(a.w.tile, hdr.n_tile, a.n_kv, kTileCost, u_end); w.next(a.n_kv)) {
         AttnEntry e = w.e;
@@ -266,6 +274,15 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         // halves in use by both tiles, the first one of neither among them
         const int hf = max(h00, h10), hl = keys ? 0 : min(h01, h11);
         const uint32_t base0 = cp0, base1 = cp1;
+        if (items > 0 && keys != keys_before) {
+          // tile 1 changes hands between the two warps, whose instructions are not ordered: both wait until all of both are
+          // complete (a commit is for products the thread has issued; without any, it only says so)
+          if (elect_one()) { if (issued) umma_commit(handed); else mbar_arrive(handed); }
+          __syncwarp();
+          wait_phase(handed, switches & 1u, limit, s_abort, a.status);
+          ++switches;
+        }
+        keys_before = keys;
         wait_phase(q_full, items & 1u, limit, s_abort, a.status);
         ++items;
         bool gave_q = false;
@@ -341,50 +358,51 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             cp0 += 2; cp1 += 2;
           } else {
 #pragma unroll 1
-          for (int t = keys ? kb & 1 : 0; t < (keys ? (kb & 1) + 1 : 2); ++t) {
-            const int h0 = t ? h10 : h00, h1 = t ? h11 : h01;
-            const int hb = has_v ? min(h1, 2 * kv + 2) : h0;
+            for (int t = keys ? kb & 1 : 0; t < (keys ? (kb & 1) + 1 : 2); ++t) {
+              const int h0 = t ? h10 : h00, h1 = t ? h11 : h01;
+              const int hb = has_v ? min(h1, 2 * kv + 2) : h0;
 #pragma unroll 1
-            for (int h = max(h0, 2 * kv); h < hb; ++h) {
-              const uint32_t cp = t ? cp1 : cp0;
-              if (h == h0) wait_phase(o_empty(t), ((t ? no1 : no0) & 1u) ^ 1u, limit, s_abort, a.status);
-              ok = wait_phase(p_full(t, cp & 1u), (cp >> 1) & 1u, limit, s_abort, a.status) && ok;
-              tc_fence_after();
-              if (elect_one()) {
-                if (ok) {
-                  const uint32_t p = tm_s + t * 128 + (h & 1) * 32, o = tm_o + t * D;
-                  const uint64_t d = dv + (h & 1) * (8192 >> 4);
-                  umma_ts(o, p, d, idesc_pv, h == h0 ? 0u : 1u);
+              for (int h = max(h0, 2 * kv); h < hb; ++h) {
+                const uint32_t cp = t ? cp1 : cp0;
+                if (h == h0) wait_phase(o_empty(t), ((t ? no1 : no0) & 1u) ^ 1u, limit, s_abort, a.status);
+                ok = wait_phase(p_full(t, cp & 1u), (cp >> 1) & 1u, limit, s_abort, a.status) && ok;
+                tc_fence_after();
+                if (elect_one()) {
+                  if (ok) {
+                    const uint32_t p = tm_s + t * 128 + (h & 1) * 32, o = tm_o + t * D;
+                    const uint64_t d = dv + (h & 1) * (8192 >> 4);
+                    umma_ts(o, p, d, idesc_pv, h == h0 ? 0u : 1u);
 #pragma unroll
-                  for (int kk = 1; kk < 4; ++kk) umma_ts(o, p + kk * 8, d + kk * (2048 >> 4), idesc_pv, 1u);
+                    for (int kk = 1; kk < 4; ++kk) umma_ts(o, p + kk * 8, d + kk * (2048 >> 4), idesc_pv, 1u);
+                  }
+                  umma_commit(pv_done(t, cp));
                 }
-                umma_commit(pv_done(t, cp));
+                __syncwarp();
+                cp0 += 1 - t; cp1 += t;
+              }
+              if (elect_one()) {
+                if (has_k && 2 * kb < h1 && 2 * kb + 2 > h0) {
+                  if (ok) {
+                    const uint32_t ds = tm_s + t * 128;
+                    const uint64_t d = dq + (keys ? 0 : t) * (Cfg::kTile >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk)
+                      umma_bf16(ds, d + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16, dk + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16, idesc_qk,
+                                kk != 0 ? 1u : 0u);
+                  }
+                  umma_commit(s_full(t));
+                }
+                if (keys || t == 1) {
+                  if (has_v) umma_commit(empty_bar(vs));
+                  if (has_k) umma_commit(empty_bar(ks));
+                  if (last_k) umma_commit(q_empty);
+                }
               }
               __syncwarp();
-              cp0 += 1 - t; cp1 += t;
             }
-            if (elect_one()) {
-              if (has_k && 2 * kb < h1 && 2 * kb + 2 > h0) {
-                if (ok) {
-                  const uint32_t ds = tm_s + t * 128;
-                  const uint64_t d = dq + (keys ? 0 : t) * (Cfg::kTile >> 4);
-#pragma unroll
-                  for (int kk = 0; kk < D / 16; ++kk)
-                    umma_bf16(ds, d + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16, dk + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16, idesc_qk,
-                              kk != 0 ? 1u : 0u);
-                }
-                umma_commit(s_full(t));
-              }
-              if (keys || t == 1) {
-                if (has_v) umma_commit(empty_bar(vs));
-                if (has_k) umma_commit(empty_bar(ks));
-                if (last_k) umma_commit(q_empty);
-              }
-            }
-            __syncwarp();
-          }
           }
           gave_q = gave_q || last_k;
+          issued = true;
         }
         if (!gave_q) {
           if (elect_one()) mbar_arrive(q_empty);
@@ -412,6 +430,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       const bool keys = e.n_tok <= tokens;
       const TileSpan sp = tile_span(e, keys ? 0 : t, tokens, a.window);
       const bool valid = tok < sp.n;                       // (tok < tokens holds for rows below tokens * group)
+      const bool any_row = __any_sync(0xffffffffu, valid);
       const int pos = valid ? sp.pos0 + tok : -1;
       int h0, h1;
       sp.halves(e.b0 + blk, e.b0 + blk + take, &h0, &h1);
@@ -440,21 +459,37 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         f2_split(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])), l0, l1);
         sum = l0 + l1;
       };
+      auto hand_over = [&](int half) {
+        l += sum;
+        tmem_st16(ts + half * 32, p[0]);
+        tmem_st16(ts + half * 32 + 16, p[1]);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(t, cs & 1u));
+        ++cs;
+      };
 #pragma unroll 1
-      for (int h = h0; h < h1; h = next_half(keys, h), ++cs) {
+      for (int h = h0; h < h1; h = next_half(keys, h)) {
         if (h == h0 || (h & 1) == 0) {
           wait_phase(s_full(t), cb & 1u, limit, s_abort, a.status);
           tc_fence_after();
           ++cb;
         }
+        if (!any_row) {                                    // nothing of this warp's rows is wanted
+          if (lane == 0) mbar_arrive(p_full(t, cs & 1u));
+          ++cs;
+          continue;
+        }
         const uint32_t th = ts + (h & 1) * kTileHalf;
         tmem_ld32(th, x[0]);
         tmem_ld32(th + 32, x[1]);
         tmem_ld_wait();
+        const bool plain = h >= f0 && h < f1;              // nothing to mask
         bool over = true;
-        if (h >= f0 && h < f1) {
+        if (plain) {
           weights(m);
-          over = !(sum <= 256.f);                          // (true too for a row without a reference: its sum is not a number)
+          over = valid && !(sum <= 256.f);                 // (true too for a row without a reference: its sum is not a number)
         }
         if (__builtin_expect(__any_sync(0xffffffffu, over), 0)) {
           const int first = h * kTileHalf;
@@ -462,7 +497,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
 #pragma unroll
             for (int i = 0; i < 64; ++i) x[i >> 5][i & 31] ^= 0x80000000u;
           }
-          if (!(h >= f0 && h < f1)) {
+          if (!plain) {
             const int c_hi = pos - first, c_lo = a.window > 0 ? pos - a.window + 1 - first : -1;
 #pragma unroll
             for (int i = 0; i < 64; ++i)
@@ -476,7 +511,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
 #pragma unroll
             for (int i = 0; i < 8; ++i) mx[i] = max3(mx[i], __uint_as_float(x[c >> 5][(c & 31) + i]), __uint_as_float(x[c >> 5][(c & 31) + 8 + i]));
           const float bm = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * sl2;
-          const bool grow = bm > m + 8.f || (over && bm > m && h >= f0 && h < f1);
+          const bool grow = bm > m + 8.f || (plain && over && bm > m);
           if (h > h0 && __any_sync(0xffffffffu, grow)) {
             // the product of the half before has to be in O (this one's is not asked for yet)
             wait_phase(pv_done(t, cs - 1), ((cs - 1) >> 1) & 1u, limit, s_abort, a.status);
@@ -496,13 +531,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
           if (grow) m = bm;
           weights(m == -INFINITY ? 0.f : m);               // (every score -infinity: weights of 0)
         }
-        l += sum;
-        tmem_st16(ts + (h & 1) * 32, p[0]);
-        tmem_st16(ts + (h & 1) * 32 + 16, p[1]);
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(p_full(t, cs & 1u));
+        hand_over(h & 1);
       }
       const bool any = h1 > h0;
 
@@ -573,7 +602,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         // with `keys` the tiles share the columns out (D = 64: tile 0 takes them)
         const int c_begin = keys ? t * 64 : 0, c_end = keys ? min(D, (t + 1) * 64) : D;
 #pragma unroll 1
-        for (int c = c_begin; c < c_end; c += 64) {
+        for (int c = c_begin; c < c_end && any_row; c += 64) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             if (any) {
@@ -609,6 +638,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             for (int i = 0; i < 64; ++i) part[256 + (c + i) * 128 + row] = __uint_as_float(x[i >> 5][i & 31]);
           }
         }
+        if (!keys && any && !any_row && lane == 0) mbar_arrive(o_empty(t));
         if (keys) {                                           // both have read both
           tc_fence_before();
           named_sync(1, 256);

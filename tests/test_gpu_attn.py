@@ -314,6 +314,18 @@ def test_attention_many_requests(n_req):
     run_attn("bf16", 16, 4, 64, 16, 0, lens, seed=n_req, pad_rows=9)
 
 
+def test_attention_long_and_short_items_in_turn():
+    """Requests with more and with fewer than 128 rows in turn, several of both in every CTA's share, some of them cut."""
+    rng = np.random.default_rng(77)
+    lens = []
+    for i in range(60):
+        n = int(rng.choice([3, 5, 9, 17, 33, 70]))
+        lens.append((n, n + int(rng.integers(0, 400))))
+    run_attn("bf16", 16, 2, 64, 16, 0, lens, seed=77)
+    run_attn("fp16", 28, 4, 128, 32, 0, lens[:30], seed=78)
+    run_attn("bf16", 16, 2, 128, 64, 150, lens[:40], seed=79)
+
+
 def test_attention_one_long_request():
     """A single token and a few tokens over a long cache: the keys of one request are shared out and joined."""
     run_attn("bf16", 8, 1, 128, 64, 0, [(1, 20011)], seed=5)
@@ -375,6 +387,39 @@ def test_plan_bad_lengths_are_latched():
     for qs, kv in (([0, 3, 99], [3, 3]), ([0, 5, 4], [5, 5]), ([0, 1, 2], [1, 65]), ([0, 1, 2], [-1, 1]), ([0, 41, 42], [41, 1])):
         h.plan(i32(qs), i32(kv), 60, 40)
         assert h.sync_status() == B.FT_ERR_INVALID_ARG and h.sync_status() == 0
+    h.destroy()
+
+
+def test_waits_that_run_out_are_reported_and_leave_the_handle_usable():
+    """A producer withholds one copy: the bounded waits give up, the kernels return, the status says so once, and the next
+    calls are right again."""
+    hq, hkv, d, page = 8, 2, 128, 16
+    q, cache, table, cols, q_start, kv, max_new = make_attn("bf16", hq, hkv, d, page, 0, [(1, 900), (60, 300), (2, 700)], seed=21)
+    ref, _, wabs, vabs = R.attention(q, cache, table, q_start, kv, page, 0, d ** -0.5)
+    h = A.FtAttn(A.make_config(n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_tokens=page, n_pages=cache.shape[0], max_requests=3,
+                               max_tokens=6400, max_pages=cols))
+    qd, cd, td = q.to(DEV), cache.to(DEV), table.to(DEV)
+    x = torch.randn(6400, hq + 2 * hkv, d, device=DEV).bfloat16()
+    ids = torch.arange(6400, device=DEV, dtype=torch.int32)
+    rope_cache = torch.zeros_like(cd)
+    many = lambda o: h.qk_rope(x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], o, rope_cache, ids, torch.full_like(ids, -1))
+    good = torch.empty(6400, hq, d, device=DEV).bfloat16()
+    many(good)
+    for mask in (1, 2, 4):
+        h.debug_inject(mask, 2000)
+        out, o = torch.zeros_like(qd), torch.zeros_like(good)
+        if mask == 4:
+            many(o)
+        else:
+            h.plan(i32(q_start), i32(kv), q.shape[0], max_new)
+            h.forward(qd, cd, td, out)
+        assert h.sync_status() == B.FT_ERR_TIMEOUT and h.sync_status() == 0
+        h.debug_inject(0, 0)
+        h.plan(i32(q_start), i32(kv), q.shape[0], max_new)
+        h.forward(qd, cd, td, out)
+        many(o)
+        assert h.sync_status() == 0 and torch.equal(o, good)
+        assert ((out.double().cpu() - ref).abs() <= R.attention_bound("bf16", ref, wabs, vabs, 12.0)).all()
     h.destroy()
 
 
