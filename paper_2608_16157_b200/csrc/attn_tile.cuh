@@ -271,8 +271,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         tile_span(e, keys ? 0 : 1, tokens, a.window).halves(kb0, kb0 + take, &h10, &h11);
         h00 = first_half(keys, 0, h00);
         h10 = first_half(keys, 1, h10);
-        // halves in use by both tiles, the first one of neither among them
-        const int hf = max(h00, h10), hl = keys ? 0 : min(h01, h11);
+        // steps [f0, f1): both tiles use all of blocks j - 1 and j, the first half of neither among them
+        const int f0 = max(1, ((max(h00, h10) + 2) >> 1) + 1 - kb0), f1 = keys ? 0 : min(take, (min(h01, h11) >> 1) - kb0);
         const uint32_t base0 = cp0, base1 = cp1;
         if (items > 0 && keys != keys_before) {
           // tile 1 changes hands between the two warps, whose instructions are not ordered: both wait until all of both are
@@ -294,6 +294,86 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         // step j: P V of block j - lag, Q K^T of block j; the ring holds V and K in this order
 #pragma unroll 1
         for (int j = 0; j < take + lag; ++j) {
+          if (j == f0 && f0 < f1) {
+            // Steps in which both tiles use every half of both blocks.  What bounds a long prompt is this warp's own time (the
+            // scalar code around 32 products a step: they take 2048 of 3500 clocks), so it holds nothing else, and the ring's next
+            // two tiles are waited for where the warp would wait for weights.
+            const uint32_t b0 = cp0 & 1u, b1 = cp1 & 1u;
+            const uint32_t pa0 = p_full(0, b0), pb0 = p_full(0, b0 ^ 1u), pa1 = p_full(1, b1), pb1 = p_full(1, b1 ^ 1u);
+            const uint32_t va0 = pv_done(0, b0), vb0 = pv_done(0, b0 ^ 1u), va1 = pv_done(1, b1), vb1 = pv_done(1, b1 ^ 1u);
+            uint32_t xa0 = (cp0 >> 1) & 1u, xb0 = ((cp0 + 1) >> 1) & 1u, xa1 = (cp1 >> 1) & 1u, xb1 = ((cp1 + 1) >> 1) & 1u;
+            uint32_t vs = rs, vph = rph;
+            step(rs, rph);
+            uint32_t ks = rs, kph = rph;
+            step(rs, rph);
+            bool ok = wait_phase(full_bar(vs), vph, limit, s_abort, a.status);
+            ok = wait_phase(full_bar(ks), kph, limit, s_abort, a.status) && ok;
+#pragma unroll 1
+            for (; j < f1; ++j) {
+              const uint64_t dv = umma_desc(ring + vs * Cfg::kTile, 16384, 1024), dk = umma_desc(ring + ks * Cfg::kTile, 16, 1024);
+              const uint32_t give_v = empty_bar(vs), give_k = empty_bar(ks);
+              auto pv = [&](int t, int half) {
+#pragma unroll
+                for (int kk = half * 4; kk < half * 4 + 4; ++kk)
+                  umma_ts(tm_o + t * D, tm_s + t * 128 + kk * 8, dv + kk * (2048 >> 4), idesc_pv, 1u);
+              };
+              auto qk = [&](int t) {
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk)
+                  umma_bf16(tm_s + t * 128, dq + (t * Cfg::kTile + (kk >> 2) * 16384 + (kk & 3) * 32) / 16,
+                            dk + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16, idesc_qk, kk != 0 ? 1u : 0u);
+              };
+              ok = wait_phase(pa0, xa0, limit, s_abort, a.status) && ok;
+              tc_fence_after();
+              if (elect_one()) {
+                if (ok) pv(0, 0);
+                umma_commit(va0);
+              }
+              __syncwarp();
+              ok = wait_phase(pb0, xb0, limit, s_abort, a.status) && ok;
+              tc_fence_after();
+              if (elect_one()) {
+                if (ok) { pv(0, 1); }
+                umma_commit(vb0);
+                if (ok) { qk(0); }
+                umma_commit(s_full(0));
+              }
+              __syncwarp();
+              ok = wait_phase(pa1, xa1, limit, s_abort, a.status) && ok;
+              tc_fence_after();
+              if (elect_one()) {
+                if (ok) pv(1, 0);
+                umma_commit(va1);
+              }
+              __syncwarp();
+              if (j + 1 < f1) {
+                vs = rs; vph = rph;
+                step(rs, rph);
+                ks = rs; kph = rph;
+                step(rs, rph);
+                ok = wait_phase(full_bar(vs), vph, limit, s_abort, a.status) && ok;
+                ok = wait_phase(full_bar(ks), kph, limit, s_abort, a.status) && ok;
+              }
+              ok = wait_phase(pb1, xb1, limit, s_abort, a.status) && ok;
+              tc_fence_after();
+              if (elect_one()) {
+                if (ok) { pv(1, 1); }
+                umma_commit(vb1);
+                if (ok) { qk(1); }
+                umma_commit(s_full(1));
+                umma_commit(give_v);
+                umma_commit(give_k);
+                if (j == take - 1) umma_commit(q_empty);
+              }
+              __syncwarp();
+              xa0 ^= 1u; xb0 ^= 1u; xa1 ^= 1u; xb1 ^= 1u;
+            }
+            cp0 += 2 * (f1 - f0);
+            cp1 += 2 * (f1 - f0);
+            issued = true;
+            gave_q = f1 == take;
+            // (j is the first step behind them)
+          }
           const int kb = kb0 + j, kv = kb - lag;
           const bool has_v = j >= lag, has_k = j < take;
           bool ok = true;
@@ -322,84 +402,48 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
           }
           tc_fence_after();
           const uint64_t dv = umma_desc(vt, 16384, 1024), dk = umma_desc(ring + ks * Cfg::kTile, 16, 1024);
-          if (has_v && has_k && 2 * kb - 2 > hf && 2 * kb + 2 <= hl) {
-            // every half of both blocks in use by both tiles
-            const uint32_t ppa = (cp0 >> 1) & 1u, ppb = (cp1 >> 1) & 1u;
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-              const uint32_t cp = t ? cp1 : cp0, ph = t ? ppb : ppa;
-#pragma unroll
-              for (int half = 0; half < 2; ++half) {
-                ok = wait_phase(p_full(t, (cp + half) & 1u), half && (cp & 1u) ? ph ^ 1u : ph, limit, s_abort, a.status) && ok;
-                tc_fence_after();
-                if (elect_one()) {
-                  if (ok)
-#pragma unroll
-                    for (int kk = half * 4; kk < half * 4 + 4; ++kk)
-                      umma_ts(tm_o + t * D, tm_s + t * 128 + kk * 8, dv + kk * (2048 >> 4), idesc_pv, 1u);
-                  umma_commit(pv_done(t, cp + half));
-                  if (half == 1) {
-                    if (ok)
-#pragma unroll
-                      for (int kk = 0; kk < D / 16; ++kk)
-                        umma_bf16(tm_s + t * 128, dq + (t * Cfg::kTile + (kk >> 2) * 16384 + (kk & 3) * 32) / 16,
-                                  dk + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16, idesc_qk, kk != 0 ? 1u : 0u);
-                    umma_commit(s_full(t));
-                    if (t == 1) {
-                      umma_commit(empty_bar(vs));
-                      umma_commit(empty_bar(ks));
-                      if (last_k) umma_commit(q_empty);
-                    }
-                  }
-                }
-                __syncwarp();
-              }
-            }
-            cp0 += 2; cp1 += 2;
-          } else {
 #pragma unroll 1
-            for (int t = keys ? kb & 1 : 0; t < (keys ? (kb & 1) + 1 : 2); ++t) {
-              const int h0 = t ? h10 : h00, h1 = t ? h11 : h01;
-              const int hb = has_v ? min(h1, 2 * kv + 2) : h0;
+          for (int t = keys ? kb & 1 : 0; t < (keys ? (kb & 1) + 1 : 2); ++t) {
+            const int h0 = t ? h10 : h00, h1 = t ? h11 : h01;
+            const int hb = has_v ? min(h1, 2 * kv + 2) : h0;
 #pragma unroll 1
-              for (int h = max(h0, 2 * kv); h < hb; ++h) {
-                const uint32_t cp = t ? cp1 : cp0;
-                if (h == h0) wait_phase(o_empty(t), ((t ? no1 : no0) & 1u) ^ 1u, limit, s_abort, a.status);
-                ok = wait_phase(p_full(t, cp & 1u), (cp >> 1) & 1u, limit, s_abort, a.status) && ok;
-                tc_fence_after();
-                if (elect_one()) {
-                  if (ok) {
-                    const uint32_t p = tm_s + t * 128 + (h & 1) * 32, o = tm_o + t * D;
-                    const uint64_t d = dv + (h & 1) * (8192 >> 4);
-                    umma_ts(o, p, d, idesc_pv, h == h0 ? 0u : 1u);
-#pragma unroll
-                    for (int kk = 1; kk < 4; ++kk) umma_ts(o, p + kk * 8, d + kk * (2048 >> 4), idesc_pv, 1u);
-                  }
-                  umma_commit(pv_done(t, cp));
-                }
-                __syncwarp();
-                cp0 += 1 - t; cp1 += t;
-              }
+            for (int h = max(h0, 2 * kv); h < hb; ++h) {
+              const uint32_t cp = t ? cp1 : cp0;
+              if (h == h0) wait_phase(o_empty(t), ((t ? no1 : no0) & 1u) ^ 1u, limit, s_abort, a.status);
+              ok = wait_phase(p_full(t, cp & 1u), (cp >> 1) & 1u, limit, s_abort, a.status) && ok;
+              tc_fence_after();
               if (elect_one()) {
-                if (has_k && 2 * kb < h1 && 2 * kb + 2 > h0) {
-                  if (ok) {
-                    const uint32_t ds = tm_s + t * 128;
-                    const uint64_t d = dq + (keys ? 0 : t) * (Cfg::kTile >> 4);
+                if (ok) {
+                  const uint32_t p = tm_s + t * 128 + (h & 1) * 32, o = tm_o + t * D;
+                  const uint64_t d = dv + (h & 1) * (8192 >> 4);
+                  umma_ts(o, p, d, idesc_pv, h == h0 ? 0u : 1u);
 #pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk)
-                      umma_bf16(ds, d + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16, dk + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16, idesc_qk,
-                                kk != 0 ? 1u : 0u);
-                  }
-                  umma_commit(s_full(t));
+                  for (int kk = 1; kk < 4; ++kk) umma_ts(o, p + kk * 8, d + kk * (2048 >> 4), idesc_pv, 1u);
                 }
-                if (keys || t == 1) {
-                  if (has_v) umma_commit(empty_bar(vs));
-                  if (has_k) umma_commit(empty_bar(ks));
-                  if (last_k) umma_commit(q_empty);
-                }
+                umma_commit(pv_done(t, cp));
               }
               __syncwarp();
+              cp0 += 1 - t; cp1 += t;
             }
+            if (elect_one()) {
+              if (has_k && 2 * kb < h1 && 2 * kb + 2 > h0) {
+                if (ok) {
+                  const uint32_t ds = tm_s + t * 128;
+                  const uint64_t d = dq + (keys ? 0 : t) * (Cfg::kTile >> 4);
+#pragma unroll
+                  for (int kk = 0; kk < D / 16; ++kk)
+                    umma_bf16(ds, d + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16, dk + ((kk >> 2) * 16384 + (kk & 3) * 32) / 16, idesc_qk,
+                              kk != 0 ? 1u : 0u);
+                }
+                umma_commit(s_full(t));
+              }
+              if (keys || t == 1) {
+                if (has_v) umma_commit(empty_bar(vs));
+                if (has_k) umma_commit(empty_bar(ks));
+                if (last_k) umma_commit(q_empty);
+              }
+            }
+            __syncwarp();
           }
           gave_q = gave_q || last_k;
           issued = true;
