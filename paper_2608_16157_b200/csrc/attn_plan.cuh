@@ -129,21 +129,24 @@ __device__ __forceinline__ void load_l2(T &out, const T *p) {
 // A CTA's walk over its share: `take` blocks from block `blk` of (entry k, head).
 struct WorkWalk {
   int k, head, blk, take, u;              // u: position of the item's first block
-  AttnEntry e;
-  bool have;                              // e is entry k
-  __device__ __forceinline__ void start(const AttnStart &s) { k = s.k; head = s.head; blk = s.blk; e = s.e; have = true; }
+  AttnEntry e, ahead;                     // entry k and, with its last head, the next one
+  __device__ __forceinline__ void start(const AttnStart &s) { k = s.k; head = s.head; blk = s.blk; e = s.e; }
   // false: the share is done
-  __device__ __forceinline__ bool load(const AttnEntry *list, int n, int n_kv, int cost, int end) {
+  __device__ __forceinline__ bool load(int n, int n_kv, int cost, int end) {
     if (k >= n) return false;
-    if (!have) load_l2(e, list + k);
-    have = true;
     u = e.unit0 * n_kv + head * (e.nb + cost) + cost;
     take = min(e.nb, end - u) - blk;
     return take > 0;
   }
-  __device__ __forceinline__ void next(int n_kv) {
+  // to be called for every item, before `next`: early, for the load to be over by then
+  __device__ __forceinline__ void fetch(const AttnEntry *list, int n, int n_kv, int end) {
+    if (head == n_kv - 1 && k + 1 < n && u + e.nb < end) load_l2(ahead, list + k + 1);
+  }
+  // (a share that ends with the item needs no other entry: `load` finds nothing left of this one)
+  __device__ __forceinline__ void next(int n_kv, int end) {
+    if (u + e.nb >= end) { blk = e.nb; return; }
     blk = 0;
-    if (++head == n_kv) { head = 0; ++k; have = false; }
+    if (++head == n_kv) { head = 0; ++k; e = ahead; }
   }
 };
 

@@ -136,7 +136,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
     // ------------------------------ producer ------------------------------
     const bool hook = g_debug_withhold & kWithholdAttnStream;
     // one 5-D box per page (or 64 tokens of one): 64 elements, tokens, 64-element chunks of D, keys and values
-    for (; w.load(a.w.dec, hdr.n_dec, a.n_kv, kDecCost, u_end); w.next(a.n_kv)) {
+    for (; w.load(hdr.n_dec, a.n_kv, kDecCost, u_end); w.next(a.n_kv, u_end)) {
       const AttnEntry &e = w.e;
       const int blk = w.blk, take = w.take, head = w.head;
       const int hi = max(0, e.pos0 + e.n_tok), lo = a.window > 0 ? max(0, e.pos0 - a.window + 1) : 0;
@@ -176,6 +176,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
         if (++s == Cfg::kStages) { s = 0; ph ^= 1u; }
       }
       if (*s_abort) break;
+      w.fetch(a.w.dec, hdr.n_dec, a.n_kv, u_end);
     }
     // copies of a CTA that gave up must land before its shared memory goes away
     abort_drain(s_abort);
@@ -187,7 +188,8 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
   // this warp's 16 keys of a block: in box key0 / box_rows, whose parts are [keys, values][chunk of D][token][64 elements]
   const int key0 = (warp & 3) * 16, chunk = box_rows * 128;
   const uint32_t my_keys = (key0 >> box_shift) * (box_rows * D * 4) + (key0 & (box_rows - 1)) * 128, my_values = my_keys + box_rows * D * 2;
-  for (; w.load(a.w.dec, hdr.n_dec, a.n_kv, kDecCost, u_end); w.next(a.n_kv)) {
+  for (; w.load(hdr.n_dec, a.n_kv, kDecCost, u_end); w.next(a.n_kv, u_end)) {
+    w.fetch(a.w.dec, hdr.n_dec, a.n_kv, u_end);
     const AttnEntry &e = w.e;
     const int blk = w.blk, take = w.take, head = w.head;
     const int hi = max(0, e.pos0 + e.n_tok), lo = a.window > 0 ? max(0, e.pos0 - a.window + 1) : 0;

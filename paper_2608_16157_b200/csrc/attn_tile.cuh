@@ -184,7 +184,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       const bool hook = g_debug_withhold & kWithholdAttnTile;
       const int page_tokens = 1 << a.page_shift;
       const int box_shift = min(a.page_shift, 6), box_rows = 1 << box_shift, boxes = kTileKeys >> box_shift;
-      for (; w.load(a.w.tile, hdr.n_tile, a.n_kv, kTileCost, u_end) && !*s_abort; w.next(a.n_kv)) {
+      for (; w.load(hdr.n_tile, a.n_kv, kTileCost, u_end) && !*s_abort; w.next(a.n_kv, u_end)) {
+        w.fetch(a.w.tile, hdr.n_tile, a.n_kv, u_end);
         AttnEntry e = w.e;
         e.n_tok = uniform(e.n_tok); e.pos0 = uniform(e.pos0); e.b0 = uniform(e.b0); e.tok0 = uniform(e.tok0);
         const int take = uniform(w.take), blk = w.blk, head = w.head;
@@ -259,7 +260,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       uint32_t switches = 0;
       bool issued = false, keys_before = false;
       const uint64_t dq = umma_desc(q_smem, 16, 1024);
-      for (; w.load(a.w.tile, hdr.n_tile, a.n_kv, kTileCost, u_end); w.next(a.n_kv)) {
+      for (; w.load(hdr.n_tile, a.n_kv, kTileCost, u_end); w.next(a.n_kv, u_end)) {
+        w.fetch(a.w.tile, hdr.n_tile, a.n_kv, u_end);
         AttnEntry e = w.e;
         e.n_tok = uniform(e.n_tok); e.pos0 = uniform(e.pos0); e.b0 = uniform(e.b0);
         const int take = uniform(w.take), kb0 = e.b0 + w.blk;
@@ -468,7 +470,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     const bool negate = a.scale_log2 < 0.f;
     uint32_t cs = 0, cb = 0;                               // halves and blocks so far
     const uint32_t ts = tm_s + t * 128 + lanes;
-    for (; w.load(a.w.tile, hdr.n_tile, a.n_kv, kTileCost, u_end); w.next(a.n_kv)) {
+    for (; w.load(hdr.n_tile, a.n_kv, kTileCost, u_end); w.next(a.n_kv, u_end)) {
       const AttnEntry &e = w.e;
       const int take = w.take, blk = w.blk, head = w.head;
       const bool keys = e.n_tok <= tokens;
@@ -479,9 +481,9 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       int h0, h1;
       sp.halves(e.b0 + blk, e.b0 + blk + take, &h0, &h1);
       h0 = first_half(keys, t, h0);
-      // halves in which every row of the tile attends to every key, after the first one
-      int f0 = h0 + 1, f1 = negate ? h0 : min(h1, (sp.pos0 + 1) / kTileHalf);
-      if (a.window > 0) f0 = max(f0, (sp.pos0 + sp.n - 1 - a.window + kTileHalf) / kTileHalf);
+      // halves in which every row of the tile attends to every key
+      const int f0 = a.window > 0 ? max(h0, (sp.pos0 + sp.n - 1 - a.window + kTileHalf) / kTileHalf) : h0;
+      const int f1 = min(h1, (sp.pos0 + 1) / kTileHalf);
       float m = valid ? -INFINITY : 0.f, l = 0.f;          // reference (log2 units) and sum of the row
       uint32_t x[2][32], p[2][16];
       float sum;
@@ -529,7 +531,8 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         tmem_ld32(th, x[0]);
         tmem_ld32(th + 32, x[1]);
         tmem_ld_wait();
-        const bool plain = h >= f0 && h < f1;              // nothing to mask
+        const bool clear = h >= f0 && h < f1;              // nothing to mask
+        const bool plain = clear && h > h0 && !negate;     // and a reference to begin with
         bool over = true;
         if (plain) {
           weights(m);
@@ -541,7 +544,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
 #pragma unroll
             for (int i = 0; i < 64; ++i) x[i >> 5][i & 31] ^= 0x80000000u;
           }
-          if (!plain) {
+          if (!clear) {
             const int c_hi = pos - first, c_lo = a.window > 0 ? pos - a.window + 1 - first : -1;
 #pragma unroll
             for (int i = 0; i < 64; ++i)
@@ -580,6 +583,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       const bool any = h1 > h0;
 
       // ------------------------------ result of the item ------------------------------
+      w.fetch(a.w.tile, hdr.n_tile, a.n_kv, u_end);
       if (sp.n > 0) {
         if (any) {
           wait_phase(pv_done(t, cs - 1), ((cs - 1) >> 1) & 1u, limit, s_abort, a.status);
