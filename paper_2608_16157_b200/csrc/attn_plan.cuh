@@ -7,6 +7,8 @@
 // another.  Block 0 writes what belongs to requests and the work partition, the other blocks the per-token arrays, the
 // released and the new pages.  Reads are of the step's old state alone: the stack below n_free, columns below held_r;
 // writes are of the stack from n_free up and columns from held_r up.
+// Bound: latency (a few KB): launch, the lengths, the scans, then block 0's partition.  Measured, launches back to back: 3.5 us for
+// 8 requests, 5.5 us for 250 mixed ones with 63 chunks among them or not.
 #pragma once
 #include "async.cuh"
 

@@ -8,7 +8,8 @@
 // Two forms.  Few tokens: a lane group keeps the cosines and sines of its token in registers and walks over
 // `heads_per_group` heads.  Many tokens: resident blocks, to whose shared memory a producer warp brings whole tokens and their
 // table rows with bulk copies, several tokens ahead (the position is only known after a load, the table row after another:
-// held in registers meanwhile, the data of too few tokens is on its way: 84 us against a copy's 55 us for 16384 tokens).
+// held in registers meanwhile, the data of too few tokens is on its way: 84 us for 16384 tokens of 32 + 2 x 4 heads of 128).
+// Measured with these heads: 65.4 us for 16384 tokens (5.27 TB/s; a copy takes 52.5), 7.2 us for 1021, 2.4 us for 8.
 #pragma once
 #include "async.cuh"
 #include "common.cuh"

@@ -12,6 +12,10 @@
 // At the end of a (request, head) the warps' (m, l, O) are joined in shared memory.  A request that was cut leaves its
 // parts in global memory; the CTA that arrives last (a counter per request and head) joins them in the order of the
 // CTAs, so results do not depend on who is last.
+// Measured (32 query and 4 kv heads of 128): 302 us for 128 requests with 2.03 GB of cache (6.74 TB/s, the rate of a copy), 17.4 us for 8
+// requests of 4000 tokens, 8.2 us for one of 1000, where launch, tables, first block and join follow one another.  More rows a
+// request (several tiles in a warp, or a group of warps each) lose against the tiled kernel on long contexts: 283 and 300 against
+// 247 us for 16 drafts of 5 rows x 8 heads of 64 over 32768 tokens.
 // Values that no row attends to (behind the last token, before a window) are zeroed in shared memory before use: their
 // weights are 0, but what stands there may be NaN.
 #pragma once
