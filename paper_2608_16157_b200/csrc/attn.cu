@@ -280,6 +280,8 @@ ft_status_t ft_attn_create(const ft_attn_config_t *cfg, ft_attn_t **out) {
   ft_attn *h = new (std::nothrow) ft_attn();
   if (!h) return FT_ERR_OOM;
   h->cfg = *cfg;
+  // a window no request outgrows hides nothing; left as it is, position - window could leave 32 bits
+  if (cfg->window >= (long long)cfg->max_pages * cfg->page_tokens) h->cfg.window = 0;
   h->page_shift = cfg->page_tokens == 16 ? 4 : cfg->page_tokens == 32 ? 5 : cfg->page_tokens == 64 ? 6 : 7;
   rc = allocate(h);
   if (rc != FT_OK) {
