@@ -183,7 +183,10 @@ __global__ void __launch_bounds__(256) attn_rope_kernel(const RopeArgs a) {
             x[V + 2 * i] *= inv * w2; x[V + 2 * i + 1] *= inv * w3;
           }
         }
-        if (a.interleaved) {
+        if (pair < 0) {                       // not rotated: an infinity must not reach its neighbour as infinity * 0
+#pragma unroll
+          for (int i = 0; i < 2 * V; ++i) y[i] = x[i];
+        } else if (a.interleaved) {
 #pragma unroll
           for (int i = 0; i < V; ++i) {
             y[2 * i] = x[2 * i] * c[i] - x[2 * i + 1] * s[i];

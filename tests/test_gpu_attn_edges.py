@@ -17,3 +17,38 @@ def test_a_window_wider_than_any_request_is_no_window(window):
     """Also for requests whose first rows stand before position 0 (more new rows than cached tokens)."""
     run_attn("bf16", 8, 2, 128, 16, window, [(1, 0), (40, 13), (2, 1), (30, 3), (60, 300), (1, 70)], seed=1)
     run_attn("fp16", 16, 2, 64, 32, window, [(40, 13), (300, 7), (0, 9), (2, 100)], seed=2)
+
+
+@pytest.mark.parametrize("d,rot,inter,norm,pad", [(128, 64, False, False, 0), (128, 64, False, True, 4), (64, 0, False, False, 0), (64, 32, True, False, 4),
+                                                  (128, 16, True, True, 0), (64, 24, False, False, 0)])
+@pytest.mark.parametrize("t", [5, 9001])
+def test_qk_rope_infinities_stay_in_their_element(d, rot, inter, norm, pad, t):
+    """An infinity or a NaN outside the rotated part reaches no other element: without a norm what is not rotated is copied; with
+    one (infinite mean square) every other finite element becomes 0."""
+    hq, hkv, page = 6, 2, 16
+    n_pages = R.ceil_div(t, page)
+    g = torch.Generator().manual_seed(d + rot)
+    x = torch.randn(t, (hq + 2 * hkv) * d + pad, generator=g).bfloat16()
+    view = x[:, :(hq + 2 * hkv) * d].unflatten(1, (hq + 2 * hkv, d))
+    bad = [rot + i for i in (0, 1, (d - rot) // 2, (d - rot) // 2 + 3, d - rot - 1)]
+    for i, b in enumerate(bad):
+        view[i % t, i % (hq + hkv), b] = [float("inf"), -float("inf"), float("nan")][i % 3]
+    cs = torch.randn(t, rot, generator=g).to(DEV) if rot else None
+    w = (1 + 0.3 * torch.randn(d, generator=g)).bfloat16().to(DEV) if norm else None
+    ids = torch.arange(t, dtype=torch.int32, device=DEV)
+    xd = x.to(DEV)[:, :(hq + 2 * hkv) * d].unflatten(1, (hq + 2 * hkv, d))
+    out, cache = torch.zeros(t, hq, d, device=DEV).bfloat16(), torch.zeros(n_pages, 2, hkv, page, d, device=DEV).bfloat16()
+    h = A.FtAttn(A.make_config(n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_tokens=page, n_pages=n_pages, max_requests=1, max_tokens=t, max_pages=4))
+    h.qk_rope(xd[:, :hq], xd[:, hq:hq + hkv], xd[:, hq + hkv:], out, cache, ids, ids, cs, w_q=w, w_k=w)
+    assert h.sync_status() == 0
+    keys = cache[:, 0].permute(0, 2, 1, 3).reshape(n_pages * page, hkv, d)[:t]
+    got, src = torch.cat([out, keys], 1).cpu(), view[:, :hq + hkv]
+    if not norm:
+        assert torch.equal(torch.nan_to_num(got[..., rot:], 9e9, 8e9, 7e9), torch.nan_to_num(src[..., rot:], 9e9, 8e9, 7e9))
+        assert torch.isfinite(got[..., :rot]).all()
+    else:
+        hit = ~torch.isfinite(src.float()).all(-1)                    # heads with an infinity or a NaN
+        assert torch.isfinite(got[~hit].float()).all() and hit.sum() == min(len(bad), t)
+        inf = torch.isinf(src.float()).any(-1)
+        assert torch.equal(torch.isnan(got[inf]), torch.isinf(src[inf])) and (torch.nan_to_num(got[inf].float()) == 0).all()
+    h.destroy()
