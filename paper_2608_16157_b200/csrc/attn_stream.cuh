@@ -84,6 +84,11 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(p));
   return p != 0;
 }
+// Of a row with reference m (log2 units) and sum l: the factor of its results and log(sum_j exp(s_j)).  Only an empty sum is a
+// row that attends to nothing; a sum that is not a number (an infinite or NaN score) stays one.
+__device__ __forceinline__ float row_inv(float l) { return l == 0.f ? 0.f : 1.f / l; }
+__device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147180559945f; }
+
 // Bounded wait without anything between the polls (limit: g_wait_polls, read once): a wait is on the critical path of every
 // block several times.  Returns false, after latching, if the phase never completes.
 __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, uint32_t limit, volatile int *abort_flag, uint32_t *status) {
@@ -337,12 +342,12 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
     constexpr int kCols = D / 4;                       // a thread owns 4 columns of every (kConsumers / kCols)-th row
     const int col = (tid % kCols) * 4, row0 = tid / kCols;
     auto write_row = [&](int r, float mm, float ll, float4 v) {
-      const float inv = ll > 0.f ? 1.f / ll : 0.f;
+      const float inv = row_inv(ll);
       const int tok = r / a.group, hq = head * a.group + r - tok * a.group;
       const long long t = e.tok0 + tok;
       *reinterpret_cast<uint2 *>(a.out + t * a.out_stride + hq * D + col) =
           make_uint2(pack_pair<BF16>(v.x * inv, v.y * inv), pack_pair<BF16>(v.z * inv, v.w * inv));
-      if (a.lse && col == 0) a.lse[t * a.n_q + hq] = ll > 0.f ? (mm + log2f(ll)) * 0.693147180559945f : -INFINITY;
+      if (a.lse && col == 0) a.lse[t * a.n_q + hq] = row_lse(mm, ll);
     };
     float *part = a.part + (size_t)(blockIdx.x * 2 + (blockIdx.x == c_first ? 1 : 0)) * Cfg::kPart;
     for (int r = row0; r < rows; r += Cfg::kConsumers / kCols) {

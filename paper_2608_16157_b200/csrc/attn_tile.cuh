@@ -624,7 +624,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
           __syncwarp();
         };
         auto store_lse = [&](float mm, float ll) {
-          if (a.lse && valid) a.lse[tg * a.n_q + hq] = ll > 0.f ? (mm + log2f(ll)) * 0.693147180559945f : -INFINITY;
+          if (a.lse && valid) a.lse[tg * a.n_q + hq] = row_lse(mm, ll);
         };
         const bool whole = take == e.nb;
         // (an item that began in the share before leaves its part in the CTA's first place, one that goes on in its second)
@@ -649,7 +649,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
           l = l * f_own + lo_sum * f_other;
           m = mj;
         }
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = row_inv(l);
         const uint32_t other_o = tm_o + (1 - t) * D + lanes;
         // with `keys` the tiles share the columns out (D = 64: tile 0 takes them)
         const int c_begin = keys ? t * 64 : 0, c_end = keys ? min(D, (t + 1) * 64) : D;
@@ -746,7 +746,7 @@ __global__ void __launch_bounds__(128) attn_join_kernel(const AttnFwdArgs a) {
     ll = ll * ex2(mm - bm) + lc * ex2(mc - bm);
     mm = mn;
   }
-  const float bm = mm == -INFINITY ? 0.f : mm, inv = ll > 0.f ? 1.f / ll : 0.f;
+  const float bm = mm == -INFINITY ? 0.f : mm, inv = row_inv(ll);
   float acc[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) acc[i] = 0.f;
@@ -767,7 +767,7 @@ __global__ void __launch_bounds__(128) attn_join_kernel(const AttnFwdArgs a) {
     for (int z = 0; z < 4; ++z) v[z] = pack_pair<BF16>(acc[i * 8 + 2 * z] * inv, acc[i * 8 + 2 * z + 1] * inv);
     dst[i] = make_uint4(v[0], v[1], v[2], v[3]);
   }
-  if (a.lse && c0 == 0) a.lse[tg * a.n_q + hq] = ll > 0.f ? (mm + log2f(ll)) * 0.693147180559945f : -INFINITY;
+  if (a.lse && c0 == 0) a.lse[tg * a.n_q + hq] = row_lse(mm, ll);
 }
 
 }  // namespace ftmoe

@@ -52,3 +52,31 @@ def test_qk_rope_infinities_stay_in_their_element(d, rot, inter, norm, pad, t):
         inf = torch.isinf(src.float()).any(-1)
         assert torch.equal(torch.isnan(got[inf]), torch.isinf(src[inf])) and (torch.nan_to_num(got[inf].float()) == 0).all()
     h.destroy()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_lse_of_rows_with_infinite_or_nan_scores(d):
+    """Such a row is no row that attends to nothing: its result and its lse are NaN, those of the others do not change."""
+    hq, hkv, page = 8, 2, 16
+    lens = [(1, 70), (1, 900), (40, 300), (200, 700), (1, 33), (50, 60)]
+    q, cache, table, cols, q_start, kv, max_new = make_attn("bf16", hq, hkv, d, page, 0, lens, seed=3)
+    h = A.FtAttn(A.make_config(n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_tokens=page, n_pages=cache.shape[0], max_requests=len(lens),
+                               max_tokens=q.shape[0], max_pages=cols))
+    h.plan(i32(q_start), i32(kv), q.shape[0], max_new)
+    q[int(q_start[1]), :, 0] = 1.0                    # (its score with the infinite key is +infinity)
+    res = []
+    for bad in (False, True):
+        if bad:        # kv head 1, the first element of one key of the first four requests
+            for r, (j, v) in enumerate(((5, "nan"), (640, "inf"), (7, "nan"), (130, "nan"))):
+                cache[int(table[r, j // page]), 0, 1, j % page, 0] = float(v)
+        out, lse = torch.zeros_like(q, device=DEV).contiguous(), torch.zeros(q.shape[0], hq, device=DEV)
+        h.forward(q.to(DEV), cache.to(DEV), table.to(DEV)[:, :cols], out, lse=lse)
+        assert h.sync_status() == 0
+        res.append((out.cpu(), lse.cpu()))
+    (o0, l0), (o1, l1) = res
+    assert torch.isfinite(l0).all()
+    nan = torch.zeros_like(l0, dtype=torch.bool)
+    nan[:int(q_start[4]), hq // 2:] = True          # (every row of these requests attends to the key in question)
+    assert torch.isnan(l1[nan]).all() and torch.isnan(o1[nan]).all()
+    assert torch.equal(l1[~nan], l0[~nan]) and torch.equal(o1[~nan], o0[~nan])
+    h.destroy()
