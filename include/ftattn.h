@@ -20,6 +20,8 @@
  *   - Indices found on the device that cannot be (a page id outside the pool, a slot outside the cache, a position
  *     beyond the rotation table, lengths that contradict the host's bounds) are skipped, never followed, and latched
  *     in a device status word: ft_attn_sync_status returns FT_ERR_INVALID_ARG once.
+ *     A page id outside the pool in a block table counts as a page of zeros for ft_attn_forward: no other request's
+ *     keys and values are read for it.
  *   - T = 0 or n_req = 0 is a no-op (ft_attn_slots and ft_attn_plan still record an empty step).
  *
  * Cache of one layer: [n_pages][2][n_kv_heads][page_tokens][head_dim] in the handle's dtype, contiguous, 16-byte aligned,

@@ -163,9 +163,9 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
           pages = next;
           i0 = 0;
           if (b + per < blk + take) next = pages_of(b + per);
-          if ((uint32_t)pages >= (uint32_t)a.n_pages) {                // never followed: page 0 instead, and reported
+          if ((uint32_t)pages >= (uint32_t)a.n_pages) {                // never followed: a box beyond the pool, which is zeros
             atomicOr(a.status, kStatBadIndex);
-            pages = 0;
+            pages = a.n_pages;
           }
         }
         const int key0 = (e.b0 + b) * kDecKeys;

@@ -200,10 +200,10 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
           const int key = (e.b0 + b) * kTileKeys + lane * box_rows;
           return lane < boxes && key < hi && key + box_rows > lo ? __ldcg(row + (key >> a.page_shift)) : 0;
         };
-        auto checked = [&](int page) -> int {              // never followed out of the pool: page 0 instead, and reported
+        auto checked = [&](int page) -> int {              // never followed: a box beyond the pool, which is zeros
           if (__builtin_expect((uint32_t)page >= (uint32_t)a.n_pages, 0)) {
             atomicOr(a.status, kStatBadIndex);
-            page = 0;
+            page = a.n_pages;
           }
           return page;
         };

@@ -80,3 +80,34 @@ def test_lse_of_rows_with_infinite_or_nan_scores(d):
     assert torch.isnan(l1[nan]).all() and torch.isnan(o1[nan]).all()
     assert torch.equal(l1[~nan], l0[~nan]) and torch.equal(o1[~nan], o0[~nan])
     h.destroy()
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,d,page", [("bf16", 8, 2, 64, 16), ("fp16", 16, 2, 128, 32), ("bf16", 8, 1, 128, 128), ("fp16", 4, 4, 64, 64)])
+def test_attention_of_a_bad_page_reads_no_other_page(dtype, hq, hkv, d, page):
+    """A page id outside the pool stands for a page of zeros: results do not depend on what any other request's pages hold, and the
+    requests with good tables are what they were."""
+    lens = [(1, 500), (60, 700), (1, 400), (60, 500), (1, 4 * page), (40, 4 * page)]
+    q, cache, table, cols, q_start, kv, max_new = make_attn(dtype, hq, hkv, d, page, 0, lens, seed=4)
+    owner = {int(p): r for r in range(len(lens)) for p in table[r, :R.ceil_div(lens[r][1], page)]}
+    zero = min(p for p in range(cache.shape[0]) if p not in owner)          # a page of nobody, for the reference
+    zeros = table.clone()
+    cache[zero] = 0
+    for r, b, p in ((0, 2, cache.shape[0]), (1, 1, -1), (1, 3, 1 << 30), (4, 0, -(1 << 31))):
+        table[r, b], zeros[r, b] = p, zero
+    h = A.FtAttn(A.make_config(n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_tokens=page, n_pages=cache.shape[0], max_requests=len(lens),
+                               max_tokens=q.shape[0], max_pages=cols, dtype=dtype))
+    ref, lse_ref, wabs, vabs = R.attention(q, cache, zeros, q_start, kv, page, 0, d ** -0.5)
+    bound = R.attention_bound(dtype, ref, wabs, vabs, float(lse_ref.abs().max()))
+    poison = cache.clone()
+    for p in range(cache.shape[0]):                              # every page that is not of the requests with bad entries
+        if owner.get(p) not in (0, 1, 4):
+            poison[p] = float("nan")
+    for c, rows in ((cache, range(len(lens))), (poison, (0, 1, 4))):
+        h.plan(i32(q_start), i32(kv), q.shape[0], max_new)
+        out = torch.zeros(q.shape, dtype=q.dtype, device=DEV)
+        h.forward(q.to(DEV), c.to(DEV), table.to(DEV), out)
+        assert h.sync_status() == B.FT_ERR_INVALID_ARG and h.sync_status() == 0
+        for r in rows:
+            z = slice(int(q_start[r]), int(q_start[r + 1]))
+            assert ((out[z].double().cpu() - ref[z]).abs() <= bound[z]).all(), r
+    h.destroy()
