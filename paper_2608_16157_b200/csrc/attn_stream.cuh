@@ -118,6 +118,7 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
   auto full_bar = [&](int s) { return bars + 8u * s; };
   auto empty_bar = [&](int s) { return bars + 8u * (Cfg::kStages + s); };
 
+  grid_let_next();
   if (tid == 0) {
     for (int s = 0; s < Cfg::kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 4); }
     *s_abort = 0;
@@ -126,7 +127,6 @@ attn_stream_kernel(const __grid_constant__ CUtensorMap tm, const AttnFwdArgs a) 
   }
   __syncthreads();
   grid_wait();
-  grid_let_next();                          // only now: the tiled kernel relies on it
   const AttnPlanHdr hdr = *a.w.hdr;
   const AttnStart start = a.w.dec_start[blockIdx.x];     // (stale beyond the shares in use: not looked at)
   const long long u_first = (long long)blockIdx.x * hdr.dec_quota;

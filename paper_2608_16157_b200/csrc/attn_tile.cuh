@@ -159,9 +159,7 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
-  // The kernel before in the stream is the streaming kernel of the same call, which lets this one start only after its own wait:
-  // all before it is complete.  This one shares no output with it and starts on the SMs it leaves; it waits at its end, so that
-  // what follows has both behind it.
+  grid_wait();
   AttnPlanHdr hdr;
   AttnStart st;                                        // (stale beyond the shares in use: not looked at)
   load_l2(hdr, a.w.hdr);
@@ -169,7 +167,6 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   const long long u_first = (long long)blockIdx.x * hdr.tile_quota;
   if (u_first >= hdr.tile_units) {
     if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
-    grid_wait();
     return;
   }
   const int u_end = (int)min(u_first + hdr.tile_quota, (long long)hdr.tile_units);
@@ -714,7 +711,6 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
-  grid_wait();
 }
 
 // Joins the parts of the items that several CTAs of the tiled kernel shared, in the order of the CTAs:

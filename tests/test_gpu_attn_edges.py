@@ -111,3 +111,61 @@ def test_attention_of_a_bad_page_reads_no_other_page(dtype, hq, hkv, d, page):
             z = slice(int(q_start[r]), int(q_start[r + 1]))
             assert ((out[z].double().cpu() - ref[z]).abs() <= bound[z]).all(), r
     h.destroy()
+
+
+@pytest.mark.parametrize("chunk", [1, 40])
+def test_steps_replayed_from_a_graph(chunk):
+    """slots, qk_rope and forward captured once; every replay takes the lengths, tables and activations that are there then."""
+    hq, hkv, d, page, n_pages, n_req, cols = 8, 2, 128, 16, 200, 6, 40
+    h = A.FtAttn(A.make_config(n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_tokens=page, n_pages=n_pages, max_requests=n_req,
+                               max_tokens=n_req * chunk, max_pages=cols))
+    t = n_req * chunk
+    rng, g = np.random.default_rng(chunk), torch.Generator().manual_seed(chunk)
+    z = lambda *n: torch.zeros(*n, dtype=torch.int32, device=DEV)
+    new, ctx, tab, fr, nf = z(n_req), z(n_req), z(n_req, cols), i32(rng.permutation(n_pages)), i32([n_pages])
+    o = dict(q_start=z(n_req + 1), kv_len=z(n_req), n_free_out=z(1), admitted=z(n_req), position=z(t), slot=z(t))
+    x, cs = torch.zeros(t, hq + 2 * hkv, d, device=DEV).bfloat16(), torch.randn(cols * page, d, generator=g).to(DEV)
+    q, out = (torch.zeros(t, hq, d, device=DEV).bfloat16() for _ in range(2))
+    cache = torch.zeros(n_pages, 2, hkv, page, d, device=DEV).bfloat16()
+
+    def step():
+        h.slots(new, ctx, tab, fr, nf, chunk, **o)
+        for _ in range(2):                                     # two layers (of one cache)
+            h.qk_rope(x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], q, cache, o["position"], o["slot"], cs)
+            h.forward(q, cache, tab, out)
+
+    state = [tab, fr, cache, q, out, *o.values()]
+    first = [s.clone() for s in state]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()                                                 # (nothing to do yet: all lengths are 0)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for s, f in zip(state, first):
+        s.copy_(f)
+    for i in range(12):
+        lens = [int(rng.integers(0, chunk + 1)) if rng.random() < 0.8 else chunk for _ in range(n_req)]
+        if i == 7:
+            lens[2] = -1
+        new.copy_(i32(lens))
+        x.copy_(torch.randn(x.shape, generator=g).bfloat16())
+        before = [s.clone() for s in state]
+        graph.replay()
+        assert h.sync_status() == 0
+        replayed = [s.clone() for s in state]
+        for s, b in zip(state, before):
+            s.copy_(b)
+        step()                                                 # the same step by calls: the same bits
+        assert h.sync_status() == 0
+        assert all(torch.equal(a, b) for a, b in zip(state, replayed))
+        assert o["admitted"].tolist() == [int(n >= 0) for n in lens]
+        rows = int(o["q_start"][-1])
+        ref, _, wabs, vabs = R.attention(q[:rows].cpu(), cache.cpu(), tab.cpu(), o["q_start"].tolist(), o["kv_len"].tolist(), page, 0, d ** -0.5)
+        assert ((out[:rows].double().cpu() - ref).abs() <= R.attention_bound("bf16", ref, wabs, vabs, 60.0)).all()
+        ctx.copy_(o["kv_len"])
+        nf.copy_(o["n_free_out"])
+    del graph
+    h.destroy()
