@@ -22,7 +22,8 @@
  *     in a device status word: ft_attn_sync_status returns FT_ERR_INVALID_ARG once.
  *     A page id outside the pool in a block table counts as a page of zeros for ft_attn_forward: no other request's
  *     keys and values are read for it.
- *   - T = 0 or n_req = 0 is a no-op (ft_attn_slots and ft_attn_plan still record an empty step).
+ *   - T = 0 or n_req = 0 is a no-op (ft_attn_slots and ft_attn_plan still record an empty step, and ft_attn_slots writes
+ *     its outputs: q_start[0] = 0, n_free_out, rows of -1).  Arrays without elements may be NULL.
  *
  * Cache of one layer: [n_pages][2][n_kv_heads][page_tokens][head_dim] in the handle's dtype, contiguous, 16-byte aligned,
  *   keys at index 0 and values at index 1 of the second axis.  Slot of a token = page id * page_tokens + offset.

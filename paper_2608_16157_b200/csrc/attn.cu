@@ -308,10 +308,10 @@ ft_status_t ft_attn_slots(ft_attn_t *h, int n_req, int T, int max_new, const int
                           int32_t *q_start, int32_t *kv_len, int32_t *n_free_out, int32_t *admitted, int32_t *position,
                           int32_t *slot, void *stream) {
   if (!h || !step_ok(h, n_req, T, max_new)) return FT_ERR_INVALID_ARG;
-  if (!new_len || !ctx_len || !table || !free_pages || !n_free || !q_start || !kv_len || !n_free_out || !admitted ||
+  if (!free_pages || !n_free || !q_start || !n_free_out || (n_req > 0 && (!new_len || !ctx_len || !table || !kv_len || !admitted)) ||
       (T > 0 && (!position || !slot)))
     return FT_ERR_INVALID_ARG;
-  if (table_stride < h->cfg.max_pages || n_free_out == n_free || kv_len == ctx_len) return FT_ERR_INVALID_ARG;
+  if (table_stride < h->cfg.max_pages || n_free_out == n_free || (n_req > 0 && kv_len == ctx_len)) return FT_ERR_INVALID_ARG;
   DeviceScope dev(h->cfg.device);
   FA_CUDA(dev.err);
   AttnSlotsArgs a;

@@ -287,14 +287,16 @@ __global__ void __launch_bounds__(NT) attn_slots_kernel(const AttnSlotsArgs a) {
   __syncthreads();
 
   if (blockIdx.x == 0) {
-    if (bad && r < a.n_req) atomicOr(a.status, kStatBadIndex);
+    if (bad && (r < a.n_req || r == 0)) atomicOr(a.status, kStatBadIndex);
     if (r < a.n_req) {
-      a.q_start[r] = q0;
       a.kv_len[r] = kv;
       a.admitted[r] = adm ? 1 : 0;
-      if (r == a.n_req - 1) a.q_start[r + 1] = q1;
+      a.q_start[r + 1] = q1;
     }
-    if (r == 0) *a.n_free_out = avail - taken;
+    if (r == 0) {
+      a.q_start[0] = 0;
+      *a.n_free_out = avail - taken;
+    }
     // (a request that is not admitted keeps its rows, which attend to nothing; rows past T do not exist)
     build_work<NT>(a, q1 > a.T ? 0 : n, q0, adm ? kv : 0, s_warp, s_freed, s_q, s_kv, s_need, s_unit);
     return;

@@ -169,3 +169,24 @@ def test_steps_replayed_from_a_graph(chunk):
         nf.copy_(o["n_free_out"])
     del graph
     h.destroy()
+
+
+@pytest.mark.parametrize("t", [0, 3])
+def test_a_step_without_requests(t):
+    h = A.FtAttn(A.make_config(n_q_heads=8, n_kv_heads=2, head_dim=64, page_tokens=16, n_pages=6, max_requests=4, max_tokens=8, max_pages=4))
+    z = lambda n: torch.full((n,), 9, dtype=torch.int32, device=DEV)
+    fr = i32([4, 2, 0, 1, 3, 5])
+    for tab in (torch.zeros(0, 4, dtype=torch.int32, device=DEV), torch.zeros(2, 4, dtype=torch.int32, device=DEV)):
+        o = dict(q_start=z(1), kv_len=z(0), n_free_out=z(1), admitted=z(0), position=z(t), slot=z(t))
+        h.slots(z(0), z(0), tab, fr, i32([5]), 0, **o)
+        assert h.sync_status() == 0
+        assert o["q_start"].tolist() == [0] and o["n_free_out"].tolist() == [5] and fr.tolist() == [4, 2, 0, 1, 3, 5]
+        assert o["position"].tolist() == [-1] * t and o["slot"].tolist() == [-1] * t
+        q, out = torch.zeros(t, 8, 64, device=DEV).bfloat16(), torch.full((t, 8, 64), 7.0, device=DEV).bfloat16()
+        h.forward(q, torch.zeros(6, 2, 2, 16, 64, device=DEV).bfloat16(), tab, out)
+        assert h.sync_status() == 0 and (out == 7.0).all()
+    h.slots(z(0), z(0), tab, fr, i32([7]), 0, **o)            # more free pages than there are
+    assert h.sync_status() == B.FT_ERR_INVALID_ARG
+    h.plan(z(1), z(0), t, 0)
+    assert h.sync_status() == 0
+    h.destroy()
