@@ -263,7 +263,8 @@ __global__ void __launch_bounds__(NT) attn_slots_kernel(const AttnSlotsArgs a) {
     if (fin) n = 0;
     if (ctx < 0 || (long long)ctx + n > cap) { bad = true; if (ctx < 0 || ctx > cap) ctx = 0; }
     held = (int)(((long long)ctx + p - 1) >> a.page_shift);
-    freed = fin ? held : 0;
+    if (fin && held > a.n_pages) bad = true;         // (nor may the sum of the requests leave 32 bits)
+    freed = fin && !bad ? held : 0;
   }
   const unsigned long long inc = block_scan<NT>(pack2((uint32_t)n, (uint32_t)freed), s_warp, &tot);
   const int q1 = (int)(uint32_t)inc, q0 = q1 - n, f1 = (int)(inc >> 32);

@@ -190,3 +190,17 @@ def test_a_step_without_requests(t):
     h.plan(z(1), z(0), t, 0)
     assert h.sync_status() == 0
     h.destroy()
+
+
+def test_released_pages_are_counted_beyond_32_bits():
+    """1024 finished requests that claim 2^22 + 1 pages each: more than the pool has, whatever the sum is modulo 2^32."""
+    cols = (1 << 22) + 1
+    h = A.FtAttn(A.make_config(n_q_heads=1, n_kv_heads=1, head_dim=64, page_tokens=16, n_pages=4096, max_requests=1024, max_tokens=8, max_pages=cols))
+    tab = torch.empty(1024, cols, dtype=torch.int32, device=DEV)
+    fr = torch.arange(4096, dtype=torch.int32, device=DEV)
+    z = lambda n: torch.zeros(n, dtype=torch.int32, device=DEV)
+    o = dict(q_start=z(1025), kv_len=z(1024), n_free_out=z(1), admitted=z(1024), position=z(8), slot=z(8))
+    h.slots(torch.full((1024,), -1, dtype=torch.int32, device=DEV), torch.full((1024,), cols * 16, dtype=torch.int32, device=DEV), tab, fr, i32([64]), 0, **o)
+    assert h.sync_status() == B.FT_ERR_INVALID_ARG
+    assert o["n_free_out"].tolist() == [64] and torch.equal(fr.cpu(), torch.arange(4096, dtype=torch.int32))
+    h.destroy()
