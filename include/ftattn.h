@@ -47,11 +47,11 @@ typedef struct {
   uint32_t struct_size;   /* = sizeof(ft_attn_config_t) */
   int32_t device;         /* CUDA device ordinal */
   int32_t dtype;          /* ft_attn_dtype_t: queries, keys, values, outputs, norm weights */
-  int32_t n_q_heads;      /* Hq */
+  int32_t n_q_heads;      /* Hq, <= 1024 */
   int32_t n_kv_heads;     /* Hkv, divides Hq; query head h reads key/value head h / (Hq/Hkv); Hq/Hkv <= 64 */
   int32_t head_dim;       /* D: 64 or 128 */
   int32_t page_tokens;    /* 16, 32, 64 or 128 */
-  int32_t n_pages;        /* pages of a layer's cache; n_pages * page_tokens < 2^31 */
+  int32_t n_pages;        /* pages of a layer's cache, < 2^22; n_pages * page_tokens < 2^31 */
   int32_t max_requests;   /* requests of one step, <= 1024 */
   int32_t max_tokens;     /* new tokens of one step, <= 2^20 */
   int32_t max_pages;      /* columns of the block table; max_pages * page_tokens < 2^31 */
@@ -61,7 +61,9 @@ typedef struct {
 /* Bytes of one layer's cache (0 if the configuration is not supported). */
 size_t ft_attn_cache_bytes(const ft_attn_config_t *cfg);
 
-/* FT_ERR_INVALID_ARG: a value out of its range; FT_ERR_UNSUPPORTED: head_dim or page_tokens that is not listed above;
+/* FT_ERR_INVALID_ARG: a value out of its range; FT_ERR_UNSUPPORTED: head_dim or page_tokens that is not listed above, or a
+ * step whose work units (key blocks of 64 tokens x n_kv_heads, of max_pages * page_tokens tokens for each of max_requests
+ * requests, and for each of max_tokens / (2 * floor(128 * Hkv / Hq)) + max_requests pieces) would not be counted in 31 bits;
  * FT_ERR_OOM: no device memory for the scratch. */
 ft_status_t ft_attn_create(const ft_attn_config_t *cfg, ft_attn_t **out);
 ft_status_t ft_attn_destroy(ft_attn_t *h);
