@@ -111,52 +111,52 @@ class Decoder:
 
 
 def serve(dec, prompts, n_new, chunk=48, log=None):
-    """Serves all prompts with the decoder's request rows; returns the answers of each."""
-    rows = dec.attn.cfg.max_requests
+    """Serves all prompts with the decoder's request rows; returns the answers of each.
+
+    Pages go by the requests' age (their order): while one waits for pages, younger ones bring no tokens, and if it cannot go on
+    although it is alone, the youngest gives its pages back and starts again later.  So the oldest always gets on, and all end."""
+    cfg = dec.attn.cfg
+    if n_new < 1 or not all(prompts):
+        raise ValueError("a request needs a prompt and at least one answer")
+    if any(-(-(len(p) + n_new - 1) // cfg.page_tokens) > min(cfg.n_pages, cfg.max_pages) for p in prompts):
+        raise ValueError("a request does not fit the page pool or its row of the block table")
     waiting, answers = list(range(len(prompts))), [[] for _ in prompts]
-    run = [None] * rows                      # [request, tokens given so far]; "done": pages go back in the next step
+    run = [None] * cfg.max_requests          # [request, tokens given so far]; "done": pages go back in the next step
+    blocked = None                           # the oldest request that got no pages in the last step
     while waiting or any(r is not None for r in run):
-        for i in range(rows):
-            if run[i] is None and waiting:
-                run[i] = [waiting.pop(0), 0]
-        new_len, tokens, take, left = [], [], [], dec.attn.cfg.max_tokens
-        for r in run:
-            if r == "done":
-                new_len.append(-1)
-                take.append(0)
-                continue
-            n = 0
-            if r is not None:
-                text = list(prompts[r[0]]) + answers[r[0]]
-                n = min(len(text) - r[1], chunk, left)
-                tokens += text[r[1]:r[1] + n]
-                left -= n
-            new_len.append(n)
-            take.append(n)
-        got, admitted = dec.step(new_len, tokens)
-        if log:
-            log(f"step: {sum(1 for n in new_len if n > 0)} requests, {len(tokens)} tokens, {sum(1 for n in new_len if n < 0)} finished, "
-                f"{sum(1 for n, a in zip(new_len, admitted) if n > 0 and not a)} wait for pages")
         for i, r in enumerate(run):
-            if r == "done":
-                run[i] = None
-            elif r is not None and take[i]:
-                if not admitted[i]:
-                    continue                 # waits for pages
-                r[1] += take[i]
-                if r[1] == len(prompts[r[0]]) + len(answers[r[0]]):
-                    answers[r[0]].append(got[i])
-                    if len(answers[r[0]]) == n_new:
+            if r is None and waiting:
+                run[i] = [waiting.pop(0), 0]
+        active = sorted((r[0], i) for i, r in enumerate(run) if r is not None and r != "done")
+        take, text, left = [0] * len(run), [[]] * len(run), cfg.max_tokens
+        for request, i in active:
+            if blocked is not None and request > blocked:
+                break
+            rest = (list(prompts[request]) + answers[request])[run[i][1]:]
+            take[i] = min(len(rest), chunk, left)
+            text[i] = rest[:take[i]]
+            left -= take[i]
+        new_len = [-1 if r == "done" else n for r, n in zip(run, take)]
+        got, admitted = dec.step(new_len, sum(text, []))
+        waits = [request for request, i in active if take[i] and not admitted[i]]
+        if log:
+            log(f"step: {sum(n > 0 for n in take)} requests, {sum(take)} tokens, {run.count('done')} finished, {len(waits)} wait for pages")
+        run = [None if r == "done" else r for r in run]
+        for request, i in active:
+            if take[i] and admitted[i]:
+                run[i][1] += take[i]
+                if run[i][1] == len(prompts[request]) + len(answers[request]):
+                    answers[request].append(got[i])
+                    if len(answers[request]) == n_new:
                         run[i] = "done"
-        if not any(admitted[i] for i, n in enumerate(new_len) if n > 0) and not any(n < 0 for n in new_len):
-            # everybody waits for everybody's pages: the youngest request starts again later
-            held = [i for i, r in enumerate(run) if r is not None and r != "done" and r[1]]
-            if len(held) < 2:
-                raise RuntimeError("a request does not fit the page pool")
-            last = max(held, key=lambda i: run[i][0])
-            waiting.insert(0, run[last][0])
-            answers[run[last][0]] = []
-            run[last] = "done"
+        blocked = min(waits, default=None)
+        if waits and sum(n > 0 for n in take) == 1:
+            last, i = max((request, i) for request, i in active if request == blocked or run[i][1])
+            if last == blocked:
+                raise RuntimeError("pages are missing from the pool")
+            waiting.insert(0, last)
+            answers[last] = []
+            run[i] = "done"
     return answers
 
 
