@@ -204,3 +204,110 @@ def test_released_pages_are_counted_beyond_32_bits():
     assert h.sync_status() == B.FT_ERR_INVALID_ARG
     assert o["n_free_out"].tolist() == [64] and torch.equal(fr.cpu(), torch.arange(4096, dtype=torch.int32))
     h.destroy()
+
+
+def tile_runs(lens, group, n_kv, window, grid):
+    """Longest run of steps of the tiled kernel in which both tiles use every half of two successive blocks, from the work
+    partition (items of two tiles of 128 // group tokens, blocks of 128 keys, three units an item besides its blocks)."""
+    tokens = 128 // group
+    entries, unit = [], 0
+    for n, kv in lens:
+        if n * group <= 16:
+            continue
+        for first in range(0, n, 2 * tokens):
+            m, pos0 = min(2 * tokens, n - first), kv - n + first
+            hi = max(0, pos0 + m)
+            lo = min(hi, max(0, pos0 - window + 1)) if window else 0
+            nb = max(1, R.ceil_div(hi, 128) - lo // 128)
+            entries.append((m, pos0, lo // 128, nb, unit))
+            unit += nb + 3
+    quota = max(1, R.ceil_div(unit * n_kv, grid))
+    best = 0
+    for m, pos0, b0, nb, unit0 in entries:
+        if m <= tokens:
+            continue
+        spans = []
+        for t in range(2):
+            n = min(tokens, m - t * tokens)
+            hi, lo = pos0 + t * tokens + n, max(0, pos0 + t * tokens - window + 1) if window else 0
+            spans.append((lo // 64, R.ceil_div(max(0, hi), 64)))
+        for head in range(n_kv):
+            u = unit0 * n_kv + head * (nb + 3) + 3
+            for c in range(u // quota, (u + nb - 1) // quota + 1):
+                k0, k1 = b0 + max(0, c * quota - u), b0 + min(nb, (c + 1) * quota - u)
+                h0, h1 = max(max(2 * k0, s[0]) for s in spans), min(min(2 * k1, s[1]) for s in spans)
+                best = max(best, min(k1 - k0, (h1 >> 1) - k0) - max(1, ((h0 + 2) >> 1) + 1 - k0))
+    return best
+
+
+def check_rows(dtype, hq, hkv, d, page, window, lens, rows, shape_keys=None, seed=0):
+    """Attention of whole requests, checked at `rows` packed rows against the 64-bit form (each as a request of one token)."""
+    q, cache, table, cols, q_start, kv, max_new = make_attn(dtype, hq, hkv, d, page, window, lens, seed=seed)
+    if shape_keys:
+        shape_keys(q, cache, table, kv)
+    t = q.shape[0]
+    h = A.FtAttn(A.make_config(n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_tokens=page, n_pages=cache.shape[0], max_requests=len(lens),
+                               max_tokens=t, max_pages=cols, dtype=dtype, window=window))
+    out, lse = torch.full((t, hq, d), 77.0, dtype=q.dtype, device=DEV), torch.full((t, hq), 77.0, device=DEV)
+    qd, cd, td = q.to(DEV), cache.to(DEV), table.to(DEV)
+    h.plan(i32(q_start), i32(kv), t, max_new)
+    h.forward(qd, cd, td, out, lse=lse)
+    again = out.clone()
+    h.forward(qd, cd, td, out)
+    assert h.sync_status() == 0 and torch.equal(again, out) and torch.isfinite(out).all() and torch.isfinite(lse).all()
+    req = np.searchsorted(q_start, rows, side="right") - 1
+    pos = [int(kv[r]) - int(q_start[r + 1]) + int(i) for r, i in zip(req, rows)]
+    ref, lse_ref, wabs, vabs = R.attention(q[rows], cache, table[req], list(range(len(rows) + 1)), [p + 1 for p in pos], page, window, d ** -0.5)
+    smax = float(lse_ref.abs().max())
+    err, bound = (out[rows].double().cpu() - ref).abs(), R.attention_bound(dtype, ref, wabs, vabs, smax)
+    assert (err <= bound).all(), float((err / bound).max())
+    assert ((lse[rows].double().cpu() - lse_ref).abs() <= 2.0 ** -15 * (1 + smax)).all()
+    h.destroy()
+
+
+def sample(rng, t, n):
+    return np.unique(np.concatenate([[0, 1, 127, 128, t // 2, t - 129, t - 2, t - 1], rng.integers(0, t, n)]))
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,d,page,window,lens", [
+    ("bf16", 32, 4, 128, 64, 0, [(4100, 4100)]), ("fp16", 32, 4, 128, 16, 0, [(2100, 6007)]),
+    ("bf16", 64, 8, 64, 32, 0, [(3001, 4100)]), ("fp16", 10, 10, 64, 128, 0, [(5000, 5000)]),
+    ("bf16", 16, 4, 128, 32, 1500, [(3000, 5000), (1, 900)]), ("fp16", 64, 8, 64, 16, 2049, [(2500, 6001)])])
+def test_attention_of_long_prompts(dtype, hq, hkv, d, page, window, lens):
+    """Shares of many blocks: the issuing warp's steady state runs for many steps, its ring and its parities wrap."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert tile_runs(lens, hq // hkv, hkv, window, sms) >= 8
+    check_rows(dtype, hq, hkv, d, page, window, lens, sample(np.random.default_rng(d + page), lens[0][0], 56), seed=page)
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,d", [("bf16", 32, 4, 128), ("fp16", 16, 2, 64)])
+def test_attention_of_a_long_prompt_with_growing_scores(dtype, hq, hkv, d):
+    """The score of a key grows with its position, by more than the 2^8 that a reference allows from block to block: results are
+    rescaled in every block."""
+    page, n = 32, 4000
+
+    def grow(q, cache, table, kv):
+        u = torch.randn(d, generator=torch.Generator().manual_seed(5))
+        u /= u.norm()
+        j = torch.arange(n)
+        k = cache[table[0].long()[j // page], 0, :, j % page].float() * 0.5 + (0.1 * d ** 0.5 / 4) * j[:, None, None] * u
+        cache[table[0].long()[j // page], 0, :, j % page] = k.to(cache.dtype)
+        q.copy_((q.float() * 0.25 + 4 * u).to(q.dtype))
+
+    check_rows(dtype, hq, hkv, d, page, 0, [(n, n)], sample(np.random.default_rng(7), n, 40), shape_keys=grow, seed=9)
+
+
+def test_attention_of_many_work_items():
+    """Work lists longer than a block of the partition has threads, and longer than the positions it keeps in shared memory."""
+    rng = np.random.default_rng(8)
+    lens = [(int(rng.integers(5, 12)), 0) for _ in range(250)]
+    lens = [(n, n + int(rng.integers(0, 60))) for n, _ in lens]
+    assert 256 < sum(R.ceil_div(n, 4) for n, _ in lens) < 2048
+    run_attn("bf16", 64, 1, 64, 16, 0, lens, seed=1)
+    lens = [(n, kv) for n, kv in lens for _ in range(4)]
+    assert sum(R.ceil_div(n, 4) for n, _ in lens) > 2048 and len(lens) <= 1024
+    run_attn("fp16", 64, 1, 64, 32, 0, lens, seed=2)
+
+
+def test_attention_of_a_prompt_of_many_work_items():
+    check_rows("bf16", 64, 1, 64, 64, 0, [(8400, 8400)], sample(np.random.default_rng(3), 8400, 40), seed=6)
