@@ -48,6 +48,16 @@ __device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a_tmem, uint64_t b,
       "r"(a_tmem), "l"(b), "r"(idesc), "r"(acc)
       : "memory");
 }
+// Whether the phase is complete, without waiting for it.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 // A value all lanes hold, in a uniform register.
 __device__ __forceinline__ int uniform(int v) { return __reduce_max_sync(0xffffffffu, v); }
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
@@ -299,8 +309,9 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         for (int j = 0; j < take + lag; ++j) {
           if (j == f0 && f0 < f1) {
             // Steps in which both tiles use every half of both blocks.  What bounds a long prompt is this warp's own time (the
-            // scalar code around 32 products a step: they take 2048 of 3500 clocks), so it holds nothing else, and the ring's next
-            // two tiles are waited for where the warp would wait for weights.
+            // scalar code around the 32 products of a step), so it holds nothing else, and the ring's next two tiles are looked for
+            // where the warp would wait for weights.  Looked for only: waiting there holds this step's last products back when
+            // the tiles come late (pages of 16: 515 tokens behind 7000 113 us against 102).
             const uint32_t b0 = cp0 & 1u, b1 = cp1 & 1u;
             const uint32_t pa0 = p_full(0, b0), pb0 = p_full(0, b0 ^ 1u), pa1 = p_full(1, b1), pb1 = p_full(1, b1 ^ 1u);
             const uint32_t va0 = pv_done(0, b0), vb0 = pv_done(0, b0 ^ 1u), va1 = pv_done(1, b1), vb1 = pv_done(1, b1 ^ 1u);
@@ -349,13 +360,13 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 umma_commit(va1);
               }
               __syncwarp();
+              bool there = true;
               if (j + 1 < f1) {
                 vs = rs; vph = rph;
                 step(rs, rph);
                 ks = rs; kph = rph;
                 step(rs, rph);
-                ok = wait_phase(full_bar(vs), vph, limit, s_abort, a.status) && ok;
-                ok = wait_phase(full_bar(ks), kph, limit, s_abort, a.status) && ok;
+                there = mbar_test(full_bar(vs), vph) && mbar_test(full_bar(ks), kph);
               }
               ok = wait_phase(pb1, xb1, limit, s_abort, a.status) && ok;
               tc_fence_after();
@@ -369,6 +380,10 @@ attn_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 if (j == take - 1) umma_commit(q_empty);
               }
               __syncwarp();
+              if (!there) {
+                ok = wait_phase(full_bar(vs), vph, limit, s_abort, a.status) && ok;
+                ok = wait_phase(full_bar(ks), kph, limit, s_abort, a.status) && ok;
+              }
               xa0 ^= 1u; xb0 ^= 1u; xa1 ^= 1u; xb1 ^= 1u;
             }
             cp0 += 2 * (f1 - f0);
