@@ -111,6 +111,8 @@ ft_status_t ft_attn_qk_rope(ft_attn_t *h, int T, const void *q, int64_t q_stride
  * position P = kv_len - n + i and attends to the cached tokens j <= P (and j > P - window):
  * out = sum_j softmax_j(scale * q.k_j) v_j, lse = log(sum_j exp(scale * q.k_j)).  A row that attends to nothing gets
  * zeros and lse = -infinity; a row with an infinite positive or NaN score among those it attends to gets NaN in both.
+ * The weights are rounded to the dtype before they multiply the values (as matrix operands); scores, maxima and sums are float.
+ * A value v_j that is itself infinite or NaN can make rows of the same request and step NaN that do not attend to j (weight 0).
  * Rows of no request are not written.
  *   q, out: DEVICE [T][Hq][D], strides in elements from token to token, 16-byte aligned, strides % 8 == 0
  *           and <= 2^23

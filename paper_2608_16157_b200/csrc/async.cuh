@@ -67,8 +67,8 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// Programmatic dependent launch: a kernel lets the next one of the stream be scheduled at once, and touches global memory only
-// after everything before it is complete.
+// Programmatic dependent launch: a kernel lets the next one of the stream be scheduled at once.  Only a kernel's own grid_wait makes
+// what the grids before it wrote visible to it.
 __device__ __forceinline__ void grid_let_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ uint4 lds_v4(uint32_t addr) {

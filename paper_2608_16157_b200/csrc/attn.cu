@@ -141,7 +141,7 @@ cudaError_t allow_smem() {
 }
 
 // A launch the stream's next kernel may be scheduled beside: every kernel here waits for all before it (grid_wait) before it
-// touches global memory, so only launch latency and prologues overlap.
+// touches memory that a kernel or a copy of the stream writes, so only launch latency and prologues overlap.
 template <typename... P, typename... Args>
 cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, Args &&...args) {
   cudaLaunchConfig_t cfg = {};

@@ -17,10 +17,12 @@
 // whether any exceeds 2^8; only then (and in a row's first half block) the maximum is taken, O rescaled in tensor memory and the
 // half repeated (the maximum is also taken where a mask is applied).  The result is the same, since weights and sum share one
 // reference; 16-bit weights up to 2^8 have the same relative rounding.
-// Measured at D = 128: a unit of 256 rows x 128 keys 3860 clocks (1.83 us): a tile's softmax 2700 and, behind it, its two products 1160;
-// pipe and special-function units are busy 2048 each.  A prompt of 16384 tokens with 32 heads: 1.77 - 1.84 ms in short bursts (1.2
-// PFLOP/s), 2.13 ms (1.03) in a long run under the power limit; of 4096: 159 us.  Two threads a row (16 softmax
-// warps of 96 registers) made a unit 1.90 us and that prompt 2.09 ms.
+// Measured, D = 128: a unit of 256 rows x 128 keys 1.88 us (items of 32 and 64 blocks, one a CTA; 3700 clocks at 1965 MHz).  A clock
+// trace, of the loop before the issuing warp's steady state had one of its own: 3860 clocks, of them a tile's softmax 2700 and, behind
+// it, its two products 1160; pipe and special-function units are busy 2048 each.  D = 64: 1.85 us, the same exponentials.  A prompt
+// of 16384 tokens with 32 heads of 128: 1.79 - 1.87 ms in short bursts (1.2 PFLOP/s), 2.11 - 2.17 ms (1.03) in a long run under the
+// power limit; of 4096: 159 - 166 us.  Two threads a row (16 softmax warps of 96 registers) made a unit 1.90 us against 1.85 in the same
+// run and that prompt 2.09 ms.  168 registers a thread; 68 (D = 128) and 32 (D = 64) bytes spilled.
 // P is rounded to the values' type for the second product; scores, maxima, sums and O stay in 32 bits.
 #pragma once
 #include <type_traits>
