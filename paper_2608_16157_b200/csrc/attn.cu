@@ -6,8 +6,8 @@
 
 #include <cstring>
 #include <new>
-#include <utility>
 
+#include "host.cuh"
 #include "attn_plan.cuh"
 #include "attn_rope.cuh"
 #include "attn_stream.cuh"
@@ -66,17 +66,6 @@ ft_status_t check_config(const ft_attn_config_t *c) {
   if (blocks * c->max_requests * c->n_kv_heads >= (1ll << 31) || blocks * entries * c->n_kv_heads >= (1ll << 31)) return FT_ERR_UNSUPPORTED;
   return FT_OK;
 }
-
-// Restores the calling thread's current device when the entry point returns.
-struct DeviceScope {
-  int prev = -1;
-  cudaError_t err;
-  explicit DeviceScope(int dev) {
-    err = cudaGetDevice(&prev);
-    if (err == cudaSuccess && prev != dev) err = cudaSetDevice(dev); else prev = -1;
-  }
-  ~DeviceScope() { if (prev >= 0) (void)cudaSetDevice(prev); }
-};
 
 void free_all(ft_attn *h) {
   (void)cudaFree(h->status_dev);
@@ -138,23 +127,6 @@ cudaError_t allow_smem() {
   if (e == cudaSuccess)
     e = cudaFuncSetAttribute(attn_tile_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, TileCfg<D>::kSmem);
   return e;
-}
-
-// A launch the stream's next kernel may be scheduled beside: every kernel here waits for all before it (grid_wait) before it
-// touches memory that a kernel or a copy of the stream writes, so only launch latency and prologues overlap.
-template <typename... P, typename... Args>
-cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, Args &&...args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
 }
 
 template <int D, bool BF16>

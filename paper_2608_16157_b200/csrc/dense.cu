@@ -1,0 +1,248 @@
+// Host side of include/ftdense.h: handle, validation, launches.
+#include "../../include/ftdense.h"
+
+#include <cuda_runtime.h>
+
+#include <atomic>
+#include <new>
+
+#include "dense_logp.cuh"
+#include "dense_norm.cuh"
+#include "dense_w4.cuh"
+#include "host.cuh"
+
+using namespace ftmoe;
+
+struct ft_dense {
+  int device = 0, sm_count = 148;
+  uint32_t *status_dev = nullptr;
+  uint64_t launches = 0;
+};
+
+namespace {
+
+std::atomic<int> g_dense_cuda_error{cudaSuccess};   // the CUDA error behind the latest FT_ERR_CUDA / FT_ERR_OOM
+
+#define FD_CUDA(expr)                                                                       \
+  do {                                                                                      \
+    cudaError_t e_ = (expr);                                                                \
+    if (e_ != cudaSuccess) {                                                                \
+      g_dense_cuda_error = e_;                                                              \
+      (void)cudaGetLastError();                                                             \
+      return e_ == cudaErrorMemoryAllocation ? FT_ERR_OOM : FT_ERR_CUDA;                    \
+    }                                                                                       \
+  } while (0)
+
+bool type16(int dtype) { return dtype == FT_DENSE_BF16 || dtype == FT_DENSE_FP16; }
+bool aligned(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+bool w4_ok(int64_t n, int64_t k, int group) {
+  return n >= 1 && n <= (1 << 24) && (group == 32 || group == 64 || group == 128) && k >= group && k <= 65536 && k % group == 0;
+}
+
+template <bool BF16, bool RES32>
+cudaError_t launch_norm(const NormArgs &a, bool wide, cudaStream_t st) {
+  const int threads = a.lanes > kNormThreads ? a.lanes : kNormThreads, rows = threads / a.lanes;
+  const unsigned grid = (unsigned)((a.T + rows - 1) / rows);
+  return wide ? launch(add_norm_kernel<BF16, RES32, 8>, grid, threads, 0, st, a) : launch(add_norm_kernel<BF16, RES32, 1>, grid, threads, 0, st, a);
+}
+
+template <bool BF16, int G, bool ZERO>
+cudaError_t launch_w4_stream(const ft_dense *h, const W4Args &a, cudaStream_t st) {
+  const int grid = 2 * h->sm_count;
+  // blocks of a cluster share the k of their tiles: as many as leave every cluster some tiles, so that shares are even
+  int cluster = 1;
+  while (cluster < kW4MaxCluster && grid / cluster > a.g.tiles / 4 && a.g.kb > cluster * kW4Warps) cluster *= 2;
+  int n = grid / cluster;
+  if (n > a.g.tiles) n = a.g.tiles;
+  if (a.T <= 8) return launch_clusters(w4_stream_kernel<BF16, G, ZERO, 1, 4>, dim3(n * cluster), kW4Warps * 32, 0, cluster, st, a, cluster);
+  return launch_clusters(w4_stream_kernel<BF16, G, ZERO, 2, 2>, dim3(n * cluster, (a.T + 15) / 16), kW4Warps * 32, 0, cluster, st, a, cluster);
+}
+
+template <bool BF16>
+cudaError_t launch_w4(const ft_dense *h, const W4Args &a, bool zero, cudaStream_t st) {
+  switch (a.g.group) {
+    case 32: return zero ? launch_w4_stream<BF16, 32, true>(h, a, st) : launch_w4_stream<BF16, 32, false>(h, a, st);
+    case 64: return zero ? launch_w4_stream<BF16, 64, true>(h, a, st) : launch_w4_stream<BF16, 64, false>(h, a, st);
+    default: return zero ? launch_w4_stream<BF16, 128, true>(h, a, st) : launch_w4_stream<BF16, 128, false>(h, a, st);
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+const char *ft_dense_last_cuda_error(void) { return cudaGetErrorString((cudaError_t)g_dense_cuda_error.load()); }
+
+ft_status_t ft_dense_create(int device, ft_dense_t **out) {
+  if (!out) return FT_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (device < 0) return FT_ERR_INVALID_ARG;
+  DeviceScope dev(device);
+  FD_CUDA(dev.err);
+  ft_dense *h = new (std::nothrow) ft_dense();
+  if (!h) return FT_ERR_OOM;
+  h->device = device;
+  cudaError_t e = cudaDeviceGetAttribute(&h->sm_count, cudaDevAttrMultiProcessorCount, device);
+  if (e == cudaSuccess) e = cudaMalloc(&h->status_dev, 256);
+  if (e == cudaSuccess) e = cudaMemset(h->status_dev, 0, 256);
+  if (e == cudaSuccess) e = cudaDeviceSynchronize();
+  if (e != cudaSuccess) {
+    (void)cudaFree(h->status_dev);
+    delete h;
+    FD_CUDA(e);
+  }
+  *out = h;
+  return FT_OK;
+}
+
+ft_status_t ft_dense_destroy(ft_dense_t *h) {
+  if (!h) return FT_OK;
+  DeviceScope dev(h->device);
+  cudaError_t e = cudaDeviceSynchronize();
+  (void)cudaFree(h->status_dev);
+  delete h;
+  FD_CUDA(e);
+  return FT_OK;
+}
+
+ft_status_t ft_dense_add_norm(ft_dense_t *h, int T, int d, int dtype, int res_dtype, int flags, const void *y, int64_t y_stride,
+                              const void *res, int64_t res_stride, const void *gate, int64_t gate_stride, int gate_step,
+                              const void *w_post, const void *w_pre, float w_offset, float eps, float res_scale, float y_scale,
+                              void *res_out, int64_t res_out_stride, void *out, int64_t out_stride, void *stream) {
+  if (!h || T < 0 || d < 1 || !type16(dtype) || (res_dtype != dtype && res_dtype != FT_DENSE_FP32) || (flags & ~FT_DENSE_NORM_POST))
+    return FT_ERR_INVALID_ARG;
+  if (!(eps >= 0.f) || (gate_step != 0 && gate_step != 1)) return FT_ERR_INVALID_ARG;
+  if (d > 1024 * kNormElems) return FT_ERR_UNSUPPORTED;
+  if (T == 0) return FT_OK;
+  if ((!y && !res) || (!res_out && !out)) return FT_ERR_INVALID_ARG;
+  const bool res32 = res_dtype == FT_DENSE_FP32;
+  if (!aligned(y, 2) || !aligned(gate, 2) || !aligned(w_post, 2) || !aligned(w_pre, 2) || !aligned(out, 2) || !aligned(res, res32 ? 4 : 2) ||
+      !aligned(res_out, res32 ? 4 : 2))
+    return FT_ERR_INVALID_ARG;
+  if ((y && T > 1 && y_stride < d) || (res && T > 1 && res_stride < d) || (res_out && T > 1 && res_out_stride < d) || (out && T > 1 && out_stride < d) ||
+      (gate && gate_stride < 0))
+    return FT_ERR_INVALID_ARG;
+  // a row is read whole before it is written, but only by its own threads
+  if ((res_out && res_out == res && T > 1 && res_out_stride != res_stride) || (out && out == y && T > 1 && out_stride != y_stride)) return FT_ERR_INVALID_ARG;
+  DeviceScope dev(h->device);
+  FD_CUDA(dev.err);
+  NormArgs a;
+  a.T = T; a.d = d; a.post = y && (flags & FT_DENSE_NORM_POST) ? 1 : 0; a.gate_step = gate_step;
+  a.y = static_cast<const uint16_t *>(y); a.gate = static_cast<const uint16_t *>(gate);
+  a.w_post = static_cast<const uint16_t *>(w_post); a.w_pre = static_cast<const uint16_t *>(w_pre);
+  a.res = res; a.res_out = res_out; a.out = static_cast<uint16_t *>(out);
+  a.y_stride = y_stride; a.res_stride = res_stride; a.gate_stride = gate_stride; a.res_out_stride = res_out_stride; a.out_stride = out_stride;
+  a.w_offset = w_offset; a.eps = eps; a.res_scale = res_scale; a.y_scale = y_scale;
+  // 16-byte pieces where every row starts on one
+  auto rows16 = [&](const void *p, int64_t stride, int bytes) { return !p || (aligned(p, 16) && (T == 1 || stride * bytes % 16 == 0)); };
+  const bool wide = d % 8 == 0 && rows16(y, y_stride, 2) && rows16(res, res_stride, res32 ? 4 : 2) && rows16(res_out, res_out_stride, res32 ? 4 : 2) &&
+                    rows16(out, out_stride, 2) && (!gate || gate_step == 0 || rows16(gate, gate_stride, 2)) && aligned(w_post, 16) && aligned(w_pre, 16);
+  a.lanes = 32;
+  while (a.lanes * kNormElems < d) a.lanes *= 2;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool bf = dtype == FT_DENSE_BF16;
+  FD_CUDA(bf ? (res32 ? launch_norm<true, true>(a, wide, st) : launch_norm<true, false>(a, wide, st))
+             : (res32 ? launch_norm<false, true>(a, wide, st) : launch_norm<false, false>(a, wide, st)));
+  h->launches += 1;
+  return FT_OK;
+}
+
+size_t ft_dense_w4_bytes(int64_t n, int64_t k, int group, int has_zeros) {
+  if (!w4_ok(n, k, group)) return 0;
+  const W4Geom g = w4_geom(n, k, group);
+  return (size_t)g.zeros_at + (has_zeros ? ((size_t)g.tiles * g.groups * 16 + 15) / 16 * 16 : 0);
+}
+
+ft_status_t ft_dense_w4_pack(ft_dense_t *h, int64_t n, int64_t k, int group, int dtype, const uint8_t *codes, int64_t codes_stride,
+                             const void *scales, const uint8_t *zeros, void *image, void *stream) {
+  if (!h || !type16(dtype)) return FT_ERR_INVALID_ARG;
+  if (!w4_ok(n, k, group)) return FT_ERR_UNSUPPORTED;
+  if (!codes || !scales || !image || (n > 1 && codes_stride < k / 2) || !aligned(scales, 2) || !aligned(image, 16)) return FT_ERR_INVALID_ARG;
+  DeviceScope dev(h->device);
+  FD_CUDA(dev.err);
+  const W4Geom g = w4_geom(n, k, group);
+  const long long work = (long long)g.tiles * g.kb * 32 + (long long)g.tiles * g.groups * 8;
+  const long long blocks = (work + 255) / 256;
+  const unsigned grid = (unsigned)(blocks < 16ll * h->sm_count ? blocks : 16ll * h->sm_count);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const uint16_t *sc = static_cast<const uint16_t *>(scales);
+  FD_CUDA(dtype == FT_DENSE_BF16 ? launch(w4_pack_kernel<true>, grid, 256, 0, st, g, codes, codes_stride, sc, zeros, static_cast<uint8_t *>(image))
+                                 : launch(w4_pack_kernel<false>, grid, 256, 0, st, g, codes, codes_stride, sc, zeros, static_cast<uint8_t *>(image)));
+  h->launches += 1;
+  return FT_OK;
+}
+
+ft_status_t ft_dense_w4_forward(ft_dense_t *h, int T, int64_t n, int64_t k, int group, int dtype, int has_zeros, const void *x,
+                                int64_t x_stride, const void *image, const void *bias, void *y, int64_t y_stride, int out_dtype,
+                                void *stream) {
+  if (!h || T < 0 || !type16(dtype) || (out_dtype != dtype && out_dtype != FT_DENSE_FP32)) return FT_ERR_INVALID_ARG;
+  if (!w4_ok(n, k, group)) return FT_ERR_UNSUPPORTED;
+  if (T == 0) return FT_OK;
+  const bool out32 = out_dtype == FT_DENSE_FP32;
+  if (!x || !image || !y || !aligned(x, 16) || !aligned(image, 16) || !aligned(bias, 2) || !aligned(y, out32 ? 4 : 2)) return FT_ERR_INVALID_ARG;
+  if (T > 1 && (x_stride < k || x_stride % 8 || y_stride < n)) return FT_ERR_INVALID_ARG;
+  DeviceScope dev(h->device);
+  FD_CUDA(dev.err);
+  W4Args a;
+  a.g = w4_geom(n, k, group);
+  a.T = T; a.out32 = out32 ? 1 : 0;
+  a.x = static_cast<const uint16_t *>(x); a.bias = static_cast<const uint16_t *>(bias);
+  a.image = static_cast<const uint8_t *>(image); a.y = y;
+  a.x_stride = x_stride; a.y_stride = y_stride;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  FD_CUDA(dtype == FT_DENSE_BF16 ? launch_w4<true>(h, a, has_zeros != 0, st) : launch_w4<false>(h, a, has_zeros != 0, st));
+  h->launches += 1;
+  return FT_OK;
+}
+
+ft_status_t ft_dense_logprobs(ft_dense_t *h, int T, int64_t vocab, int dtype, const void *logits, int64_t stride, float scale,
+                              const int32_t *tokens, int64_t tokens_stride, int n_tokens, float *logprob, float *entropy, int top_k,
+                              int32_t *top_ids, float *top_logprobs, void *stream) {
+  if (!h || T < 0 || vocab < 1 || vocab > (1 << 30) || (!type16(dtype) && dtype != FT_DENSE_FP32) || !(scale > 0.f) || !(scale < INFINITY) ||
+      n_tokens < 0 || top_k < 0 || top_k > kLogpTop)
+    return FT_ERR_INVALID_ARG;
+  if (T == 0) return FT_OK;
+  const bool given = tokens && n_tokens > 0;
+  if (!logits || (given && !logprob) || (top_k > 0 && (!top_ids || !top_logprobs)) || (n_tokens > 0 && !tokens)) return FT_ERR_INVALID_ARG;
+  if (!aligned(logits, dtype == FT_DENSE_FP32 ? 4 : 2) || !aligned(tokens, 4) || !aligned(logprob, 4) || !aligned(entropy, 4) || !aligned(top_ids, 4) ||
+      !aligned(top_logprobs, 4) || (T > 1 && (stride < vocab || (given && tokens_stride < n_tokens))))
+    return FT_ERR_INVALID_ARG;
+  DeviceScope dev(h->device);
+  FD_CUDA(dev.err);
+  LogpArgs a;
+  a.logits = logits; a.stride = stride; a.T = T; a.vocab = (int32_t)vocab; a.n_tokens = given ? n_tokens : 0; a.top_k = top_k; a.scale = scale;
+  a.tokens = given ? tokens : nullptr; a.tokens_stride = tokens_stride;
+  a.logprob = logprob; a.entropy = entropy; a.top_logprobs = top_logprobs; a.top_ids = top_ids;
+  a.status = h->status_dev;
+  int cluster = 1;
+  while (cluster < kLogpCluster && (long long)T * cluster * 2 <= 2ll * h->sm_count && vocab >= 8192ll * cluster) cluster *= 2;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const dim3 grid((unsigned)T * cluster);
+  FD_CUDA(dtype == FT_DENSE_BF16   ? launch_clusters(logprobs_kernel<kLogpBf16>, grid, kLogpThreads, 0, cluster, st, a, cluster)
+          : dtype == FT_DENSE_FP16 ? launch_clusters(logprobs_kernel<kLogpFp16>, grid, kLogpThreads, 0, cluster, st, a, cluster)
+                                   : launch_clusters(logprobs_kernel<kLogpFp32>, grid, kLogpThreads, 0, cluster, st, a, cluster));
+  h->launches += 1;
+  return FT_OK;
+}
+
+ft_status_t ft_dense_sync_status(ft_dense_t *h) {
+  if (!h) return FT_ERR_INVALID_ARG;
+  DeviceScope dev(h->device);
+  FD_CUDA(dev.err);
+  FD_CUDA(cudaDeviceSynchronize());
+  uint32_t st = 0;
+  FD_CUDA(cudaMemcpy(&st, h->status_dev, sizeof(st), cudaMemcpyDeviceToHost));
+  if (!st) return FT_OK;
+  FD_CUDA(cudaMemset(h->status_dev, 0, sizeof(st)));
+  FD_CUDA(cudaDeviceSynchronize());
+  return (st & kStatTimeout) ? FT_ERR_TIMEOUT : FT_ERR_INVALID_ARG;
+}
+
+ft_status_t ft_dense_launch_count(ft_dense_t *h, uint64_t *out) {
+  if (!h || !out) return FT_ERR_INVALID_ARG;
+  *out = h->launches;
+  return FT_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,176 @@
+// A block's output joins the residual stream and the next block's input is normed, in one pass:
+//   u = y, or y * rsqrt(mean(y^2) + eps) * (o + w_post);  r' = a r + b gate u;  h = r' * rsqrt(mean(r'^2) + eps) * (o + w_pre)
+// Bound: HBM (y, r and a gate per element read once, r' and h written once) for many tokens, launch latency for few.
+// `lanes` threads (32 .. 1024, a power of two) share a row; a thread holds kNormElems of its elements from the loads to the stores,
+// so that a row is read once whatever is written over it.  A vector (8 elements) a load where every address allows 16-byte accesses,
+// else single elements, neighbouring threads on neighbouring elements.
+#pragma once
+#include "async.cuh"
+#include "common.cuh"
+
+namespace ftmoe {
+
+constexpr int kNormElems = 16;             // elements of a row per thread: 1024 threads hold rows of 16384
+constexpr int kNormThreads = 256;          // threads of a block while a row needs no more
+
+struct NormArgs {
+  int32_t T, d, lanes, post, gate_step;
+  const uint16_t *y, *gate, *w_post, *w_pre;
+  const void *res;
+  void *res_out;
+  uint16_t *out;
+  long long y_stride, res_stride, gate_stride, res_out_stride, out_stride;
+  float w_offset, eps, res_scale, y_scale;
+};
+
+template <bool BF16>
+__device__ __forceinline__ float to_float(uint16_t v) {
+  return BF16 ? bf16_bits_to_float(v) : __half2float(__ushort_as_half(v));
+}
+template <bool BF16>
+__device__ __forceinline__ uint16_t from_float(float v) {
+  return BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v)) : __half_as_ushort(__float2half_rn(v));
+}
+template <bool BF16>
+__device__ __forceinline__ void to_float2(uint32_t v, float &a, float &b) {
+  a = to_float<BF16>((uint16_t)v);
+  b = to_float<BF16>((uint16_t)(v >> 16));
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t from_float2(float a, float b) {
+  if (BF16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&v);
+  }
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+// VEC elements of a 16-bit or a float array.
+template <bool BF16, int VEC>
+__device__ __forceinline__ void load_16(const uint16_t *p, float *x) {
+  if constexpr (VEC == 8) {
+    const uint4 v = *reinterpret_cast<const uint4 *>(p);
+    to_float2<BF16>(v.x, x[0], x[1]); to_float2<BF16>(v.y, x[2], x[3]);
+    to_float2<BF16>(v.z, x[4], x[5]); to_float2<BF16>(v.w, x[6], x[7]);
+  } else {
+    x[0] = to_float<BF16>(*p);
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void load_32(const float *p, float *x) {
+  if constexpr (VEC == 8) {
+    const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  } else {
+    x[0] = *p;
+  }
+}
+template <bool BF16, int VEC>
+__device__ __forceinline__ void store_16(uint16_t *p, const float *x) {
+  if constexpr (VEC == 8)
+    *reinterpret_cast<uint4 *>(p) = make_uint4(from_float2<BF16>(x[0], x[1]), from_float2<BF16>(x[2], x[3]), from_float2<BF16>(x[4], x[5]),
+                                               from_float2<BF16>(x[6], x[7]));
+  else
+    *p = from_float<BF16>(x[0]);
+}
+template <int VEC>
+__device__ __forceinline__ void store_32(float *p, const float *x) {
+  if constexpr (VEC == 8) {
+    *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4 *>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+    *p = x[0];
+  }
+}
+
+// Sum over the threads of a row; `s` holds a float per warp.  All threads of the block take part.
+__device__ __forceinline__ float row_sum(float v, int lanes, float *s) {
+  v = warp_sum(v);
+  if (lanes == 32) return v;
+  const int warp = threadIdx.x >> 5, n = lanes >> 5, first = warp & ~(n - 1);
+  __syncthreads();                          // (the sums before are read)
+  if ((threadIdx.x & 31) == 0) s[warp] = v;
+  __syncthreads();
+  float t = 0.f;
+  for (int i = 0; i < n; ++i) t += s[first + i];
+  return t;
+}
+
+template <bool BF16, bool RES32, int VEC>
+__global__ void __launch_bounds__(1024) add_norm_kernel(const NormArgs a) {
+  constexpr int N = kNormElems / VEC;
+  __shared__ float s_sum[32];
+  grid_let_next();
+  grid_wait();
+  const int rows = blockDim.x / a.lanes, lane = threadIdx.x & (a.lanes - 1);
+  const long long t = (long long)blockIdx.x * rows + threadIdx.x / a.lanes;
+  const bool live = t < a.T;                // (a row past the end takes part in the sums)
+  float r[kNormElems], u[kNormElems];
+#pragma unroll
+  for (int i = 0; i < kNormElems; ++i) r[i] = u[i] = 0.f;
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int i = (j * a.lanes + lane) * VEC;
+      if (live && i < a.d) f(i, j * VEC);
+    }
+  };
+  if (a.y) each([&](int i, int j) { load_16<BF16, VEC>(a.y + t * a.y_stride + i, u + j); });
+  if (a.res) each([&](int i, int j) {
+    if (RES32) load_32<VEC>(static_cast<const float *>(a.res) + t * a.res_stride + i, r + j);
+    else load_16<BF16, VEC>(static_cast<const uint16_t *>(a.res) + t * a.res_stride + i, r + j);
+  });
+  if (a.post) {
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kNormElems; ++i) sum = fmaf(u[i], u[i], sum);
+    const float inv = rsqrtf(row_sum(sum, a.lanes, s_sum) / (float)a.d + a.eps);
+#pragma unroll
+    for (int i = 0; i < kNormElems; ++i) u[i] *= inv;
+    if (a.w_post) each([&](int i, int j) {
+      float w[VEC];
+      load_16<BF16, VEC>(a.w_post + i, w);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) u[j + k] *= a.w_offset + w[k];
+    });
+  }
+  if (a.y && a.gate) each([&](int i, int j) {
+    float g[VEC];
+    if (a.gate_step) load_16<BF16, VEC>(a.gate + t * a.gate_stride + i, g);
+    else {
+      g[0] = to_float<BF16>(a.gate[t * a.gate_stride]);
+#pragma unroll
+      for (int k = 1; k < VEC; ++k) g[k] = g[0];
+    }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) u[j + k] *= g[k];
+  });
+#pragma unroll
+  for (int i = 0; i < kNormElems; ++i) r[i] = a.res ? (a.y ? fmaf(a.y_scale, u[i], a.res_scale * r[i]) : a.res_scale * r[i]) : a.y_scale * u[i];
+  if (a.res_out) each([&](int i, int j) {
+    if (RES32) store_32<VEC>(static_cast<float *>(a.res_out) + t * a.res_out_stride + i, r + j);
+    else store_16<BF16, VEC>(static_cast<uint16_t *>(a.res_out) + t * a.res_out_stride + i, r + j);
+  });
+  if (!a.out) return;
+  float sum = 0.f;
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) sum = (j * a.lanes + lane) * VEC + k < a.d ? fmaf(r[j * VEC + k], r[j * VEC + k], sum) : sum;
+  const float inv = rsqrtf(row_sum(sum, a.lanes, s_sum) / (float)a.d + a.eps);
+  each([&](int i, int j) {
+    float h[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) h[k] = r[j + k] * inv;
+    if (a.w_pre) {
+      float w[VEC];
+      load_16<BF16, VEC>(a.w_pre + i, w);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) h[k] *= a.w_offset + w[k];
+    }
+    store_16<BF16, VEC>(a.out + t * a.out_stride + i, h);
+  });
+}
+
+}  // namespace ftmoe
