@@ -47,24 +47,31 @@ cudaError_t launch_norm(const NormArgs &a, bool wide, cudaStream_t st) {
   return wide ? launch(add_norm_kernel<BF16, RES32, 8>, grid, threads, 0, st, a) : launch(add_norm_kernel<BF16, RES32, 1>, grid, threads, 0, st, a);
 }
 
-template <bool BF16, int G, bool ZERO>
+template <bool BF16, int G, bool ZERO, int NT>
 cudaError_t launch_w4_stream(const ft_dense *h, const W4Args &a, cudaStream_t st) {
-  const int grid = 2 * h->sm_count;
-  // blocks of a cluster share the k of their tiles: as many as leave every cluster some tiles, so that shares are even
-  int cluster = 1;
-  while (cluster < kW4MaxCluster && grid / cluster > a.g.tiles / 4 && a.g.kb > cluster * kW4Warps) cluster *= 2;
-  int n = grid / cluster;
-  if (n > a.g.tiles) n = a.g.tiles;
-  if (a.T <= 8) return launch_clusters(w4_stream_kernel<BF16, G, ZERO, 1, 4>, dim3(n * cluster), kW4Warps * 32, 0, cluster, st, a, cluster);
-  return launch_clusters(w4_stream_kernel<BF16, G, ZERO, 2, 2>, dim3(n * cluster, (a.T + 15) / 16), kW4Warps * 32, 0, cluster, st, a, cluster);
+  W4Stream p;
+  w4_stream_share(a.g, h->sm_count, kW4Warps<NT>, p);
+  const int smem = w4_stream_memory<NT>(a.g, p);
+  cudaError_t e = cudaFuncSetAttribute(w4_stream_kernel<BF16, G, ZERO, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  const int per_block = kW4Warps<NT> / p.wk, want = (a.g.quads + per_block - 1) / per_block, fit = h->sm_count / p.cluster;
+  return launch_clusters(w4_stream_kernel<BF16, G, ZERO, NT>, dim3((want < fit ? want : fit) * p.cluster, (a.T + 8 * NT - 1) / (8 * NT)), kW4Warps<NT> * 32, smem,
+                         p.cluster, st, a, p);
+}
+
+template <bool BF16, int G, bool ZERO>
+cudaError_t launch_w4_tokens(const ft_dense *h, const W4Args &a, cudaStream_t st) {
+  if (a.T <= 8) return launch_w4_stream<BF16, G, ZERO, 1>(h, a, st);
+  if (a.T <= 16) return launch_w4_stream<BF16, G, ZERO, 2>(h, a, st);
+  return launch_w4_stream<BF16, G, ZERO, 4>(h, a, st);
 }
 
 template <bool BF16>
 cudaError_t launch_w4(const ft_dense *h, const W4Args &a, bool zero, cudaStream_t st) {
   switch (a.g.group) {
-    case 32: return zero ? launch_w4_stream<BF16, 32, true>(h, a, st) : launch_w4_stream<BF16, 32, false>(h, a, st);
-    case 64: return zero ? launch_w4_stream<BF16, 64, true>(h, a, st) : launch_w4_stream<BF16, 64, false>(h, a, st);
-    default: return zero ? launch_w4_stream<BF16, 128, true>(h, a, st) : launch_w4_stream<BF16, 128, false>(h, a, st);
+    case 32: return zero ? launch_w4_tokens<BF16, 32, true>(h, a, st) : launch_w4_tokens<BF16, 32, false>(h, a, st);
+    case 64: return zero ? launch_w4_tokens<BF16, 64, true>(h, a, st) : launch_w4_tokens<BF16, 64, false>(h, a, st);
+    default: return zero ? launch_w4_tokens<BF16, 128, true>(h, a, st) : launch_w4_tokens<BF16, 128, false>(h, a, st);
   }
 }
 
@@ -150,8 +157,7 @@ ft_status_t ft_dense_add_norm(ft_dense_t *h, int T, int d, int dtype, int res_dt
 
 size_t ft_dense_w4_bytes(int64_t n, int64_t k, int group, int has_zeros) {
   if (!w4_ok(n, k, group)) return 0;
-  const W4Geom g = w4_geom(n, k, group);
-  return (size_t)g.zeros_at + (has_zeros ? ((size_t)g.tiles * g.groups * 16 + 15) / 16 * 16 : 0);
+  return (size_t)w4_geom(n, k, group, has_zeros != 0).bytes();
 }
 
 ft_status_t ft_dense_w4_pack(ft_dense_t *h, int64_t n, int64_t k, int group, int dtype, const uint8_t *codes, int64_t codes_stride,
@@ -161,9 +167,8 @@ ft_status_t ft_dense_w4_pack(ft_dense_t *h, int64_t n, int64_t k, int group, int
   if (!codes || !scales || !image || (n > 1 && codes_stride < k / 2) || !aligned(scales, 2) || !aligned(image, 16)) return FT_ERR_INVALID_ARG;
   DeviceScope dev(h->device);
   FD_CUDA(dev.err);
-  const W4Geom g = w4_geom(n, k, group);
-  const long long work = (long long)g.tiles * g.kb * 32 + (long long)g.tiles * g.groups * 8;
-  const long long blocks = (work + 255) / 256;
+  const W4Geom g = w4_geom(n, k, group, zeros != nullptr);
+  const long long blocks = ((long long)g.quads * g.nb + 7) / 8;
   const unsigned grid = (unsigned)(blocks < 16ll * h->sm_count ? blocks : 16ll * h->sm_count);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const uint16_t *sc = static_cast<const uint16_t *>(scales);
@@ -185,11 +190,11 @@ ft_status_t ft_dense_w4_forward(ft_dense_t *h, int T, int64_t n, int64_t k, int 
   DeviceScope dev(h->device);
   FD_CUDA(dev.err);
   W4Args a;
-  a.g = w4_geom(n, k, group);
+  a.g = w4_geom(n, k, group, has_zeros != 0);
   a.T = T; a.out32 = out32 ? 1 : 0;
   a.x = static_cast<const uint16_t *>(x); a.bias = static_cast<const uint16_t *>(bias);
   a.image = static_cast<const uint8_t *>(image); a.y = y;
-  a.x_stride = x_stride; a.y_stride = y_stride;
+  a.x_stride = x_stride; a.y_stride = y_stride; a.status = h->status_dev;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   FD_CUDA(dtype == FT_DENSE_BF16 ? launch_w4<true>(h, a, has_zeros != 0, st) : launch_w4<false>(h, a, has_zeros != 0, st));
   h->launches += 1;

@@ -22,7 +22,7 @@ def test_every_declared_symbol_is_exported_and_bound():
 
 
 @pytest.mark.parametrize("n,k,group,zeros,size", [
-    (16, 64, 64, False, 512 + 32), (1, 32, 32, False, 512 + 64), (17, 128, 128, True, 2 * (1024 + 32 + 16)), (130, 96, 32, True, 9 * (1024 + 128 + 64)),
+    (16, 64, 64, False, 1024 + 256), (1, 32, 32, False, 1024 + 512), (17, 128, 128, True, 2048 + 192), (130, 160, 32, True, 2 * (2 * (4096 + 768) + 1024 + 768)),
     (5120, 2048, 128, False, 5120 * 1024 + 5120 * 16 * 2),
 ])
 def test_bytes_of_an_image(n, k, group, zeros, size):
