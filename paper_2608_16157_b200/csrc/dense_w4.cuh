@@ -16,6 +16,8 @@
 // w4_stream_kernel, up to 32 tokens: weights on M, tokens on N = 8, 16 or 32.  Bound: HBM for large matrices (N K / 2 bytes), launch and
 // latency for small ones.
 #pragma once
+#include <type_traits>
+
 #include "async.cuh"
 #include "cluster.cuh"
 #include "common.cuh"
@@ -306,51 +308,57 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32, 1) w4_stream_kernel(const W
       load_x(0, x[0]);
       if constexpr (kHalves == 2) load_x(1, x[1]);
       wait(slot, phase);
-      const uint32_t rec = slots_at + slot * p.slot_bytes, sc_at = rec + m * 2 * kW4TileBytes;
+      const uint32_t rec = slots_at + slot * p.slot_bytes;
+      // full quads without a test between the tiles, so that their chains overlap
+      auto multiply = [&](const int m, auto full) {
+        const uint32_t sc_at = rec + m * 2 * kW4TileBytes;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        if (kHalves == 1 && half == 1) load_x(1, x[0]);
-        const uint32_t (&xr)[NT][8] = x[kHalves == 2 ? half : 0];
-        uint4 sc[kSub];
-        uint2 z[kSub];
-#pragma unroll
-        for (int s = 0; s < kSub; ++s) {
-          const int at = half * kGroups / 2 + s;
-          sc[s] = lds_v4(sc_at + at * 128 + gr * 16);
-          if (ZERO) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(z[s].x), "=r"(z[s].y) : "r"(sc_at + kGroups * 128 + at * 64 + gr * 8));
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          if (r >= m) break;
-          const uint4 w = lds_v4(rec + (half * m + r) * kW4TileBytes + lane * 16);
-          const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+        for (int half = 0; half < 2; ++half) {
+          if (kHalves == 1 && half == 1) load_x(1, x[0]);
+          const uint32_t (&xr)[NT][8] = x[kHalves == 2 ? half : 0];
+          uint4 sc[kSub];
+          uint2 z[kSub];
 #pragma unroll
           for (int s = 0; s < kSub; ++s) {
-            uint32_t lo = BF16 ? 0x41c041c0u : 0x4e004e00u, hi = lo;      // 16 + 8
-            if (ZERO) w4_zero_pairs<BF16>((r < 2 ? z[s].x : z[s].y) >> (16 * (r & 1)), lo, hi);
-            float sum[NT][4];
+            const int at = half * kGroups / 2 + s;
+            sc[s] = lds_v4(sc_at + at * 128 + gr * 16);
+            if (ZERO) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(z[s].x), "=r"(z[s].y) : "r"(sc_at + kGroups * 128 + at * 64 + gr * 8));
+          }
 #pragma unroll
-            for (int j = s * (4 / kSub); j < (s + 1) * (4 / kSub); ++j) {
-              uint32_t c[4];
-              w4_expand<BF16>(con, words[j], c);
-              c[0] = sub_pair<BF16>(c[0], lo); c[1] = sub_pair<BF16>(c[1], hi);
-              c[2] = sub_pair<BF16>(c[2], lo); c[3] = sub_pair<BF16>(c[3], hi);
-              const float none[4] = {0.f, 0.f, 0.f, 0.f};
+          for (int r = 0; r < 4; ++r) {
+            if (!decltype(full)::value && r >= m) break;
+            const uint4 w = lds_v4(rec + (half * m + r) * kW4TileBytes + lane * 16);
+            const uint32_t words[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-              for (int t = 0; t < NT; ++t) mma_16816<BF16>(sum[t], c, xr[t][2 * j], xr[t][2 * j + 1], j == s * (4 / kSub) ? none : sum[t]);
-            }
-            float s0, s1;
-            to_float2<BF16>(r == 0 ? sc[s].x : r == 1 ? sc[s].y : r == 2 ? sc[s].z : sc[s].w, s0, s1);
+            for (int s = 0; s < kSub; ++s) {
+              uint32_t lo = BF16 ? 0x41c041c0u : 0x4e004e00u, hi = lo;      // 16 + 8
+              if (ZERO) w4_zero_pairs<BF16>((r < 2 ? z[s].x : z[s].y) >> (16 * (r & 1)), lo, hi);
+              float sum[NT][4];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              acc[r][t][0] = fmaf(s0, sum[t][0], acc[r][t][0]);
-              acc[r][t][1] = fmaf(s0, sum[t][1], acc[r][t][1]);
-              acc[r][t][2] = fmaf(s1, sum[t][2], acc[r][t][2]);
-              acc[r][t][3] = fmaf(s1, sum[t][3], acc[r][t][3]);
+              for (int j = s * (4 / kSub); j < (s + 1) * (4 / kSub); ++j) {
+                uint32_t c[4];
+                w4_expand<BF16>(con, words[j], c);
+                c[0] = sub_pair<BF16>(c[0], lo); c[1] = sub_pair<BF16>(c[1], hi);
+                c[2] = sub_pair<BF16>(c[2], lo); c[3] = sub_pair<BF16>(c[3], hi);
+                const float none[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int t = 0; t < NT; ++t) mma_16816<BF16>(sum[t], c, xr[t][2 * j], xr[t][2 * j + 1], j == s * (4 / kSub) ? none : sum[t]);
+              }
+              float s0, s1;
+              to_float2<BF16>(r == 0 ? sc[s].x : r == 1 ? sc[s].y : r == 2 ? sc[s].z : sc[s].w, s0, s1);
+#pragma unroll
+              for (int t = 0; t < NT; ++t) {
+                acc[r][t][0] = fmaf(s0, sum[t][0], acc[r][t][0]);
+                acc[r][t][1] = fmaf(s0, sum[t][1], acc[r][t][1]);
+                acc[r][t][2] = fmaf(s1, sum[t][2], acc[r][t][2]);
+                acc[r][t][3] = fmaf(s1, sum[t][3], acc[r][t][3]);
+              }
             }
           }
         }
-      }
+      };
+      if (NT == 1 && m == 4) multiply(4, std::true_type());
+      else multiply(m, std::false_type());
       __syncwarp();
       if (i + 1 < n_b) bring(); else held = slot;     // (the last one of a quad holds the sums first)
       if (++slot == p.slots) { slot = 0; phase ^= 1u; }
