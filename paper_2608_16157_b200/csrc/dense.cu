@@ -1,6 +1,7 @@
 // Host side of include/ftdense.h: handle, validation, launches.
 #include "../../include/ftdense.h"
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include <atomic>
@@ -9,6 +10,7 @@
 #include "dense_logp.cuh"
 #include "dense_norm.cuh"
 #include "dense_w4.cuh"
+#include "dense_w4_tile.cuh"
 #include "host.cuh"
 
 using namespace ftmoe;
@@ -16,6 +18,7 @@ using namespace ftmoe;
 struct ft_dense {
   int device = 0, sm_count = 148;
   uint32_t *status_dev = nullptr;
+  void *encode = nullptr;          // cuTensorMapEncodeTiled
   uint64_t launches = 0;
 };
 
@@ -66,8 +69,39 @@ cudaError_t launch_w4_tokens(const ft_dense *h, const W4Args &a, cudaStream_t st
   return launch_w4_stream<BF16, G, ZERO, 4>(h, a, st);
 }
 
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// x as [T][k]; a box is 64 k of a tile's tokens, rows of 128 bytes with the 128-byte swizzle.
+bool make_x_map(const ft_dense *h, CUtensorMap *tm, const W4Args &a, int tokens) {
+  const cuuint64_t dims[2] = {(cuuint64_t)a.g.k, (cuuint64_t)a.T}, strides[1] = {(cuuint64_t)a.x_stride * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)tokens}, ones[2] = {1, 1};
+  return reinterpret_cast<EncodeTiledFn>(h->encode)(tm, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<uint16_t *>(a.x), dims, strides, box, ones,
+                                                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool BF16, int BN>
+cudaError_t launch_w4_tile(const ft_dense *h, const W4Args &a, const W4Tile &p, cudaStream_t st) {
+  CUtensorMap tm;
+  if (!make_x_map(h, &tm, a, p.bn)) return cudaErrorInvalidValue;
+  const int smem = w4_tile_smem<BN>(p), units = p.row_tiles * p.tok_tiles, fit = h->sm_count / p.cluster;
+  cudaError_t e = cudaFuncSetAttribute(w4_tile_kernel<BF16, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  return launch_clusters(w4_tile_kernel<BF16, BN>, dim3((p.cluster > 1 || units < fit ? units : fit) * p.cluster), kW4TileThreads, smem, p.cluster, st, tm, a, p);
+}
+
+template <bool BF16>
+cudaError_t launch_w4_many(const ft_dense *h, const W4Args &a, cudaStream_t st) {
+  const W4Tile p = w4_tile_share(a.g, a.T, h->sm_count);
+  if (p.bn <= 64) return launch_w4_tile<BF16, 64>(h, a, p, st);
+  if (p.bn <= 128) return launch_w4_tile<BF16, 128>(h, a, p, st);
+  return launch_w4_tile<BF16, 256>(h, a, p, st);
+}
+
 template <bool BF16>
 cudaError_t launch_w4(const ft_dense *h, const W4Args &a, bool zero, cudaStream_t st) {
+  if (a.T > 32) return launch_w4_many<BF16>(h, a, st);
   switch (a.g.group) {
     case 32: return zero ? launch_w4_tokens<BF16, 32, true>(h, a, st) : launch_w4_tokens<BF16, 32, false>(h, a, st);
     case 64: return zero ? launch_w4_tokens<BF16, 64, true>(h, a, st) : launch_w4_tokens<BF16, 64, false>(h, a, st);
@@ -94,6 +128,9 @@ ft_status_t ft_dense_create(int device, ft_dense_t **out) {
   if (e == cudaSuccess) e = cudaMalloc(&h->status_dev, 256);
   if (e == cudaSuccess) e = cudaMemset(h->status_dev, 0, 256);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
+  cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+  if (e == cudaSuccess) e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &h->encode, cudaEnableDefault, &found);
+  if (e == cudaSuccess && (!h->encode || found != cudaDriverEntryPointSuccess)) e = cudaErrorNotSupported;
   if (e != cudaSuccess) {
     (void)cudaFree(h->status_dev);
     delete h;

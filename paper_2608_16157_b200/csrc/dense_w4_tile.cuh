@@ -1,0 +1,346 @@
+// Products with 4-bit weights for many tokens, on the 5th-generation tensor cores.  Image and formula: dense_w4.cuh.
+//
+// A block takes 128 rows (two quads) x up to BN tokens and walks along k.  Bound: the tensor cores for many tokens (2 T N K flops), HBM and the
+// expansion of the codes for few.
+//   raw warp      brings the records of 128 k (bulk copies)
+//   x warp        brings x, 64 k of the tokens at a time (TMA, 128-byte swizzle)
+//   expanding     turn codes into the exact 16-bit numbers q - z, rows of 64 k with the same swizzle
+//   mma warp      rows on M = 128, tokens on N; one accumulator in tensor memory per group of k, two in turn
+//   adding warps  take a group's sums out, a row a thread, and add them times the row's scale to float sums in registers
+// So a scale multiplies a float sum and no weight is rounded: with scales in the operands each weight would be (8 bits of scale times 4 of
+// code), and that rounding alone is as large as that of a 16-bit result.  The additions run beside the tensor cores: at 256 tokens a group
+// of 128 k takes these 1024 clocks and a warp's 128 additions a few hundred.
+// With a cluster of c blocks each takes 1/c of k, and the sums are added over distributed shared memory, in the blocks' order.
+#pragma once
+#include "dense_w4.cuh"
+#include "float2.cuh"
+#include "tcgen.cuh"
+
+namespace ftmoe {
+
+constexpr int kW4TileThreads = 512, kW4Stages = 4, kW4Raw = 3;
+
+struct W4Tile {
+  int32_t bn, cluster, row_tiles, tok_tiles;     // tokens of a tile (a multiple of 16)
+  int32_t raw_bytes;                             // of a slot: two records
+};
+
+template <int BN>
+struct W4TileCfg {
+  static constexpr int kAdd = BN > 128 ? 8 : 4, kExpand = BN > 128 ? 4 : 8;      // warps
+  static constexpr int kCols = BN / (kAdd / 4);                                  // tokens of an adding warp
+  static constexpr int kStage = 128 * 128 + BN * 128;                            // 64 k of 128 rows and of the tokens
+  static constexpr int kBars = 2 * kW4Raw + 3 * kW4Stages + 4;
+};
+template <int BN>
+inline int w4_tile_smem(const W4Tile &p) {
+  return 1024 + kW4Stages * W4TileCfg<BN>::kStage + kW4Raw * p.raw_bytes + W4TileCfg<BN>::kBars * 8 + 32;
+}
+
+// Tokens of a tile and blocks that share k: the split with the least clocks of the SM with the most to do.  A block of 128 k takes 4 clocks a
+// token in the tensor cores, not less than its codes take to expand, nor than its groups' sums to be added; a unit 4000 more, and 2000 over a cluster.
+inline W4Tile w4_tile_share(const W4Geom &g, int T, int sm_count) {
+  W4Tile best{};
+  double least = 1e30;
+  const int row_tiles = (g.quads + 1) / 2, per = kW4Block / g.group;
+  for (int bn = 32; bn <= 256; bn += 16) {
+    if (bn > 32 && bn - 16 >= T) break;
+    for (int cluster = 1; cluster <= kW4MaxCluster && (cluster == 1 || g.nb >= 2 * cluster); cluster *= 2) {
+      const int tok_tiles = (T + bn - 1) / bn;
+      const long long units = (long long)row_tiles * tok_tiles, fit = sm_count / cluster;
+      if (cluster > 1 && units > fit) continue;
+      double block = 4. * bn;
+      const double expand = bn > 128 ? 500 : 300, add = per * (bn > 128 ? 100 + bn : 100 + 2. * bn);
+      if (block < expand) block = expand;
+      if (block < add) block = add;
+      const double cost = (double)((units + fit - 1) / fit) * ((double)(g.nb + cluster - 1) / cluster * block + 4000 + (cluster > 1 ? 2000 : 0));
+      if (cost < least) {
+        least = cost;
+        best.bn = bn; best.cluster = cluster; best.row_tiles = row_tiles; best.tok_tiles = tok_tiles;
+      }
+    }
+  }
+  best.raw_bytes = (2 * g.record(4) + 127) / 128 * 128;
+  return best;
+}
+
+template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+template <bool BF16, int BN>
+__global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const W4Args a, const W4Tile p) {
+  using Cfg = W4TileCfg<BN>;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  unsigned char *s_rec = smem + kW4Stages * Cfg::kStage;
+  uint64_t *s_bar = reinterpret_cast<uint64_t *>(s_rec + kW4Raw * p.raw_bytes);
+  uint32_t *s_tmem = reinterpret_cast<uint32_t *>(s_bar + Cfg::kBars);
+  volatile int *s_abort = reinterpret_cast<volatile int *>(s_tmem + 2);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t stage0 = smem_u32(smem), rec0 = smem_u32(s_rec), bars = smem_u32(s_bar);
+  auto raw_full = [&](int i) { return bars + 8u * i; };
+  auto raw_empty = [&](int i) { return bars + 8u * (kW4Raw + i); };
+  auto x_full = [&](int i) { return bars + 8u * (2 * kW4Raw + i); };
+  auto w_full = [&](int i) { return bars + 8u * (2 * kW4Raw + kW4Stages + i); };
+  auto st_empty = [&](int i) { return bars + 8u * (2 * kW4Raw + 2 * kW4Stages + i); };
+  auto d_full = [&](int i) { return bars + 8u * (2 * kW4Raw + 3 * kW4Stages + i); };
+  auto d_empty = [&](int i) { return bars + 8u * (2 * kW4Raw + 3 * kW4Stages + 2 + i); };
+  auto wait = [&](uint32_t bar, uint32_t phase) { return mbar_try_wait(bar, phase) || mbar_wait(bar, phase, s_abort, a.status); };
+
+  grid_let_next();
+  if (tid == 0) {
+    for (int i = 0; i < kW4Raw; ++i) { mbar_init(raw_full(i), 1); mbar_init(raw_empty(i), Cfg::kAdd + Cfg::kExpand); }
+    for (int i = 0; i < kW4Stages; ++i) { mbar_init(x_full(i), 1); mbar_init(w_full(i), Cfg::kExpand); mbar_init(st_empty(i), 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(d_full(i), 1); mbar_init(d_empty(i), Cfg::kAdd); }
+    *s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(s_tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *s_tmem;
+  grid_wait();
+
+  const W4Geom &g = a.g;
+  const int cluster = p.cluster, rank = blockIdx.x % cluster, units = p.row_tiles * p.tok_tiles, n_cl = gridDim.x / cluster, cl = blockIdx.x / cluster;
+  const int b0 = (int)((long long)g.nb * rank / cluster), b1 = (int)((long long)g.nb * (rank + 1) / cluster);
+  const int per = kW4Block / g.group, rec4 = g.record(4);       // groups of a record
+  constexpr int kFirstAdd = 16 - Cfg::kAdd, kFirstExpand = 4;
+
+  if (warp < 4) {
+    regs_down<56>();
+    if (warp == 0 && lane == 0) {
+      // ------------------------------ x ------------------------------
+      int s = 0;
+      uint32_t ph = 1;
+      for (int u = cl; u < units; u += n_cl) {
+        const int tok0 = u / p.row_tiles * p.bn;
+        for (int h = 2 * b0; h < 2 * b1; ++h) {
+          wait(st_empty(s), ph);
+          mbar_expect_tx(x_full(s), p.bn * 128);
+          tma_load_2d(stage0 + s * Cfg::kStage + 128 * 128, &tm_x, h * 64, tok0, x_full(s));
+          if (++s == kW4Stages) { s = 0; ph ^= 1; }
+          if (*s_abort) break;
+        }
+      }
+    } else if (warp == 2 && lane == 0) {
+      // ------------------------------ records ------------------------------
+      int s = 0;
+      uint32_t ph = 1;
+      for (int u = cl; u < units; u += n_cl) {
+        const int quad = u % p.row_tiles * 2, two = quad + 1 < g.quads;
+        const int r0 = g.record(g.tiles_of(quad)), r1 = two ? g.record(g.tiles_of(quad + 1)) : 0;
+        const uint8_t *src0 = a.image + g.quad_at(quad), *src1 = a.image + g.quad_at(quad + 1);
+        for (int b = b0; b < b1; ++b) {
+          wait(raw_empty(s), ph);
+          mbar_expect_tx(raw_full(s), r0 + r1);
+          bulk_g2s(rec0 + s * p.raw_bytes, src0 + (long long)b * r0, r0, raw_full(s));
+          if (two) bulk_g2s(rec0 + s * p.raw_bytes + rec4, src1 + (long long)b * r1, r1, raw_full(s));
+          if (++s == kW4Raw) { s = 0; ph ^= 1; }
+          if (*s_abort) break;
+        }
+      }
+    } else if (warp == 1 && lane == 0) {
+      // ------------------------------ mma ------------------------------
+      const uint32_t idesc = (1u << 4) | (BF16 ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)(p.bn >> 3) << 17) | ((128u >> 4) << 24);
+      const int steps = 8 / per;                      // instructions of a group
+      int s = 0, d = 0, at = 0;
+      uint32_t ph = 0, dph = 1;
+      for (int u = cl; u < units; u += n_cl)
+        for (int h = 2 * b0; h < 2 * b1; ++h) {
+          const bool ok = wait(x_full(s), ph) && wait(w_full(s), ph);
+          tc_fence_after();
+          const uint32_t base = stage0 + s * Cfg::kStage;
+          const uint64_t da = umma_desc(base, 16, 1024), db = umma_desc(base + 128 * 128, 16, 1024);
+#pragma unroll
+          for (int k16 = 0; k16 < 4; ++k16) {
+            if (at == 0) {
+              wait(d_empty(d), dph);
+              tc_fence_after();
+            }
+            if (ok) umma_bf16(tmem + d * 256, da + 2 * k16, db + 2 * k16, idesc, at != 0);
+            if (++at == steps) {
+              umma_commit(d_full(d));
+              at = 0;
+              d ^= 1;
+              if (d == 0) dph ^= 1;
+            }
+          }
+          umma_commit(st_empty(s));
+          if (++s == kW4Stages) { s = 0; ph ^= 1; }
+          if (*s_abort) break;
+        }
+    }
+  } else if (warp < kFirstExpand + Cfg::kExpand) {
+    // ------------------------------ expansion ------------------------------
+    regs_down<104>();
+    const int me = warp - kFirstExpand, gr = lane >> 2, q = lane & 3;
+    const W4Const<BF16> con;
+    int s = 0, rs = 0;
+    uint32_t ph = 1, rph = 0;
+    for (int u = cl; u < units; u += n_cl) {
+      const int quad0 = u % p.row_tiles * 2;
+      for (int b = b0; b < b1; ++b) {
+        wait(raw_full(rs), rph);
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          wait(st_empty(s), ph);
+          const uint32_t dst0 = stage0 + s * Cfg::kStage;
+#pragma unroll
+          for (int j = 0; j < 8 / Cfg::kExpand; ++j) {
+            const int piece = me + j * Cfg::kExpand, quad = piece >> 2, tile = piece & 3;
+            const int m = quad0 + quad < g.quads ? g.tiles_of(quad0 + quad) : 0;
+            if (tile >= m) continue;                  // (rows that are not there: what their operands hold reaches no other row)
+            const uint32_t rec = rec0 + rs * p.raw_bytes + quad * rec4;
+            const uint4 w = lds_v4(rec + (half * m + tile) * kW4TileBytes + lane * 16);
+            const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+            const int row = quad * 64 + tile * 16 + w4_row(gr);
+            const uint32_t dst = dst0 + row * 128;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              uint32_t lo = BF16 ? 0x41c041c0u : 0x4e004e00u, hi = lo;      // 16 + 8
+              if (g.zeros) {
+                uint32_t z;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=r"(z) : "r"(rec + m * 2 * kW4TileBytes + per * 128 + (half * 2 + h) * per / 4 * 64 + gr * 8 + tile * 2));
+                w4_zero_pairs<BF16>(z, lo, hi);
+              }
+              uint32_t c0[4], c1[4];
+              w4_expand<BF16>(con, words[2 * h], c0);
+              w4_expand<BF16>(con, words[2 * h + 1], c1);
+              const uint32_t at = ((4 * h + q) ^ (row & 7)) << 4;
+              asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst + at), "r"(sub_pair<BF16>(c0[0], lo)), "r"(sub_pair<BF16>(c0[2], lo)),
+                           "r"(sub_pair<BF16>(c1[0], lo)), "r"(sub_pair<BF16>(c1[2], lo)) : "memory");
+              asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst + 8 * 128 + at), "r"(sub_pair<BF16>(c0[1], hi)), "r"(sub_pair<BF16>(c0[3], hi)),
+                           "r"(sub_pair<BF16>(c1[1], hi)), "r"(sub_pair<BF16>(c1[3], hi)) : "memory");
+            }
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(w_full(s));
+          if (++s == kW4Stages) { s = 0; ph ^= 1; }
+        }
+        if (lane == 0) mbar_arrive(raw_empty(rs));
+        if (++rs == kW4Raw) { rs = 0; rph ^= 1; }
+        if (*s_abort) break;
+      }
+    }
+  }
+  if (warp >= kFirstAdd) {
+    // ------------------------------ sums ------------------------------
+    regs_up<176>();
+    const int row = (warp & 3) * 32 + lane, col0 = (warp - kFirstAdd) / 4 * Cfg::kCols, cols = min(Cfg::kCols, p.bn - col0);
+    const int r8 = row & 7, gr = (r8 & 3) * 2 + (r8 >> 2), quad = row >> 6;
+    const uint32_t lane_tmem = tmem + ((uint32_t)((warp & 3) * 32) << 16) + col0;
+    int rs = 0, d = 0;
+    uint32_t rph = 0, dph = 0;
+    for (int u = cl; u < units; u += n_cl) {
+      const int quad0 = u % p.row_tiles * 2, n = (quad0 * 4) * 16 + row;
+      const int m = quad0 + quad < g.quads ? g.tiles_of(quad0 + quad) : 0;
+      // the row's scales in a record: groups 128 bytes apart
+      const uint32_t sc_at = quad * rec4 + m * 2 * kW4TileBytes + gr * 16 + ((row >> 4) & 3) * 4 + ((row >> 3) & 1) * 2;
+      uint64_t acc[Cfg::kCols / 2];
+#pragma unroll
+      for (int i = 0; i < Cfg::kCols / 2; ++i) acc[i] = 0;
+      for (int b = b0; b < b1; ++b) {
+        wait(raw_full(rs), rph);
+        uint32_t sc[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          sc[i] = 0;
+          if (i < per && m > 0) asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc[i]) : "r"(rec0 + rs * p.raw_bytes + sc_at + i * 128));
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(raw_empty(rs));
+        if (++rs == kW4Raw) { rs = 0; rph ^= 1; }
+#pragma unroll 1
+        for (int i = 0; i < per; ++i) {
+          const float scale = to_float<BF16>((uint16_t)(i == 0 ? sc[0] : i == 1 ? sc[1] : i == 2 ? sc[2] : sc[3]));
+          const uint64_t scale2 = f2(scale, scale);
+          wait(d_full(d), dph);
+          tc_fence_after();
+#pragma unroll
+          for (int c = 0; c < Cfg::kCols; c += 32) {
+            if (c >= cols) break;
+            uint32_t v[32];
+            tmem_ld32(lane_tmem + d * 256 + c, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              acc[c / 2 + j] = fma2(f2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), scale2, acc[c / 2 + j]);
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(d_empty(d));
+          d ^= 1;
+          if (d == 0) dph ^= 1;
+        }
+        if (*s_abort) break;
+      }
+      const int tok0 = u / p.row_tiles * p.bn + col0, n_tok = min(cols, a.T - tok0);
+      if (cluster == 1) {
+        if (n < g.n && !*s_abort) {
+          const float bias = a.bias ? to_float<BF16>(a.bias[n]) : 0.f;
+#pragma unroll
+          for (int i = 0; i < Cfg::kCols / 2; ++i) {
+            float v0, v1;
+            f2_split(acc[i], v0, v1);
+            if (2 * i < n_tok) w4_put<BF16>(a, tok0 + 2 * i, n, v0 + bias);
+            if (2 * i + 1 < n_tok) w4_put<BF16>(a, tok0 + 2 * i + 1, n, v1 + bias);
+          }
+        }
+      } else {
+        // (one unit a cluster) token c of the tile goes to block c / share, where its sums stand [block][token][row]
+        const int share = (p.bn + cluster - 1) / cluster;
+        __syncwarp();
+        cluster_sync_all();                              // every block is done with its stages
+#pragma unroll
+        for (int i = 0; i < Cfg::kCols / 2; ++i) {
+          float v[2];
+          f2_split(acc[i], v[0], v[1]);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int c = col0 + 2 * i + e;
+            if (c < p.bn) {
+              const int owner = c / share;
+              const uint32_t to = stage0 + ((rank * share + c - owner * share) * 128 + row) * 4;
+              asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa_u32(to, owner)), "f"(v[e]) : "memory");
+            }
+          }
+        }
+      }
+    }
+  } else if (cluster > 1) {
+    __syncwarp();
+    cluster_sync_all();
+  }
+  __syncwarp();
+  abort_drain(s_abort);
+  tc_fence_before();
+  if (cluster > 1) {
+    cluster_sync_all();
+    const int share = (p.bn + cluster - 1) / cluster, tok0 = cl / p.row_tiles * p.bn + rank * share;
+    const int n_tok = min(min(share, p.bn - rank * share), a.T - tok0), row0 = cl % p.row_tiles * 128;
+    const float *part = reinterpret_cast<const float *>(smem);
+    if (!*s_abort)
+      for (int i = tid; i < n_tok * 128; i += kW4TileThreads) {
+        const int t = i >> 7, n = row0 + (i & 127);
+        float v = 0.f;
+        for (int r = 0; r < cluster; ++r) v += part[(r * share) * 128 + i];
+        if (n < g.n) w4_store<BF16>(a, tok0 + t, n, v);
+      }
+  } else {
+    __syncthreads();
+  }
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+}  // namespace ftmoe
