@@ -79,11 +79,6 @@ __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *tm,
       "l"(tm), "r"(x), "r"(y), "r"(z), "r"(v), "r"(w), "r"(bar)
       : "memory");
 }
-__device__ __forceinline__ bool elect_one() {
-  uint32_t p;
-  asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(p));
-  return p != 0;
-}
 // Of a row with reference m (log2 units) and sum l: the factor of its results and log(sum_j exp(s_j)).  Only an empty sum is a
 // row that attends to nothing; a sum that is not a number (an infinite or NaN score) stays one.
 __device__ __forceinline__ float row_inv(float l) { return l == 0.f ? 0.f : 1.f / l; }

@@ -13,7 +13,6 @@
 // With a cluster of c blocks each takes 1/c of k, and the sums are added over distributed shared memory, in the blocks' order.
 #pragma once
 #include "dense_w4.cuh"
-#include "float2.cuh"
 #include "tcgen.cuh"
 
 namespace ftmoe {
@@ -67,7 +66,7 @@ inline W4Tile w4_tile_share(const W4Geom &g, int T, int sm_count) {
 template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-template <bool BF16, int BN>
+template <bool BF16, bool ZERO, int BN>
 __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const W4Args a, const W4Tile p) {
   using Cfg = W4TileCfg<BN>;
   extern __shared__ unsigned char smem_raw[];
@@ -113,109 +112,149 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
   constexpr int kFirstAdd = 16 - Cfg::kAdd, kFirstExpand = 4;
 
   if (warp < 4) {
-    regs_down<56>();
-    if (warp == 0 && lane == 0) {
+    regs_down<80>();
+    // (whole warps walk through the loops, so that what a copy or a product is given stands in uniform registers; one lane issues)
+    if (warp == 0) {
       // ------------------------------ x ------------------------------
       int s = 0;
       uint32_t ph = 1;
       for (int u = cl; u < units; u += n_cl) {
         const int tok0 = u / p.row_tiles * p.bn;
-        for (int h = 2 * b0; h < 2 * b1; ++h) {
+        for (int h = 2 * b0; h < 2 * b1 && !*s_abort; ++h) {
           wait(st_empty(s), ph);
-          mbar_expect_tx(x_full(s), p.bn * 128);
-          tma_load_2d(stage0 + s * Cfg::kStage + 128 * 128, &tm_x, h * 64, tok0, x_full(s));
+          if (elect_one()) {
+            mbar_expect_tx(x_full(s), p.bn * 128);
+            tma_load_2d(stage0 + s * Cfg::kStage + 128 * 128, &tm_x, h * 64, tok0, x_full(s));
+          }
           if (++s == kW4Stages) { s = 0; ph ^= 1; }
-          if (*s_abort) break;
         }
       }
-    } else if (warp == 2 && lane == 0) {
+    } else if (warp == 2) {
       // ------------------------------ records ------------------------------
       int s = 0;
       uint32_t ph = 1;
       for (int u = cl; u < units; u += n_cl) {
-        const int quad = u % p.row_tiles * 2, two = quad + 1 < g.quads;
+        const int quad = u % p.row_tiles * 2;
+        const bool two = quad + 1 < g.quads;
         const int r0 = g.record(g.tiles_of(quad)), r1 = two ? g.record(g.tiles_of(quad + 1)) : 0;
-        const uint8_t *src0 = a.image + g.quad_at(quad), *src1 = a.image + g.quad_at(quad + 1);
-        for (int b = b0; b < b1; ++b) {
+        const uint8_t *src0 = a.image + g.quad_at(quad) + (long long)b0 * r0, *src1 = a.image + g.quad_at(quad + 1) + (long long)b0 * r1;
+        for (int b = b0; b < b1 && !*s_abort; ++b, src0 += r0, src1 += r1) {
           wait(raw_empty(s), ph);
-          mbar_expect_tx(raw_full(s), r0 + r1);
-          bulk_g2s(rec0 + s * p.raw_bytes, src0 + (long long)b * r0, r0, raw_full(s));
-          if (two) bulk_g2s(rec0 + s * p.raw_bytes + rec4, src1 + (long long)b * r1, r1, raw_full(s));
+          if (elect_one()) {
+            mbar_expect_tx(raw_full(s), r0 + r1);
+            bulk_g2s(rec0 + s * p.raw_bytes, src0, r0, raw_full(s));
+            if (two) bulk_g2s(rec0 + s * p.raw_bytes + rec4, src1, r1, raw_full(s));
+          }
           if (++s == kW4Raw) { s = 0; ph ^= 1; }
-          if (*s_abort) break;
         }
       }
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
       // ------------------------------ mma ------------------------------
       const uint32_t idesc = (1u << 4) | (BF16 ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)(p.bn >> 3) << 17) | ((128u >> 4) << 24);
-      const int steps = 8 / per;                      // instructions of a group
-      int s = 0, d = 0, at = 0;
+      const uint32_t tmem_u = uniform(tmem), stage_u = uniform(stage0);
+      int s = 0, d = 0;
       uint32_t ph = 0, dph = 1;
-      for (int u = cl; u < units; u += n_cl)
-        for (int h = 2 * b0; h < 2 * b1; ++h) {
-          const bool ok = wait(x_full(s), ph) && wait(w_full(s), ph);
-          tc_fence_after();
-          const uint32_t base = stage0 + s * Cfg::kStage;
-          const uint64_t da = umma_desc(base, 16, 1024), db = umma_desc(base + 128 * 128, 16, 1024);
+      auto run = [&](auto steps) {                   // instructions of a group of k
+        constexpr int kSteps = decltype(steps)::value, kOnce = kSteps < 4 ? kSteps : 4;
+        for (int u = cl; u < units; u += n_cl)
+          for (int b = b0; b < b1 && !*s_abort; ++b)
 #pragma unroll
-          for (int k16 = 0; k16 < 4; ++k16) {
-            if (at == 0) {
-              wait(d_empty(d), dph);
-              tc_fence_after();
+            for (int half = 0; half < 2; ++half) {
+              wait(x_full(s), ph);
+              const bool ok = wait(w_full(s), ph);
+              const uint32_t base = stage_u + s * Cfg::kStage;
+              const uint64_t da = umma_desc(base, 16, 1024), db = umma_desc(base + 128 * 128, 16, 1024);
+#pragma unroll
+              for (int k0 = 0; k0 < 4; k0 += kOnce) {
+                const int at = half * 4 + k0;
+                if (at % kSteps == 0) wait(d_empty(d), dph);
+                tc_fence_after();
+                if (elect_one()) {
+                  if (ok)
+#pragma unroll
+                    for (int k16 = k0; k16 < k0 + kOnce; ++k16)
+                      umma_bf16(tmem_u + d * 256, da + 2 * k16, db + 2 * k16, idesc, (half * 4 + k16) % kSteps != 0);
+                  if ((at + kOnce) % kSteps == 0) umma_commit(d_full(d));
+                }
+                __syncwarp();
+                if ((at + kOnce) % kSteps == 0) {
+                  d ^= 1;
+                  if (d == 0) dph ^= 1;
+                }
+              }
+              if (elect_one()) umma_commit(st_empty(s));
+              __syncwarp();
+              if (++s == kW4Stages) { s = 0; ph ^= 1; }
             }
-            if (ok) umma_bf16(tmem + d * 256, da + 2 * k16, db + 2 * k16, idesc, at != 0);
-            if (++at == steps) {
-              umma_commit(d_full(d));
-              at = 0;
-              d ^= 1;
-              if (d == 0) dph ^= 1;
-            }
-          }
-          umma_commit(st_empty(s));
-          if (++s == kW4Stages) { s = 0; ph ^= 1; }
-          if (*s_abort) break;
-        }
+      };
+      if (per == 1) run(std::integral_constant<int, 8>());
+      else if (per == 2) run(std::integral_constant<int, 4>());
+      else run(std::integral_constant<int, 2>());
     }
   } else if (warp < kFirstExpand + Cfg::kExpand) {
     // ------------------------------ expansion ------------------------------
-    regs_down<104>();
+    // A warp has tiles me, me + kExpand, ... of the eight; what is not there (rows past the last) is expanded from whatever the slot holds:
+    // its operands reach no other row.
+    regs_down<96>();
+    constexpr int kMine = 8 / Cfg::kExpand;
     const int me = warp - kFirstExpand, gr = lane >> 2, q = lane & 3;
     const W4Const<BF16> con;
+    uint32_t dst[kMine][2];                          // of 8 k of row p, for either 32 k; row p + 8 stands 1024 bytes on
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+      const int row = (me + j * Cfg::kExpand) * 16 + w4_row(gr);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) dst[j][h] = stage0 + row * 128 + (((4 * h + q) ^ (row & 7)) << 4);
+    }
     int s = 0, rs = 0;
     uint32_t ph = 1, rph = 0;
     for (int u = cl; u < units; u += n_cl) {
       const int quad0 = u % p.row_tiles * 2;
-      for (int b = b0; b < b1; ++b) {
+      uint32_t src[kMine], z_at[kMine], next[kMine];           // codes, zero points, from half to half
+#pragma unroll
+      for (int j = 0; j < kMine; ++j) {
+        const int t = me + j * Cfg::kExpand, quad = t >> 2, m = quad0 + quad < g.quads ? g.tiles_of(quad0 + quad) : 1;
+        const uint32_t rec = rec0 + quad * rec4;
+        src[j] = rec + min(t & 3, m - 1) * kW4TileBytes + lane * 16;
+        next[j] = m * kW4TileBytes;
+        z_at[j] = rec + m * 2 * kW4TileBytes + per * 128 + gr * 8 + (t & 3) * 2;
+      }
+      for (int b = b0; b < b1 && !*s_abort; ++b) {
         wait(raw_full(rs), rph);
-#pragma unroll 1
+        uint4 w[2][kMine];
+        uint32_t z[2][2][kMine];
+        const uint32_t at = rs * p.raw_bytes;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int j = 0; j < kMine; ++j) {
+            w[half][j] = lds_v4(src[j] + at + half * next[j]);
+            if (ZERO)
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+                asm volatile("ld.shared.u16 %0, [%1];" : "=r"(z[half][h][j]) : "r"(z_at[j] + at + (half * 2 + h) * per / 4 * 64));
+          }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(raw_empty(rs));
+        if (++rs == kW4Raw) { rs = 0; rph ^= 1; }
+#pragma unroll
         for (int half = 0; half < 2; ++half) {
           wait(st_empty(s), ph);
-          const uint32_t dst0 = stage0 + s * Cfg::kStage;
+          const uint32_t to = s * Cfg::kStage;
 #pragma unroll
-          for (int j = 0; j < 8 / Cfg::kExpand; ++j) {
-            const int piece = me + j * Cfg::kExpand, quad = piece >> 2, tile = piece & 3;
-            const int m = quad0 + quad < g.quads ? g.tiles_of(quad0 + quad) : 0;
-            if (tile >= m) continue;                  // (rows that are not there: what their operands hold reaches no other row)
-            const uint32_t rec = rec0 + rs * p.raw_bytes + quad * rec4;
-            const uint4 w = lds_v4(rec + (half * m + tile) * kW4TileBytes + lane * 16);
-            const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-            const int row = quad * 64 + tile * 16 + w4_row(gr);
-            const uint32_t dst = dst0 + row * 128;
+          for (int j = 0; j < kMine; ++j) {
+            const uint32_t words[4] = {w[half][j].x, w[half][j].y, w[half][j].z, w[half][j].w};
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               uint32_t lo = BF16 ? 0x41c041c0u : 0x4e004e00u, hi = lo;      // 16 + 8
-              if (g.zeros) {
-                uint32_t z;
-                asm volatile("ld.shared.u16 %0, [%1];" : "=r"(z) : "r"(rec + m * 2 * kW4TileBytes + per * 128 + (half * 2 + h) * per / 4 * 64 + gr * 8 + tile * 2));
-                w4_zero_pairs<BF16>(z, lo, hi);
-              }
+              if (ZERO) w4_zero_pairs<BF16>(z[half][h][j], lo, hi);
               uint32_t c0[4], c1[4];
               w4_expand<BF16>(con, words[2 * h], c0);
               w4_expand<BF16>(con, words[2 * h + 1], c1);
-              const uint32_t at = ((4 * h + q) ^ (row & 7)) << 4;
-              asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst + at), "r"(sub_pair<BF16>(c0[0], lo)), "r"(sub_pair<BF16>(c0[2], lo)),
+              const uint32_t a0 = dst[j][h] + to;
+              asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a0), "r"(sub_pair<BF16>(c0[0], lo)), "r"(sub_pair<BF16>(c0[2], lo)),
                            "r"(sub_pair<BF16>(c1[0], lo)), "r"(sub_pair<BF16>(c1[2], lo)) : "memory");
-              asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst + 8 * 128 + at), "r"(sub_pair<BF16>(c0[1], hi)), "r"(sub_pair<BF16>(c0[3], hi)),
+              asm volatile("st.shared.v4.u32 [%0+1024], {%1,%2,%3,%4};" ::"r"(a0), "r"(sub_pair<BF16>(c0[1], hi)), "r"(sub_pair<BF16>(c0[3], hi)),
                            "r"(sub_pair<BF16>(c1[1], hi)), "r"(sub_pair<BF16>(c1[3], hi)) : "memory");
             }
           }
@@ -224,15 +263,12 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
           if (lane == 0) mbar_arrive(w_full(s));
           if (++s == kW4Stages) { s = 0; ph ^= 1; }
         }
-        if (lane == 0) mbar_arrive(raw_empty(rs));
-        if (++rs == kW4Raw) { rs = 0; rph ^= 1; }
-        if (*s_abort) break;
       }
     }
   }
   if (warp >= kFirstAdd) {
     // ------------------------------ sums ------------------------------
-    regs_up<176>();
+    regs_up<168>();
     const int row = (warp & 3) * 32 + lane, col0 = (warp - kFirstAdd) / 4 * Cfg::kCols, cols = min(Cfg::kCols, p.bn - col0);
     const int r8 = row & 7, gr = (r8 & 3) * 2 + (r8 >> 2), quad = row >> 6;
     const uint32_t lane_tmem = tmem + ((uint32_t)((warp & 3) * 32) << 16) + col0;
@@ -243,76 +279,93 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
       const int m = quad0 + quad < g.quads ? g.tiles_of(quad0 + quad) : 0;
       // the row's scales in a record: groups 128 bytes apart
       const uint32_t sc_at = quad * rec4 + m * 2 * kW4TileBytes + gr * 16 + ((row >> 4) & 3) * 4 + ((row >> 3) & 1) * 2;
-      uint64_t acc[Cfg::kCols / 2];
+      float acc[Cfg::kCols];
 #pragma unroll
-      for (int i = 0; i < Cfg::kCols / 2; ++i) acc[i] = 0;
-      for (int b = b0; b < b1; ++b) {
+      for (int i = 0; i < Cfg::kCols; ++i) acc[i] = 0.f;
+      // a record's scales, read one record ahead, so that its slot is free as soon as its codes are expanded
+      uint32_t sc[4], sc_next[4] = {0, 0, 0, 0};
+      auto fetch = [&]() {
         wait(raw_full(rs), rph);
-        uint32_t sc[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          sc[i] = 0;
-          if (i < per && m > 0) asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc[i]) : "r"(rec0 + rs * p.raw_bytes + sc_at + i * 128));
-        }
+        for (int i = 0; i < 4; ++i)
+          if (i < per) asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc_next[i]) : "r"(rec0 + rs * p.raw_bytes + sc_at + i * 128));
         __syncwarp();
         if (lane == 0) mbar_arrive(raw_empty(rs));
         if (++rs == kW4Raw) { rs = 0; rph ^= 1; }
+      };
+      fetch();
+      for (int b = b0; b < b1 && !*s_abort; ++b) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[i] = sc_next[i];
+        if (b + 1 < b1) fetch();
 #pragma unroll 1
         for (int i = 0; i < per; ++i) {
-          const float scale = to_float<BF16>((uint16_t)(i == 0 ? sc[0] : i == 1 ? sc[1] : i == 2 ? sc[2] : sc[3]));
-          const uint64_t scale2 = f2(scale, scale);
+          const float scale = to_float<BF16>((uint16_t)sc[0]);
+          sc[0] = sc[1]; sc[1] = sc[2]; sc[2] = sc[3];
           wait(d_full(d), dph);
           tc_fence_after();
 #pragma unroll
-          for (int c = 0; c < Cfg::kCols; c += 32) {
+          for (int c = 0; c < Cfg::kCols; c += 16) {
             if (c >= cols) break;
-            uint32_t v[32];
-            tmem_ld32(lane_tmem + d * 256 + c, v);
+            uint32_t v[16];
+            tmem_ld16(lane_tmem + d * 256 + c, v);
             tmem_ld_wait();
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-              acc[c / 2 + j] = fma2(f2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), scale2, acc[c / 2 + j]);
+            for (int j = 0; j < 16; ++j) acc[c + j] = fmaf(__uint_as_float(v[j]), scale, acc[c + j]);
           }
+          if (b + 1 == b1 && i + 1 == per) break;      // (the unit's last accumulator is kept)
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(d_empty(d));
           d ^= 1;
           if (d == 0) dph ^= 1;
         }
-        if (*s_abort) break;
       }
-      const int tok0 = u / p.row_tiles * p.bn + col0, n_tok = min(cols, a.T - tok0);
-      if (cluster == 1) {
-        if (n < g.n && !*s_abort) {
-          const float bias = a.bias ? to_float<BF16>(a.bias[n]) : 0.f;
+      // The sums go back to the accumulator they were last read from, to leave it by a loop of few instructions (written out for every
+      // register, the stores were 40 KB of code, which cost more to fetch than to run: 50 us a unit).
 #pragma unroll
-          for (int i = 0; i < Cfg::kCols / 2; ++i) {
-            float v0, v1;
-            f2_split(acc[i], v0, v1);
-            if (2 * i < n_tok) w4_put<BF16>(a, tok0 + 2 * i, n, v0 + bias);
-            if (2 * i + 1 < n_tok) w4_put<BF16>(a, tok0 + 2 * i + 1, n, v1 + bias);
-          }
+      for (int c = 0; c < Cfg::kCols; c += 16)
+        if (c < cols) tmem_st16f(lane_tmem + d * 256 + c, acc + c);
+      tmem_st_wait();
+      __syncwarp();
+      const int tok0 = u / p.row_tiles * p.bn + col0, n_tok = min(cols, a.T - tok0);
+      const uint32_t out_tmem = lane_tmem + d * 256;
+      if (cluster == 1) {
+        const float bias = a.bias && n < g.n ? to_float<BF16>(a.bias[n]) : 0.f;
+        const bool store = n < g.n && !*s_abort;
+#pragma unroll 1
+        for (int c = 0; c < n_tok; c += 8) {
+          uint32_t v[8];
+          tmem_ld8(out_tmem + c, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (store && c + j < n_tok) w4_put<BF16>(a, tok0 + c + j, n, __uint_as_float(v[j]) + bias);
         }
       } else {
         // (one unit a cluster) token c of the tile goes to block c / share, where its sums stand [block][token][row]
         const int share = (p.bn + cluster - 1) / cluster;
         __syncwarp();
         cluster_sync_all();                              // every block is done with its stages
+        int owner = col0 / share, left = share - col0 % share;
+#pragma unroll 1
+        for (int c = 0; c < cols; c += 8) {
+          uint32_t v[8];
+          tmem_ld8(out_tmem + c, v);
+          tmem_ld_wait();
 #pragma unroll
-        for (int i = 0; i < Cfg::kCols / 2; ++i) {
-          float v[2];
-          f2_split(acc[i], v[0], v[1]);
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int c = col0 + 2 * i + e;
-            if (c < p.bn) {
-              const int owner = c / share;
-              const uint32_t to = stage0 + ((rank * share + c - owner * share) * 128 + row) * 4;
-              asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa_u32(to, owner)), "f"(v[e]) : "memory");
-            }
+          for (int j = 0; j < 8; ++j) {
+            const uint32_t to = stage0 + ((rank * share + share - left) * 128 + row) * 4;
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa_u32(to, owner)), "f"(__uint_as_float(v[j])) : "memory");
+            if (--left == 0) { left = share; ++owner; }
           }
         }
       }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(d_empty(d));
+      d ^= 1;
+      if (d == 0) dph ^= 1;
     }
   } else if (cluster > 1) {
     __syncwarp();
