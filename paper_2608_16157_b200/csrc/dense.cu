@@ -82,10 +82,10 @@ bool make_x_map(const ft_dense *h, CUtensorMap *tm, const W4Args &a, int tokens)
 }
 
 template <bool BF16, bool ZERO, int BN>
-cudaError_t launch_w4_tile(const ft_dense *h, const W4Args &a, const W4Tile &p, cudaStream_t st) {
+cudaError_t launch_w4_tile(const ft_dense *h, const W4Args &a, W4Tile p, cudaStream_t st) {
   CUtensorMap tm;
   if (!make_x_map(h, &tm, a, p.bn)) return cudaErrorInvalidValue;
-  const int smem = w4_tile_smem<BN>(p), units = p.row_tiles * p.tok_tiles, fit = h->sm_count / p.cluster;
+  const int smem = w4_tile_memory<BN>(a.g, p), units = p.row_tiles * p.tok_tiles, fit = h->sm_count / p.cluster;
   cudaError_t e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZERO, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   return launch_clusters(w4_tile_kernel<BF16, ZERO, BN>, dim3((p.cluster > 1 || units < fit ? units : fit) * p.cluster), kW4TileThreads, smem, p.cluster, st, tm, a, p);
@@ -95,8 +95,7 @@ template <bool BF16, bool ZERO>
 cudaError_t launch_w4_many(const ft_dense *h, const W4Args &a, cudaStream_t st) {
   const W4Tile p = w4_tile_share(a.g, a.T, h->sm_count);
   if (p.bn <= 64) return launch_w4_tile<BF16, ZERO, 64>(h, a, p, st);
-  if (p.bn <= 128) return launch_w4_tile<BF16, ZERO, 128>(h, a, p, st);
-  return launch_w4_tile<BF16, ZERO, 256>(h, a, p, st);
+  return launch_w4_tile<BF16, ZERO, kW4Acc>(h, a, p, st);
 }
 
 template <bool BF16>

@@ -2,11 +2,10 @@
 //
 // Image of a matrix (w4_pack_kernel): for each quad (64 rows: four tiles of 16, the last quad with as many as there are rows for) and each
 // block of 128 k, one contiguous record:
-//   codes : [half of 64 k][tile] 512 bytes; lane (g, q) = 4g + q of a warp owns 16 of them = 4 words, word j holds rows p and p+8 of the tile,
-//           p = g/2 + 4 (g%2), at k = 32 (j/2) + 8q + 4 (j%2) .. +3 of the half: the A fragments of one mma.sync m16n8k16, whose rows and
-//           K order are free (x in the same order: 16 bytes of a token a lane).  Neighbouring g are four rows apart, so that 16-byte
-//           stores of a warp to 128-byte-swizzled rows meet no bank twice.
-//   scales: [group of k][g][4 tiles] pairs (row p, row p+8) in the activations' type: 16 bytes a lane for four tiles
+//   codes : [half of 64 k][tile] 512 bytes; lane (g, q) = 4g + q of a warp owns 16 of them = 4 words, word j holds rows g and g+8 of the tile at
+//           k = 16j + 4q .. +3 of the half: the A fragments of one mma.sync m16n8k16, whose K order is free (x in the same order: 8 bytes of a
+//           token a lane), and what a lane writes to tensor memory for 16 rows x 16 k
+//   scales: [group of k][g][4 tiles] pairs (row g, row g+8) in the activations' type: 16 bytes a lane for four tiles
 //   zeros : the same places, a byte each (only with zero points)
 // Rows are padded to 16, k to 128, with scales of 0.  A quad's records follow one another along k: a warp's share of a row of quads is one
 // stretch of memory.
@@ -50,9 +49,6 @@ inline W4Geom w4_geom(long long n, long long k, int group, bool zeros) {
 // Position of nibble pair i (0 .. 3) of a word: (low half's bit, high half's bit); a nibble may run over bit 31 to bit 0.
 template <bool BF16> __host__ __device__ constexpr int w4_bit(int i) { return BF16 ? (i < 3 ? 3 + 4 * i : 15) : (i == 0 ? 6 : i == 1 ? 10 : i == 2 ? 2 : 14); }
 
-// Row of a tile that lane group g holds (and that plus 8).
-__host__ __device__ __forceinline__ constexpr int w4_row(int g) { return (g >> 1) + 4 * (g & 1); }
-
 __device__ __forceinline__ uint32_t rotl32(uint32_t v, int n) { return __funnelshift_l(v, v, n); }
 
 // The two constants of the expansion, kept in registers (an instruction takes only one as a literal).
@@ -69,7 +65,7 @@ struct W4Const {
     return d;
   }
 };
-// Codes 16 + q of a word as four pairs: rows p, p+8 at the first two k, then at the next two.
+// Codes 16 + q of a word as four pairs: rows g, g+8 at the first two k, then at the next two.
 template <bool BF16>
 __device__ __forceinline__ void w4_expand(const W4Const<BF16> &c, uint32_t w, uint32_t (&p)[4]) {
   p[0] = c.pick(w);
@@ -120,16 +116,16 @@ __global__ void __launch_bounds__(256) w4_pack_kernel(const W4Geom g, const uint
       const int tile = quad * 4 + part % m;
       uint32_t w[4] = {0, 0, 0, 0};
       for (int half = 0; half < 2; ++half) {
-        const long long row = (long long)tile * 16 + w4_row(gr) + 8 * half;
-        for (int h = 0; h < 2; ++h) {
-          const int k = block * kW4Block + part / m * 64 + 32 * h + 8 * q;
+        const long long row = (long long)tile * 16 + gr + 8 * half;
+        for (int j = 0; j < 4; ++j) {
+          const int k = block * kW4Block + part / m * 64 + 16 * j + 4 * q;
           if (row >= g.n || k >= g.k) continue;            // (k is a multiple of 32)
           const uint8_t *src = codes + row * codes_stride + k / 2;
 #pragma unroll
-          for (int b = 0; b < 4; ++b) {                     // k + 2b, k + 2b + 1: word 2h + b/2, pair 2 (b % 2) + half
+          for (int b = 0; b < 2; ++b) {                     // k + 2b, k + 2b + 1: pair 2b + half
             const uint32_t c = src[b];
-            const int bit = w4_bit<BF16>(2 * (b & 1) + half);
-            w[2 * h + b / 2] |= rotl32(c & 15u, bit) | rotl32(c >> 4, bit + 16);
+            const int bit = w4_bit<BF16>(2 * b + half);
+            w[j] |= rotl32(c & 15u, bit) | rotl32(c >> 4, bit + 16);
           }
         }
       }
@@ -140,7 +136,7 @@ __global__ void __launch_bounds__(256) w4_pack_kernel(const W4Geom g, const uint
       const int kg = block * per + s;
       uint32_t v = 0, z = 0;
       for (int half = 0; half < 2; ++half) {
-        const long long row = (long long)(quad * 4 + q) * 16 + w4_row(gr) + 8 * half;
+        const long long row = (long long)(quad * 4 + q) * 16 + gr + 8 * half;
         if (row >= g.n || kg >= k_groups) continue;
         v |= (uint32_t)scales[row * k_groups + kg] << (16 * half);
         if (zeros) z |= min((uint32_t)zeros[row * k_groups + kg], 15u) << (8 * half);
@@ -261,7 +257,7 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32, 1) w4_stream_kernel(const W
   // the lane's tokens; those past the last one read it again: their results are not stored
   const uint16_t *x_at[NT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) x_at[t] = a.x + (long long)min(tok0 + 8 * t + gr, a.T - 1) * a.x_stride + q * 8;
+  for (int t = 0; t < NT; ++t) x_at[t] = a.x + (long long)min(tok0 + 8 * t + gr, a.T - 1) * a.x_stride + q * 4;
   grid_wait();
   if (n_b > 0) {
     enter();
@@ -298,10 +294,10 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32, 1) w4_stream_kernel(const W
         for (int t = 0; t < NT; ++t) {
           const uint16_t *src = x_at[t] + b * kW4Block + half * 64;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (G == kW4Block || b * kW4Block + half * 64 + 32 * h < g.k) v = *reinterpret_cast<const uint4 *>(src + 32 * h);
-            xr[t][4 * h] = v.x; xr[t][4 * h + 1] = v.y; xr[t][4 * h + 2] = v.z; xr[t][4 * h + 3] = v.w;
+          for (int j = 0; j < 4; ++j) {
+            uint2 v = make_uint2(0u, 0u);
+            if (G == kW4Block || b * kW4Block + half * 64 + 16 * j < g.k) v = *reinterpret_cast<const uint2 *>(src + 16 * j);
+            xr[t][2 * j] = v.x; xr[t][2 * j + 1] = v.y;
           }
         }
       };
@@ -368,7 +364,7 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32, 1) w4_stream_kernel(const W
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int n = (quad * 4 + r) * 16 + w4_row(gr) + (e & 2) * 4;
+          const int n = (quad * 4 + r) * 16 + gr + (e & 2) * 4;
           if (n >= g.n) continue;
           const float bias = a.bias ? to_float<BF16>(a.bias[n]) : 0.f;
 #pragma unroll
@@ -398,8 +394,8 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32, 1) w4_stream_kernel(const W
       const int n_hold = max(0, min(wk, g.nb - rank * wk));             // warps of the group that had records
       for (int o = (warp - first_warp) * 32 + lane; o < kOut; o += wk * 32) {
         // result o: row n and token t; where an accumulator of the warps has it
-        const int n = o % (kTiles * 16), t = o / (kTiles * 16), row = n & 7;
-        const int at = w4_slot((n >> 4) * NT + (t >> 3), (t & 1) + ((n & 8) >> 2), (((row & 3) * 2 + (row >> 2)) << 2) + ((t & 7) >> 1));
+        const int n = o % (kTiles * 16), t = o / (kTiles * 16);
+        const int at = w4_slot((n >> 4) * NT + (t >> 3), (t & 1) + ((n & 8) >> 2), (n & 7) * 4 + ((t & 7) >> 1));
         float v = 0.f;
         for (int w = 0; w < n_hold; ++w) v += reinterpret_cast<const float *>(smem + s_held[first_warp + w])[at];
         if (cluster == 1) {

@@ -4,8 +4,8 @@
 // expansion of the codes for few.
 //   raw warp      brings the records of 128 k (bulk copies)
 //   x warp        brings x, 64 k of the tokens at a time (TMA, 128-byte swizzle)
-//   expanding     turn codes into the exact 16-bit numbers q - z, rows of 64 k with the same swizzle
-//   mma warp      rows on M = 128, tokens on N; one accumulator in tensor memory per group of k, two in turn
+//   expanding     turn codes into the exact 16-bit numbers q - z and leave them in tensor memory, 64 k at a time
+//   mma warp      rows on M = 128 (A from tensor memory), tokens on N (B from shared memory); one accumulator per group of k, two in turn
 //   adding warps  take a group's sums out, a row a thread, and add them times the row's scale to float sums in registers
 // So a scale multiplies a float sum and no weight is rounded: with scales in the operands each weight would be (8 bits of scale times 4 of
 // code), and that rounding alone is as large as that of a 16-bit result.  The additions run beside the tensor cores: at 256 tokens a group
@@ -17,23 +17,30 @@
 
 namespace ftmoe {
 
-constexpr int kW4TileThreads = 512, kW4Stages = 4, kW4Raw = 3;
+constexpr int kW4TileThreads = 512, kW4Ops = 4, kW4Raw = 3;     // operands of 64 k in tensor memory, slots of records
+constexpr int kW4Acc = 192, kW4OpAt = 2 * kW4Acc;               // columns of an accumulator; where the operands stand (32 columns each)
+static_assert(kW4OpAt + kW4Ops * 32 <= 512, "tensor memory");
 
 struct W4Tile {
   int32_t bn, cluster, row_tiles, tok_tiles;     // tokens of a tile (a multiple of 16)
   int32_t raw_bytes;                             // of a slot: two records
+  int32_t ring_bytes;                            // of the tokens' stages, where the sums of a cluster's blocks go in the end
 };
 
 template <int BN>
 struct W4TileCfg {
-  static constexpr int kAdd = BN > 128 ? 8 : 4, kExpand = BN > 128 ? 4 : 8;      // warps
+  static constexpr int kAdd = BN > 64 ? 8 : 4, kExpand = BN > 64 ? 4 : 8;        // warps
   static constexpr int kCols = BN / (kAdd / 4);                                  // tokens of an adding warp
-  static constexpr int kStage = 128 * 128 + BN * 128;                            // 64 k of 128 rows and of the tokens
-  static constexpr int kBars = 2 * kW4Raw + 3 * kW4Stages + 4;
+  static constexpr int kStage = BN * 128, kStages = BN > 64 ? 6 : 8;             // 64 k of the tokens
+  static constexpr int kBars = 2 * kW4Raw + 2 * kStages + 2 * kW4Ops + 4;
 };
+// Fills in the sizes; returns the bytes of dynamic shared memory.
 template <int BN>
-inline int w4_tile_smem(const W4Tile &p) {
-  return 1024 + kW4Stages * W4TileCfg<BN>::kStage + kW4Raw * p.raw_bytes + W4TileCfg<BN>::kBars * 8 + 32;
+inline int w4_tile_memory(const W4Geom &g, W4Tile &p) {
+  const int stages = W4TileCfg<BN>::kStages * W4TileCfg<BN>::kStage, join = p.cluster > 1 ? (p.bn + p.cluster - 1) / p.cluster * p.cluster * 512 : 0;
+  p.raw_bytes = (2 * g.record(4) + 127) / 128 * 128;
+  p.ring_bytes = stages > join ? stages : join;
+  return 1024 + p.ring_bytes + kW4Raw * p.raw_bytes + W4TileCfg<BN>::kBars * 8 + 32;
 }
 
 // Tokens of a tile and blocks that share k: the split with the least clocks of the SM with the most to do.  A block of 128 k takes 4 clocks a
@@ -42,14 +49,14 @@ inline W4Tile w4_tile_share(const W4Geom &g, int T, int sm_count) {
   W4Tile best{};
   double least = 1e30;
   const int row_tiles = (g.quads + 1) / 2, per = kW4Block / g.group;
-  for (int bn = 32; bn <= 256; bn += 16) {
+  for (int bn = 32; bn <= kW4Acc; bn += 16) {
     if (bn > 32 && bn - 16 >= T) break;
     for (int cluster = 1; cluster <= kW4MaxCluster && (cluster == 1 || g.nb >= 2 * cluster); cluster *= 2) {
       const int tok_tiles = (T + bn - 1) / bn;
       const long long units = (long long)row_tiles * tok_tiles, fit = sm_count / cluster;
       if (cluster > 1 && units > fit) continue;
       double block = 4. * bn;
-      const double expand = bn > 128 ? 500 : 300, add = per * (bn > 128 ? 100 + bn : 100 + 2. * bn);
+      const double expand = bn > 64 ? 500 : 300, add = per * (bn > 64 ? 100 + bn : 100 + 2. * bn);
       if (block < expand) block = expand;
       if (block < add) block = add;
       const double cost = (double)((units + fit - 1) / fit) * ((double)(g.nb + cluster - 1) / cluster * block + 4000 + (cluster > 1 ? 2000 : 0));
@@ -59,7 +66,6 @@ inline W4Tile w4_tile_share(const W4Geom &g, int T, int sm_count) {
       }
     }
   }
-  best.raw_bytes = (2 * g.record(4) + 127) / 128 * 128;
   return best;
 }
 
@@ -71,7 +77,7 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
   using Cfg = W4TileCfg<BN>;
   extern __shared__ unsigned char smem_raw[];
   unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  unsigned char *s_rec = smem + kW4Stages * Cfg::kStage;
+  unsigned char *s_rec = smem + p.ring_bytes;
   uint64_t *s_bar = reinterpret_cast<uint64_t *>(s_rec + kW4Raw * p.raw_bytes);
   uint32_t *s_tmem = reinterpret_cast<uint32_t *>(s_bar + Cfg::kBars);
   volatile int *s_abort = reinterpret_cast<volatile int *>(s_tmem + 2);
@@ -79,17 +85,20 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
   const uint32_t stage0 = smem_u32(smem), rec0 = smem_u32(s_rec), bars = smem_u32(s_bar);
   auto raw_full = [&](int i) { return bars + 8u * i; };
   auto raw_empty = [&](int i) { return bars + 8u * (kW4Raw + i); };
-  auto x_full = [&](int i) { return bars + 8u * (2 * kW4Raw + i); };
-  auto w_full = [&](int i) { return bars + 8u * (2 * kW4Raw + kW4Stages + i); };
-  auto st_empty = [&](int i) { return bars + 8u * (2 * kW4Raw + 2 * kW4Stages + i); };
-  auto d_full = [&](int i) { return bars + 8u * (2 * kW4Raw + 3 * kW4Stages + i); };
-  auto d_empty = [&](int i) { return bars + 8u * (2 * kW4Raw + 3 * kW4Stages + 2 + i); };
+  constexpr int kX = 2 * kW4Raw, kW = kX + 2 * Cfg::kStages, kD = kW + 2 * kW4Ops;
+  auto x_full = [&](int i) { return bars + 8u * (kX + i); };
+  auto x_empty = [&](int i) { return bars + 8u * (kX + Cfg::kStages + i); };
+  auto w_full = [&](int i) { return bars + 8u * (kW + i); };
+  auto w_empty = [&](int i) { return bars + 8u * (kW + kW4Ops + i); };
+  auto d_full = [&](int i) { return bars + 8u * (kD + i); };
+  auto d_empty = [&](int i) { return bars + 8u * (kD + 2 + i); };
   auto wait = [&](uint32_t bar, uint32_t phase) { return mbar_try_wait(bar, phase) || mbar_wait(bar, phase, s_abort, a.status); };
 
   grid_let_next();
   if (tid == 0) {
     for (int i = 0; i < kW4Raw; ++i) { mbar_init(raw_full(i), 1); mbar_init(raw_empty(i), Cfg::kAdd + Cfg::kExpand); }
-    for (int i = 0; i < kW4Stages; ++i) { mbar_init(x_full(i), 1); mbar_init(w_full(i), Cfg::kExpand); mbar_init(st_empty(i), 1); }
+    for (int i = 0; i < Cfg::kStages; ++i) { mbar_init(x_full(i), 1); mbar_init(x_empty(i), 1); }
+    for (int i = 0; i < kW4Ops; ++i) { mbar_init(w_full(i), Cfg::kExpand); mbar_init(w_empty(i), 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(d_full(i), 1); mbar_init(d_empty(i), Cfg::kAdd); }
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -121,12 +130,12 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
       for (int u = cl; u < units; u += n_cl) {
         const int tok0 = u / p.row_tiles * p.bn;
         for (int h = 2 * b0; h < 2 * b1 && !*s_abort; ++h) {
-          wait(st_empty(s), ph);
+          wait(x_empty(s), ph);
           if (elect_one()) {
             mbar_expect_tx(x_full(s), p.bn * 128);
-            tma_load_2d(stage0 + s * Cfg::kStage + 128 * 128, &tm_x, h * 64, tok0, x_full(s));
+            tma_load_2d(stage0 + s * Cfg::kStage, &tm_x, h * 64, tok0, x_full(s));
           }
-          if (++s == kW4Stages) { s = 0; ph ^= 1; }
+          if (++s == Cfg::kStages) { s = 0; ph ^= 1; }
         }
       }
     } else if (warp == 2) {
@@ -152,8 +161,8 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
       // ------------------------------ mma ------------------------------
       const uint32_t idesc = (1u << 4) | (BF16 ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)(p.bn >> 3) << 17) | ((128u >> 4) << 24);
       const uint32_t tmem_u = uniform(tmem), stage_u = uniform(stage0);
-      int s = 0, d = 0;
-      uint32_t ph = 0, dph = 1;
+      int s = 0, o = 0, d = 0;
+      uint32_t ph = 0, oph = 0, dph = 1;
       auto run = [&](auto steps) {                   // instructions of a group of k
         constexpr int kSteps = decltype(steps)::value, kOnce = kSteps < 4 ? kSteps : 4;
         for (int u = cl; u < units; u += n_cl)
@@ -161,9 +170,9 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
               wait(x_full(s), ph);
-              const bool ok = wait(w_full(s), ph);
-              const uint32_t base = stage_u + s * Cfg::kStage;
-              const uint64_t da = umma_desc(base, 16, 1024), db = umma_desc(base + 128 * 128, 16, 1024);
+              const bool ok = wait(w_full(o), oph);
+              const uint64_t x_desc = umma_desc(stage_u + s * Cfg::kStage, 16, 1024);
+              const uint32_t w_at = tmem_u + kW4OpAt + o * 32;
 #pragma unroll
               for (int k0 = 0; k0 < 4; k0 += kOnce) {
                 const int at = half * 4 + k0;
@@ -173,7 +182,7 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
                   if (ok)
 #pragma unroll
                     for (int k16 = k0; k16 < k0 + kOnce; ++k16)
-                      umma_bf16(tmem_u + d * 256, da + 2 * k16, db + 2 * k16, idesc, (half * 4 + k16) % kSteps != 0);
+                      umma_ts(tmem_u + d * kW4Acc, w_at + 8 * k16, x_desc + 2 * k16, idesc, (half * 4 + k16) % kSteps != 0);
                   if ((at + kOnce) % kSteps == 0) umma_commit(d_full(d));
                 }
                 __syncwarp();
@@ -182,9 +191,13 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
                   if (d == 0) dph ^= 1;
                 }
               }
-              if (elect_one()) umma_commit(st_empty(s));
+              if (elect_one()) {
+                umma_commit(w_empty(o));
+                umma_commit(x_empty(s));
+              }
               __syncwarp();
-              if (++s == kW4Stages) { s = 0; ph ^= 1; }
+              if (++s == Cfg::kStages) { s = 0; ph ^= 1; }
+              if (++o == kW4Ops) { o = 0; oph ^= 1; }
             }
       };
       if (per == 1) run(std::integral_constant<int, 8>());
@@ -193,19 +206,13 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
     }
   } else if (warp < kFirstExpand + Cfg::kExpand) {
     // ------------------------------ expansion ------------------------------
-    // A warp has tiles me, me + kExpand, ... of the eight; what is not there (rows past the last) is expanded from whatever the slot holds:
-    // its operands reach no other row.
+    // A warp has the tiles of its quarter of tensor memory, both or one of them; what is not there (rows past the last) is expanded from
+    // whatever the slot holds: its operands reach no other row.
     regs_down<96>();
     constexpr int kMine = 8 / Cfg::kExpand;
-    const int me = warp - kFirstExpand, gr = lane >> 2, q = lane & 3;
+    const int tile0 = 2 * (warp & 3) + (kMine == 1 ? (warp - kFirstExpand) >> 2 : 0), gr = lane >> 2;
     const W4Const<BF16> con;
-    uint32_t dst[kMine][2];                          // of 8 k of row p, for either 32 k; row p + 8 stands 1024 bytes on
-#pragma unroll
-    for (int j = 0; j < kMine; ++j) {
-      const int row = (me + j * Cfg::kExpand) * 16 + w4_row(gr);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) dst[j][h] = stage0 + row * 128 + (((4 * h + q) ^ (row & 7)) << 4);
-    }
+    const uint32_t dst = tmem + kW4OpAt + ((uint32_t)(tile0 * 16) << 16);
     int s = 0, rs = 0;
     uint32_t ph = 1, rph = 0;
     for (int u = cl; u < units; u += n_cl) {
@@ -213,7 +220,7 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
       uint32_t src[kMine], z_at[kMine], next[kMine];           // codes, zero points, from half to half
 #pragma unroll
       for (int j = 0; j < kMine; ++j) {
-        const int t = me + j * Cfg::kExpand, quad = t >> 2, m = quad0 + quad < g.quads ? g.tiles_of(quad0 + quad) : 1;
+        const int t = tile0 + j, quad = t >> 2, m = quad0 + quad < g.quads ? g.tiles_of(quad0 + quad) : 1;
         const uint32_t rec = rec0 + quad * rec4;
         src[j] = rec + min(t & 3, m - 1) * kW4TileBytes + lane * 16;
         next[j] = m * kW4TileBytes;
@@ -239,38 +246,37 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
         if (++rs == kW4Raw) { rs = 0; rph ^= 1; }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          wait(st_empty(s), ph);
-          const uint32_t to = s * Cfg::kStage;
+          wait(w_empty(s), ph);
+          tc_fence_after();
 #pragma unroll
           for (int j = 0; j < kMine; ++j) {
             const uint32_t words[4] = {w[half][j].x, w[half][j].y, w[half][j].z, w[half][j].w};
+            uint32_t r[16];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int i = 0; i < 4; ++i) {
               uint32_t lo = BF16 ? 0x41c041c0u : 0x4e004e00u, hi = lo;      // 16 + 8
-              if (ZERO) w4_zero_pairs<BF16>(z[half][h][j], lo, hi);
-              uint32_t c0[4], c1[4];
-              w4_expand<BF16>(con, words[2 * h], c0);
-              w4_expand<BF16>(con, words[2 * h + 1], c1);
-              const uint32_t a0 = dst[j][h] + to;
-              asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a0), "r"(sub_pair<BF16>(c0[0], lo)), "r"(sub_pair<BF16>(c0[2], lo)),
-                           "r"(sub_pair<BF16>(c1[0], lo)), "r"(sub_pair<BF16>(c1[2], lo)) : "memory");
-              asm volatile("st.shared.v4.u32 [%0+1024], {%1,%2,%3,%4};" ::"r"(a0), "r"(sub_pair<BF16>(c0[1], hi)), "r"(sub_pair<BF16>(c0[3], hi)),
-                           "r"(sub_pair<BF16>(c1[1], hi)), "r"(sub_pair<BF16>(c1[3], hi)) : "memory");
+              if (ZERO) w4_zero_pairs<BF16>(z[half][i / 2][j], lo, hi);
+              uint32_t c[4];
+              w4_expand<BF16>(con, words[i], c);
+              r[4 * i] = sub_pair<BF16>(c[0], lo); r[4 * i + 1] = sub_pair<BF16>(c[2], lo);
+              r[4 * i + 2] = sub_pair<BF16>(c[1], hi); r[4 * i + 3] = sub_pair<BF16>(c[3], hi);
             }
+            tmem_st_16x256b_x4(dst + ((uint32_t)(j * 16) << 16) + s * 32, r);
           }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          tmem_st_wait();
+          tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(w_full(s));
-          if (++s == kW4Stages) { s = 0; ph ^= 1; }
+          if (++s == kW4Ops) { s = 0; ph ^= 1; }
         }
       }
     }
   }
   if (warp >= kFirstAdd) {
     // ------------------------------ sums ------------------------------
-    regs_up<168>();
+    regs_up<160>();
     const int row = (warp & 3) * 32 + lane, col0 = (warp - kFirstAdd) / 4 * Cfg::kCols, cols = min(Cfg::kCols, p.bn - col0);
-    const int r8 = row & 7, gr = (r8 & 3) * 2 + (r8 >> 2), quad = row >> 6;
+    const int gr = row & 7, quad = row >> 6;
     const uint32_t lane_tmem = tmem + ((uint32_t)((warp & 3) * 32) << 16) + col0;
     int rs = 0, d = 0;
     uint32_t rph = 0, dph = 0;
@@ -308,7 +314,7 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
           for (int c = 0; c < Cfg::kCols; c += 16) {
             if (c >= cols) break;
             uint32_t v[16];
-            tmem_ld16(lane_tmem + d * 256 + c, v);
+            tmem_ld16(lane_tmem + d * kW4Acc + c, v);
             tmem_ld_wait();
 #pragma unroll
             for (int j = 0; j < 16; ++j) acc[c + j] = fmaf(__uint_as_float(v[j]), scale, acc[c + j]);
@@ -325,11 +331,11 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
       // register, the stores were 40 KB of code, which cost more to fetch than to run: 50 us a unit).
 #pragma unroll
       for (int c = 0; c < Cfg::kCols; c += 16)
-        if (c < cols) tmem_st16f(lane_tmem + d * 256 + c, acc + c);
+        if (c < cols) tmem_st16f(lane_tmem + d * kW4Acc + c, acc + c);
       tmem_st_wait();
       __syncwarp();
       const int tok0 = u / p.row_tiles * p.bn + col0, n_tok = min(cols, a.T - tok0);
-      const uint32_t out_tmem = lane_tmem + d * 256;
+      const uint32_t out_tmem = lane_tmem + d * kW4Acc;
       if (cluster == 1) {
         const float bias = a.bias && n < g.n ? to_float<BF16>(a.bias[n]) : 0.f;
         const bool store = n < g.n && !*s_abort;
