@@ -81,21 +81,20 @@ bool make_x_map(const ft_dense *h, CUtensorMap *tm, const W4Args &a, int tokens)
                                                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool BF16, bool ZERO, int BN>
+template <bool BF16, bool ZERO, bool EXACT>
 cudaError_t launch_w4_tile(const ft_dense *h, const W4Args &a, W4Tile p, cudaStream_t st) {
   CUtensorMap tm;
   if (!make_x_map(h, &tm, a, p.bn)) return cudaErrorInvalidValue;
-  const int smem = w4_tile_memory<BN>(a.g, p), units = p.row_tiles * p.tok_tiles, fit = h->sm_count / p.cluster;
-  cudaError_t e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZERO, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const int smem = w4_tile_memory<EXACT>(a.g, p), units = p.row_tiles * p.tok_tiles, fit = h->sm_count / p.cluster;
+  cudaError_t e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZERO, EXACT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  return launch_clusters(w4_tile_kernel<BF16, ZERO, BN>, dim3((p.cluster > 1 || units < fit ? units : fit) * p.cluster), kW4TileThreads, smem, p.cluster, st, tm, a, p);
+  return launch_clusters(w4_tile_kernel<BF16, ZERO, EXACT>, dim3((p.cluster > 1 || units < fit ? units : fit) * p.cluster), kW4TileThreads, smem, p.cluster, st, tm, a, p);
 }
 
 template <bool BF16, bool ZERO>
 cudaError_t launch_w4_many(const ft_dense *h, const W4Args &a, cudaStream_t st) {
-  const W4Tile p = w4_tile_share(a.g, a.T, h->sm_count);
-  if (p.bn <= 64) return launch_w4_tile<BF16, ZERO, 64>(h, a, p, st);
-  return launch_w4_tile<BF16, ZERO, kW4Acc>(h, a, p, st);
+  const W4Tile p = w4_tile_share(a.g, a.T, a.out32 != 0, h->sm_count);
+  return a.out32 ? launch_w4_tile<BF16, ZERO, true>(h, a, p, st) : launch_w4_tile<BF16, ZERO, false>(h, a, p, st);
 }
 
 template <bool BF16>

@@ -80,6 +80,13 @@ __device__ __forceinline__ uint32_t sub_pair(uint32_t a, uint32_t b) {
   else asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
+template <bool BF16>
+__device__ __forceinline__ uint32_t mul_pair(uint32_t a, uint32_t b) {
+  uint32_t d;
+  if (BF16) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  else asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
 // 16 + z of both rows of a pair of zero-point bytes, each as a pair.
 template <bool BF16>
 __device__ __forceinline__ void w4_zero_pairs(uint32_t z, uint32_t &lo, uint32_t &hi) {

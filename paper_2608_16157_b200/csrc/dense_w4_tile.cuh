@@ -1,15 +1,16 @@
 // Products with 4-bit weights for many tokens, on the 5th-generation tensor cores.  Image and formula: dense_w4.cuh.
 //
-// A block takes 128 rows (two quads) x up to BN tokens and walks along k.  Bound: the tensor cores for many tokens (2 T N K flops), HBM and the
+// A block takes 128 rows (two quads) x up to 192 tokens and walks along k.  Bound: the tensor cores for many tokens (2 T N K flops), HBM and the
 // expansion of the codes for few.
 //   raw warp      brings the records of 128 k (bulk copies)
-//   x warp        brings x, 64 k of the tokens at a time (TMA, 128-byte swizzle)
-//   expanding     turn codes into the exact 16-bit numbers q - z and leave them in tensor memory, 64 k at a time
-//   mma warp      rows on M = 128 (A from tensor memory), tokens on N (B from shared memory); one accumulator per group of k, two in turn
-//   adding warps  take a group's sums out, a row a thread, and add them times the row's scale to float sums in registers
-// So a scale multiplies a float sum and no weight is rounded: with scales in the operands each weight would be (8 bits of scale times 4 of
-// code), and that rounding alone is as large as that of a 16-bit result.  The additions run beside the tensor cores: at 256 tokens a group
-// of 128 k takes these 1024 clocks and a warp's 128 additions a few hundred.
+//   x warp        brings x (TMA, 64 k of the tokens a box, 128-byte swizzle)
+//   expanding     turn codes into 16-bit numbers and leave them in tensor memory
+//   mma warp      rows on M = 128 (A from tensor memory), tokens on N (B from shared memory)
+// Two forms.  For 16-bit results the operands are the weights s (q - z), rounded once to the type (8 or 11 bits of scale times 4 of code do
+// not fit it): an error of the size of the result's own rounding, 0.0013 of the result in bf16 where that is 0.0017.  The tensor core adds
+// over all of k, and four warps take the sums out while it works on the next unit.  For float results (EXACT) the operands are the exact q - z,
+// a group of k has an accumulator of its own (two in turn), and eight warps add its sums times the row's scale to float sums in registers;
+// that takes about twice as long (reading an accumulator beside the tensor core costs 70 clocks for 16 tokens of 32 rows).
 // With a cluster of c blocks each takes 1/c of k, and the sums are added over distributed shared memory, in the blocks' order.
 #pragma once
 #include "dense_w4.cuh"
@@ -17,9 +18,9 @@
 
 namespace ftmoe {
 
-constexpr int kW4TileThreads = 512, kW4Ops = 4, kW4Raw = 3;     // operands of 64 k in tensor memory, slots of records
-constexpr int kW4Acc = 192, kW4OpAt = 2 * kW4Acc;               // columns of an accumulator; where the operands stand (32 columns each)
-static_assert(kW4OpAt + kW4Ops * 32 <= 512, "tensor memory");
+constexpr int kW4TileThreads = 512, kW4Ops = 2;                 // operands of 128 k in tensor memory
+constexpr int kW4Acc = 192, kW4OpAt = 2 * kW4Acc;               // columns of an accumulator; where the operands stand (64 columns each)
+static_assert(kW4OpAt + kW4Ops * 64 <= 512, "tensor memory");
 
 struct W4Tile {
   int32_t bn, cluster, row_tiles, tok_tiles;     // tokens of a tile (a multiple of 16)
@@ -27,25 +28,26 @@ struct W4Tile {
   int32_t ring_bytes;                            // of the tokens' stages, where the sums of a cluster's blocks go in the end
 };
 
-template <int BN>
+template <bool EXACT>
 struct W4TileCfg {
-  static constexpr int kAdd = BN > 64 ? 8 : 4, kExpand = BN > 64 ? 4 : 8;        // warps
-  static constexpr int kCols = BN / (kAdd / 4);                                  // tokens of an adding warp
-  static constexpr int kStage = BN * 128, kStages = BN > 64 ? 6 : 8;             // 64 k of the tokens
-  static constexpr int kBars = 2 * kW4Raw + 2 * kStages + 2 * kW4Ops + 4;
+  static constexpr int kAdd = EXACT ? 8 : 4, kExpand = EXACT ? 4 : 8;            // warps
+  static constexpr int kCols = kW4Acc / (kAdd / 4);                              // tokens of an adding warp
+  static constexpr int kStage = kW4Acc * 256, kStages = 3;                       // 128 k of the tokens: two boxes of 64
+  static constexpr int kRaw = EXACT ? 3 : 6;                                     // slots of records
+  static constexpr int kBars = 2 * kRaw + 2 * kStages + 2 * kW4Ops + 4;
 };
 // Fills in the sizes; returns the bytes of dynamic shared memory.
-template <int BN>
+template <bool EXACT>
 inline int w4_tile_memory(const W4Geom &g, W4Tile &p) {
-  const int stages = W4TileCfg<BN>::kStages * W4TileCfg<BN>::kStage, join = p.cluster > 1 ? (p.bn + p.cluster - 1) / p.cluster * p.cluster * 512 : 0;
+  const int stages = W4TileCfg<EXACT>::kStages * W4TileCfg<EXACT>::kStage, join = p.cluster > 1 ? (p.bn + p.cluster - 1) / p.cluster * p.cluster * 512 : 0;
   p.raw_bytes = (2 * g.record(4) + 127) / 128 * 128;
   p.ring_bytes = stages > join ? stages : join;
-  return 1024 + p.ring_bytes + kW4Raw * p.raw_bytes + W4TileCfg<BN>::kBars * 8 + 32;
+  return 1024 + p.ring_bytes + W4TileCfg<EXACT>::kRaw * p.raw_bytes + W4TileCfg<EXACT>::kBars * 8 + 32;
 }
 
 // Tokens of a tile and blocks that share k: the split with the least clocks of the SM with the most to do.  A block of 128 k takes 4 clocks a
 // token in the tensor cores, not less than its codes take to expand, nor than its groups' sums to be added; a unit 4000 more, and 2000 over a cluster.
-inline W4Tile w4_tile_share(const W4Geom &g, int T, int sm_count) {
+inline W4Tile w4_tile_share(const W4Geom &g, int T, bool exact, int sm_count) {
   W4Tile best{};
   double least = 1e30;
   const int row_tiles = (g.quads + 1) / 2, per = kW4Block / g.group;
@@ -56,7 +58,7 @@ inline W4Tile w4_tile_share(const W4Geom &g, int T, int sm_count) {
       const long long units = (long long)row_tiles * tok_tiles, fit = sm_count / cluster;
       if (cluster > 1 && units > fit) continue;
       double block = 4. * bn;
-      const double expand = bn > 64 ? 500 : 300, add = per * (bn > 64 ? 100 + bn : 100 + 2. * bn);
+      const double expand = exact ? 700 : 400, add = exact ? per * (300 + 4. * bn) : 0.;
       if (block < expand) block = expand;
       if (block < add) block = add;
       const double cost = (double)((units + fit - 1) / fit) * ((double)(g.nb + cluster - 1) / cluster * block + 4000 + (cluster > 1 ? 2000 : 0));
@@ -72,20 +74,21 @@ inline W4Tile w4_tile_share(const W4Geom &g, int T, int sm_count) {
 template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-template <bool BF16, bool ZERO, int BN>
+template <bool BF16, bool ZERO, bool EXACT>
 __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const W4Args a, const W4Tile p) {
-  using Cfg = W4TileCfg<BN>;
+  using Cfg = W4TileCfg<EXACT>;
+  constexpr int kRaw = Cfg::kRaw;
   extern __shared__ unsigned char smem_raw[];
   unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char *s_rec = smem + p.ring_bytes;
-  uint64_t *s_bar = reinterpret_cast<uint64_t *>(s_rec + kW4Raw * p.raw_bytes);
+  uint64_t *s_bar = reinterpret_cast<uint64_t *>(s_rec + kRaw * p.raw_bytes);
   uint32_t *s_tmem = reinterpret_cast<uint32_t *>(s_bar + Cfg::kBars);
   volatile int *s_abort = reinterpret_cast<volatile int *>(s_tmem + 2);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t stage0 = smem_u32(smem), rec0 = smem_u32(s_rec), bars = smem_u32(s_bar);
   auto raw_full = [&](int i) { return bars + 8u * i; };
-  auto raw_empty = [&](int i) { return bars + 8u * (kW4Raw + i); };
-  constexpr int kX = 2 * kW4Raw, kW = kX + 2 * Cfg::kStages, kD = kW + 2 * kW4Ops;
+  auto raw_empty = [&](int i) { return bars + 8u * (kRaw + i); };
+  constexpr int kX = 2 * kRaw, kW = kX + 2 * Cfg::kStages, kD = kW + 2 * kW4Ops;
   auto x_full = [&](int i) { return bars + 8u * (kX + i); };
   auto x_empty = [&](int i) { return bars + 8u * (kX + Cfg::kStages + i); };
   auto w_full = [&](int i) { return bars + 8u * (kW + i); };
@@ -96,7 +99,7 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
 
   grid_let_next();
   if (tid == 0) {
-    for (int i = 0; i < kW4Raw; ++i) { mbar_init(raw_full(i), 1); mbar_init(raw_empty(i), Cfg::kAdd + Cfg::kExpand); }
+    for (int i = 0; i < kRaw; ++i) { mbar_init(raw_full(i), 1); mbar_init(raw_empty(i), EXACT ? Cfg::kAdd + Cfg::kExpand : Cfg::kExpand); }
     for (int i = 0; i < Cfg::kStages; ++i) { mbar_init(x_full(i), 1); mbar_init(x_empty(i), 1); }
     for (int i = 0; i < kW4Ops; ++i) { mbar_init(w_full(i), Cfg::kExpand); mbar_init(w_empty(i), 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(d_full(i), 1); mbar_init(d_empty(i), Cfg::kAdd); }
@@ -121,7 +124,7 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
   constexpr int kFirstAdd = 16 - Cfg::kAdd, kFirstExpand = 4;
 
   if (warp < 4) {
-    regs_down<80>();
+    if constexpr (EXACT) regs_down<80>();
     // (whole warps walk through the loops, so that what a copy or a product is given stands in uniform registers; one lane issues)
     if (warp == 0) {
       // ------------------------------ x ------------------------------
@@ -129,11 +132,13 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
       uint32_t ph = 1;
       for (int u = cl; u < units; u += n_cl) {
         const int tok0 = u / p.row_tiles * p.bn;
-        for (int h = 2 * b0; h < 2 * b1 && !*s_abort; ++h) {
+        for (int b = b0; b < b1 && !*s_abort; ++b) {
           wait(x_empty(s), ph);
           if (elect_one()) {
-            mbar_expect_tx(x_full(s), p.bn * 128);
-            tma_load_2d(stage0 + s * Cfg::kStage, &tm_x, h * 64, tok0, x_full(s));
+            const uint32_t to = stage0 + s * Cfg::kStage;
+            mbar_expect_tx(x_full(s), 2 * p.bn * 128);
+            tma_load_2d(to, &tm_x, b * kW4Block, tok0, x_full(s));
+            tma_load_2d(to + kW4Acc * 128, &tm_x, b * kW4Block + 64, tok0, x_full(s));
           }
           if (++s == Cfg::kStages) { s = 0; ph ^= 1; }
         }
@@ -154,7 +159,7 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
             bulk_g2s(rec0 + s * p.raw_bytes, src0, r0, raw_full(s));
             if (two) bulk_g2s(rec0 + s * p.raw_bytes + rec4, src1, r1, raw_full(s));
           }
-          if (++s == kW4Raw) { s = 0; ph ^= 1; }
+          if (++s == kRaw) { s = 0; ph ^= 1; }
         }
       }
     } else if (warp == 1) {
@@ -163,44 +168,51 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
       const uint32_t tmem_u = uniform(tmem), stage_u = uniform(stage0);
       int s = 0, o = 0, d = 0;
       uint32_t ph = 0, oph = 0, dph = 1;
-      auto run = [&](auto steps) {                   // instructions of a group of k
-        constexpr int kSteps = decltype(steps)::value, kOnce = kSteps < 4 ? kSteps : 4;
-        for (int u = cl; u < units; u += n_cl)
-          for (int b = b0; b < b1 && !*s_abort; ++b)
+      auto run = [&](auto steps) {                   // EXACT: instructions of a group of k
+        constexpr int kSteps = decltype(steps)::value;
+        for (int u = cl; u < units; u += n_cl) {
+          if (!EXACT) wait(d_empty(d), dph);
+          for (int b = b0, dead = 0; b < b1 && !dead; ++b) {
+            dead = *s_abort;
+            wait(x_full(s), ph);
+            const bool ok = wait(w_full(o), oph);
+            const uint64_t x_desc = umma_desc(stage_u + s * Cfg::kStage, 16, 1024);
+            const uint32_t w_at = tmem_u + kW4OpAt + o * 64;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              wait(x_full(s), ph);
-              const bool ok = wait(w_full(o), oph);
-              const uint64_t x_desc = umma_desc(stage_u + s * Cfg::kStage, 16, 1024);
-              const uint32_t w_at = tmem_u + kW4OpAt + o * 32;
-#pragma unroll
-              for (int k0 = 0; k0 < 4; k0 += kOnce) {
-                const int at = half * 4 + k0;
-                if (at % kSteps == 0) wait(d_empty(d), dph);
-                tc_fence_after();
-                if (elect_one()) {
-                  if (ok)
-#pragma unroll
-                    for (int k16 = k0; k16 < k0 + kOnce; ++k16)
-                      umma_ts(tmem_u + d * kW4Acc, w_at + 8 * k16, x_desc + 2 * k16, idesc, (half * 4 + k16) % kSteps != 0);
-                  if ((at + kOnce) % kSteps == 0) umma_commit(d_full(d));
-                }
-                __syncwarp();
-                if ((at + kOnce) % kSteps == 0) {
-                  d ^= 1;
-                  if (d == 0) dph ^= 1;
-                }
-              }
+            for (int k0 = 0; k0 < 8; k0 += kSteps) {
+              if (EXACT) wait(d_empty(d), dph);
+              tc_fence_after();
               if (elect_one()) {
-                umma_commit(w_empty(o));
-                umma_commit(x_empty(s));
+                if (ok)
+#pragma unroll
+                  for (int k16 = k0; k16 < k0 + kSteps; ++k16)
+                    umma_ts(tmem_u + d * kW4Acc, w_at + 8 * k16, x_desc + (k16 / 4 * kW4Acc * 128 + k16 % 4 * 32) / 16, idesc,
+                            k16 != k0 || (!EXACT && b != b0));
+                if (EXACT) umma_commit(d_full(d));
               }
               __syncwarp();
-              if (++s == Cfg::kStages) { s = 0; ph ^= 1; }
-              if (++o == kW4Ops) { o = 0; oph ^= 1; }
+              if (EXACT) {
+                d ^= 1;
+                if (d == 0) dph ^= 1;
+              }
             }
+            if (elect_one()) {
+              umma_commit(w_empty(o));
+              umma_commit(x_empty(s));
+            }
+            __syncwarp();
+            if (++s == Cfg::kStages) { s = 0; ph ^= 1; }
+            if (++o == kW4Ops) { o = 0; oph ^= 1; }
+          }
+          if (!EXACT) {
+            if (elect_one()) umma_commit(d_full(d));
+            __syncwarp();
+            d ^= 1;
+            if (d == 0) dph ^= 1;
+          }
+        }
       };
-      if (per == 1) run(std::integral_constant<int, 8>());
+      if (!EXACT || per == 1) run(std::integral_constant<int, 8>());
       else if (per == 2) run(std::integral_constant<int, 4>());
       else run(std::integral_constant<int, 2>());
     }
@@ -208,7 +220,7 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
     // ------------------------------ expansion ------------------------------
     // A warp has the tiles of its quarter of tensor memory, both or one of them; what is not there (rows past the last) is expanded from
     // whatever the slot holds: its operands reach no other row.
-    regs_down<96>();
+    if constexpr (EXACT) regs_down<96>();
     constexpr int kMine = 8 / Cfg::kExpand;
     const int tile0 = 2 * (warp & 3) + (kMine == 1 ? (warp - kFirstExpand) >> 2 : 0), gr = lane >> 2;
     const W4Const<BF16> con;
@@ -217,25 +229,30 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
     uint32_t ph = 1, rph = 0;
     for (int u = cl; u < units; u += n_cl) {
       const int quad0 = u % p.row_tiles * 2;
-      uint32_t src[kMine], z_at[kMine], next[kMine];           // codes, zero points, from half to half
+      uint32_t src[kMine], sc_at[kMine], z_at[kMine], next[kMine];           // codes, scales, zero points, from half to half
 #pragma unroll
       for (int j = 0; j < kMine; ++j) {
         const int t = tile0 + j, quad = t >> 2, m = quad0 + quad < g.quads ? g.tiles_of(quad0 + quad) : 1;
         const uint32_t rec = rec0 + quad * rec4;
         src[j] = rec + min(t & 3, m - 1) * kW4TileBytes + lane * 16;
         next[j] = m * kW4TileBytes;
+        sc_at[j] = rec + m * 2 * kW4TileBytes + gr * 16 + (t & 3) * 4;
         z_at[j] = rec + m * 2 * kW4TileBytes + per * 128 + gr * 8 + (t & 3) * 2;
       }
-      for (int b = b0; b < b1 && !*s_abort; ++b) {
+      for (int b = b0, dead = 0; b < b1 && !dead; ++b) {
+        dead = *s_abort;
         wait(raw_full(rs), rph);
         uint4 w[2][kMine];
-        uint32_t z[2][2][kMine];
+        uint32_t z[2][2][kMine], sc[2][2][kMine];
         const uint32_t at = rs * p.raw_bytes;
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
           for (int j = 0; j < kMine; ++j) {
             w[half][j] = lds_v4(src[j] + at + half * next[j]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              if (!EXACT) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sc[half][h][j]) : "r"(sc_at[j] + at + (half * 2 + h) * per / 4 * 128));
             if (ZERO)
 #pragma unroll
               for (int h = 0; h < 2; ++h)
@@ -243,11 +260,11 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
           }
         __syncwarp();
         if (lane == 0) mbar_arrive(raw_empty(rs));
-        if (++rs == kW4Raw) { rs = 0; rph ^= 1; }
+        if (++rs == kRaw) { rs = 0; rph ^= 1; }
+        wait(w_empty(s), ph);
+        tc_fence_after();
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          wait(w_empty(s), ph);
-          tc_fence_after();
+        for (int half = 0; half < 2; ++half)
 #pragma unroll
           for (int j = 0; j < kMine; ++j) {
             const uint32_t words[4] = {w[half][j].x, w[half][j].y, w[half][j].z, w[half][j].w};
@@ -260,21 +277,25 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
               w4_expand<BF16>(con, words[i], c);
               r[4 * i] = sub_pair<BF16>(c[0], lo); r[4 * i + 1] = sub_pair<BF16>(c[2], lo);
               r[4 * i + 2] = sub_pair<BF16>(c[1], hi); r[4 * i + 3] = sub_pair<BF16>(c[3], hi);
+              if (!EXACT) {
+                const uint32_t s_lo = __byte_perm(sc[half][i / 2][j], 0, 0x1010), s_hi = __byte_perm(sc[half][i / 2][j], 0, 0x3232);
+                r[4 * i] = mul_pair<BF16>(r[4 * i], s_lo); r[4 * i + 1] = mul_pair<BF16>(r[4 * i + 1], s_lo);
+                r[4 * i + 2] = mul_pair<BF16>(r[4 * i + 2], s_hi); r[4 * i + 3] = mul_pair<BF16>(r[4 * i + 3], s_hi);
+              }
             }
-            tmem_st_16x256b_x4(dst + ((uint32_t)(j * 16) << 16) + s * 32, r);
+            tmem_st_16x256b_x4(dst + ((uint32_t)(j * 16) << 16) + s * 64 + half * 32, r);
           }
-          tmem_st_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(w_full(s));
-          if (++s == kW4Ops) { s = 0; ph ^= 1; }
-        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(w_full(s));
+        if (++s == kW4Ops) { s = 0; ph ^= 1; }
       }
     }
   }
   if (warp >= kFirstAdd) {
     // ------------------------------ sums ------------------------------
-    regs_up<160>();
+    if constexpr (EXACT) regs_up<160>();
     const int row = (warp & 3) * 32 + lane, col0 = (warp - kFirstAdd) / 4 * Cfg::kCols, cols = min(Cfg::kCols, p.bn - col0);
     const int gr = row & 7, quad = row >> 6;
     const uint32_t lane_tmem = tmem + ((uint32_t)((warp & 3) * 32) << 16) + col0;
@@ -284,56 +305,62 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
       const int quad0 = u % p.row_tiles * 2, n = (quad0 * 4) * 16 + row;
       const int m = quad0 + quad < g.quads ? g.tiles_of(quad0 + quad) : 0;
       // the row's scales in a record: groups 128 bytes apart
-      const uint32_t sc_at = quad * rec4 + m * 2 * kW4TileBytes + gr * 16 + ((row >> 4) & 3) * 4 + ((row >> 3) & 1) * 2;
-      float acc[Cfg::kCols];
+      if constexpr (EXACT) {
+        const uint32_t sc_at = quad * rec4 + m * 2 * kW4TileBytes + gr * 16 + ((row >> 4) & 3) * 4 + ((row >> 3) & 1) * 2;
+        float acc[Cfg::kCols];
 #pragma unroll
-      for (int i = 0; i < Cfg::kCols; ++i) acc[i] = 0.f;
-      // a record's scales, read one record ahead, so that its slot is free as soon as its codes are expanded
-      uint32_t sc[4], sc_next[4] = {0, 0, 0, 0};
-      auto fetch = [&]() {
-        wait(raw_full(rs), rph);
+        for (int i = 0; i < Cfg::kCols; ++i) acc[i] = 0.f;
+        // a record's scales, read one record ahead, so that its slot is free as soon as its codes are expanded
+        uint32_t sc[4], sc_next[4] = {0, 0, 0, 0};
+        auto fetch = [&]() {
+          wait(raw_full(rs), rph);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (i < per) asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc_next[i]) : "r"(rec0 + rs * p.raw_bytes + sc_at + i * 128));
-        __syncwarp();
-        if (lane == 0) mbar_arrive(raw_empty(rs));
-        if (++rs == kW4Raw) { rs = 0; rph ^= 1; }
-      };
-      fetch();
-      for (int b = b0; b < b1 && !*s_abort; ++b) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sc[i] = sc_next[i];
-        if (b + 1 < b1) fetch();
-#pragma unroll 1
-        for (int i = 0; i < per; ++i) {
-          const float scale = to_float<BF16>((uint16_t)sc[0]);
-          sc[0] = sc[1]; sc[1] = sc[2]; sc[2] = sc[3];
-          wait(d_full(d), dph);
-          tc_fence_after();
-#pragma unroll
-          for (int c = 0; c < Cfg::kCols; c += 16) {
-            if (c >= cols) break;
-            uint32_t v[16];
-            tmem_ld16(lane_tmem + d * kW4Acc + c, v);
-            tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 16; ++j) acc[c + j] = fmaf(__uint_as_float(v[j]), scale, acc[c + j]);
-          }
-          if (b + 1 == b1 && i + 1 == per) break;      // (the unit's last accumulator is kept)
-          tc_fence_before();
+          for (int i = 0; i < 4; ++i)
+            if (i < per) asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc_next[i]) : "r"(rec0 + rs * p.raw_bytes + sc_at + i * 128));
           __syncwarp();
-          if (lane == 0) mbar_arrive(d_empty(d));
-          d ^= 1;
-          if (d == 0) dph ^= 1;
-        }
-      }
-      // The sums go back to the accumulator they were last read from, to leave it by a loop of few instructions (written out for every
-      // register, the stores were 40 KB of code, which cost more to fetch than to run: 50 us a unit).
+          if (lane == 0) mbar_arrive(raw_empty(rs));
+          if (++rs == kRaw) { rs = 0; rph ^= 1; }
+        };
+        fetch();
+        for (int b = b0, dead = 0; b < b1 && !dead; ++b) {
+          dead = *s_abort;
 #pragma unroll
-      for (int c = 0; c < Cfg::kCols; c += 16)
-        if (c < cols) tmem_st16f(lane_tmem + d * kW4Acc + c, acc + c);
-      tmem_st_wait();
-      __syncwarp();
+          for (int i = 0; i < 4; ++i) sc[i] = sc_next[i];
+          if (b + 1 < b1) fetch();
+#pragma unroll 1
+          for (int i = 0; i < per; ++i) {
+            const float scale = to_float<BF16>((uint16_t)sc[0]);
+            sc[0] = sc[1]; sc[1] = sc[2]; sc[2] = sc[3];
+            wait(d_full(d), dph);
+            tc_fence_after();
+#pragma unroll
+            for (int c = 0; c < Cfg::kCols; c += 16) {
+              if (c >= cols) break;
+              uint32_t v[16];
+              tmem_ld16(lane_tmem + d * kW4Acc + c, v);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 16; ++j) acc[c + j] = fmaf(__uint_as_float(v[j]), scale, acc[c + j]);
+            }
+            if (b + 1 == b1 && i + 1 == per) break;      // (the unit's last accumulator is kept)
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(d_empty(d));
+            d ^= 1;
+            if (d == 0) dph ^= 1;
+          }
+        }
+        // The sums go back to the accumulator they were last read from, to leave it by a loop of few instructions (written out for every
+        // register, the stores were 40 KB of code, which cost more to fetch than to run: 50 us a unit).
+#pragma unroll
+        for (int c = 0; c < Cfg::kCols; c += 16)
+          if (c < cols) tmem_st16f(lane_tmem + d * kW4Acc + c, acc + c);
+        tmem_st_wait();
+        __syncwarp();
+      } else {
+        wait(d_full(d), dph);
+        tc_fence_after();
+      }
       const int tok0 = u / p.row_tiles * p.bn + col0, n_tok = min(cols, a.T - tok0);
       const uint32_t out_tmem = lane_tmem + d * kW4Acc;
       if (cluster == 1) {

@@ -132,7 +132,7 @@ def run_w4(t, n, k, group, dtype, *, zeros=False, bias=False, out32=False, x_pad
     before = buf.clone()
     h.w4(x, w, out, bias=b)
     assert h.sync_status() == 0
-    ref, err = R.w4(x, R.w4_weights(codes, scales, z), b)
+    ref, err = R.w4(x, R.w4_weights(codes, scales, z), b, out.dtype)
     assert ((out.double() - ref).abs() <= err + R.rounding(ref, out.dtype)).all()
     same_outside(out, buf, before)
     h.destroy()
@@ -151,12 +151,14 @@ def test_w4_rows_and_tokens(n, t):
 def test_w4_depths_and_groups(k, group, dtype):
     for t, n in ((1, 272), (6, 40), (13, 300), (70, 150)):
         run_w4(t, n, k, group, dtype, zeros=t % 2 == 1, out32=t == 13, seed=k + t)
+    run_w4(70, 150, k, group, dtype, zeros=True, out32=True, seed=k)
 
 
-@pytest.mark.parametrize("t", [1, 5, 12, 35, 130, 300, 520])
+@pytest.mark.parametrize("t", [1, 5, 12, 32, 33, 130, 300, 520])
 @pytest.mark.parametrize("n,k,group,dtype,zeros", [(5120, 2048, 128, "bf16", False), (2048, 4096, 32, "fp16", True), (9001, 1024, 64, "bf16", True)])
 def test_w4_wide(t, n, k, group, dtype, zeros):
     run_w4(t, n, k, group, dtype, zeros=zeros, seed=t)
+    run_w4(t, n, k, group, dtype, zeros=not zeros, out32=True, bias=True, seed=t)
 
 
 @pytest.mark.parametrize("x_pad,y_pad,y_shift", [(8, 0, 0), (64, 3, 1), (0, 1, 0), (24, 0, 1)])
@@ -179,7 +181,7 @@ def test_w4_outliers_infinities_and_nan_stay_in_their_token(t):
     x = x.bfloat16()
     out = torch.empty(t, 300, device=DEV)
     h.w4(x, w, out)
-    ref, err = R.w4(x, R.w4_weights(codes, scales, None), None)
+    ref, err = R.w4(x, R.w4_weights(codes, scales, None), None, out.dtype)
     assert ((out.double() - ref).abs() <= err + R.rounding(ref, torch.float32)).all()
     x2 = x.clone()
     x2[0, 500], x2[2, 3] = float("inf"), NAN
