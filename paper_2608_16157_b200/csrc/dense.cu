@@ -17,6 +17,7 @@ using namespace ftmoe;
 
 struct ft_dense {
   int device = 0, sm_count = 148;
+  int clusters[kW4MaxCluster + 1] = {};   // of each size that fit at once, a block an SM
   uint32_t *status_dev = nullptr;
   void *encode = nullptr;          // cuTensorMapEncodeTiled
   uint64_t launches = 0;
@@ -53,11 +54,9 @@ cudaError_t launch_norm(const NormArgs &a, bool wide, cudaStream_t st) {
 template <bool BF16, int G, bool ZERO, int NT>
 cudaError_t launch_w4_stream(const ft_dense *h, const W4Args &a, cudaStream_t st) {
   W4Stream p;
-  w4_stream_share(a.g, h->sm_count, kW4Warps<NT>, p);
+  w4_stream_share(a.g, h->clusters, kW4Warps<NT>, p);
   const int smem = w4_stream_memory<NT>(a.g, p);
-  cudaError_t e = cudaFuncSetAttribute(w4_stream_kernel<BF16, G, ZERO, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
-  const int per_block = kW4Warps<NT> / p.wk, want = (a.g.quads + per_block - 1) / per_block, fit = h->sm_count / p.cluster;
+  const int per_block = kW4Warps<NT> / p.wk, want = (a.g.quads + per_block - 1) / per_block, fit = h->clusters[p.cluster];
   return launch_clusters(w4_stream_kernel<BF16, G, ZERO, NT>, dim3((want < fit ? want : fit) * p.cluster, (a.T + 8 * NT - 1) / (8 * NT)), kW4Warps<NT> * 32, smem,
                          p.cluster, st, a, p);
 }
@@ -85,15 +84,13 @@ template <bool BF16, bool ZERO, bool EXACT>
 cudaError_t launch_w4_tile(const ft_dense *h, const W4Args &a, W4Tile p, cudaStream_t st) {
   CUtensorMap tm;
   if (!make_x_map(h, &tm, a, p.bn)) return cudaErrorInvalidValue;
-  const int smem = w4_tile_memory<EXACT>(a.g, p), units = p.row_tiles * p.tok_tiles, fit = h->sm_count / p.cluster;
-  cudaError_t e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZERO, EXACT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
+  const int smem = w4_tile_memory<EXACT>(a.g, p), units = p.row_tiles * p.tok_tiles, fit = h->clusters[p.cluster];
   return launch_clusters(w4_tile_kernel<BF16, ZERO, EXACT>, dim3((p.cluster > 1 || units < fit ? units : fit) * p.cluster), kW4TileThreads, smem, p.cluster, st, tm, a, p);
 }
 
 template <bool BF16, bool ZERO>
 cudaError_t launch_w4_many(const ft_dense *h, const W4Args &a, cudaStream_t st) {
-  const W4Tile p = w4_tile_share(a.g, a.T, a.out32 != 0, h->sm_count);
+  const W4Tile p = w4_tile_share(a.g, a.T, a.out32 != 0, h->clusters);
   return a.out32 ? launch_w4_tile<BF16, ZERO, true>(h, a, p, st) : launch_w4_tile<BF16, ZERO, false>(h, a, p, st);
 }
 
@@ -105,6 +102,47 @@ cudaError_t launch_w4(const ft_dense *h, const W4Args &a, bool zero, cudaStream_
     case 64: return zero ? launch_w4_tokens<BF16, 64, true>(h, a, st) : launch_w4_tokens<BF16, 64, false>(h, a, st);
     default: return zero ? launch_w4_tokens<BF16, 128, true>(h, a, st) : launch_w4_tokens<BF16, 128, false>(h, a, st);
   }
+}
+
+constexpr int kMaxSmem = 227 * 1024;
+
+template <bool BF16, int G, bool ZERO>
+cudaError_t allow_smem_stream() {
+  cudaError_t e = cudaFuncSetAttribute(w4_stream_kernel<BF16, G, ZERO, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(w4_stream_kernel<BF16, G, ZERO, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(w4_stream_kernel<BF16, G, ZERO, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+  return e;
+}
+template <bool BF16, bool ZERO>
+cudaError_t allow_smem() {
+  cudaError_t e = allow_smem_stream<BF16, 32, ZERO>();
+  if (e == cudaSuccess) e = allow_smem_stream<BF16, 64, ZERO>();
+  if (e == cudaSuccess) e = allow_smem_stream<BF16, 128, ZERO>();
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZERO, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZERO, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+  return e;
+}
+
+// How many clusters of a size run at once when each block takes an SM (the SMs of a cluster stand together, so not all are used).
+cudaError_t count_clusters(ft_dense *h) {
+  for (int c = 1; c <= kW4MaxCluster; ++c) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(c * h->sm_count);
+    cfg.blockDim = dim3(kW4TileThreads);
+    cfg.dynamicSmemBytes = kMaxSmem;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = c;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    int n = h->sm_count;
+    const cudaError_t e = c == 1 ? cudaSuccess : cudaOccupancyMaxActiveClusters(&n, w4_tile_kernel<true, false, false>, &cfg);
+    if (e != cudaSuccess) return e;
+    h->clusters[c] = n;
+  }
+  return cudaSuccess;
 }
 
 }  // namespace
@@ -128,6 +166,11 @@ ft_status_t ft_dense_create(int device, ft_dense_t **out) {
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
   if (e == cudaSuccess) e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &h->encode, cudaEnableDefault, &found);
+  if (e == cudaSuccess) e = allow_smem<true, true>();
+  if (e == cudaSuccess) e = allow_smem<true, false>();
+  if (e == cudaSuccess) e = allow_smem<false, true>();
+  if (e == cudaSuccess) e = allow_smem<false, false>();
+  if (e == cudaSuccess) e = count_clusters(h);
   if (e == cudaSuccess && (!h->encode || found != cudaDriverEntryPointSuccess)) e = cudaErrorNotSupported;
   if (e != cudaSuccess) {
     (void)cudaFree(h->status_dev);

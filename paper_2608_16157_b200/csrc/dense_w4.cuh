@@ -188,17 +188,19 @@ struct W4Stream {        // how the quads are shared out
 };
 // Shares the quads out.  A warp of a group of `workers` does ceil(nb / workers) records of each of its group's quads, then the group adds its
 // sums, which takes about as long as a record (two, over a cluster); the split with the least of both is taken, and of equals the one with the
-// fewer warps to a quad.
-inline void w4_stream_share(const W4Geom &g, int sm_count, int warps, W4Stream &s) {
+// fewer warps to a quad.  `clusters`: how many clusters of a size the GPU holds at once.
+inline void w4_stream_share(const W4Geom &g, const int *clusters, int warps, W4Stream &s) {
   double best = 1e30;
-  for (int workers = 1; workers <= warps * kW4MaxCluster; workers *= 2) {
-    if (workers > 1 && workers / 2 >= g.nb) break;
-    const int cluster = workers > warps ? workers / warps : 1, wk = workers / cluster, groups = sm_count / cluster * (warps / wk);
+  auto consider = [&](int cluster, int wk) {
+    const int groups = clusters[cluster] * (warps / wk), workers = cluster * wk;
+    if (groups == 0 || (workers > 1 && workers >= 2 * g.nb)) return;
     const double cost = (double)((g.quads + groups - 1) / groups) * ((g.nb + workers - 1) / workers + (workers == 1 ? 0.5 : cluster == 1 ? 1. : 2.));
     if (cost < best) { best = cost; s.cluster = cluster; s.wk = wk; }
-  }
+  };
+  for (int wk = 1; wk <= warps; wk *= 2) consider(1, wk);
+  for (int cluster = 2; cluster <= kW4MaxCluster; ++cluster) consider(cluster, warps);
 }
-template <int NT> constexpr int kW4Join = 64 * 8 * NT;     // floats of a buffer of sums of a cluster's blocks
+template <int NT> constexpr int kW4Join = 64 * 8 * NT + 32 * kW4MaxCluster;     // floats of a buffer of sums of a cluster's blocks
 // The slots' size and number, as many as fit; returns the bytes of dynamic shared memory.
 template <int NT>
 inline int w4_stream_memory(const W4Geom &g, W4Stream &s) {
@@ -280,6 +282,7 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32, 1) w4_stream_kernel(const W
     else __syncwarp();
   };
 
+  const int share = (kOut / 32 + cluster - 1) / cluster * 32;           // results that a block of a cluster finishes
   int slot = 0, turn = 0;
   uint32_t phase = 0;
   for (int quad = group; quad < g.quads; quad += n_groups) {
@@ -408,16 +411,17 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32, 1) w4_stream_kernel(const W
         if (cluster == 1) {
           if (tok0 + t < a.T && row0 + n < g.n) w4_store<BF16>(a, tok0 + t, row0 + n, v);
         } else {
-          const int owner = (o >> 5) % cluster, to = turn * kW4Join<NT> + rank * (kOut / cluster) + (o >> 5) / cluster * 32 + (o & 31);
+          const int owner = (o >> 5) % cluster, to = turn * kW4Join<NT> + rank * share + (o >> 5) / cluster * 32 + (o & 31);
           asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa_u32(smem_u32(s_join + to), owner)), "f"(v) : "memory");
         }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // (the slot's next contents come by a bulk copy)
       if (cluster > 1) {
         cluster_sync_all();
-        const int share = kOut / cluster;
         for (int i = tid; i < share; i += kW4Warps<NT> * 32) {
-          const int o = ((i >> 5) * cluster + rank) * 32 + (i & 31), n = o % (kTiles * 16), t = o / (kTiles * 16);
+          const int o = ((i >> 5) * cluster + rank) * 32 + (i & 31);
+          if (o >= kOut) break;
+          const int n = o % (kTiles * 16), t = o / (kTiles * 16);
           float v = 0.f;
           for (int w = 0; w < cluster; ++w) v += s_join[turn * kW4Join<NT> + w * share + i];
           if (tok0 + t < a.T && row0 + n < g.n) w4_store<BF16>(a, tok0 + t, row0 + n, v);

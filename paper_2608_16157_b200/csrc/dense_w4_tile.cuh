@@ -45,23 +45,23 @@ inline int w4_tile_memory(const W4Geom &g, W4Tile &p) {
   return 1024 + p.ring_bytes + W4TileCfg<EXACT>::kRaw * p.raw_bytes + W4TileCfg<EXACT>::kBars * 8 + 32;
 }
 
-// Tokens of a tile and blocks that share k: the split with the least clocks of the SM with the most to do.  A block of 128 k takes 4 clocks a
+// Tokens of a tile and blocks that share k (`clusters`: how many clusters of a size the GPU holds at once): the split with the least clocks of the SM with the most to do.  A block of 128 k takes 4 clocks a
 // token in the tensor cores, not less than its codes take to expand, nor than its groups' sums to be added; a unit 4000 more, and 2000 over a cluster.
-inline W4Tile w4_tile_share(const W4Geom &g, int T, bool exact, int sm_count) {
+inline W4Tile w4_tile_share(const W4Geom &g, int T, bool exact, const int *clusters) {
   W4Tile best{};
   double least = 1e30;
   const int row_tiles = (g.quads + 1) / 2, per = kW4Block / g.group;
   for (int bn = 32; bn <= kW4Acc; bn += 16) {
     if (bn > 32 && bn - 16 >= T) break;
-    for (int cluster = 1; cluster <= kW4MaxCluster && (cluster == 1 || g.nb >= 2 * cluster); cluster *= 2) {
+    for (int cluster = 1; cluster <= kW4MaxCluster && (cluster == 1 || g.nb >= 2 * cluster); ++cluster) {
       const int tok_tiles = (T + bn - 1) / bn;
-      const long long units = (long long)row_tiles * tok_tiles, fit = sm_count / cluster;
-      if (cluster > 1 && units > fit) continue;
+      const long long units = (long long)row_tiles * tok_tiles, fit = clusters[cluster];
+      if (fit == 0 || (cluster > 1 && units > fit)) continue;
       double block = 4. * bn;
       const double expand = exact ? 700 : 400, add = exact ? per * (300 + 4. * bn) : 0.;
       if (block < expand) block = expand;
       if (block < add) block = add;
-      const double cost = (double)((units + fit - 1) / fit) * ((double)(g.nb + cluster - 1) / cluster * block + 4000 + (cluster > 1 ? 2000 : 0));
+      const double cost = (double)((units + fit - 1) / fit) * ((double)((g.nb + cluster - 1) / cluster) * block + 4000 + (cluster > 1 ? 2000 : 0));
       if (cost < least) {
         least = cost;
         best.bn = bn; best.cluster = cluster; best.row_tiles = row_tiles; best.tok_tiles = tok_tiles;
@@ -239,46 +239,47 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
         sc_at[j] = rec + m * 2 * kW4TileBytes + gr * 16 + (t & 3) * 4;
         z_at[j] = rec + m * 2 * kW4TileBytes + per * 128 + gr * 8 + (t & 3) * 2;
       }
-      for (int b = b0, dead = 0; b < b1 && !dead; ++b) {
-        dead = *s_abort;
-        wait(raw_full(rs), rph);
+      struct Rec {
         uint4 w[2][kMine];
-        uint32_t z[2][2][kMine], sc[2][2][kMine];
+        uint32_t z[2][2][kMine], sc[2][2][kMine];    // per half and 32 k of it
+      };
+      auto take = [&](Rec &r) {
+        wait(raw_full(rs), rph);
         const uint32_t at = rs * p.raw_bytes;
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
           for (int j = 0; j < kMine; ++j) {
-            w[half][j] = lds_v4(src[j] + at + half * next[j]);
+            r.w[half][j] = lds_v4(src[j] + at + half * next[j]);
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-              if (!EXACT) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sc[half][h][j]) : "r"(sc_at[j] + at + (half * 2 + h) * per / 4 * 128));
-            if (ZERO)
-#pragma unroll
-              for (int h = 0; h < 2; ++h)
-                asm volatile("ld.shared.u16 %0, [%1];" : "=r"(z[half][h][j]) : "r"(z_at[j] + at + (half * 2 + h) * per / 4 * 64));
+            for (int h = 0; h < 2; ++h) {
+              if (!EXACT) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r.sc[half][h][j]) : "r"(sc_at[j] + at + (half * 2 + h) * per / 4 * 128));
+              if (ZERO) asm volatile("ld.shared.u16 %0, [%1];" : "=r"(r.z[half][h][j]) : "r"(z_at[j] + at + (half * 2 + h) * per / 4 * 64));
+            }
           }
+      };
+      auto give_back = [&]() {                       // (the record has been read)
         __syncwarp();
         if (lane == 0) mbar_arrive(raw_empty(rs));
         if (++rs == kRaw) { rs = 0; rph ^= 1; }
-        wait(w_empty(s), ph);
-        tc_fence_after();
+      };
+      auto expand = [&](const Rec &rec) {
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
           for (int j = 0; j < kMine; ++j) {
-            const uint32_t words[4] = {w[half][j].x, w[half][j].y, w[half][j].z, w[half][j].w};
+            const uint32_t words[4] = {rec.w[half][j].x, rec.w[half][j].y, rec.w[half][j].z, rec.w[half][j].w};
             uint32_t r[16];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               uint32_t lo = BF16 ? 0x41c041c0u : 0x4e004e00u, hi = lo;      // 16 + 8
-              if (ZERO) w4_zero_pairs<BF16>(z[half][i / 2][j], lo, hi);
+              if (ZERO) w4_zero_pairs<BF16>(rec.z[half][i / 2][j], lo, hi);
               uint32_t c[4];
               w4_expand<BF16>(con, words[i], c);
               r[4 * i] = sub_pair<BF16>(c[0], lo); r[4 * i + 1] = sub_pair<BF16>(c[2], lo);
               r[4 * i + 2] = sub_pair<BF16>(c[1], hi); r[4 * i + 3] = sub_pair<BF16>(c[3], hi);
               if (!EXACT) {
-                const uint32_t s_lo = __byte_perm(sc[half][i / 2][j], 0, 0x1010), s_hi = __byte_perm(sc[half][i / 2][j], 0, 0x3232);
+                const uint32_t sc = rec.sc[half][i / 2][j], s_lo = __byte_perm(sc, 0, 0x1010), s_hi = __byte_perm(sc, 0, 0x3232);
                 r[4 * i] = mul_pair<BF16>(r[4 * i], s_lo); r[4 * i + 1] = mul_pair<BF16>(r[4 * i + 1], s_lo);
                 r[4 * i + 2] = mul_pair<BF16>(r[4 * i + 2], s_hi); r[4 * i + 3] = mul_pair<BF16>(r[4 * i + 3], s_hi);
               }
@@ -290,6 +291,25 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
         __syncwarp();
         if (lane == 0) mbar_arrive(w_full(s));
         if (++s == kW4Ops) { s = 0; ph ^= 1; }
+      };
+      // the next record is read while one is expanded
+      Rec r0, r1;
+      int b = b0, dead = 0;
+      auto step = [&](const Rec &now, Rec &then) {
+        dead = *s_abort;
+        give_back();
+        if (b + 1 < b1) take(then);
+        wait(w_empty(s), ph);
+        tc_fence_after();
+        expand(now);
+        ++b;
+      };
+      take(r0);
+      while (true) {
+        step(r0, r1);
+        if (b >= b1 || dead) break;
+        step(r1, r0);
+        if (b >= b1 || dead) break;
       }
     }
   }
@@ -366,14 +386,19 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
       if (cluster == 1) {
         const float bias = a.bias && n < g.n ? to_float<BF16>(a.bias[n]) : 0.f;
         const bool store = n < g.n && !*s_abort;
+        using Out = std::conditional_t<EXACT, float, uint16_t>;
+        Out *out = static_cast<Out *>(a.y) + (long long)tok0 * a.y_stride + n;
 #pragma unroll 1
-        for (int c = 0; c < n_tok; c += 8) {
-          uint32_t v[8];
-          tmem_ld8(out_tmem + c, v);
+        for (int c = 0; c < n_tok; c += 16) {
+          uint32_t v[16];
+          tmem_ld16(out_tmem + c, v);
           tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (store && c + j < n_tok) w4_put<BF16>(a, tok0 + c + j, n, __uint_as_float(v[j]) + bias);
+          for (int j = 0; j < 16; ++j, out += a.y_stride)
+            if (store && c + j < n_tok) {
+              const float sum = __uint_as_float(v[j]) + bias;
+              if constexpr (EXACT) *out = sum; else *out = from_float<BF16>(sum);
+            }
         }
       } else {
         // (one unit a cluster) token c of the tile goes to block c / share, where its sums stand [block][token][row]
