@@ -104,6 +104,18 @@ cudaError_t launch_w4(const ft_dense *h, const W4Args &a, bool zero, cudaStream_
   }
 }
 
+// A row to a cluster of blocks of 512 threads while two a SM take them all, as many as leave a thread some pieces; many rows to smaller blocks,
+// whose ends overlap with the others' passes; short rows to the smallest.
+template <int TY>
+cudaError_t launch_logprobs(const ft_dense *h, const LogpArgs &a, cudaStream_t st) {
+  const long long pieces = a.vocab / LogpType<TY>::kVec, places = 2ll * h->sm_count;
+  if (pieces <= 1024 && a.T > h->sm_count) return launch(logprobs_kernel<TY, 128>, dim3((unsigned)a.T), 128, 0, st, a, 1);
+  if (a.T > places) return launch(logprobs_kernel<TY, 256>, dim3((unsigned)a.T), 256, 0, st, a, 1);
+  int cluster = 1;
+  while (cluster < kLogpCluster && 2ll * a.T * cluster <= places && pieces >= 1024 * cluster) cluster *= 2;
+  return launch_clusters(logprobs_kernel<TY, 512>, dim3((unsigned)a.T * cluster), 512, 0, cluster, st, a, cluster);
+}
+
 constexpr int kMaxSmem = 227 * 1024;
 
 template <bool BF16, int G, bool ZERO>
@@ -298,13 +310,9 @@ ft_status_t ft_dense_logprobs(ft_dense_t *h, int T, int64_t vocab, int dtype, co
   a.tokens = given ? tokens : nullptr; a.tokens_stride = tokens_stride;
   a.logprob = logprob; a.entropy = entropy; a.top_logprobs = top_logprobs; a.top_ids = top_ids;
   a.status = h->status_dev;
-  int cluster = 1;
-  while (cluster < kLogpCluster && (long long)T * cluster * 2 <= 2ll * h->sm_count && vocab >= 8192ll * cluster) cluster *= 2;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const dim3 grid((unsigned)T * cluster);
-  FD_CUDA(dtype == FT_DENSE_BF16   ? launch_clusters(logprobs_kernel<kLogpBf16>, grid, kLogpThreads, 0, cluster, st, a, cluster)
-          : dtype == FT_DENSE_FP16 ? launch_clusters(logprobs_kernel<kLogpFp16>, grid, kLogpThreads, 0, cluster, st, a, cluster)
-                                   : launch_clusters(logprobs_kernel<kLogpFp32>, grid, kLogpThreads, 0, cluster, st, a, cluster));
+  FD_CUDA(dtype == FT_DENSE_BF16   ? launch_logprobs<kLogpBf16>(h, a, static_cast<cudaStream_t>(stream))
+          : dtype == FT_DENSE_FP16 ? launch_logprobs<kLogpFp16>(h, a, static_cast<cudaStream_t>(stream))
+                                   : launch_logprobs<kLogpFp32>(h, a, static_cast<cudaStream_t>(stream)));
   h->launches += 1;
   return FT_OK;
 }

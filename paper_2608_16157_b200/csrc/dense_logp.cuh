@@ -1,11 +1,12 @@
 // Log probabilities of given tokens, entropy and the most likely alternatives of rows of logits, in one pass over them.
 // Bound: HBM (T x vocab logits read once); for few rows launch and the chain load -> exponentials -> join.
-//   l = c x;  S = sum 2^((x - m) c log2 e),  U = sum of the same times its exponent;  lse and entropy follow from S, U and m
-// A cluster of blocks shares a row while there are fewer rows than SMs.  Every thread walks over its 16-byte pieces of the row with a
-// running maximum m, S and U of its own (rescaled only where a piece brings a new maximum), which are joined at the end in a fixed
-// order.  The maxima also find the alternatives: the k-th largest of the threads' maxima is a lower bound of the k-th largest logit, so
-// only threads whose maximum reaches it (k of them, and ties) read their pieces again, from L2, and keep what reaches it.  The main
-// loop thus does nothing for them.  Candidates are ranked by counting, as keys (logit, then lowest id).
+//   t = x c - r in units of log 2 (c with log2 e in it);  S = sum 2^t,  U = sum 2^t t;  lse and entropy follow from S, U and r
+// A cluster of blocks shares a row while there are fewer rows than places for blocks.  Every thread walks over its 16-byte pieces of the row,
+// four at a time, with a reference r = its running maximum times c, S and U of its own, which are rescaled only where four pieces bring a new
+// maximum, and joined at the end in a fixed order.  The maxima also find the alternatives: the k-th largest of the threads' maxima is a lower
+// bound of the k-th largest logit, so only threads whose maximum reaches it (k of them, and ties) look into their pieces again, and of these
+// only into those fours whose maximum, kept in 16 bits, reaches it.  The main loop thus does next to nothing for them.  Candidates are
+// ranked by counting, as keys (logit, then lowest id).
 #pragma once
 #include "async.cuh"
 #include "cluster.cuh"
@@ -13,7 +14,7 @@
 
 namespace ftmoe {
 
-constexpr int kLogpThreads = 512, kLogpWarps = kLogpThreads / 32, kLogpTop = 32, kLogpCluster = 8;
+constexpr int kLogpTop = 32, kLogpCluster = 8, kLogpMarks = 32;
 
 struct LogpArgs {
   const void *logits;
@@ -31,25 +32,56 @@ enum { kLogpBf16 = 0, kLogpFp16 = 1, kLogpFp32 = 2 };
 template <int TY>
 struct LogpType {
   static constexpr int kBytes = TY == kLogpFp32 ? 4 : 2, kVec = 16 / kBytes;     // elements of a 16-byte piece
+  // What a -infinity is raised to, so that 0 times an exponent is 0.
+  static __device__ __forceinline__ float floor_value() { return TY == kLogpFp16 ? -65504.f : -1.0141204801825835e30f; }   // (-2^99.68: bf16 0xf14d)
+  static __device__ __forceinline__ uint32_t floor_bits() { return TY == kLogpFp16 ? 0xfbfffbffu : TY == kLogpBf16 ? 0xf14df14du : 0xf14d0000u; }
   static __device__ __forceinline__ float at(const void *p, long long i) {
     if (TY == kLogpFp32) return static_cast<const float *>(p)[i];
     const uint16_t v = static_cast<const uint16_t *>(p)[i];
     return TY == kLogpBf16 ? bf16_bits_to_float(v) : __half2float(__ushort_as_half(v));
   }
+  // Largest of the words' elements; a NaN among other values does not count.
+  static __device__ __forceinline__ uint32_t max_word(uint32_t a, uint32_t b) {
+    uint32_t d;
+    if (TY == kLogpFp32) asm("max.f32 %0, %1, %2;" : "=f"(reinterpret_cast<float &>(d)) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)));
+    else if (TY == kLogpBf16) asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    else asm("max.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+  }
+  static __device__ __forceinline__ float max_of(uint32_t w) {
+    float x, y;
+    split(w, x, y);
+    return TY == kLogpFp32 ? x : fmaxf(x, y);
+  }
+  // The same with a NaN counting above all.
+  static __device__ __forceinline__ uint32_t max_nan(uint32_t a, uint32_t b) {
+    uint32_t d;
+    if (TY == kLogpFp32) asm("max.NaN.f32 %0, %1, %2;" : "=f"(reinterpret_cast<float &>(d)) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)));
+    else if (TY == kLogpBf16) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+  }
+  static __device__ __forceinline__ uint32_t raise_word(uint32_t a) { return max_nan(a, floor_bits()); }
+  static __device__ __forceinline__ void split(uint32_t w, float &x, float &y) {
+    if constexpr (TY == kLogpFp32) {
+      x = y = __uint_as_float(w);
+    } else if constexpr (TY == kLogpBf16) {
+      x = __uint_as_float(w << 16);
+      y = __uint_as_float(w & 0xffff0000u);
+    } else {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+      x = f.x;
+      y = f.y;
+    }
+  }
   static __device__ __forceinline__ void unpack(const uint4 &v, float (&x)[kVec]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if constexpr (TY == kLogpFp32) {
-        x[i] = __uint_as_float(w[i]);
-      } else if constexpr (TY == kLogpBf16) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      } else {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
-        x[2 * i] = f.x;
-        x[2 * i + 1] = f.y;
-      }
+      float lo, hi;
+      split(w[i], lo, hi);
+      x[i * kVec / 4] = lo;
+      if (TY != kLogpFp32) x[i * kVec / 4 + kVec / 4 - 1] = hi;
     }
   }
 };
@@ -67,41 +99,39 @@ __device__ __forceinline__ uint32_t logp_order(float x) {
 }
 __device__ __forceinline__ float logp_value(uint32_t o) { return __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o); }
 
-// Running maximum, sum and weighted sum of exponents; m starts at the lowest finite value, so that x - m is never infinity - infinity
-// for a -infinity.
+// Of some logits: the largest, m, and the sums of 2^t and 2^t t with t = x c2 - (m c2 + del); del is what the product m c2 lost when it was
+// rounded, so that sums with different references can be joined exactly.  m = -infinity: none yet (s then is 0, or NaN).
 struct LogpAcc {
-  float m = -3.402823466e38f, s = 0.f, u = 0.f;
-  __device__ __forceinline__ void raise(float to, float c2) {     // to > m
-    const float d = (m - to) * c2;
-    if (d < -200.f) {
-      if (!(s != s)) s = 0.f;
+  float m = -INFINITY, del = 0.f, s = 0.f, u = 0.f;
+  __device__ __forceinline__ void rescale(float to_m, float to_del, float c2) {
+    const float d = fmaf(m - to_m, c2, del - to_del);
+    if (!(d >= -200.f)) {                 // (-infinity and NaN too: what there is, a NaN stays)
+      if (s == s) s = 0.f;
       u = 0.f;
     } else {
       const float f = exp2_approx(d);
       u = f * fmaf(d, s, u);
       s *= f;
     }
-    m = to;
-  }
-  __device__ __forceinline__ void add(float x, float c2) {
-    const float t = (x - m) * c2, e = exp2_approx(t);
-    s += e;
-    u = fmaf(e, fmaxf(t, -1000.f), u);       // (0 times -infinity)
+    m = to_m;
+    del = to_del;
   }
   __device__ __forceinline__ void join(LogpAcc o, float c2) {
-    if (o.m > m) raise(o.m, c2);
-    else if (m > o.m) o.raise(m, c2);
+    if (o.m > m) rescale(o.m, o.del, c2);
+    else o.rescale(m, del, c2);
     s += o.s;
     u += o.u;
   }
 };
 
+template <int WARPS>
 struct LogpSmem {
-  float m[kLogpWarps], s[kLogpWarps], u[kLogpWarps];
-  uint32_t best[kLogpWarps][32];                       // the threads' maxima, sorted descending, per warp
+  float acc[4][WARPS];
+  uint32_t best[WARPS][32];                            // the threads' maxima, sorted descending, per warp
+  uint16_t mark[kLogpMarks][WARPS * 32];               // maxima of a thread's fours, as the upper half of logp_order
   uint64_t key[kLogpCluster * kLogpTop];               // block 0 of the cluster: candidates of all blocks
-  uint64_t own[kLogpWarps * kLogpTop];
-  float part[kLogpCluster][3];
+  uint64_t own[WARPS * kLogpTop];
+  float part[kLogpCluster][4];
   uint32_t n_own, n_all, tau;
 };
 
@@ -136,11 +166,11 @@ __device__ __forceinline__ uint32_t add_cluster_u32(uint32_t addr, uint32_t v) {
   return old;
 }
 
-template <int TY>
-__global__ void __launch_bounds__(kLogpThreads, 2) logprobs_kernel(const LogpArgs a, const int cluster) {
+template <int TY, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprobs_kernel(const LogpArgs a, const int cluster) {
   using Y = LogpType<TY>;
-  constexpr int E = Y::kVec;
-  __shared__ LogpSmem sm;
+  constexpr int E = Y::kVec, kWarps = THREADS / 32, kAhead = 4;
+  __shared__ LogpSmem<kWarps> sm;
   grid_let_next();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = blockIdx.x % cluster;
@@ -163,43 +193,103 @@ __global__ void __launch_bounds__(kLogpThreads, 2) logprobs_kernel(const LogpArg
     tok = a.tokens[row * a.tokens_stride + tid];
     if (tok >= 0 && tok < a.vocab) x_tok = Y::at(base, tok);
   }
+  // `plain`: exponents in one instruction from the rounded product ref = m c2, -infinities at the floor; not while the maximum is so small or the
+  // scale so large that the floor would count, or a product overflow
   LogpAcc acc;
+  float ref = 0.f;
+  bool plain = false;
+  auto raise = [&](float to) {
+    plain = fabsf(to) < 1e29f && c2 < 1e8f && (Y::floor_value() - to) * c2 < -200.f;
+    ref = plain ? to * c2 : 0.f;
+    acc.rescale(to, plain ? -fmaf(to, c2, -ref) : 0.f, c2);
+  };
+  auto add_one = [&](float x) {                  // any x, not above the maximum
+    if (x == -INFINITY) return;
+    const float t = plain ? fmaf(x, c2, -ref) : (x - acc.m) * c2, e = exp2_approx(t);
+    acc.s += e;
+    acc.u = fmaf(e, fmaxf(t, -1000.f), acc.u);
+  };
+  auto add_word = [&](uint32_t w) {              // plain
+    float x, y;
+    Y::split(Y::raise_word(w), x, y);
+    const float t = fmaf(x, c2, -ref), e = exp2_approx(t);
+    acc.s += e;
+    acc.u = fmaf(e, t, acc.u);
+    if (TY != kLogpFp32) {
+      const float t2 = fmaf(y, c2, -ref), e2 = exp2_approx(t2);
+      acc.s += e2;
+      acc.u = fmaf(e2, t2, acc.u);
+    }
+  };
   auto edge_index = [&](int i) { return i < head ? i : n_vec * E + i; };
   const bool has_edge = rank == 0 && tid < edge;
   const float x_edge = has_edge ? Y::at(base, edge_index(tid)) : -INFINITY;
   if (has_edge) {
-    if (x_edge > acc.m) acc.raise(x_edge, c2);
-    acc.add(x_edge, c2);
+    if (x_edge > acc.m) raise(x_edge);
+    add_one(x_edge);
   }
-  auto take = [&](const uint4 &v) {
-    float x[E];
-    Y::unpack(v, x);
-    float mx = x[0];
+  // fours of pieces; several fours to a mark where a thread has many
+  const int fours = (v1 - v0 + kAhead * THREADS - 1) / (kAhead * THREADS);
+  int shift = 0;
+  while ((fours - 1) >> shift >= kLogpMarks) ++shift;
+  auto take = [&](const uint4 (&q)[kAhead], int four) {
+    uint32_t mx = Y::max_word(Y::max_word(q[0].x, q[0].y), Y::max_word(q[0].z, q[0].w));
 #pragma unroll
-    for (int i = 1; i < E; ++i) mx = fmaxf(mx, x[i]);
-    if (mx > acc.m) acc.raise(mx, c2);
+    for (int i = 1; i < kAhead; ++i) mx = Y::max_word(mx, Y::max_word(Y::max_word(q[i].x, q[i].y), Y::max_word(q[i].z, q[i].w)));
+    const float top = Y::max_of(mx);
+    if (a.top_k > 0) {
+      const uint16_t now = (uint16_t)(logp_order(top) >> 16);
+      uint16_t &mark = sm.mark[four >> shift][tid];
+      mark = (four & ((1 << shift) - 1)) == 0 || now > mark ? now : mark;
+    }
+    if (top > acc.m) raise(top);
+    if (plain) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) acc.add(x[i], c2);
+      for (int i = 0; i < kAhead; ++i) { add_word(q[i].x); add_word(q[i].y); add_word(q[i].z); add_word(q[i].w); }
+    } else if (acc.m == -INFINITY) {             // nothing but -infinities, or NaN among them
+      uint32_t any = 0xff800000u;
+      if (TY == kLogpBf16) any = 0xff80ff80u;
+      if (TY == kLogpFp16) any = 0xfc00fc00u;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) any = Y::max_nan(Y::max_nan(any, Y::max_nan(q[i].x, q[i].y)), Y::max_nan(q[i].z, q[i].w));
+      float x, y;
+      Y::split(any, x, y);
+      if (x != x || y != y) acc.s = NAN;
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < kAhead * 4; ++i) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) w = i == 4 * j ? q[j].x : i == 4 * j + 1 ? q[j].y : i == 4 * j + 2 ? q[j].z : i == 4 * j + 3 ? q[j].w : w;
+        float x, y;
+        Y::split(w, x, y);
+        add_one(x);
+        if (TY != kLogpFp32) add_one(y);
+      }
+    }
   };
-  constexpr int kAhead = 4;
-  int v = v0 + tid;
-  for (; v + (kAhead - 1) * kLogpThreads < v1; v += kAhead * kLogpThreads) {
+  constexpr uint32_t kNone = TY == kLogpFp32 ? 0xff800000u : TY == kLogpBf16 ? 0xff80ff80u : 0xfc00fc00u;      // -infinities
+  auto load = [&](uint4 (&q)[kAhead], int four, bool on) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int v = v0 + (four * kAhead + i) * THREADS + tid;
+      q[i] = make_uint4(kNone, kNone, kNone, kNone);
+      if (on && v < v1) q[i] = vec[v];
+    }
+  };
+  for (int f = 0; f < fours; ++f) {
     uint4 q[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) q[i] = vec[v + i * kLogpThreads];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) take(q[i]);
+    load(q, f, true);
+    take(q, f);
   }
-  for (; v < v1; v += kLogpThreads) take(vec[v]);
 
   // alternatives: the k-th largest of the threads' maxima
-  const bool seen = acc.s > 0.f || acc.s != acc.s;
-  const uint32_t mine = seen ? logp_order(acc.m) : 0u;
+  const uint32_t mine = logp_order(acc.m);
   if (a.top_k > 0) {
     uint32_t b = warp_sort(mine, lane);
     sm.best[warp][lane] = b;
 #pragma unroll
-    for (int n = 1; n < kLogpWarps; n *= 2) {
+    for (int n = 1; n < kWarps; n *= 2) {
       __syncthreads();
       if ((warp & (2 * n - 1)) == 0) {
         b = warp_merge(b, sm.best[warp + n][31 - lane], lane);
@@ -229,58 +319,74 @@ __global__ void __launch_bounds__(kLogpThreads, 2) logprobs_kernel(const LogpArg
         }
       };
       keep(x_edge, has_edge ? edge_index(tid) : 0, has_edge && again);
-      for (int w = v0 + warp * 32; w < v1; w += kLogpThreads) {
-        const int p = w + lane;
-        const bool ok = again && p < v1;
-        float x[E];
-        if (ok) Y::unpack(vec[p], x);
-        else
+      const int marks = fours > 0 ? ((fours - 1) >> shift) + 1 : 0;
+      for (int k = 0; k < marks; ++k) {
+        const bool on = again && sm.mark[k][tid] >= (uint16_t)(tau >> 16);
+        if (!__any_sync(0xffffffffu, on)) continue;
+        for (int f = k << shift; f < min(fours, (k + 1) << shift); ++f) {
+          uint4 q[kAhead];
+          load(q, f, on);
+#pragma unroll 1
+          for (int i = 0; i < kAhead; ++i) {
+            const uint4 p = i == 0 ? q[0] : i == 1 ? q[1] : i == 2 ? q[2] : q[3];
+            float x[E];
+            Y::unpack(p, x);
+            float mx = x[0];
 #pragma unroll
-          for (int i = 0; i < E; ++i) x[i] = -INFINITY;
-        float mx = x[0];
+            for (int j = 1; j < E; ++j) mx = fmaxf(mx, x[j]);
+            if (!__any_sync(0xffffffffu, logp_order(mx) >= tau)) continue;
+            const int id = head + (v0 + (f * kAhead + i) * THREADS + tid) * E;
+#pragma unroll 1
+            for (int j = 0; j < E; ++j) {
+              float xj = x[0];
 #pragma unroll
-        for (int i = 1; i < E; ++i) mx = fmaxf(mx, x[i]);
-        if (!__any_sync(0xffffffffu, ok && logp_order(mx) >= tau)) continue;
-#pragma unroll
-        for (int i = 0; i < E; ++i) keep(x[i], head + p * E + i, ok);
+              for (int l = 1; l < E; ++l) xj = j == l ? x[l] : xj;
+              keep(xj, id + j, on);
+            }
+          }
+        }
       }
       const bool have = lane < a.top_k && list != 0;
-      const uint32_t m = __ballot_sync(0xffffffffu, have);
+      const uint32_t mask = __ballot_sync(0xffffffffu, have);
       uint32_t at = 0;
-      if (lane == 0) at = atomicAdd(&sm.n_own, (uint32_t)__popc(m));
+      if (lane == 0) at = atomicAdd(&sm.n_own, (uint32_t)__popc(mask));
       at = __shfl_sync(0xffffffffu, at, 0);
       if (have) sm.own[at + lane] = list;
     }
   }
 
   // join of the block's sums
+  auto join_lanes = [&](LogpAcc &x, int half) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    LogpAcc other;
-    other.m = __shfl_down_sync(0xffffffffu, acc.m, o);
-    other.s = __shfl_down_sync(0xffffffffu, acc.s, o);
-    other.u = __shfl_down_sync(0xffffffffu, acc.u, o);
-    acc.join(other, c2);
-  }
-  if (lane == 0) { sm.m[warp] = acc.m; sm.s[warp] = acc.s; sm.u[warp] = acc.u; }
+    for (int o = 16; o > 0; o >>= 1) {
+      if (o > half) continue;
+      LogpAcc other;
+      other.m = __shfl_down_sync(0xffffffffu, x.m, o);
+      other.del = __shfl_down_sync(0xffffffffu, x.del, o);
+      other.s = __shfl_down_sync(0xffffffffu, x.s, o);
+      other.u = __shfl_down_sync(0xffffffffu, x.u, o);
+      x.join(other, c2);
+    }
+  };
+  join_lanes(acc, 16);
+  if (lane == 0) { sm.acc[0][warp] = acc.m; sm.acc[1][warp] = acc.del; sm.acc[2][warp] = acc.s; sm.acc[3][warp] = acc.u; }
   __syncthreads();
   // to block 0 of the cluster: the block's sums, and of its candidates the k best
   if (cluster > 1) cluster_wait();
   auto lead = [&](const void *p) { return cluster > 1 ? mapa_u32(smem_u32(p), 0) : smem_u32(p); };
-  if (tid == 0) {
+  if (warp == 0) {
     LogpAcc all;
-    all.m = sm.m[0]; all.s = sm.s[0]; all.u = sm.u[0];
-    for (int w = 1; w < kLogpWarps; ++w) {
-      LogpAcc o;
-      o.m = sm.m[w]; o.s = sm.s[w]; o.u = sm.u[w];
-      all.join(o, c2);
+    if (lane < kWarps) { all.m = sm.acc[0][lane]; all.del = sm.acc[1][lane]; all.s = sm.acc[2][lane]; all.u = sm.acc[3][lane]; }
+    join_lanes(all, kWarps / 2);
+    if (lane == 0) {
+      st_cluster_f32(lead(&sm.part[rank][0]), all.m);
+      st_cluster_f32(lead(&sm.part[rank][1]), all.del);
+      st_cluster_f32(lead(&sm.part[rank][2]), all.s);
+      st_cluster_f32(lead(&sm.part[rank][3]), all.u);
     }
-    st_cluster_f32(lead(&sm.part[rank][0]), all.m);
-    st_cluster_f32(lead(&sm.part[rank][1]), all.s);
-    st_cluster_f32(lead(&sm.part[rank][2]), all.u);
   }
   const int n_own = a.top_k > 0 ? (int)sm.n_own : 0;
-  for (int i = tid; i < n_own; i += kLogpThreads) {
+  for (int i = tid; i < n_own; i += THREADS) {
     const uint64_t k = sm.own[i];
     int above = 0;
     for (int j = 0; j < n_own; ++j) above += sm.own[j] > k;
@@ -289,21 +395,22 @@ __global__ void __launch_bounds__(kLogpThreads, 2) logprobs_kernel(const LogpArg
   if (cluster > 1) cluster_sync_all(); else __syncthreads();
   if (rank != 0) return;
 
+  // every thread joins the cluster's sums, in the same order
   LogpAcc all;
-  all.m = sm.part[0][0]; all.s = sm.part[0][1]; all.u = sm.part[0][2];
+  all.m = sm.part[0][0]; all.del = sm.part[0][1]; all.s = sm.part[0][2]; all.u = sm.part[0][3];
   for (int r = 1; r < cluster; ++r) {
     LogpAcc o;
-    o.m = sm.part[r][0]; o.s = sm.part[r][1]; o.u = sm.part[r][2];
+    o.m = sm.part[r][0]; o.del = sm.part[r][1]; o.s = sm.part[r][2]; o.u = sm.part[r][3];
     all.join(o, c2);
   }
   constexpr float kLn2 = 0.693147180559945f;
   const bool bad = !(all.s < INFINITY), none = all.s == 0.f;
-  const float log2_s = log2f(all.s);
-  auto logprob = [&](float x) { return bad ? NAN : none ? -INFINITY : (x - all.m) * a.scale - log2_s * kLn2; };
+  const float log2_s = log2f(all.s), rest = (log2_s + all.del) * kLn2;
+  auto logprob = [&](float x) { return bad ? NAN : none ? -INFINITY : fmaf(x - all.m, a.scale, -rest); };
   if (tid == 0 && a.entropy) a.entropy[row] = bad ? NAN : none ? 0.f : fmaxf((log2_s - all.u / all.s) * kLn2, 0.f);
   if (a.tokens)
-    for (int i = tid; i < a.n_tokens; i += kLogpThreads) {
-      if (i >= kLogpThreads) {
+    for (int i = tid; i < a.n_tokens; i += THREADS) {
+      if (i >= THREADS) {
         tok = a.tokens[row * a.tokens_stride + i];
         if (tok >= 0 && tok < a.vocab) x_tok = Y::at(base, tok);
       }
@@ -314,7 +421,7 @@ __global__ void __launch_bounds__(kLogpThreads, 2) logprobs_kernel(const LogpArg
     }
   if (a.top_k > 0) {
     const int n = (int)sm.n_all;
-    for (int i = tid; i < n; i += kLogpThreads) {
+    for (int i = tid; i < n; i += THREADS) {
       const uint64_t k = sm.key[i];
       int above = 0;
       for (int j = 0; j < n; ++j) above += sm.key[j] > k;
