@@ -104,16 +104,16 @@ cudaError_t launch_w4(const ft_dense *h, const W4Args &a, bool zero, cudaStream_
   }
 }
 
-// A row to a cluster of blocks of 512 threads while two a SM take them all, as many as leave a thread some pieces; many rows to smaller blocks,
+// A row to a cluster of blocks of 512 threads while one a SM takes them all, as many as leave a thread some pieces; more rows to smaller blocks,
 // whose ends overlap with the others' passes; short rows to the smallest.
 template <int TY>
 cudaError_t launch_logprobs(const ft_dense *h, const LogpArgs &a, cudaStream_t st) {
-  const long long pieces = a.vocab / LogpType<TY>::kVec, places = 2ll * h->sm_count;
-  if (pieces <= 1024 && a.T > h->sm_count) return launch(logprobs_kernel<TY, 128>, dim3((unsigned)a.T), 128, 0, st, a, 1);
-  if (a.T > places) return launch(logprobs_kernel<TY, 256>, dim3((unsigned)a.T), 256, 0, st, a, 1);
+  const long long pieces = a.vocab / LogpType<TY>::kVec, places = h->sm_count;
+  if (pieces <= 1024 && a.T > places) return launch(logprobs_kernel<TY, 128>, dim3((unsigned)a.T), 128, sizeof(LogpSmem<4>), st, a, 1);
+  if (a.T > places) return launch(logprobs_kernel<TY, 256>, dim3((unsigned)a.T), 256, sizeof(LogpSmem<8>), st, a, 1);
   int cluster = 1;
   while (cluster < kLogpCluster && 2ll * a.T * cluster <= places && pieces >= 1024 * cluster) cluster *= 2;
-  return launch_clusters(logprobs_kernel<TY, 512>, dim3((unsigned)a.T * cluster), 512, 0, cluster, st, a, cluster);
+  return launch_clusters(logprobs_kernel<TY, 512>, dim3((unsigned)a.T * cluster), 512, sizeof(LogpSmem<16>), cluster, st, a, cluster);
 }
 
 constexpr int kMaxSmem = 227 * 1024;
@@ -133,6 +133,11 @@ cudaError_t allow_smem() {
   if (e == cudaSuccess) e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZERO, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZERO, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
   return e;
+}
+
+template <int TY>
+cudaError_t allow_smem_logprobs() {
+  return cudaFuncSetAttribute(logprobs_kernel<TY, 512>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(LogpSmem<16>));
 }
 
 // How many clusters of a size run at once when each block takes an SM (the SMs of a cluster stand together, so not all are used).
@@ -182,6 +187,9 @@ ft_status_t ft_dense_create(int device, ft_dense_t **out) {
   if (e == cudaSuccess) e = allow_smem<true, false>();
   if (e == cudaSuccess) e = allow_smem<false, true>();
   if (e == cudaSuccess) e = allow_smem<false, false>();
+  if (e == cudaSuccess) e = allow_smem_logprobs<kLogpBf16>();
+  if (e == cudaSuccess) e = allow_smem_logprobs<kLogpFp16>();
+  if (e == cudaSuccess) e = allow_smem_logprobs<kLogpFp32>();
   if (e == cudaSuccess) e = count_clusters(h);
   if (e == cudaSuccess && (!h->encode || found != cudaDriverEntryPointSuccess)) e = cudaErrorNotSupported;
   if (e != cudaSuccess) {

@@ -5,12 +5,14 @@
 // four at a time, with a reference r = its running maximum times c, S and U of its own, which are rescaled only where four pieces bring a new
 // maximum, and joined at the end in a fixed order.  The maxima also find the alternatives: the k-th largest of the threads' maxima is a lower
 // bound of the k-th largest logit, so only threads whose maximum reaches it (k of them, and ties) look into their pieces again, and of these
-// only into those fours whose maximum, kept in 16 bits, reaches it.  The main loop thus does next to nothing for them.  Candidates are
-// ranked by counting, as keys (logit, then lowest id).
+// only into those fours whose maximum, kept in 16 bits, reaches it.  The four with a thread's maximum waits in shared memory (read again from
+// global memory it took 2.4 us a row, the rows under way being more than L2 holds).  The main loop thus does next to nothing for them.
+// Candidates are ranked by counting, as keys (logit, then lowest id).
 #pragma once
 #include "async.cuh"
 #include "cluster.cuh"
 #include "common.cuh"
+#include "float2.cuh"
 
 namespace ftmoe {
 
@@ -128,6 +130,7 @@ template <int WARPS>
 struct LogpSmem {
   float acc[4][WARPS];
   uint32_t best[WARPS][32];                            // the threads' maxima, sorted descending, per warp
+  uint4 four[4][WARPS * 32];                           // the thread's four with its maximum
   uint16_t mark[kLogpMarks][WARPS * 32];               // maxima of a thread's fours, as the upper half of logp_order
   uint64_t key[kLogpCluster * kLogpTop];               // block 0 of the cluster: candidates of all blocks
   uint64_t own[WARPS * kLogpTop];
@@ -167,10 +170,11 @@ __device__ __forceinline__ uint32_t add_cluster_u32(uint32_t addr, uint32_t v) {
 }
 
 template <int TY, int THREADS>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprobs_kernel(const LogpArgs a, const int cluster) {
+__global__ void __launch_bounds__(THREADS, 768 / THREADS) logprobs_kernel(const LogpArgs a, const int cluster) {
   using Y = LogpType<TY>;
   constexpr int E = Y::kVec, kWarps = THREADS / 32, kAhead = 4;
-  __shared__ LogpSmem<kWarps> sm;
+  extern __shared__ __align__(16) unsigned char smem[];
+  LogpSmem<kWarps> &sm = *reinterpret_cast<LogpSmem<kWarps> *>(smem);
   grid_let_next();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = blockIdx.x % cluster;
@@ -209,17 +213,14 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprobs_kernel(const
     acc.s += e;
     acc.u = fmaf(e, fmaxf(t, -1000.f), acc.u);
   };
-  auto add_word = [&](uint32_t w) {              // plain
-    float x, y;
-    Y::split(Y::raise_word(w), x, y);
-    const float t = fmaf(x, c2, -ref), e = exp2_approx(t);
-    acc.s += e;
-    acc.u = fmaf(e, t, acc.u);
-    if (TY != kLogpFp32) {
-      const float t2 = fmaf(y, c2, -ref), e2 = exp2_approx(t2);
-      acc.s += e2;
-      acc.u = fmaf(e2, t2, acc.u);
-    }
+  // plain: two logits at a time, in packed arithmetic
+  auto add_pair = [&](float x, float y, uint64_t c22, uint64_t ref2, uint64_t &s2, uint64_t &u2) {
+    const uint64_t t = fma2(f2(x, y), c22, ref2);
+    float t0, t1;
+    f2_split(t, t0, t1);
+    const uint64_t e = f2(exp2_approx(t0), exp2_approx(t1));
+    s2 = add2(s2, e);
+    u2 = fma2(e, t, u2);
   };
   auto edge_index = [&](int i) { return i < head ? i : n_vec * E + i; };
   const bool has_edge = rank == 0 && tid < edge;
@@ -232,6 +233,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprobs_kernel(const
   const int fours = (v1 - v0 + kAhead * THREADS - 1) / (kAhead * THREADS);
   int shift = 0;
   while ((fours - 1) >> shift >= kLogpMarks) ++shift;
+  int best_four = -1;
   auto take = [&](const uint4 (&q)[kAhead], int four) {
     uint32_t mx = Y::max_word(Y::max_word(q[0].x, q[0].y), Y::max_word(q[0].z, q[0].w));
 #pragma unroll
@@ -239,13 +241,37 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprobs_kernel(const
     const float top = Y::max_of(mx);
     if (a.top_k > 0) {
       const uint16_t now = (uint16_t)(logp_order(top) >> 16);
-      uint16_t &mark = sm.mark[four >> shift][tid];
-      mark = (four & ((1 << shift) - 1)) == 0 || now > mark ? now : mark;
+      if (shift == 0) sm.mark[four][tid] = now;
+      else {
+        uint16_t &mark = sm.mark[four >> shift][tid];
+        mark = (four & ((1 << shift) - 1)) == 0 || now > mark ? now : mark;
+      }
     }
-    if (top > acc.m) raise(top);
-    if (plain) {
+    if (top > acc.m) {
+      raise(top);
+      best_four = four;
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) { add_word(q[i].x); add_word(q[i].y); add_word(q[i].z); add_word(q[i].w); }
+      for (int i = 0; i < kAhead; ++i) sm.four[i][tid] = q[i];
+    }
+    if (plain) {
+      const uint64_t c22 = f2(c2, c2), ref2 = f2(-ref, -ref);
+      uint64_t s2 = f2(acc.s, 0.f), u2 = f2(acc.u, 0.f);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; j += TY == kLogpFp32 ? 2 : 1) {
+          float x, y;
+          Y::split(Y::raise_word(w[j]), x, y);
+          if (TY == kLogpFp32) y = __uint_as_float(Y::raise_word(w[j + 1 < 4 ? j + 1 : j]));
+          add_pair(x, y, c22, ref2, s2, u2);
+        }
+      }
+      float lo, hi;
+      f2_split(s2, lo, hi);
+      acc.s = lo + hi;
+      f2_split(u2, lo, hi);
+      acc.u = lo + hi;
     } else if (acc.m == -INFINITY) {             // nothing but -infinities, or NaN among them
       uint32_t any = 0xff800000u;
       if (TY == kLogpBf16) any = 0xff80ff80u;
@@ -269,18 +295,30 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprobs_kernel(const
     }
   };
   constexpr uint32_t kNone = TY == kLogpFp32 ? 0xff800000u : TY == kLogpBf16 ? 0xff80ff80u : 0xfc00fc00u;      // -infinities
-  auto load = [&](uint4 (&q)[kAhead], int four, bool on) {
+  auto load = [&](uint4 (&q)[kAhead], int four) {
+    if (v0 + (four + 1) * kAhead * THREADS <= v1) {
+      const uint4 *p = vec + v0 + four * kAhead * THREADS + tid;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) q[i] = ld_stream_16(p + i * THREADS);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const int v = v0 + (four * kAhead + i) * THREADS + tid;
       q[i] = make_uint4(kNone, kNone, kNone, kNone);
-      if (on && v < v1) q[i] = vec[v];
+      if (v < v1) q[i] = ld_stream_16(vec + v);
     }
   };
-  for (int f = 0; f < fours; ++f) {
-    uint4 q[kAhead];
-    load(q, f, true);
-    take(q, f);
+  // (the next four are on their way while one is taken)
+  uint4 qa[kAhead], qb[kAhead];
+  if (fours > 0) load(qa, 0);
+  for (int f = 0; f < fours; f += 2) {
+    if (f + 1 < fours) load(qb, f + 1);
+    take(qa, f);
+    if (f + 1 < fours) {
+      if (f + 2 < fours) load(qa, f + 2);
+      take(qb, f + 1);
+    }
   }
 
   // alternatives: the k-th largest of the threads' maxima
@@ -300,58 +338,108 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprobs_kernel(const
     __syncthreads();
     const uint32_t tau = sm.tau;
     const bool again = mine >= tau;
-    if (__any_sync(0xffffffffu, again)) {
-      uint64_t list = 0;                      // lane i: the warp's i-th best key
-      uint64_t least = 0;                     // the k-th best one
-      auto keep = [&](float x, int id, bool ok) {
+    const int marks = fours > 0 ? ((fours - 1) >> shift) + 1 : 0;
+    const uint16_t tau_mark = (uint16_t)(tau >> 16);
+    // as a rule a few more than k reach it: each thread adds its own to the block's list
+    if (again) {
+      bool room = true;
+      auto add = [&](float x, int id) {
         const uint32_t o = logp_order(x);
-        const uint64_t key = ((uint64_t)o << 32) | (0xffffffffu - (uint32_t)id);
-        uint32_t todo = __ballot_sync(0xffffffffu, ok && o >= tau && key > least);
-        while (todo) {
-          const int from = __ffs(todo) - 1;
-          todo &= todo - 1;
-          const uint64_t k = __shfl_sync(0xffffffffu, key, from);
-          if (k <= least) continue;
-          const int pos = __popc(__ballot_sync(0xffffffffu, list > k));
-          const uint64_t up = __shfl_up_sync(0xffffffffu, list, 1);
-          list = lane < pos ? list : lane == pos ? k : up;
-          least = __shfl_sync(0xffffffffu, list, a.top_k - 1);
+        if (o < tau || !room) return;
+        const uint32_t at = atomicAdd(&sm.n_own, 1u);
+        room = at < kWarps * kLogpTop;
+        if (room) sm.own[at] = ((uint64_t)o << 32) | (0xffffffffu - (uint32_t)id);
+      };
+      if (has_edge) add(x_edge, edge_index(tid));
+      auto look = [&](const uint4 (&q)[kAhead], int f) {
+#pragma unroll 1
+        for (int i = 0; i < kAhead; ++i) {
+          const uint4 p = i == 0 ? q[0] : i == 1 ? q[1] : i == 2 ? q[2] : q[3];
+          if (logp_order(Y::max_of(Y::max_word(Y::max_word(p.x, p.y), Y::max_word(p.z, p.w)))) < tau) continue;
+          float x[E];
+          Y::unpack(p, x);
+          const int id = head + (v0 + (f * kAhead + i) * THREADS + tid) * E;
+#pragma unroll
+          for (int j = 0; j < E; ++j) add(x[j], id + j);
         }
       };
-      keep(x_edge, has_edge ? edge_index(tid) : 0, has_edge && again);
-      const int marks = fours > 0 ? ((fours - 1) >> shift) + 1 : 0;
-      for (int k = 0; k < marks; ++k) {
-        const bool on = again && sm.mark[k][tid] >= (uint16_t)(tau >> 16);
-        if (!__any_sync(0xffffffffu, on)) continue;
+      if (best_four >= 0) {                    // (the maximum may stand outside the pieces)
+        uint4 q[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) q[i] = sm.four[i][tid];
+        look(q, best_four);
+      }
+      // (each thread to its own next mark first, so that a warp's loads go out together)
+      for (int k = -1; room;) {
+        while (++k < marks && (sm.mark[k][tid] < tau_mark || (shift == 0 && k == best_four))) {
+        }
+        if (k >= marks) break;
         for (int f = k << shift; f < min(fours, (k + 1) << shift); ++f) {
-          uint4 q[kAhead];
-          load(q, f, on);
+          if (f == best_four) continue;
+          load(qb, f);
+          look(qb, f);
+        }
+      }
+    }
+    __syncthreads();
+    // more of them (many equal logits, say): the warps keep lists of their k best
+    const bool many = sm.n_own > kWarps * kLogpTop;
+    __syncthreads();
+    if (many) {
+      if (tid == 0) sm.n_own = 0;
+      __syncthreads();
+      if (__any_sync(0xffffffffu, again)) {
+        uint64_t list = 0;                      // lane i: the warp's i-th best key
+        uint64_t least = 0;                     // the k-th best one
+        auto keep = [&](float x, int id, bool ok) {
+          const uint32_t o = logp_order(x);
+          const uint64_t key = ((uint64_t)o << 32) | (0xffffffffu - (uint32_t)id);
+          uint32_t todo = __ballot_sync(0xffffffffu, ok && o >= tau && key > least);
+          while (todo) {
+            const int from = __ffs(todo) - 1;
+            todo &= todo - 1;
+            const uint64_t k = __shfl_sync(0xffffffffu, key, from);
+            if (k <= least) continue;
+            const int pos = __popc(__ballot_sync(0xffffffffu, list > k));
+            const uint64_t up = __shfl_up_sync(0xffffffffu, list, 1);
+            list = lane < pos ? list : lane == pos ? k : up;
+            least = __shfl_sync(0xffffffffu, list, a.top_k - 1);
+          }
+        };
+        keep(x_edge, has_edge ? edge_index(tid) : 0, has_edge && again);
+        for (int k = 0; k < marks; ++k) {
+          const bool on = again && sm.mark[k][tid] >= tau_mark;
+          if (!__any_sync(0xffffffffu, on)) continue;
+          for (int f = k << shift; f < min(fours, (k + 1) << shift); ++f) {
+            uint4 q[kAhead];
+            load(q, f);
 #pragma unroll 1
-          for (int i = 0; i < kAhead; ++i) {
-            const uint4 p = i == 0 ? q[0] : i == 1 ? q[1] : i == 2 ? q[2] : q[3];
-            float x[E];
-            Y::unpack(p, x);
-            float mx = x[0];
+            for (int i = 0; i < kAhead; ++i) {
+              const uint4 p = i == 0 ? q[0] : i == 1 ? q[1] : i == 2 ? q[2] : q[3];
+              float x[E];
+              Y::unpack(p, x);
+              float mx = x[0];
 #pragma unroll
-            for (int j = 1; j < E; ++j) mx = fmaxf(mx, x[j]);
-            if (!__any_sync(0xffffffffu, logp_order(mx) >= tau)) continue;
-            const int id = head + (v0 + (f * kAhead + i) * THREADS + tid) * E;
+              for (int j = 1; j < E; ++j) mx = fmaxf(mx, x[j]);
+              if (!__any_sync(0xffffffffu, logp_order(mx) >= tau)) continue;
+              const int id = head + (v0 + (f * kAhead + i) * THREADS + tid) * E;
 #pragma unroll 1
-            for (int j = 0; j < E; ++j) {
-              float xj = x[0];
+              for (int j = 0; j < E; ++j) {
+                float xj = x[0];
 #pragma unroll
-              for (int l = 1; l < E; ++l) xj = j == l ? x[l] : xj;
-              keep(xj, id + j, on);
+                for (int l = 1; l < E; ++l) xj = j == l ? x[l] : xj;
+                keep(xj, id + j, on);
+              }
             }
           }
         }
+        const bool have = lane < a.top_k && list != 0;
+        const uint32_t mask = __ballot_sync(0xffffffffu, have);
+        uint32_t at = 0;
+        if (lane == 0) at = atomicAdd(&sm.n_own, (uint32_t)__popc(mask));
+        at = __shfl_sync(0xffffffffu, at, 0);
+        if (have) sm.own[at + lane] = list;
       }
-      const bool have = lane < a.top_k && list != 0;
-      const uint32_t mask = __ballot_sync(0xffffffffu, have);
-      uint32_t at = 0;
-      if (lane == 0) at = atomicAdd(&sm.n_own, (uint32_t)__popc(mask));
-      at = __shfl_sync(0xffffffffu, at, 0);
-      if (have) sm.own[at + lane] = list;
     }
   }
 
