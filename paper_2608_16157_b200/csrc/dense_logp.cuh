@@ -170,7 +170,7 @@ __device__ __forceinline__ uint32_t add_cluster_u32(uint32_t addr, uint32_t v) {
 }
 
 template <int TY, int THREADS>
-__global__ void __launch_bounds__(THREADS, 768 / THREADS) logprobs_kernel(const LogpArgs a, const int cluster) {
+__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) logprobs_kernel(const LogpArgs a, const int cluster) {
   using Y = LogpType<TY>;
   constexpr int E = Y::kVec, kWarps = THREADS / 32, kAhead = 4;
   extern __shared__ __align__(16) unsigned char smem[];
