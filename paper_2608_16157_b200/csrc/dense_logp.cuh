@@ -3,9 +3,10 @@
 //   t = x c - r in units of log 2 (c with log2 e in it);  S = sum 2^t,  U = sum 2^t t;  lse and entropy follow from S, U and r
 // A cluster of blocks shares a row while there are fewer rows than places for blocks.  Every thread walks over its 16-byte pieces of the row,
 // four at a time, with a reference r = its running maximum times c, S and U of its own, which are rescaled only where four pieces bring a new
-// maximum, and joined at the end in a fixed order.  The maxima also find the alternatives: the k-th largest of the threads' maxima is a lower
-// bound of the k-th largest logit, so only threads whose maximum reaches it (k of them, and ties) look into their pieces again, and of these
-// only into those fours whose maximum, kept in 16 bits, reaches it.  The four with a thread's maximum waits in shared memory (read again from
+// maximum, and joined at the end in a fixed order.  The maxima also find the alternatives: where q warps have j threads each whose maximum
+// reaches a value, and q j >= k, that value is a lower bound of the k-th largest logit (with q and j near the root of k hardly more than k
+// reach it); so only threads whose maximum reaches it look into their pieces again, and of these only into those fours whose maximum, kept
+// in 16 bits, reaches it.  The four with a thread's maximum waits in shared memory (read again from
 // global memory it took 2.4 us a row, the rows under way being more than L2 holds).  The main loop thus does next to nothing for them.
 // Candidates are ranked by counting, as keys (logit, then lowest id).
 #pragma once
@@ -118,50 +119,23 @@ struct LogpAcc {
     m = to_m;
     del = to_del;
   }
-  __device__ __forceinline__ void join(LogpAcc o, float c2) {
-    if (o.m > m) rescale(o.m, o.del, c2);
-    else o.rescale(m, del, c2);
-    s += o.s;
-    u += o.u;
-  }
 };
 
 template <int WARPS>
 struct LogpSmem {
-  float acc[4][WARPS];
-  uint32_t best[WARPS][32];                            // the threads' maxima, sorted descending, per warp
+  uint32_t top[WARPS], nth[WARPS];                     // of the warps' maxima the largest, the j-th largest (logp_order)
+  float sum[2][WARPS];
   uint4 four[4][WARPS * 32];                           // the thread's four with its maximum
   uint16_t mark[kLogpMarks][WARPS * 32];               // maxima of a thread's fours, as the upper half of logp_order
   uint64_t key[kLogpCluster * kLogpTop];               // block 0 of the cluster: candidates of all blocks
   uint64_t own[WARPS * kLogpTop];
-  float part[kLogpCluster][4];
-  uint32_t n_own, n_all, tau;
+  float part[kLogpCluster][2];                         // and of all blocks: sums, maxima
+  uint32_t part_top[kLogpCluster];
+  uint32_t n_own, n_all;
 };
 
-// Sorts a value per lane, descending.
-__device__ __forceinline__ uint32_t warp_sort(uint32_t v, int lane) {
-#pragma unroll
-  for (int k = 2; k <= 32; k *= 2)
-#pragma unroll
-    for (int j = k / 2; j > 0; j /= 2) {
-      const uint32_t o = __shfl_xor_sync(0xffffffffu, v, j);
-      const bool keep_max = ((lane & k) == 0) == ((lane & j) == 0);
-      v = keep_max ? max(v, o) : min(v, o);
-    }
-  return v;
-}
-// Of two descending lists the 32 largest, descending.
-__device__ __forceinline__ uint32_t warp_merge(uint32_t a, uint32_t b_reversed, int lane) {
-  uint32_t v = max(a, b_reversed);
-#pragma unroll
-  for (int j = 16; j > 0; j /= 2) {
-    const uint32_t o = __shfl_xor_sync(0xffffffffu, v, j);
-    v = (lane & j) == 0 ? max(v, o) : min(v, o);
-  }
-  return v;
-}
-
 __device__ __forceinline__ void st_cluster_u64(uint32_t addr, uint64_t v) { asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory"); }
+__device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
 __device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
 __device__ __forceinline__ uint32_t add_cluster_u32(uint32_t addr, uint32_t v) {
   uint32_t old;
@@ -321,22 +295,30 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
     }
   }
 
-  // alternatives: the k-th largest of the threads' maxima
+  // the block's largest logit, and the bound for the alternatives
   const uint32_t mine = logp_order(acc.m);
-  if (a.top_k > 0) {
-    uint32_t b = warp_sort(mine, lane);
-    sm.best[warp][lane] = b;
-#pragma unroll
-    for (int n = 1; n < kWarps; n *= 2) {
-      __syncthreads();
-      if ((warp & (2 * n - 1)) == 0) {
-        b = warp_merge(b, sm.best[warp + n][31 - lane], lane);
-        sm.best[warp][lane] = b;
-      }
+  int q = 1;
+  while (q < kWarps && q * q < a.top_k) ++q;
+  {
+    uint32_t nth = 0, left = mine;
+    const uint32_t top = __reduce_max_sync(0xffffffffu, mine);
+    for (int j = 0; j < a.top_k; j += q) {               // ceil(k / q) times
+      nth = __reduce_max_sync(0xffffffffu, left);
+      if (lane == __ffs(__ballot_sync(0xffffffffu, left == nth)) - 1) left = 0;
     }
-    if (warp == 0 && lane == a.top_k - 1) sm.tau = max(b, 1u);
-    __syncthreads();
-    const uint32_t tau = sm.tau;
+    if (lane == 0) { sm.top[warp] = top; sm.nth[warp] = nth; }
+  }
+  __syncthreads();
+  const uint32_t block_top = __reduce_max_sync(0xffffffffu, lane < kWarps ? sm.top[lane] : 0u);
+  if (a.top_k > 0) {
+    const uint32_t nth = lane < kWarps ? sm.nth[lane] : 0u;
+    int above = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      const uint32_t o = __shfl_sync(0xffffffffu, nth, i);
+      above += o > nth || (o == nth && i < lane);
+    }
+    const uint32_t tau = max(__shfl_sync(0xffffffffu, nth, __ffs(__ballot_sync(0xffffffffu, lane < kWarps && above == q - 1)) - 1), 1u);
     const bool again = mine >= tau;
     const int marks = fours > 0 ? ((fours - 1) >> shift) + 1 : 0;
     const uint16_t tau_mark = (uint16_t)(tau >> 16);
@@ -443,34 +425,29 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
     }
   }
 
-  // join of the block's sums
-  auto join_lanes = [&](LogpAcc &x, int half) {
+  // the block's sums, all with its largest logit as reference
+  auto sum_lanes = [&](float &x, float &y) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-      if (o > half) continue;
-      LogpAcc other;
-      other.m = __shfl_down_sync(0xffffffffu, x.m, o);
-      other.del = __shfl_down_sync(0xffffffffu, x.del, o);
-      other.s = __shfl_down_sync(0xffffffffu, x.s, o);
-      other.u = __shfl_down_sync(0xffffffffu, x.u, o);
-      x.join(other, c2);
+      x += __shfl_xor_sync(0xffffffffu, x, o);
+      y += __shfl_xor_sync(0xffffffffu, y, o);
     }
   };
-  join_lanes(acc, 16);
-  if (lane == 0) { sm.acc[0][warp] = acc.m; sm.acc[1][warp] = acc.del; sm.acc[2][warp] = acc.s; sm.acc[3][warp] = acc.u; }
+  auto value = [](uint32_t o) { return o ? logp_value(o) : -INFINITY; };
+  acc.rescale(value(block_top), 0.f, c2);
+  sum_lanes(acc.s, acc.u);
+  if (lane == 0) { sm.sum[0][warp] = acc.s; sm.sum[1][warp] = acc.u; }
   __syncthreads();
   // to block 0 of the cluster: the block's sums, and of its candidates the k best
   if (cluster > 1) cluster_wait();
   auto lead = [&](const void *p) { return cluster > 1 ? mapa_u32(smem_u32(p), 0) : smem_u32(p); };
   if (warp == 0) {
-    LogpAcc all;
-    if (lane < kWarps) { all.m = sm.acc[0][lane]; all.del = sm.acc[1][lane]; all.s = sm.acc[2][lane]; all.u = sm.acc[3][lane]; }
-    join_lanes(all, kWarps / 2);
+    float x = lane < kWarps ? sm.sum[0][lane] : 0.f, y = lane < kWarps ? sm.sum[1][lane] : 0.f;
+    sum_lanes(x, y);
     if (lane == 0) {
-      st_cluster_f32(lead(&sm.part[rank][0]), all.m);
-      st_cluster_f32(lead(&sm.part[rank][1]), all.del);
-      st_cluster_f32(lead(&sm.part[rank][2]), all.s);
-      st_cluster_f32(lead(&sm.part[rank][3]), all.u);
+      st_cluster_u32(lead(&sm.part_top[rank]), block_top);
+      st_cluster_f32(lead(&sm.part[rank][0]), x);
+      st_cluster_f32(lead(&sm.part[rank][1]), y);
     }
   }
   const int n_own = a.top_k > 0 ? (int)sm.n_own : 0;
@@ -483,17 +460,18 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
   if (cluster > 1) cluster_sync_all(); else __syncthreads();
   if (rank != 0) return;
 
-  // every thread joins the cluster's sums, in the same order
+  // every warp joins the cluster's sums, in the same order
   LogpAcc all;
-  all.m = sm.part[0][0]; all.del = sm.part[0][1]; all.s = sm.part[0][2]; all.u = sm.part[0][3];
-  for (int r = 1; r < cluster; ++r) {
-    LogpAcc o;
-    o.m = sm.part[r][0]; o.del = sm.part[r][1]; o.s = sm.part[r][2]; o.u = sm.part[r][3];
-    all.join(o, c2);
+  {
+    const bool mine_too = lane < cluster;
+    const uint32_t o = mine_too ? sm.part_top[lane] : 0u, top = __reduce_max_sync(0xffffffffu, o);
+    if (mine_too) { all.m = value(o); all.s = sm.part[lane][0]; all.u = sm.part[lane][1]; }
+    all.rescale(value(top), 0.f, c2);
+    sum_lanes(all.s, all.u);
   }
   constexpr float kLn2 = 0.693147180559945f;
   const bool bad = !(all.s < INFINITY), none = all.s == 0.f;
-  const float log2_s = log2f(all.s), rest = (log2_s + all.del) * kLn2;
+  const float log2_s = log2f(all.s), rest = log2_s * kLn2;
   auto logprob = [&](float x) { return bad ? NAN : none ? -INFINITY : fmaf(x - all.m, a.scale, -rest); };
   if (tid == 0 && a.entropy) a.entropy[row] = bad ? NAN : none ? 0.f : fmaxf((log2_s - all.u / all.s) * kLn2, 0.f);
   if (a.tokens)
