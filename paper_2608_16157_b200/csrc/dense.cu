@@ -44,11 +44,22 @@ bool w4_ok(int64_t n, int64_t k, int group) {
   return n >= 1 && n <= (1 << 24) && (group == 32 || group == 64 || group == 128) && k >= group && k <= 65536 && k % group == 0;
 }
 
-template <bool BF16, bool RES32>
-cudaError_t launch_norm(const NormArgs &a, bool wide, cudaStream_t st) {
-  const int threads = a.lanes > kNormThreads ? a.lanes : kNormThreads, rows = threads / a.lanes;
+template <bool BF16, bool RES32, int E>
+cudaError_t launch_norm_elems(NormArgs a, bool wide, cudaStream_t st) {
+  a.lanes = 32;
+  while (a.lanes * E < a.d) a.lanes *= 2;
+  const int threads = a.lanes > 32 ? a.lanes : 128, rows = threads / a.lanes;
   const unsigned grid = (unsigned)((a.T + rows - 1) / rows);
-  return wide ? launch(add_norm_kernel<BF16, RES32, 8>, grid, threads, 0, st, a) : launch(add_norm_kernel<BF16, RES32, 1>, grid, threads, 0, st, a);
+  return wide ? launch(add_norm_kernel<BF16, RES32, 8, E>, grid, threads, 0, st, a) : launch(add_norm_kernel<BF16, RES32, 1, E>, grid, threads, 0, st, a);
+}
+
+template <bool BF16, bool RES32>
+cudaError_t launch_norm(const ft_dense *h, const NormArgs &a, bool wide, cudaStream_t st) {
+  // elements a thread: as few as leave no more threads than the SMs hold at once
+  const long long elems = (long long)a.T * a.d, threads = (long long)h->sm_count * 1024;
+  if (elems > 16 * threads || a.d > 16 * 1024) return launch_norm_elems<BF16, RES32, 32>(a, wide, st);
+  if (elems > 8 * threads || a.d > 8 * 1024) return launch_norm_elems<BF16, RES32, 16>(a, wide, st);
+  return launch_norm_elems<BF16, RES32, 8>(a, wide, st);
 }
 
 template <bool BF16, int G, bool ZERO, int NT>
@@ -218,7 +229,7 @@ ft_status_t ft_dense_add_norm(ft_dense_t *h, int T, int d, int dtype, int res_dt
   if (!h || T < 0 || d < 1 || !type16(dtype) || (res_dtype != dtype && res_dtype != FT_DENSE_FP32) || (flags & ~FT_DENSE_NORM_POST))
     return FT_ERR_INVALID_ARG;
   if (!(eps >= 0.f) || (gate_step != 0 && gate_step != 1)) return FT_ERR_INVALID_ARG;
-  if (d > 1024 * kNormElems) return FT_ERR_UNSUPPORTED;
+  if (d > kNormMaxDim) return FT_ERR_UNSUPPORTED;
   if (T == 0) return FT_OK;
   if ((!y && !res) || (!res_out && !out)) return FT_ERR_INVALID_ARG;
   const bool res32 = res_dtype == FT_DENSE_FP32;
@@ -243,12 +254,10 @@ ft_status_t ft_dense_add_norm(ft_dense_t *h, int T, int d, int dtype, int res_dt
   auto rows16 = [&](const void *p, int64_t stride, int bytes) { return !p || (aligned(p, 16) && (T == 1 || stride * bytes % 16 == 0)); };
   const bool wide = d % 8 == 0 && rows16(y, y_stride, 2) && rows16(res, res_stride, res32 ? 4 : 2) && rows16(res_out, res_out_stride, res32 ? 4 : 2) &&
                     rows16(out, out_stride, 2) && (!gate || gate_step == 0 || rows16(gate, gate_stride, 2)) && aligned(w_post, 16) && aligned(w_pre, 16);
-  a.lanes = 32;
-  while (a.lanes * kNormElems < d) a.lanes *= 2;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool bf = dtype == FT_DENSE_BF16;
-  FD_CUDA(bf ? (res32 ? launch_norm<true, true>(a, wide, st) : launch_norm<true, false>(a, wide, st))
-             : (res32 ? launch_norm<false, true>(a, wide, st) : launch_norm<false, false>(a, wide, st)));
+  FD_CUDA(bf ? (res32 ? launch_norm<true, true>(h, a, wide, st) : launch_norm<true, false>(h, a, wide, st))
+             : (res32 ? launch_norm<false, true>(h, a, wide, st) : launch_norm<false, false>(h, a, wide, st)));
   h->launches += 1;
   return FT_OK;
 }

@@ -1,17 +1,17 @@
 // A block's output joins the residual stream and the next block's input is normed, in one pass:
 //   u = y, or y * rsqrt(mean(y^2) + eps) * (o + w_post);  r' = a r + b gate u;  h = r' * rsqrt(mean(r'^2) + eps) * (o + w_pre)
 // Bound: HBM (y, r and a gate per element read once, r' and h written once) for many tokens, launch latency for few.
-// `lanes` threads (32 .. 1024, a power of two) share a row; a thread holds kNormElems of its elements from the loads to the stores,
-// so that a row is read once whatever is written over it.  A vector (8 elements) a load where every address allows 16-byte accesses,
-// else single elements, neighbouring threads on neighbouring elements.
+// `lanes` threads (32 .. 1024, a power of two) share a row; a thread holds E of its elements in float from the loads to the stores, so that
+// a row is read once, whatever is written over it.  All loads of y, r and the gate go out before the first sum.  E = 32 where there are rows
+// enough (a thread then has 128 to 256 bytes on their way), 8 or 16 for few rows, where latency counts.  A vector (8 elements) a load where
+// every address allows 16-byte accesses, else single elements, neighbouring threads on neighbouring elements.
 #pragma once
 #include "async.cuh"
 #include "common.cuh"
 
 namespace ftmoe {
 
-constexpr int kNormElems = 16;             // elements of a row per thread: 1024 threads hold rows of 16384
-constexpr int kNormThreads = 256;          // threads of a block while a row needs no more
+constexpr int kNormMaxDim = 16384;
 
 struct NormArgs {
   int32_t T, d, lanes, post, gate_step;
@@ -84,90 +84,96 @@ __device__ __forceinline__ void store_32(float *p, const float *x) {
   }
 }
 
-// Sum over the threads of a row; `s` holds a float per warp.  All threads of the block take part.
+// Sum over the threads of a row; `s` holds a float per warp.  Where a row has more than a warp, it has a block of its own.
 __device__ __forceinline__ float row_sum(float v, int lanes, float *s) {
   v = warp_sum(v);
   if (lanes == 32) return v;
-  const int warp = threadIdx.x >> 5, n = lanes >> 5, first = warp & ~(n - 1);
-  __syncthreads();                          // (the sums before are read)
-  if ((threadIdx.x & 31) == 0) s[warp] = v;
+  const int n = lanes >> 5;
+  if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
   __syncthreads();
   float t = 0.f;
-  for (int i = 0; i < n; ++i) t += s[first + i];
+  for (int i = 0; i < n; ++i) t += s[i];
   return t;
 }
 
-template <bool BF16, bool RES32, int VEC>
-__global__ void __launch_bounds__(1024) add_norm_kernel(const NormArgs a) {
-  constexpr int N = kNormElems / VEC;
-  __shared__ float s_sum[32];
+template <bool BF16, bool RES32, int VEC, int E>
+__global__ void __launch_bounds__(E == 32 ? 512 : 1024) add_norm_kernel(const NormArgs a) {
+  constexpr int N = E / VEC;
+  __shared__ float s_sum[2][32];
   grid_let_next();
+  const int lane = threadIdx.x & (a.lanes - 1);
+  const long long t = (long long)blockIdx.x * (blockDim.x / a.lanes) + threadIdx.x / a.lanes;
   grid_wait();
-  const int rows = blockDim.x / a.lanes, lane = threadIdx.x & (a.lanes - 1);
-  const long long t = (long long)blockIdx.x * rows + threadIdx.x / a.lanes;
-  const bool live = t < a.T;                // (a row past the end takes part in the sums)
-  float r[kNormElems], u[kNormElems];
+  if (t >= a.T) return;                     // (only where a row is a warp's)
+  float r[E], u[E];
+  uint32_t g[E / 2 + 1];
 #pragma unroll
-  for (int i = 0; i < kNormElems; ++i) r[i] = u[i] = 0.f;
+  for (int i = 0; i < E; ++i) r[i] = u[i] = 0.f;
   auto each = [&](auto f) {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const int i = (j * a.lanes + lane) * VEC;
-      if (live && i < a.d) f(i, j * VEC);
+      if (i < a.d) f(i, j * VEC);
     }
   };
+  const bool gate = a.y && a.gate;
   if (a.y) each([&](int i, int j) { load_16<BF16, VEC>(a.y + t * a.y_stride + i, u + j); });
   if (a.res) each([&](int i, int j) {
     if (RES32) load_32<VEC>(static_cast<const float *>(a.res) + t * a.res_stride + i, r + j);
     else load_16<BF16, VEC>(static_cast<const uint16_t *>(a.res) + t * a.res_stride + i, r + j);
   });
+  if (gate && a.gate_step) each([&](int i, int j) {
+    const uint16_t *p = a.gate + t * a.gate_stride + i;
+    if constexpr (VEC == 8) {
+      const uint4 v = *reinterpret_cast<const uint4 *>(p);
+      g[j / 2] = v.x; g[j / 2 + 1] = v.y; g[j / 2 + 2] = v.z; g[j / 2 + 3] = v.w;
+    } else {
+      if (j % 2 == 0) g[j / 2] = *p; else g[j / 2] |= (uint32_t)*p << 16;
+    }
+  });
+  else if (gate) g[0] = a.gate[t * a.gate_stride];
   if (a.post) {
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < kNormElems; ++i) sum = fmaf(u[i], u[i], sum);
-    const float inv = rsqrtf(row_sum(sum, a.lanes, s_sum) / (float)a.d + a.eps);
-#pragma unroll
-    for (int i = 0; i < kNormElems; ++i) u[i] *= inv;
+    for (int i = 0; i < E; ++i) sum = fmaf(u[i], u[i], sum);
+    const float inv = rsqrtf(row_sum(sum, a.lanes, s_sum[0]) / (float)a.d + a.eps);
     if (a.w_post) each([&](int i, int j) {
       float w[VEC];
       load_16<BF16, VEC>(a.w_post + i, w);
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) u[j + k] *= a.w_offset + w[k];
+      for (int k = 0; k < VEC; ++k) u[j + k] *= inv * (a.w_offset + w[k]);
     });
+    else
+#pragma unroll
+      for (int i = 0; i < E; ++i) u[i] *= inv;
   }
-  if (a.y && a.gate) each([&](int i, int j) {
-    float g[VEC];
-    if (a.gate_step) load_16<BF16, VEC>(a.gate + t * a.gate_stride + i, g);
-    else {
-      g[0] = to_float<BF16>(a.gate[t * a.gate_stride]);
+  if (gate && a.gate_step) each([&](int, int j) {
 #pragma unroll
-      for (int k = 1; k < VEC; ++k) g[k] = g[0];
-    }
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) u[j + k] *= g[k];
+    for (int k = 0; k < VEC; ++k) u[j + k] *= to_float<BF16>((uint16_t)(g[(j + k) / 2] >> ((j + k) % 2 * 16)));
   });
+  const float y_scale = gate && !a.gate_step ? a.y_scale * to_float<BF16>((uint16_t)g[0]) : a.y_scale;
 #pragma unroll
-  for (int i = 0; i < kNormElems; ++i) r[i] = a.res ? (a.y ? fmaf(a.y_scale, u[i], a.res_scale * r[i]) : a.res_scale * r[i]) : a.y_scale * u[i];
+  for (int i = 0; i < E; ++i) r[i] = a.res ? (a.y ? fmaf(y_scale, u[i], a.res_scale * r[i]) : a.res_scale * r[i]) : y_scale * u[i];
   if (a.res_out) each([&](int i, int j) {
     if (RES32) store_32<VEC>(static_cast<float *>(a.res_out) + t * a.res_out_stride + i, r + j);
     else store_16<BF16, VEC>(static_cast<uint16_t *>(a.res_out) + t * a.res_out_stride + i, r + j);
   });
   if (!a.out) return;
   float sum = 0.f;
+  each([&](int, int j) {
 #pragma unroll
-  for (int j = 0; j < N; ++j)
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) sum = (j * a.lanes + lane) * VEC + k < a.d ? fmaf(r[j * VEC + k], r[j * VEC + k], sum) : sum;
-  const float inv = rsqrtf(row_sum(sum, a.lanes, s_sum) / (float)a.d + a.eps);
+    for (int k = 0; k < VEC; ++k) sum = fmaf(r[j + k], r[j + k], sum);
+  });
+  const float inv = rsqrtf(row_sum(sum, a.lanes, s_sum[1]) / (float)a.d + a.eps);
   each([&](int i, int j) {
     float h[VEC];
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) h[k] = r[j + k] * inv;
     if (a.w_pre) {
-      float w[VEC];
-      load_16<BF16, VEC>(a.w_pre + i, w);
+      load_16<BF16, VEC>(a.w_pre + i, h);
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) h[k] *= a.w_offset + w[k];
+      for (int k = 0; k < VEC; ++k) h[k] = r[j + k] * (inv * (a.w_offset + h[k]));
+    } else {
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) h[k] = r[j + k] * inv;
     }
     store_16<BF16, VEC>(a.out + t * a.out_stride + i, h);
   });
