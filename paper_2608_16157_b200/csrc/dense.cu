@@ -44,13 +44,20 @@ bool w4_ok(int64_t n, int64_t k, int group) {
   return n >= 1 && n <= (1 << 24) && (group == 32 || group == 64 || group == 128) && k >= group && k <= 65536 && k % group == 0;
 }
 
+template <bool BF16, bool RES32, bool POST, bool GATE, int E>
+cudaError_t launch_norm_form(const NormArgs &a, bool wide, cudaStream_t st) {
+  const int threads = a.lanes > 32 ? a.lanes : 128, rows = threads / a.lanes;
+  const unsigned grid = (unsigned)((a.T + rows - 1) / rows);
+  return wide ? launch(add_norm_kernel<BF16, RES32, POST, GATE, 8, E>, grid, threads, 0, st, a)
+              : launch(add_norm_kernel<BF16, RES32, POST, GATE, 1, E>, grid, threads, 0, st, a);
+}
 template <bool BF16, bool RES32, int E>
 cudaError_t launch_norm_elems(NormArgs a, bool wide, cudaStream_t st) {
   a.lanes = 32;
   while (a.lanes * E < a.d) a.lanes *= 2;
-  const int threads = a.lanes > 32 ? a.lanes : 128, rows = threads / a.lanes;
-  const unsigned grid = (unsigned)((a.T + rows - 1) / rows);
-  return wide ? launch(add_norm_kernel<BF16, RES32, 8, E>, grid, threads, 0, st, a) : launch(add_norm_kernel<BF16, RES32, 1, E>, grid, threads, 0, st, a);
+  const bool gate = a.y && a.gate && a.gate_step;
+  if (a.post) return gate ? launch_norm_form<BF16, RES32, true, true, E>(a, wide, st) : launch_norm_form<BF16, RES32, true, false, E>(a, wide, st);
+  return gate ? launch_norm_form<BF16, RES32, false, true, E>(a, wide, st) : launch_norm_form<BF16, RES32, false, false, E>(a, wide, st);
 }
 
 template <bool BF16, bool RES32>

@@ -33,8 +33,14 @@ __device__ __forceinline__ uint16_t from_float(float v) {
 }
 template <bool BF16>
 __device__ __forceinline__ void to_float2(uint32_t v, float &a, float &b) {
-  a = to_float<BF16>((uint16_t)v);
-  b = to_float<BF16>((uint16_t)(v >> 16));
+  if (BF16) {
+    a = __uint_as_float(v << 16);
+    b = __uint_as_float(v & 0xffff0000u);
+  } else {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&v));
+    a = f.x;
+    b = f.y;
+  }
 }
 template <bool BF16>
 __device__ __forceinline__ uint32_t from_float2(float a, float b) {
@@ -96,17 +102,18 @@ __device__ __forceinline__ float row_sum(float v, int lanes, float *s) {
   return t;
 }
 
-template <bool BF16, bool RES32, int VEC, int E>
+template <bool BF16, bool RES32, bool POST, bool GATE, int VEC, int E>
 __global__ void __launch_bounds__(E == 32 ? 512 : 1024) add_norm_kernel(const NormArgs a) {
   constexpr int N = E / VEC;
   __shared__ float s_sum[2][32];
   grid_let_next();
   const int lane = threadIdx.x & (a.lanes - 1);
   const long long t = (long long)blockIdx.x * (blockDim.x / a.lanes) + threadIdx.x / a.lanes;
+  const uint16_t *y = a.y + t * a.y_stride, *gate = a.gate + t * a.gate_stride;
   grid_wait();
   if (t >= a.T) return;                     // (only where a row is a warp's)
   float r[E], u[E];
-  uint32_t g[E / 2 + 1];
+  uint32_t g[GATE ? (E + 1) / 2 : 1];
 #pragma unroll
   for (int i = 0; i < E; ++i) r[i] = u[i] = 0.f;
   auto each = [&](auto f) {
@@ -116,55 +123,71 @@ __global__ void __launch_bounds__(E == 32 ? 512 : 1024) add_norm_kernel(const No
       if (i < a.d) f(i, j * VEC);
     }
   };
-  const bool gate = a.y && a.gate;
-  if (a.y) each([&](int i, int j) { load_16<BF16, VEC>(a.y + t * a.y_stride + i, u + j); });
-  if (a.res) each([&](int i, int j) {
-    if (RES32) load_32<VEC>(static_cast<const float *>(a.res) + t * a.res_stride + i, r + j);
-    else load_16<BF16, VEC>(static_cast<const uint16_t *>(a.res) + t * a.res_stride + i, r + j);
-  });
-  if (gate && a.gate_step) each([&](int i, int j) {
-    const uint16_t *p = a.gate + t * a.gate_stride + i;
+  if (a.y) each([&](int i, int j) { load_16<BF16, VEC>(y + i, u + j); });
+  if (a.res) {
+    const char *res = static_cast<const char *>(a.res) + t * a.res_stride * (RES32 ? 4 : 2);
+    each([&](int i, int j) {
+      if (RES32) load_32<VEC>(reinterpret_cast<const float *>(res) + i, r + j);
+      else load_16<BF16, VEC>(reinterpret_cast<const uint16_t *>(res) + i, r + j);
+    });
+  }
+  if (GATE) each([&](int i, int j) {
     if constexpr (VEC == 8) {
-      const uint4 v = *reinterpret_cast<const uint4 *>(p);
+      const uint4 v = *reinterpret_cast<const uint4 *>(gate + i);
       g[j / 2] = v.x; g[j / 2 + 1] = v.y; g[j / 2 + 2] = v.z; g[j / 2 + 3] = v.w;
     } else {
-      if (j % 2 == 0) g[j / 2] = *p; else g[j / 2] |= (uint32_t)*p << 16;
+      if (j % 2 == 0) g[j / 2] = gate[i]; else g[j / 2] |= (uint32_t)gate[i] << 16;
     }
   });
-  else if (gate) g[0] = a.gate[t * a.gate_stride];
-  if (a.post) {
+  // what is left out counts nothing; a gate of one value a token is part of the scale
+  const float r_scale = a.res ? a.res_scale : 0.f;
+  const float y_scale = !a.y ? 0.f : !GATE && a.gate ? a.y_scale * to_float<BF16>(*gate) : a.y_scale;
+  float inv = 1.f;
+  if (POST) {
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < E; ++i) sum = fmaf(u[i], u[i], sum);
-    const float inv = rsqrtf(row_sum(sum, a.lanes, s_sum[0]) / (float)a.d + a.eps);
-    if (a.w_post) each([&](int i, int j) {
-      float w[VEC];
-      load_16<BF16, VEC>(a.w_post + i, w);
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) u[j + k] *= inv * (a.w_offset + w[k]);
-    });
-    else
-#pragma unroll
-      for (int i = 0; i < E; ++i) u[i] *= inv;
+    inv = rsqrtf(row_sum(sum, a.lanes, s_sum[0]) / (float)a.d + a.eps);
   }
-  if (gate && a.gate_step) each([&](int, int j) {
+  float sum = 0.f;
+  char *res_out = static_cast<char *>(a.res_out) + t * a.res_out_stride * (RES32 ? 4 : 2);
+  each([&](int i, int j) {
+    float f[VEC];                           // the factors of u
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) u[j + k] *= to_float<BF16>((uint16_t)(g[(j + k) / 2] >> ((j + k) % 2 * 16)));
-  });
-  const float y_scale = gate && !a.gate_step ? a.y_scale * to_float<BF16>((uint16_t)g[0]) : a.y_scale;
+    for (int k = 0; k < VEC; ++k) f[k] = 1.f;
+    if (POST) {
+      if (a.w_post) {
+        load_16<BF16, VEC>(a.w_post + i, f);
 #pragma unroll
-  for (int i = 0; i < E; ++i) r[i] = a.res ? (a.y ? fmaf(y_scale, u[i], a.res_scale * r[i]) : a.res_scale * r[i]) : y_scale * u[i];
-  if (a.res_out) each([&](int i, int j) {
-    if (RES32) store_32<VEC>(static_cast<float *>(a.res_out) + t * a.res_out_stride + i, r + j);
-    else store_16<BF16, VEC>(static_cast<uint16_t *>(a.res_out) + t * a.res_out_stride + i, r + j);
+        for (int k = 0; k < VEC; ++k) f[k] = inv * (a.w_offset + f[k]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) f[k] = inv;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < VEC; k += 2) {
+      if (GATE) {
+        float g0, g1;
+        to_float2<BF16>(VEC == 1 && j % 2 ? g[j / 2] >> 16 : g[(j + k) / 2], g0, g1);
+        f[k] *= g0;
+        if (VEC > 1) f[k + 1 < VEC ? k + 1 : k] *= g1;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+      const float v = POST || GATE ? u[j + k] * f[k] : u[j + k];
+      r[j + k] = fmaf(y_scale, v, r_scale * r[j + k]);
+      sum = fmaf(r[j + k], r[j + k], sum);
+    }
+    if (a.res_out) {
+      if (RES32) store_32<VEC>(reinterpret_cast<float *>(res_out) + i, r + j);
+      else store_16<BF16, VEC>(reinterpret_cast<uint16_t *>(res_out) + i, r + j);
+    }
   });
   if (!a.out) return;
-  float sum = 0.f;
-  each([&](int, int j) {
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) sum = fmaf(r[j + k], r[j + k], sum);
-  });
-  const float inv = rsqrtf(row_sum(sum, a.lanes, s_sum[1]) / (float)a.d + a.eps);
+  inv = rsqrtf(row_sum(sum, a.lanes, s_sum[1]) / (float)a.d + a.eps);
+  uint16_t *out = a.out + t * a.out_stride;
   each([&](int i, int j) {
     float h[VEC];
     if (a.w_pre) {
@@ -175,7 +198,7 @@ __global__ void __launch_bounds__(E == 32 ? 512 : 1024) add_norm_kernel(const No
 #pragma unroll
       for (int k = 0; k < VEC; ++k) h[k] = r[j + k] * inv;
     }
-    store_16<BF16, VEC>(a.out + t * a.out_stride + i, h);
+    store_16<BF16, VEC>(out + i, h);
   });
 }
 
