@@ -2,9 +2,9 @@
 //   u = y, or y * rsqrt(mean(y^2) + eps) * (o + w_post);  r' = a r + b gate u;  h = r' * rsqrt(mean(r'^2) + eps) * (o + w_pre)
 // Bound: HBM (y, r and a gate per element read once, r' and h written once) for many tokens, launch latency for few.
 // `lanes` threads (32 .. 1024, a power of two) share a row; a thread holds E of its elements in float from the loads to the stores, so that
-// a row is read once, whatever is written over it.  All loads of y, r and the gate go out before the first sum.  E = 32 where there are rows
-// enough (a thread then has 128 to 256 bytes on their way), 8 or 16 for few rows, where latency counts.  A vector (8 elements) a load where
-// every address allows 16-byte accesses, else single elements, neighbouring threads on neighbouring elements.
+// a row is read once, whatever is written over it.  All loads of y, r and the gate go out before the first sum.  E = 16, or 8 for few rows, where
+// latency counts.  A vector (8 elements) a load where every address allows 16-byte accesses, else single elements, neighbouring threads on
+// neighbouring elements (twice the time: the load and store units are then the bound).
 #pragma once
 #include "async.cuh"
 #include "common.cuh"
@@ -103,7 +103,7 @@ __device__ __forceinline__ float row_sum(float v, int lanes, float *s) {
 }
 
 template <bool BF16, bool RES32, bool POST, bool GATE, int VEC, int E>
-__global__ void __launch_bounds__(E == 32 ? 512 : 1024) add_norm_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(1024) add_norm_kernel(const NormArgs a) {
   constexpr int N = E / VEC;
   __shared__ float s_sum[2][32];
   grid_let_next();
