@@ -17,7 +17,7 @@ using namespace ftmoe;
 
 struct ft_dense {
   int device = 0, sm_count = 148;
-  int clusters[2][kW4MaxCluster + 1] = {};   // of each size that fit at once: a block an SM, two
+  int clusters[kW4MaxCluster + 1] = {};   // of each size that fit at once, a block an SM
   uint32_t *status_dev = nullptr;
   void *encode = nullptr;          // cuTensorMapEncodeTiled
   uint64_t launches = 0;
@@ -71,9 +71,9 @@ cudaError_t launch_norm(const ft_dense *h, const NormArgs &a, bool wide, cudaStr
 template <bool BF16, int G, bool ZERO, int NT>
 cudaError_t launch_w4_stream(const ft_dense *h, const W4Args &a, cudaStream_t st) {
   W4Stream p;
-  w4_stream_share(a.g, h->clusters[0], kW4Warps<NT>, p);
+  w4_stream_share(a.g, h->clusters, kW4Warps<NT>, p);
   const int smem = w4_stream_memory<NT>(a.g, p);
-  const int per_block = kW4Warps<NT> / p.wk, want = (a.g.quads + per_block - 1) / per_block, fit = h->clusters[0][p.cluster];
+  const int per_block = kW4Warps<NT> / p.wk, want = (a.g.quads + per_block - 1) / per_block, fit = h->clusters[p.cluster];
   return launch_clusters(w4_stream_kernel<BF16, G, ZERO, NT>, dim3((want < fit ? want : fit) * p.cluster, (a.T + 8 * NT - 1) / (8 * NT)), kW4Warps<NT> * 32, smem,
                          p.cluster, st, a, p);
 }
@@ -97,26 +97,23 @@ bool make_x_map(const ft_dense *h, CUtensorMap *tm, const W4Args &a, int tokens)
                                                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool BF16, bool ZERO, int FORM>
-cudaError_t launch_w4_tile(const ft_dense *h, const W4Args &a, cudaStream_t st) {
-  const int *clusters = h->clusters[FORM == kW4Few ? 1 : 0];
-  W4Tile p = w4_tile_share(a.g, a.T, FORM, clusters);
+template <bool BF16, bool ZERO, bool EXACT>
+cudaError_t launch_w4_tile(const ft_dense *h, const W4Args &a, W4Tile p, cudaStream_t st) {
   CUtensorMap tm;
   if (!make_x_map(h, &tm, a, p.bn)) return cudaErrorInvalidValue;
-  const int smem = w4_tile_memory<FORM>(a.g, p), units = p.row_tiles * p.tok_tiles, fit = clusters[p.cluster];
-  return launch_clusters(w4_tile_kernel<BF16, ZERO, FORM>, dim3((p.cluster > 1 || units < fit ? units : fit) * p.cluster), W4TileCfg<FORM>::kThreads, smem, p.cluster,
-                         st, tm, a, p);
+  const int smem = w4_tile_memory<EXACT>(a.g, p), units = p.row_tiles * p.tok_tiles, fit = h->clusters[p.cluster];
+  return launch_clusters(w4_tile_kernel<BF16, ZERO, EXACT>, dim3((p.cluster > 1 || units < fit ? units : fit) * p.cluster), kW4TileThreads, smem, p.cluster, st, tm, a, p);
 }
 
 template <bool BF16, bool ZERO>
 cudaError_t launch_w4_many(const ft_dense *h, const W4Args &a, cudaStream_t st) {
-  if (a.out32) return launch_w4_tile<BF16, ZERO, kW4Exact>(h, a, st);
-  return a.T <= 64 ? launch_w4_tile<BF16, ZERO, kW4Few>(h, a, st) : launch_w4_tile<BF16, ZERO, kW4Wide>(h, a, st);
+  const W4Tile p = w4_tile_share(a.g, a.T, a.out32 != 0, h->clusters);
+  return a.out32 ? launch_w4_tile<BF16, ZERO, true>(h, a, p, st) : launch_w4_tile<BF16, ZERO, false>(h, a, p, st);
 }
 
 template <bool BF16>
 cudaError_t launch_w4(const ft_dense *h, const W4Args &a, bool zero, cudaStream_t st) {
-  if (a.T > (a.out32 ? 32 : 16)) return zero ? launch_w4_many<BF16, true>(h, a, st) : launch_w4_many<BF16, false>(h, a, st);
+  if (a.T > 32) return zero ? launch_w4_many<BF16, true>(h, a, st) : launch_w4_many<BF16, false>(h, a, st);
   switch (a.g.group) {
     case 32: return zero ? launch_w4_tokens<BF16, 32, true>(h, a, st) : launch_w4_tokens<BF16, 32, false>(h, a, st);
     case 64: return zero ? launch_w4_tokens<BF16, 64, true>(h, a, st) : launch_w4_tokens<BF16, 64, false>(h, a, st);
@@ -150,9 +147,8 @@ cudaError_t allow_smem() {
   cudaError_t e = allow_smem_stream<BF16, 32, ZERO>();
   if (e == cudaSuccess) e = allow_smem_stream<BF16, 64, ZERO>();
   if (e == cudaSuccess) e = allow_smem_stream<BF16, 128, ZERO>();
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZERO, kW4Wide>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZERO, kW4Exact>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZERO, kW4Few>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem / 2);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZERO, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(w4_tile_kernel<BF16, ZERO, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
   return e;
 }
 
@@ -161,15 +157,13 @@ cudaError_t allow_smem_logprobs() {
   return cudaFuncSetAttribute(logprobs_kernel<TY, 512>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(LogpSmem<16>));
 }
 
-// How many clusters of a size run at once when each block takes an SM, or half of one (the SMs of a cluster stand together, so not all are used).
-template <int FORM>
-cudaError_t count_clusters(const ft_dense *h, int *out) {
-  using Cfg = W4TileCfg<FORM>;
+// How many clusters of a size run at once when each block takes an SM (the SMs of a cluster stand together, so not all are used).
+cudaError_t count_clusters(ft_dense *h) {
   for (int c = 1; c <= kW4MaxCluster; ++c) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(c * h->sm_count);
-    cfg.blockDim = dim3(Cfg::kThreads);
-    cfg.dynamicSmemBytes = FORM == kW4Few ? 100 * 1024 : kMaxSmem;
+    cfg.blockDim = dim3(kW4TileThreads);
+    cfg.dynamicSmemBytes = kMaxSmem;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = c;
@@ -177,10 +171,10 @@ cudaError_t count_clusters(const ft_dense *h, int *out) {
     at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    int n = Cfg::kBlocks * h->sm_count;
-    const cudaError_t e = c == 1 ? cudaSuccess : cudaOccupancyMaxActiveClusters(&n, w4_tile_kernel<true, false, FORM>, &cfg);
+    int n = h->sm_count;
+    const cudaError_t e = c == 1 ? cudaSuccess : cudaOccupancyMaxActiveClusters(&n, w4_tile_kernel<true, false, false>, &cfg);
     if (e != cudaSuccess) return e;
-    out[c] = n;
+    h->clusters[c] = n;
   }
   return cudaSuccess;
 }
@@ -213,8 +207,7 @@ ft_status_t ft_dense_create(int device, ft_dense_t **out) {
   if (e == cudaSuccess) e = allow_smem_logprobs<kLogpBf16>();
   if (e == cudaSuccess) e = allow_smem_logprobs<kLogpFp16>();
   if (e == cudaSuccess) e = allow_smem_logprobs<kLogpFp32>();
-  if (e == cudaSuccess) e = count_clusters<kW4Wide>(h, h->clusters[0]);
-  if (e == cudaSuccess) e = count_clusters<kW4Few>(h, h->clusters[1]);
+  if (e == cudaSuccess) e = count_clusters(h);
   if (e == cudaSuccess && (!h->encode || found != cudaDriverEntryPointSuccess)) e = cudaErrorNotSupported;
   if (e != cudaSuccess) {
     (void)cudaFree(h->status_dev);

@@ -1,17 +1,16 @@
 // Products with 4-bit weights for many tokens, on the 5th-generation tensor cores.  Image and formula: dense_w4.cuh.
 //
-// A block takes 128 rows (two quads) x up to 192 tokens (64) and walks along k.  Bound: the tensor cores for many tokens (2 T N K flops), HBM and the
+// A block takes 128 rows (two quads) x up to 192 tokens and walks along k.  Bound: the tensor cores for many tokens (2 T N K flops), HBM and the
 // expansion of the codes for few.
 //   raw warp      brings the records of 128 k (bulk copies)
 //   x warp        brings x (TMA, 64 k of the tokens a box, 128-byte swizzle)
 //   expanding     turn codes into 16-bit numbers and leave them in tensor memory
 //   mma warp      rows on M = 128 (A from tensor memory), tokens on N (B from shared memory)
-// Three forms.  For 16-bit results (kW4Wide) the operands are the weights s (q - z), rounded once to the type (8 or 11 bits of scale times 4 of
-// code do not fit it): an error of the size of the result's own rounding, 0.0013 of the result in bf16 where that is 0.0017.  The tensor core
-// adds over all of k, and four warps take the sums out while it works on the next unit.  Up to 64 tokens (kW4Few) the expansion is the bound, a
-// chain that eight warps do not hide: two such blocks share an SM.  For float results (kW4Exact) the operands are the exact q - z, a group of k
-// has an accumulator of its own (two in turn), and eight warps add its sums times the row's scale to float sums in registers; that takes
-// about twice as long (reading an accumulator beside the tensor core costs 70 clocks for 16 tokens of 32 rows).
+// Two forms.  For 16-bit results the operands are the weights s (q - z), rounded once to the type (8 or 11 bits of scale times 4 of code do
+// not fit it): an error of the size of the result's own rounding, 0.0013 of the result in bf16 where that is 0.0017.  The tensor core adds
+// over all of k, and four warps take the sums out while it works on the next unit.  For float results (EXACT) the operands are the exact q - z,
+// a group of k has an accumulator of its own (two in turn), and eight warps add its sums times the row's scale to float sums in registers;
+// that takes about twice as long (reading an accumulator beside the tensor core costs 70 clocks for 16 tokens of 32 rows).
 // With a cluster of c blocks each takes 1/c of k, and the sums are added over distributed shared memory, in the blocks' order.
 #pragma once
 #include "dense_w4.cuh"
@@ -19,8 +18,9 @@
 
 namespace ftmoe {
 
-enum { kW4Wide = 0, kW4Exact = 1, kW4Few = 2 };
-constexpr int kW4Ops = 2;                                        // operands of 128 k in tensor memory, 64 columns each
+constexpr int kW4TileThreads = 512, kW4Ops = 2;                 // operands of 128 k in tensor memory
+constexpr int kW4Acc = 192, kW4OpAt = 2 * kW4Acc;               // columns of an accumulator; where the operands stand (64 columns each)
+static_assert(kW4OpAt + kW4Ops * 64 <= 512, "tensor memory");
 
 struct W4Tile {
   int32_t bn, cluster, row_tiles, tok_tiles;     // tokens of a tile (a multiple of 16)
@@ -28,43 +28,37 @@ struct W4Tile {
   int32_t ring_bytes;                            // of the tokens' stages, where the sums of a cluster's blocks go in the end
 };
 
-template <int FORM>
+template <bool EXACT>
 struct W4TileCfg {
-  static constexpr int kThreads = FORM == kW4Few ? 384 : 512, kBlocks = FORM == kW4Few ? 2 : 1;           // blocks an SM
-  static constexpr int kTokens = FORM == kW4Few ? 64 : 192;                      // of a tile at most: columns of an accumulator
-  static constexpr int kOpAt = 2 * kTokens, kTmem = FORM == kW4Few ? 256 : 512;  // columns before the operands, in all
-  // warps that expand (from 4 on) and that take sums out (the last ones; kW4Few: the same, one after the other)
-  static constexpr int kExpand = FORM == kW4Exact ? 4 : 8, kAdd = FORM == kW4Wide ? 4 : 8;
-  static constexpr int kFirstAdd = kThreads / 32 - kAdd, kCols = kTokens / (kAdd / 4);                     // tokens of such a warp
-  static constexpr int kStage = kTokens * 256, kStages = 3;                      // 128 k of the tokens: two boxes of 64
-  static constexpr int kRaw = FORM == kW4Exact ? 3 : FORM == kW4Wide ? 6 : 5;    // slots of records
+  static constexpr int kAdd = EXACT ? 8 : 4, kExpand = EXACT ? 4 : 8;            // warps
+  static constexpr int kCols = kW4Acc / (kAdd / 4);                              // tokens of an adding warp
+  static constexpr int kStage = kW4Acc * 256, kStages = 3;                       // 128 k of the tokens: two boxes of 64
+  static constexpr int kRaw = EXACT ? 3 : 6;                                     // slots of records
   static constexpr int kBars = 2 * kRaw + 2 * kStages + 2 * kW4Ops + 4;
-  static_assert(kOpAt + kW4Ops * 64 <= kTmem, "tensor memory");
 };
 // Fills in the sizes; returns the bytes of dynamic shared memory.
-template <int FORM>
+template <bool EXACT>
 inline int w4_tile_memory(const W4Geom &g, W4Tile &p) {
-  const int stages = W4TileCfg<FORM>::kStages * W4TileCfg<FORM>::kStage, join = p.cluster > 1 ? (p.bn + p.cluster - 1) / p.cluster * p.cluster * 512 : 0;
+  const int stages = W4TileCfg<EXACT>::kStages * W4TileCfg<EXACT>::kStage, join = p.cluster > 1 ? (p.bn + p.cluster - 1) / p.cluster * p.cluster * 512 : 0;
   p.raw_bytes = (2 * g.record(4) + 127) / 128 * 128;
   p.ring_bytes = stages > join ? stages : join;
-  return 1024 + p.ring_bytes + W4TileCfg<FORM>::kRaw * p.raw_bytes + W4TileCfg<FORM>::kBars * 8 + 32;
+  return 1024 + p.ring_bytes + W4TileCfg<EXACT>::kRaw * p.raw_bytes + W4TileCfg<EXACT>::kBars * 8 + 32;
 }
 
-// Tokens of a tile and blocks that share k (`clusters`: how many clusters of a size the GPU holds at once): the split with the least clocks of
-// the SM with the most to do.  A block of 128 k takes 4 clocks a token in the tensor cores, not less than its codes take to expand, nor than its
-// groups' sums to be added; a unit 4000 more, and 2000 over a cluster.
-inline W4Tile w4_tile_share(const W4Geom &g, int T, int form, const int *clusters) {
+// Tokens of a tile and blocks that share k (`clusters`: how many clusters of a size the GPU holds at once): the split with the least clocks of the SM with the most to do.  A block of 128 k takes 4 clocks a
+// token in the tensor cores, not less than its codes take to expand, nor than its groups' sums to be added; a unit 4000 more, and 2000 over a cluster.
+inline W4Tile w4_tile_share(const W4Geom &g, int T, bool exact, const int *clusters) {
   W4Tile best{};
   double least = 1e30;
-  const int row_tiles = (g.quads + 1) / 2, per = kW4Block / g.group, most = form == kW4Few ? 64 : 192;
-  for (int bn = form == kW4Few ? (T + 15) / 16 * 16 : 32; bn <= most; bn += 16) {
+  const int row_tiles = (g.quads + 1) / 2, per = kW4Block / g.group;
+  for (int bn = 32; bn <= kW4Acc; bn += 16) {
     if (bn > 32 && bn - 16 >= T) break;
     for (int cluster = 1; cluster <= kW4MaxCluster && (cluster == 1 || g.nb >= 2 * cluster); ++cluster) {
       const int tok_tiles = (T + bn - 1) / bn;
       const long long units = (long long)row_tiles * tok_tiles, fit = clusters[cluster];
       if (fit == 0 || (cluster > 1 && units > fit)) continue;
       double block = 4. * bn;
-      const double expand = form == kW4Wide ? 750 : 850, add = form == kW4Exact ? per * (300 + 4. * bn) : 0.;
+      const double expand = exact ? 700 : 400, add = exact ? per * (300 + 4. * bn) : 0.;
       if (block < expand) block = expand;
       if (block < add) block = add;
       const double cost = (double)((units + fit - 1) / fit) * ((double)((g.nb + cluster - 1) / cluster) * block + 4000 + (cluster > 1 ? 2000 : 0));
@@ -80,11 +74,10 @@ inline W4Tile w4_tile_share(const W4Geom &g, int T, int form, const int *cluster
 template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-template <bool BF16, bool ZERO, int FORM>
-__global__ void __launch_bounds__(W4TileCfg<FORM>::kThreads, W4TileCfg<FORM>::kBlocks) w4_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const W4Args a, const W4Tile p) {
-  using Cfg = W4TileCfg<FORM>;
-  constexpr int kRaw = Cfg::kRaw, kAcc = Cfg::kTokens;
-  constexpr bool EXACT = FORM == kW4Exact;
+template <bool BF16, bool ZERO, bool EXACT>
+__global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const W4Args a, const W4Tile p) {
+  using Cfg = W4TileCfg<EXACT>;
+  constexpr int kRaw = Cfg::kRaw;
   extern __shared__ unsigned char smem_raw[];
   unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char *s_rec = smem + p.ring_bytes;
@@ -115,7 +108,7 @@ __global__ void __launch_bounds__(W4TileCfg<FORM>::kThreads, W4TileCfg<FORM>::kB
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "n"(Cfg::kTmem) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(s_tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
@@ -128,54 +121,7 @@ __global__ void __launch_bounds__(W4TileCfg<FORM>::kThreads, W4TileCfg<FORM>::kB
   const int cluster = p.cluster, rank = blockIdx.x % cluster, units = p.row_tiles * p.tok_tiles, n_cl = gridDim.x / cluster, cl = blockIdx.x / cluster;
   const int b0 = (int)((long long)g.nb * rank / cluster), b1 = (int)((long long)g.nb * (rank + 1) / cluster);
   const int per = kW4Block / g.group, rec4 = g.record(4);       // groups of a record
-  constexpr int kFirstAdd = Cfg::kFirstAdd, kFirstExpand = 4;
-  // a warp that takes sums out: its rows (the lanes of tensor memory that it can read) and tokens
-  const int row = (warp & 3) * 32 + lane, col0 = (warp - kFirstAdd) / 4 * Cfg::kCols, cols = min(Cfg::kCols, p.bn - col0);
-  const uint32_t lane_tmem = tmem + ((uint32_t)((warp & 3) * 32) << 16) + col0;
-  auto drain = [&](int u, int d) {
-    const int tok0 = u / p.row_tiles * p.bn + col0, n_tok = min(cols, a.T - tok0);
-    const uint32_t out_tmem = lane_tmem + d * kAcc;
-    const int n = u % p.row_tiles * 128 + row;
-    if (cluster == 1) {
-      const float bias = a.bias && n < g.n ? to_float<BF16>(a.bias[n]) : 0.f;
-      const bool store = n < g.n && !*s_abort;
-      using Out = std::conditional_t<EXACT, float, uint16_t>;
-      Out *out = static_cast<Out *>(a.y) + (long long)tok0 * a.y_stride + n;
-#pragma unroll 1
-      for (int c = 0; c < n_tok; c += 16) {
-        uint32_t v[16];
-        tmem_ld16(out_tmem + c, v);
-        tmem_ld_wait();
-#pragma unroll
-        for (int j = 0; j < 16; ++j, out += a.y_stride)
-          if (store && c + j < n_tok) {
-            const float sum = __uint_as_float(v[j]) + bias;
-            if constexpr (EXACT) *out = sum; else *out = from_float<BF16>(sum);
-          }
-      }
-    } else {
-      // (one unit a cluster) token c of the tile goes to block c / share, where its sums stand [block][token][row]
-      const int share = (p.bn + cluster - 1) / cluster;
-      __syncwarp();
-      cluster_sync_all();                              // every block is done with its stages
-      int owner = col0 / share, left = share - col0 % share;
-#pragma unroll 1
-      for (int c = 0; c < cols; c += 8) {
-        uint32_t v[8];
-        tmem_ld8(out_tmem + c, v);
-        tmem_ld_wait();
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint32_t to = stage0 + ((rank * share + share - left) * 128 + row) * 4;
-          asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa_u32(to, owner)), "f"(__uint_as_float(v[j])) : "memory");
-          if (--left == 0) { left = share; ++owner; }
-        }
-      }
-    }
-    tc_fence_before();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(d_empty(d));
-  };
+  constexpr int kFirstAdd = 16 - Cfg::kAdd, kFirstExpand = 4;
 
   if (warp < 4) {
     if constexpr (EXACT) regs_down<80>();
@@ -192,7 +138,7 @@ __global__ void __launch_bounds__(W4TileCfg<FORM>::kThreads, W4TileCfg<FORM>::kB
             const uint32_t to = stage0 + s * Cfg::kStage;
             mbar_expect_tx(x_full(s), 2 * p.bn * 128);
             tma_load_2d(to, &tm_x, b * kW4Block, tok0, x_full(s));
-            tma_load_2d(to + kAcc * 128, &tm_x, b * kW4Block + 64, tok0, x_full(s));
+            tma_load_2d(to + kW4Acc * 128, &tm_x, b * kW4Block + 64, tok0, x_full(s));
           }
           if (++s == Cfg::kStages) { s = 0; ph ^= 1; }
         }
@@ -231,7 +177,7 @@ __global__ void __launch_bounds__(W4TileCfg<FORM>::kThreads, W4TileCfg<FORM>::kB
             wait(x_full(s), ph);
             const bool ok = wait(w_full(o), oph);
             const uint64_t x_desc = umma_desc(stage_u + s * Cfg::kStage, 16, 1024);
-            const uint32_t w_at = tmem_u + Cfg::kOpAt + o * 64;
+            const uint32_t w_at = tmem_u + kW4OpAt + o * 64;
 #pragma unroll
             for (int k0 = 0; k0 < 8; k0 += kSteps) {
               if (EXACT) wait(d_empty(d), dph);
@@ -240,7 +186,7 @@ __global__ void __launch_bounds__(W4TileCfg<FORM>::kThreads, W4TileCfg<FORM>::kB
                 if (ok)
 #pragma unroll
                   for (int k16 = k0; k16 < k0 + kSteps; ++k16)
-                    umma_ts(tmem_u + d * kAcc, w_at + 8 * k16, x_desc + (k16 / 4 * kAcc * 128 + k16 % 4 * 32) / 16, idesc,
+                    umma_ts(tmem_u + d * kW4Acc, w_at + 8 * k16, x_desc + (k16 / 4 * kW4Acc * 128 + k16 % 4 * 32) / 16, idesc,
                             k16 != k0 || (!EXACT && b != b0));
                 if (EXACT) umma_commit(d_full(d));
               }
@@ -278,9 +224,9 @@ __global__ void __launch_bounds__(W4TileCfg<FORM>::kThreads, W4TileCfg<FORM>::kB
     constexpr int kMine = 8 / Cfg::kExpand;
     const int tile0 = 2 * (warp & 3) + (kMine == 1 ? (warp - kFirstExpand) >> 2 : 0), gr = lane >> 2;
     const W4Const<BF16> con;
-    const uint32_t dst = tmem + Cfg::kOpAt + ((uint32_t)(tile0 * 16) << 16);
-    int s = 0, rs = 0, d = 0;
-    uint32_t ph = 1, rph = 0, dph = 0;
+    const uint32_t dst = tmem + kW4OpAt + ((uint32_t)(tile0 * 16) << 16);
+    int s = 0, rs = 0;
+    uint32_t ph = 1, rph = 0;
     for (int u = cl; u < units; u += n_cl) {
       const int quad0 = u % p.row_tiles * 2;
       uint32_t src[kMine], sc_at[kMine], z_at[kMine], next[kMine];           // codes, scales, zero points, from half to half
@@ -365,23 +311,18 @@ __global__ void __launch_bounds__(W4TileCfg<FORM>::kThreads, W4TileCfg<FORM>::kB
         step(r1, r0);
         if (b >= b1 || dead) break;
       }
-      if constexpr (FORM == kW4Few) {
-        wait(d_full(d), dph);
-        tc_fence_after();
-        drain(u, d);
-        d ^= 1;
-        if (d == 0) dph ^= 1;
-      }
     }
   }
-  if (FORM != kW4Few && warp >= kFirstAdd) {
+  if (warp >= kFirstAdd) {
     // ------------------------------ sums ------------------------------
     if constexpr (EXACT) regs_up<160>();
+    const int row = (warp & 3) * 32 + lane, col0 = (warp - kFirstAdd) / 4 * Cfg::kCols, cols = min(Cfg::kCols, p.bn - col0);
     const int gr = row & 7, quad = row >> 6;
+    const uint32_t lane_tmem = tmem + ((uint32_t)((warp & 3) * 32) << 16) + col0;
     int rs = 0, d = 0;
     uint32_t rph = 0, dph = 0;
     for (int u = cl; u < units; u += n_cl) {
-      const int quad0 = u % p.row_tiles * 2;
+      const int quad0 = u % p.row_tiles * 2, n = (quad0 * 4) * 16 + row;
       const int m = quad0 + quad < g.quads ? g.tiles_of(quad0 + quad) : 0;
       // the row's scales in a record: groups 128 bytes apart
       if constexpr (EXACT) {
@@ -416,7 +357,7 @@ __global__ void __launch_bounds__(W4TileCfg<FORM>::kThreads, W4TileCfg<FORM>::kB
             for (int c = 0; c < Cfg::kCols; c += 16) {
               if (c >= cols) break;
               uint32_t v[16];
-              tmem_ld16(lane_tmem + d * kAcc + c, v);
+              tmem_ld16(lane_tmem + d * kW4Acc + c, v);
               tmem_ld_wait();
 #pragma unroll
               for (int j = 0; j < 16; ++j) acc[c + j] = fmaf(__uint_as_float(v[j]), scale, acc[c + j]);
@@ -433,18 +374,58 @@ __global__ void __launch_bounds__(W4TileCfg<FORM>::kThreads, W4TileCfg<FORM>::kB
         // register, the stores were 40 KB of code, which cost more to fetch than to run: 50 us a unit).
 #pragma unroll
         for (int c = 0; c < Cfg::kCols; c += 16)
-          if (c < cols) tmem_st16f(lane_tmem + d * kAcc + c, acc + c);
+          if (c < cols) tmem_st16f(lane_tmem + d * kW4Acc + c, acc + c);
         tmem_st_wait();
         __syncwarp();
       } else {
         wait(d_full(d), dph);
         tc_fence_after();
       }
-      drain(u, d);
+      const int tok0 = u / p.row_tiles * p.bn + col0, n_tok = min(cols, a.T - tok0);
+      const uint32_t out_tmem = lane_tmem + d * kW4Acc;
+      if (cluster == 1) {
+        const float bias = a.bias && n < g.n ? to_float<BF16>(a.bias[n]) : 0.f;
+        const bool store = n < g.n && !*s_abort;
+        using Out = std::conditional_t<EXACT, float, uint16_t>;
+        Out *out = static_cast<Out *>(a.y) + (long long)tok0 * a.y_stride + n;
+#pragma unroll 1
+        for (int c = 0; c < n_tok; c += 16) {
+          uint32_t v[16];
+          tmem_ld16(out_tmem + c, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 16; ++j, out += a.y_stride)
+            if (store && c + j < n_tok) {
+              const float sum = __uint_as_float(v[j]) + bias;
+              if constexpr (EXACT) *out = sum; else *out = from_float<BF16>(sum);
+            }
+        }
+      } else {
+        // (one unit a cluster) token c of the tile goes to block c / share, where its sums stand [block][token][row]
+        const int share = (p.bn + cluster - 1) / cluster;
+        __syncwarp();
+        cluster_sync_all();                              // every block is done with its stages
+        int owner = col0 / share, left = share - col0 % share;
+#pragma unroll 1
+        for (int c = 0; c < cols; c += 8) {
+          uint32_t v[8];
+          tmem_ld8(out_tmem + c, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const uint32_t to = stage0 + ((rank * share + share - left) * 128 + row) * 4;
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa_u32(to, owner)), "f"(__uint_as_float(v[j])) : "memory");
+            if (--left == 0) { left = share; ++owner; }
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(d_empty(d));
       d ^= 1;
       if (d == 0) dph ^= 1;
     }
-  } else if (cluster > 1 && (FORM != kW4Few || warp < kFirstAdd)) {
+  } else if (cluster > 1) {
     __syncwarp();
     cluster_sync_all();
   }
@@ -457,7 +438,7 @@ __global__ void __launch_bounds__(W4TileCfg<FORM>::kThreads, W4TileCfg<FORM>::kB
     const int n_tok = min(min(share, p.bn - rank * share), a.T - tok0), row0 = cl % p.row_tiles * 128;
     const float *part = reinterpret_cast<const float *>(smem);
     if (!*s_abort)
-      for (int i = tid; i < n_tok * 128; i += Cfg::kThreads) {
+      for (int i = tid; i < n_tok * 128; i += kW4TileThreads) {
         const int t = i >> 7, n = row0 + (i & 127);
         float v = 0.f;
         for (int r = 0; r < cluster; ++r) v += part[(r * share) * 128 + i];
@@ -469,7 +450,7 @@ __global__ void __launch_bounds__(W4TileCfg<FORM>::kThreads, W4TileCfg<FORM>::kB
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(Cfg::kTmem) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
 }
 
