@@ -102,7 +102,7 @@ cudaError_t launch_w4_tile(const ft_dense *h, const W4Args &a, W4Tile p, cudaStr
   CUtensorMap tm;
   if (!make_x_map(h, &tm, a, p.bn)) return cudaErrorInvalidValue;
   const int smem = w4_tile_memory<EXACT>(a.g, p), units = p.row_tiles * p.tok_tiles, fit = h->clusters[p.cluster];
-  return launch_clusters(w4_tile_kernel<BF16, ZERO, EXACT>, dim3((p.cluster > 1 || units < fit ? units : fit) * p.cluster), kW4TileThreads, smem, p.cluster, st, tm, a, p);
+  return launch_clusters(w4_tile_kernel<BF16, ZERO, EXACT>, dim3((p.cluster > 1 || units < fit ? units : fit) * p.cluster), W4TileCfg<EXACT>::kThreads, smem, p.cluster, st, tm, a, p);
 }
 
 template <bool BF16, bool ZERO>
@@ -113,7 +113,7 @@ cudaError_t launch_w4_many(const ft_dense *h, const W4Args &a, cudaStream_t st) 
 
 template <bool BF16>
 cudaError_t launch_w4(const ft_dense *h, const W4Args &a, bool zero, cudaStream_t st) {
-  if (a.T > 32) return zero ? launch_w4_many<BF16, true>(h, a, st) : launch_w4_many<BF16, false>(h, a, st);
+  if (a.T > (a.out32 ? 32 : 16)) return zero ? launch_w4_many<BF16, true>(h, a, st) : launch_w4_many<BF16, false>(h, a, st);
   switch (a.g.group) {
     case 32: return zero ? launch_w4_tokens<BF16, 32, true>(h, a, st) : launch_w4_tokens<BF16, 32, false>(h, a, st);
     case 64: return zero ? launch_w4_tokens<BF16, 64, true>(h, a, st) : launch_w4_tokens<BF16, 64, false>(h, a, st);
@@ -162,7 +162,7 @@ cudaError_t count_clusters(ft_dense *h) {
   for (int c = 1; c <= kW4MaxCluster; ++c) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(c * h->sm_count);
-    cfg.blockDim = dim3(kW4TileThreads);
+    cfg.blockDim = dim3(W4TileCfg<false>::kThreads);
     cfg.dynamicSmemBytes = kMaxSmem;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;

@@ -18,7 +18,7 @@
 
 namespace ftmoe {
 
-constexpr int kW4TileThreads = 512, kW4Ops = 2;                 // operands of 128 k in tensor memory
+constexpr int kW4Ops = 2;                                       // operands of 128 k in tensor memory
 constexpr int kW4Acc = 192, kW4OpAt = 2 * kW4Acc;               // columns of an accumulator; where the operands stand (64 columns each)
 static_assert(kW4OpAt + kW4Ops * 64 <= 512, "tensor memory");
 
@@ -30,7 +30,8 @@ struct W4Tile {
 
 template <bool EXACT>
 struct W4TileCfg {
-  static constexpr int kAdd = EXACT ? 8 : 4, kExpand = EXACT ? 4 : 8;            // warps
+  static constexpr int kThreads = EXACT ? 512 : 768, kAdd = EXACT ? 8 : 4, kExpand = EXACT ? 4 : 16;     // of its warps: the last ones, those from 4 on
+  static constexpr int kTilesEach = EXACT ? 2 : 1, kHalvesEach = EXACT ? 2 : 1;  // tiles, and halves of 64 k, of an expanding warp
   static constexpr int kCols = kW4Acc / (kAdd / 4);                              // tokens of an adding warp
   static constexpr int kStage = kW4Acc * 256, kStages = 3;                       // 128 k of the tokens: two boxes of 64
   static constexpr int kRaw = EXACT ? 3 : 6;                                     // slots of records
@@ -58,7 +59,7 @@ inline W4Tile w4_tile_share(const W4Geom &g, int T, bool exact, const int *clust
       const long long units = (long long)row_tiles * tok_tiles, fit = clusters[cluster];
       if (fit == 0 || (cluster > 1 && units > fit)) continue;
       double block = 4. * bn;
-      const double expand = exact ? 700 : 400, add = exact ? per * (300 + 4. * bn) : 0.;
+      const double expand = exact ? 850 : 750, add = exact ? per * (300 + 4. * bn) : 0.;
       if (block < expand) block = expand;
       if (block < add) block = add;
       const double cost = (double)((units + fit - 1) / fit) * ((double)((g.nb + cluster - 1) / cluster) * block + 4000 + (cluster > 1 ? 2000 : 0));
@@ -75,7 +76,7 @@ template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setma
 template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 template <bool BF16, bool ZERO, bool EXACT>
-__global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const W4Args a, const W4Tile p) {
+__global__ void __launch_bounds__(W4TileCfg<EXACT>::kThreads, 1) w4_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const W4Args a, const W4Tile p) {
   using Cfg = W4TileCfg<EXACT>;
   constexpr int kRaw = Cfg::kRaw;
   extern __shared__ unsigned char smem_raw[];
@@ -121,7 +122,7 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
   const int cluster = p.cluster, rank = blockIdx.x % cluster, units = p.row_tiles * p.tok_tiles, n_cl = gridDim.x / cluster, cl = blockIdx.x / cluster;
   const int b0 = (int)((long long)g.nb * rank / cluster), b1 = (int)((long long)g.nb * (rank + 1) / cluster);
   const int per = kW4Block / g.group, rec4 = g.record(4);       // groups of a record
-  constexpr int kFirstAdd = 16 - Cfg::kAdd, kFirstExpand = 4;
+  constexpr int kFirstAdd = Cfg::kThreads / 32 - Cfg::kAdd, kFirstExpand = 4;
 
   if (warp < 4) {
     if constexpr (EXACT) regs_down<80>();
@@ -218,11 +219,11 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
     }
   } else if (warp < kFirstExpand + Cfg::kExpand) {
     // ------------------------------ expansion ------------------------------
-    // A warp has the tiles of its quarter of tensor memory, both or one of them; what is not there (rows past the last) is expanded from
-    // whatever the slot holds: its operands reach no other row.
+    // A warp has the tiles of its quarter of tensor memory, both or one of them, with both halves of the 128 k or one; what is not there (rows
+    // past the last) is expanded from whatever the slot holds: its operands reach no other row.
     if constexpr (EXACT) regs_down<96>();
-    constexpr int kMine = 8 / Cfg::kExpand;
-    const int tile0 = 2 * (warp & 3) + (kMine == 1 ? (warp - kFirstExpand) >> 2 : 0), gr = lane >> 2;
+    constexpr int kMine = Cfg::kTilesEach, kHalves = Cfg::kHalvesEach;
+    const int tile0 = 2 * (warp & 3) + (kMine == 1 ? (warp - kFirstExpand) >> 2 & 1 : 0), half0 = kHalves == 1 ? (warp - kFirstExpand) >> 3 : 0, gr = lane >> 2;
     const W4Const<BF16> con;
     const uint32_t dst = tmem + kW4OpAt + ((uint32_t)(tile0 * 16) << 16);
     int s = 0, rs = 0;
@@ -240,21 +241,21 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
         z_at[j] = rec + m * 2 * kW4TileBytes + per * 128 + gr * 8 + (t & 3) * 2;
       }
       struct Rec {
-        uint4 w[2][kMine];
-        uint32_t z[2][2][kMine], sc[2][2][kMine];    // per half and 32 k of it
+        uint4 w[kHalves][kMine];
+        uint32_t z[kHalves][2][kMine], sc[kHalves][2][kMine];    // per half and 32 k of it
       };
       auto take = [&](Rec &r) {
         wait(raw_full(rs), rph);
         const uint32_t at = rs * p.raw_bytes;
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+        for (int half = 0; half < kHalves; ++half)
 #pragma unroll
           for (int j = 0; j < kMine; ++j) {
-            r.w[half][j] = lds_v4(src[j] + at + half * next[j]);
+            r.w[half][j] = lds_v4(src[j] + at + (half0 + half) * next[j]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              if (!EXACT) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r.sc[half][h][j]) : "r"(sc_at[j] + at + (half * 2 + h) * per / 4 * 128));
-              if (ZERO) asm volatile("ld.shared.u16 %0, [%1];" : "=r"(r.z[half][h][j]) : "r"(z_at[j] + at + (half * 2 + h) * per / 4 * 64));
+              if (!EXACT) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r.sc[half][h][j]) : "r"(sc_at[j] + at + ((half0 + half) * 2 + h) * per / 4 * 128));
+              if (ZERO) asm volatile("ld.shared.u16 %0, [%1];" : "=r"(r.z[half][h][j]) : "r"(z_at[j] + at + ((half0 + half) * 2 + h) * per / 4 * 64));
             }
           }
       };
@@ -265,7 +266,7 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
       };
       auto expand = [&](const Rec &rec) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+        for (int half = 0; half < kHalves; ++half)
 #pragma unroll
           for (int j = 0; j < kMine; ++j) {
             const uint32_t words[4] = {rec.w[half][j].x, rec.w[half][j].y, rec.w[half][j].z, rec.w[half][j].w};
@@ -284,7 +285,7 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
                 r[4 * i + 2] = mul_pair<BF16>(r[4 * i + 2], s_hi); r[4 * i + 3] = mul_pair<BF16>(r[4 * i + 3], s_hi);
               }
             }
-            tmem_st_16x256b_x4(dst + ((uint32_t)(j * 16) << 16) + s * 64 + half * 32, r);
+            tmem_st_16x256b_x4(dst + ((uint32_t)(j * 16) << 16) + s * 64 + (half0 + half) * 32, r);
           }
         tmem_st_wait();
         tc_fence_before();
@@ -438,7 +439,7 @@ __global__ void __launch_bounds__(kW4TileThreads, 1) w4_tile_kernel(const __grid
     const int n_tok = min(min(share, p.bn - rank * share), a.T - tok0), row0 = cl % p.row_tiles * 128;
     const float *part = reinterpret_cast<const float *>(smem);
     if (!*s_abort)
-      for (int i = tid; i < n_tok * 128; i += kW4TileThreads) {
+      for (int i = tid; i < n_tok * 128; i += Cfg::kThreads) {
         const int t = i >> 7, n = row0 + (i & 127);
         float v = 0.f;
         for (int r = 0; r < cluster; ++r) v += part[(r * share) * 128 + i];
