@@ -1,11 +1,14 @@
 """A small decoder served with continuous batching: the attention operators and the expert-cached MoE layer together.
 
-    python examples/serve_decoder.py [--layers 4] [--requests 12] [--new 24]
+    python examples/serve_decoder.py [--layers 4] [--requests 12] [--new 24] [--w4]
 
 Random weights, random prompts, greedy answers.  Every step is one packed batch: running requests bring one token each, prompts
 come in chunks, requests that do not get pages wait, finished ones give theirs back.  Per step the page bookkeeping runs once
 (``FtAttn.slots``); per layer: projection, ``FtAttn.qk_rope`` into the layer's cache, ``FtAttn.forward``, output projection, router
 and ``FtMoe.layer`` over the host pool of experts.  The host only reads back the answers and who was admitted.
+
+With ``--w4`` the projections and the output head have 4-bit weights with group scales (``FtDense.w4``), residual and norm between the blocks
+are one call (``FtDense.add_norm``), and the answers come with their log probabilities and the entropy (``FtDense.logprobs``).
 """
 from __future__ import annotations
 
@@ -20,16 +23,25 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 from paper_2608_16157_b200 import attention as A      # noqa: E402
 from paper_2608_16157_b200 import binding as B        # noqa: E402
+from paper_2608_16157_b200 import dense as D          # noqa: E402
 from paper_2608_16157_b200 import workload as W       # noqa: E402
 
 EPS = 1e-6
+
+
+def quantise(w, group=64):
+    """4-bit codes, two in a byte, and group scales of a [k, n] matrix, as ``FtDense.w4_pack`` takes them ([n, k / 2], [n, k / group])."""
+    g = w.float().t().contiguous().view(w.shape[1], -1, group)
+    scales = (g.abs().amax(-1) / 7).clamp(min=1e-8).to(w.dtype)
+    q = (g / scales.float()[..., None]).round().clamp(-8, 7).add(8).to(torch.uint8).reshape(w.shape[1], -1)
+    return (q[:, 0::2] | (q[:, 1::2] << 4)).contiguous(), scales
 
 
 class Decoder:
     """Weights, expert pool, caches and handles of an L-layer decoder; :meth:`step` runs one packed batch."""
 
     def __init__(self, *, layers=2, shape=W.TINY, n_q_heads=4, n_kv_heads=2, head_dim=64, vocab=512, page_tokens=16, n_pages=64,
-                 max_requests=8, max_tokens=128, max_pages=32, expert_slots=4, rope_base=1e6, seed=0, device="cuda:0"):
+                 max_requests=8, max_tokens=128, max_pages=32, expert_slots=4, rope_base=1e6, seed=0, device="cuda:0", w4=False):
         self.L, self.shape, self.vocab, self.dev = layers, shape, vocab, torch.device(device)
         self.hq, self.hkv, self.d = n_q_heads, n_kv_heads, head_dim
         g = torch.Generator(device=self.dev)
@@ -63,11 +75,20 @@ class Decoder:
         self.n_free, self.n_free_next = torch.tensor([n_pages], dtype=torch.int32, device=self.dev), i32(1)
         self.ctx, self.ctx_next = i32(max_requests), i32(max_requests)
         self.q_start, self.admitted = i32(max_requests + 1), i32(max_requests)
+        # with 4-bit weights: the handle, the matrices laid out once
+        self.dense = None
+        if w4:
+            self.dense = D.FtDense(self.dev.index)
+            pack = lambda w: self.dense.w4_pack(*quantise(w))
+            self.w4_qkv, self.w4_o, self.w4_head = [pack(w) for w in self.w_qkv], [pack(w) for w in self.w_o], pack(self.head)
+            self.answer_logprob = self.answer_entropy = None       # of the latest step's answers
         self.record = None          # a list: (layer, attention input, attention output) of every step go there
 
     def close(self):
         self.attn.destroy()
         self.moe.destroy()
+        if self.dense is not None:
+            self.dense.destroy()
         self.pool.free()
 
     @staticmethod
@@ -91,6 +112,8 @@ class Decoder:
         x = self.embed[torch.tensor(tokens, device=self.dev)]
         q_rot, out = (torch.empty(t, hq, d, dtype=torch.bfloat16, device=self.dev) for _ in range(2))
         y = torch.empty_like(x)
+        if self.dense is not None:
+            return self._step_w4(new_len, t, x, y, q_rot, out, position, slot)
         for layer in range(self.L):
             h = self._norm(x)
             qkv = h @ self.w_qkv[layer]
@@ -107,6 +130,34 @@ class Decoder:
         last = (self.q_start[1:len(new_len) + 1].long() - 1).clamp(min=0)
         answers = (self._norm(x[last]) @ self.head).float().argmax(-1)
         both = torch.stack([answers.to(torch.int32), self.admitted[:len(new_len)]]).tolist()     # one read back
+        return both[0], both[1]
+
+
+    def _step_w4(self, new_len, t, x, y, q_rot, out, position, slot):
+        """The same with 4-bit weights: x is the residual stream, y the output of the block at hand."""
+        n, hq, hkv, d, dense = len(new_len), self.hq, self.hkv, self.d, self.dense
+        h = torch.empty_like(x)
+        qkv = torch.empty(t, (hq + 2 * hkv) * d, dtype=x.dtype, device=self.dev)
+        for layer in range(self.L):
+            dense.add_norm(y if layer else None, x, x, h, eps=EPS)
+            dense.w4(h, self.w4_qkv[layer], qkv)
+            self.attn.qk_rope(qkv[:, :hq * d].unflatten(1, (hq, d)), qkv[:, hq * d:(hq + hkv) * d].unflatten(1, (hkv, d)),
+                              qkv[:, (hq + hkv) * d:].unflatten(1, (hkv, d)), q_rot, self.cache[layer], position, slot, self.cos_sin,
+                              w_q=self.w_q[layer], w_k=self.w_k[layer], eps=EPS)
+            self.attn.forward(q_rot, self.cache[layer], self.table, out)
+            if self.record is not None:
+                self.record.append((layer, h.clone(), out.clone()))
+            dense.w4(out.flatten(1), self.w4_o[layer], y)
+            dense.add_norm(y, x, x, h, eps=EPS)
+            self.moe.layer(layer, h.float() @ self.router[layer], h, y, t)
+        dense.add_norm(y, x, None, h, eps=EPS)
+        last = (self.q_start[1:n + 1].long() - 1).clamp(min=0)
+        logits = torch.empty(n, self.vocab, device=self.dev)
+        dense.w4(h[last], self.w4_head, logits)
+        answers = torch.empty(n, 1, dtype=torch.int32, device=self.dev)
+        self.answer_logprob, self.answer_entropy = torch.empty(n, 1, device=self.dev), torch.empty(n, device=self.dev)
+        dense.logprobs(logits, entropy=self.answer_entropy, top_ids=answers, top_logprobs=self.answer_logprob)
+        both = torch.stack([answers[:, 0], self.admitted[:n]]).tolist()
         return both[0], both[1]
 
 
@@ -165,15 +216,18 @@ def main():
     ap.add_argument("--layers", type=int, default=4)
     ap.add_argument("--requests", type=int, default=12)
     ap.add_argument("--new", type=int, default=24)
+    ap.add_argument("--w4", action="store_true", help="4-bit projections and output head")
     args = ap.parse_args()
     rng = np.random.default_rng(0)
-    dec = Decoder(layers=args.layers, n_pages=40)
+    dec = Decoder(layers=args.layers, n_pages=40, w4=args.w4)
     prompts = [rng.integers(0, dec.vocab, int(rng.integers(1, 150))).tolist() for _ in range(args.requests)]
     answers = serve(dec, prompts, args.new, log=print)
     for p, a in zip(prompts[:4], answers):
         print(f"prompt of {len(p)} tokens -> {a}")
     assert dec.attn.sync_status() == 0 and dec.moe.sync_status() == 0
     assert int(dec.n_free) == 40              # every page came back
+    if dec.dense is not None:
+        print("dense kernels:", dec.dense.launch_count(), " status:", dec.dense.sync_status())
     print("attention-side kernels:", dec.attn.launch_count(), " MoE kernels:", dec.moe.launch_count())
     dec.close()
 

@@ -57,10 +57,11 @@ size_t ft_dense_w4_bytes(int64_t n, int64_t k, int group, int has_zeros);
 ft_status_t ft_dense_w4_pack(ft_dense_t *h, int64_t n, int64_t k, int group, int dtype, const uint8_t *codes, int64_t codes_stride,
                              const void *scales, const uint8_t *zeros, void *image, void *stream);
 
-/* y[t][i] = sum_k x[t][k] * w[i][k] + bias[i].  x DEVICE [T][k] of `dtype`, 16-byte aligned, x_stride a multiple of 8; bias DEVICE [n] of
- * `dtype` or NULL; y DEVICE [T][n] of out_dtype (`dtype` or fp32), any alignment of whole elements.  The codes less their zero point
- * are multiplied exactly, sums are float, scales are applied to the sums of a group in float, y is rounded once.
- * n, k, group, dtype and has_zeros must be those of the image. */
+/* y[t][i] = sum_k x[t][k] * w[i][k] + bias[i].  x DEVICE [T][k] of `dtype`, 16-byte aligned, x_stride a multiple of 8 and < 2^38; bias DEVICE
+ * [n] of `dtype` or NULL; y DEVICE [T][n] of out_dtype (`dtype` or fp32), any alignment of whole elements.  Up to 16 tokens, and for fp32
+ * results at any number, the codes less their zero point are multiplied exactly, sums are float, and scales are applied to the sums of a
+ * group in float.  For 16-bit results of more tokens each weight is rounded once to `dtype` before it is multiplied (an error of the size of
+ * the result's own rounding).  y is rounded once.  n, k, group, dtype and has_zeros must be those of the image. */
 ft_status_t ft_dense_w4_forward(ft_dense_t *h, int T, int64_t n, int64_t k, int group, int dtype, int has_zeros, const void *x,
                                 int64_t x_stride, const void *image, const void *bias, void *y, int64_t y_stride, int out_dtype,
                                 void *stream);
@@ -83,6 +84,13 @@ ft_status_t ft_dense_logprobs(ft_dense_t *h, int T, int64_t vocab, int dtype, co
 
 /* Waits for the device and returns (and clears) the latched device status. */
 ft_status_t ft_dense_sync_status(ft_dense_t *h);
+/* Test hook for the failure path of the bounded device-side waits, as ft_moe_debug_inject: withhold_mask names kernels whose first producer
+ * leaves out one copy, wait_polls is the poll limit of every wait from now on (0 = the default, 2^22).  The kernel then gives up, latches
+ * FT_ERR_TIMEOUT and runs to completion; ft_dense_sync_status reports it once.  Per process and device; (0, 0) restores normal operation.
+ * Waits for the device. */
+enum { FT_DENSE_DEBUG_WITHHOLD_STREAM = 1,   /* 4-bit products of few tokens */
+       FT_DENSE_DEBUG_WITHHOLD_TILE = 2 };   /* 4-bit products of many tokens */
+ft_status_t ft_dense_debug_inject(ft_dense_t *h, uint32_t withhold_mask, uint32_t wait_polls);
 /* Number of kernels this handle has launched since create. */
 ft_status_t ft_dense_launch_count(ft_dense_t *h, uint64_t *out);
 /* Text of the CUDA runtime error behind the most recent FT_ERR_CUDA / FT_ERR_OOM of a ft_dense_ call. */

@@ -299,7 +299,7 @@ ft_status_t ft_dense_w4_forward(ft_dense_t *h, int T, int64_t n, int64_t k, int 
   if (T == 0) return FT_OK;
   const bool out32 = out_dtype == FT_DENSE_FP32;
   if (!x || !image || !y || !aligned(x, 16) || !aligned(image, 16) || !aligned(bias, 2) || !aligned(y, out32 ? 4 : 2)) return FT_ERR_INVALID_ARG;
-  if (T > 1 && (x_stride < k || x_stride % 8 || y_stride < n)) return FT_ERR_INVALID_ARG;
+  if (T > 1 && (x_stride < k || x_stride % 8 || x_stride >= (1ll << 38) || y_stride < n)) return FT_ERR_INVALID_ARG;
   DeviceScope dev(h->device);
   FD_CUDA(dev.err);
   W4Args a;
@@ -351,6 +351,18 @@ ft_status_t ft_dense_sync_status(ft_dense_t *h) {
   FD_CUDA(cudaMemset(h->status_dev, 0, sizeof(st)));
   FD_CUDA(cudaDeviceSynchronize());
   return (st & kStatTimeout) ? FT_ERR_TIMEOUT : FT_ERR_INVALID_ARG;
+}
+
+ft_status_t ft_dense_debug_inject(ft_dense_t *h, uint32_t withhold_mask, uint32_t wait_polls) {
+  if (!h) return FT_ERR_INVALID_ARG;
+  DeviceScope dev(h->device);
+  FD_CUDA(dev.err);
+  const uint32_t polls = wait_polls ? wait_polls : kDefaultWaitPolls;
+  FD_CUDA(cudaDeviceSynchronize());
+  FD_CUDA(cudaMemcpyToSymbol(g_debug_withhold, &withhold_mask, sizeof(withhold_mask)));
+  FD_CUDA(cudaMemcpyToSymbol(g_wait_polls, &polls, sizeof(polls)));
+  FD_CUDA(cudaDeviceSynchronize());
+  return FT_OK;
 }
 
 ft_status_t ft_dense_launch_count(ft_dense_t *h, uint64_t *out) {

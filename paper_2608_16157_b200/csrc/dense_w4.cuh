@@ -25,6 +25,7 @@
 namespace ftmoe {
 
 constexpr int kW4TileBytes = 512, kW4Block = 128;
+constexpr uint32_t kWithholdW4Stream = 1u, kWithholdW4Tile = 2u;   // ft_dense_debug_inject
 
 struct W4Geom {
   int32_t n, k, nb, tiles, quads, group, zeros;   // nb: blocks of 128 k
@@ -253,11 +254,13 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32, 1) w4_stream_kernel(const W
     in_left = n_b;
   };
   const uint32_t slots_at = smem_u32(s_slot);
+  bool withhold = blockIdx.x == 0 && blockIdx.y == 0 && warp == 0 && (g_debug_withhold & kWithholdW4Stream);
   auto bring = [&]() {
     if (in_quad >= g.quads) return;
-    if (lane == 0) {
+    if (lane == 0 && !*s_abort) {
       mbar_expect_tx(bars + 8 * in_slot, in_bytes);
-      bulk_g2s(slots_at + in_slot * p.slot_bytes, in_at, in_bytes, bars + 8 * in_slot);
+      if (!withhold) bulk_g2s(slots_at + in_slot * p.slot_bytes, in_at, in_bytes, bars + 8 * in_slot);     // (withheld: test hook)
+      withhold = false;
     }
     if (++in_slot == p.slots) in_slot = 0;
     in_at += workers * in_bytes;

@@ -98,6 +98,8 @@ __global__ void __launch_bounds__(W4TileCfg<EXACT>::kThreads, 1) w4_tile_kernel(
   auto d_empty = [&](int i) { return bars + 8u * (kD + 2 + i); };
   auto wait = [&](uint32_t bar, uint32_t phase) { return mbar_try_wait(bar, phase) || mbar_wait(bar, phase, s_abort, a.status); };
 
+  auto given_up = [&]() { return __any_sync(0xffffffffu, *s_abort) != 0; };      // (the same for all lanes: what follows elects one of all)
+
   grid_let_next();
   if (tid == 0) {
     for (int i = 0; i < kRaw; ++i) { mbar_init(raw_full(i), 1); mbar_init(raw_empty(i), EXACT ? Cfg::kAdd + Cfg::kExpand : Cfg::kExpand); }
@@ -133,8 +135,9 @@ __global__ void __launch_bounds__(W4TileCfg<EXACT>::kThreads, 1) w4_tile_kernel(
       uint32_t ph = 1;
       for (int u = cl; u < units; u += n_cl) {
         const int tok0 = u / p.row_tiles * p.bn;
-        for (int b = b0; b < b1 && !*s_abort; ++b) {
+        for (int b = b0; b < b1; ++b) {
           wait(x_empty(s), ph);
+          if (given_up()) break;        // (a barrier may still expect its bytes: it must not be armed again)
           if (elect_one()) {
             const uint32_t to = stage0 + s * Cfg::kStage;
             mbar_expect_tx(x_full(s), 2 * p.bn * 128);
@@ -146,6 +149,7 @@ __global__ void __launch_bounds__(W4TileCfg<EXACT>::kThreads, 1) w4_tile_kernel(
       }
     } else if (warp == 2) {
       // ------------------------------ records ------------------------------
+      bool withhold = blockIdx.x == 0 && (g_debug_withhold & kWithholdW4Tile);
       int s = 0;
       uint32_t ph = 1;
       for (int u = cl; u < units; u += n_cl) {
@@ -153,13 +157,15 @@ __global__ void __launch_bounds__(W4TileCfg<EXACT>::kThreads, 1) w4_tile_kernel(
         const bool two = quad + 1 < g.quads;
         const int r0 = g.record(g.tiles_of(quad)), r1 = two ? g.record(g.tiles_of(quad + 1)) : 0;
         const uint8_t *src0 = a.image + g.quad_at(quad) + (long long)b0 * r0, *src1 = a.image + g.quad_at(quad + 1) + (long long)b0 * r1;
-        for (int b = b0; b < b1 && !*s_abort; ++b, src0 += r0, src1 += r1) {
+        for (int b = b0; b < b1; ++b, src0 += r0, src1 += r1) {
           wait(raw_empty(s), ph);
+          if (given_up()) break;
           if (elect_one()) {
             mbar_expect_tx(raw_full(s), r0 + r1);
-            bulk_g2s(rec0 + s * p.raw_bytes, src0, r0, raw_full(s));
+            if (!withhold) bulk_g2s(rec0 + s * p.raw_bytes, src0, r0, raw_full(s));      // (withheld: test hook)
             if (two) bulk_g2s(rec0 + s * p.raw_bytes + rec4, src1, r1, raw_full(s));
           }
+          withhold = false;
           if (++s == kRaw) { s = 0; ph ^= 1; }
         }
       }
@@ -174,7 +180,7 @@ __global__ void __launch_bounds__(W4TileCfg<EXACT>::kThreads, 1) w4_tile_kernel(
         for (int u = cl; u < units; u += n_cl) {
           if (!EXACT) wait(d_empty(d), dph);
           for (int b = b0, dead = 0; b < b1 && !dead; ++b) {
-            dead = *s_abort;
+            dead = given_up();
             wait(x_full(s), ph);
             const bool ok = wait(w_full(o), oph);
             const uint64_t x_desc = umma_desc(stage_u + s * Cfg::kStage, 16, 1024);
@@ -297,7 +303,7 @@ __global__ void __launch_bounds__(W4TileCfg<EXACT>::kThreads, 1) w4_tile_kernel(
       Rec r0, r1;
       int b = b0, dead = 0;
       auto step = [&](const Rec &now, Rec &then) {
-        dead = *s_abort;
+        dead = given_up();
         give_back();
         if (b + 1 < b1) take(then);
         wait(w_empty(s), ph);
@@ -344,7 +350,7 @@ __global__ void __launch_bounds__(W4TileCfg<EXACT>::kThreads, 1) w4_tile_kernel(
         };
         fetch();
         for (int b = b0, dead = 0; b < b1 && !dead; ++b) {
-          dead = *s_abort;
+          dead = given_up();
 #pragma unroll
           for (int i = 0; i < 4; ++i) sc[i] = sc_next[i];
           if (b + 1 < b1) fetch();

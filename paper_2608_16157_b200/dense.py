@@ -27,7 +27,7 @@ _CODE = {torch.bfloat16: FT_DENSE_BF16, torch.float16: FT_DENSE_FP16, torch.floa
 # every symbol include/ftdense.h declares
 SYMBOLS = (
     "ft_dense_create", "ft_dense_destroy", "ft_dense_add_norm", "ft_dense_w4_bytes", "ft_dense_w4_pack", "ft_dense_w4_forward",
-    "ft_dense_logprobs", "ft_dense_sync_status", "ft_dense_launch_count", "ft_dense_last_cuda_error",
+    "ft_dense_logprobs", "ft_dense_sync_status", "ft_dense_debug_inject", "ft_dense_launch_count", "ft_dense_last_cuda_error",
 )
 
 _lib = None
@@ -49,6 +49,7 @@ def load():
         "ft_dense_w4_forward": (i32, [vp, i32, i64, i64, i32, i32, i32, vp, i64, vp, vp, vp, i64, i32, vp]),
         "ft_dense_logprobs": (i32, [vp, i32, i64, i32, vp, i64, f32, vp, i64, i32, vp, vp, i32, vp, vp, vp]),
         "ft_dense_sync_status": (i32, [vp]),
+        "ft_dense_debug_inject": (i32, [vp, C.c_uint32, C.c_uint32]),
         "ft_dense_launch_count": (i32, [vp, C.POINTER(C.c_uint64)]),
         "ft_dense_last_cuda_error": (C.c_char_p, []),
     }
@@ -239,6 +240,9 @@ class FtDense:
 
     def sync_status(self):
         return int(self._lib.ft_dense_sync_status(self._h))
+
+    def debug_inject(self, withhold_mask, wait_polls):
+        _check(self._lib.ft_dense_debug_inject(self._h, int(withhold_mask), int(wait_polls)), "ft_dense_debug_inject")
 
     def launch_count(self):
         n = C.c_uint64()
