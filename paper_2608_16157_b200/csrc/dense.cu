@@ -48,8 +48,9 @@ template <bool BF16, bool RES32, bool POST, bool GATE, int E>
 cudaError_t launch_norm_form(const NormArgs &a, bool wide, cudaStream_t st) {
   const int threads = a.lanes > 32 ? a.lanes : 128, rows = threads / a.lanes;
   const unsigned grid = (unsigned)((a.T + rows - 1) / rows);
-  return wide ? launch(add_norm_kernel<BF16, RES32, POST, GATE, 8, E>, grid, threads, 0, st, a)
-              : launch(add_norm_kernel<BF16, RES32, POST, GATE, 1, E>, grid, threads, 0, st, a);
+  if (!wide) return launch(add_norm_kernel<BF16, RES32, POST, GATE, 1, false, E>, grid, threads, 0, st, a);
+  return a.wide == kWideAll ? launch(add_norm_kernel<BF16, RES32, POST, GATE, 8, true, E>, grid, threads, 0, st, a)
+                            : launch(add_norm_kernel<BF16, RES32, POST, GATE, 8, false, E>, grid, threads, 0, st, a);
 }
 template <bool BF16, bool RES32, int E>
 cudaError_t launch_norm_elems(NormArgs a, bool wide, cudaStream_t st) {
@@ -256,10 +257,12 @@ ft_status_t ft_dense_add_norm(ft_dense_t *h, int T, int d, int dtype, int res_dt
   a.res = res; a.res_out = res_out; a.out = static_cast<uint16_t *>(out);
   a.y_stride = y_stride; a.res_stride = res_stride; a.gate_stride = gate_stride; a.res_out_stride = res_out_stride; a.out_stride = out_stride;
   a.w_offset = w_offset; a.eps = eps; a.res_scale = res_scale; a.y_scale = y_scale;
-  // 16-byte pieces where every row starts on one
-  auto rows16 = [&](const void *p, int64_t stride, int bytes) { return !p || (aligned(p, 16) && (T == 1 || stride * bytes % 16 == 0)); };
-  const bool wide = d % 8 == 0 && rows16(y, y_stride, 2) && rows16(res, res_stride, res32 ? 4 : 2) && rows16(res_out, res_out_stride, res32 ? 4 : 2) &&
-                    rows16(out, out_stride, 2) && (!gate || gate_step == 0 || rows16(gate, gate_stride, 2)) && aligned(w_post, 16) && aligned(w_pre, 16);
+  auto rows16 = [&](const void *p, int64_t stride, int bytes) { return aligned(p, 16) && (T == 1 || stride * bytes % 16 == 0); };
+  a.wide = (rows16(y, y_stride, 2) ? kWideY : 0u) | (rows16(res, res_stride, res32 ? 4 : 2) ? kWideRes : 0u) | (rows16(gate, gate_stride, 2) ? kWideGate : 0u) |
+           (aligned(w_post, 16) ? kWidePost : 0u) | (aligned(w_pre, 16) ? kWidePre : 0u) | (rows16(res_out, res_out_stride, res32 ? 4 : 2) ? kWideResOut : 0u) |
+           (rows16(out, out_stride, 2) ? kWideOut : 0u);
+  // eight elements at a time, unless hardly an array would have them in one access
+  const bool wide = d % 8 == 0 && ((a.wide & kWideY) || (a.wide & kWideRes));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool bf = dtype == FT_DENSE_BF16;
   FD_CUDA(bf ? (res32 ? launch_norm<true, true>(h, a, wide, st) : launch_norm<true, false>(h, a, wide, st))
@@ -294,7 +297,7 @@ ft_status_t ft_dense_w4_pack(ft_dense_t *h, int64_t n, int64_t k, int group, int
 ft_status_t ft_dense_w4_forward(ft_dense_t *h, int T, int64_t n, int64_t k, int group, int dtype, int has_zeros, const void *x,
                                 int64_t x_stride, const void *image, const void *bias, void *y, int64_t y_stride, int out_dtype,
                                 void *stream) {
-  if (!h || T < 0 || !type16(dtype) || (out_dtype != dtype && out_dtype != FT_DENSE_FP32)) return FT_ERR_INVALID_ARG;
+  if (!h || T < 0 || T > (1 << 20) || !type16(dtype) || (out_dtype != dtype && out_dtype != FT_DENSE_FP32)) return FT_ERR_INVALID_ARG;
   if (!w4_ok(n, k, group)) return FT_ERR_UNSUPPORTED;
   if (T == 0) return FT_OK;
   const bool out32 = out_dtype == FT_DENSE_FP32;

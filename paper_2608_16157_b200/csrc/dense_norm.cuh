@@ -3,8 +3,9 @@
 // Bound: HBM (y, r and a gate per element read once, r' and h written once) for many tokens, launch latency for few.
 // `lanes` threads (32 .. 1024, a power of two) share a row; a thread holds E of its elements in float from the loads to the stores, so that
 // a row is read once, whatever is written over it.  All loads of y, r and the gate go out before the first sum.  E = 16, or 8 for few rows, where
-// latency counts.  A vector (8 elements) a load where every address allows 16-byte accesses, else single elements, neighbouring threads on
-// neighbouring elements (twice the time: the load and store units are then the bound).
+// latency counts.  Where d is a multiple of 8 a thread has 8 neighbouring elements at a time, in one access for each array whose rows all
+// start on 16 bytes; else single elements, neighbouring threads on neighbouring elements (twice the time: the load and store units are
+// then the bound).
 #pragma once
 #include "async.cuh"
 #include "common.cuh"
@@ -13,8 +14,11 @@ namespace ftmoe {
 
 constexpr int kNormMaxDim = 16384;
 
+enum : uint32_t { kWideY = 1, kWideRes = 2, kWideGate = 4, kWidePost = 8, kWidePre = 16, kWideResOut = 32, kWideOut = 64, kWideAll = 127 };
+
 struct NormArgs {
   int32_t T, d, lanes, post, gate_step;
+  uint32_t wide;                     // kWide*: arrays that allow 16-byte accesses
   const uint16_t *y, *gate, *w_post, *w_pre;
   const void *res;
   void *res_out;
@@ -54,8 +58,13 @@ __device__ __forceinline__ uint32_t from_float2(float a, float b) {
 
 // VEC elements of a 16-bit or a float array.
 template <bool BF16, int VEC>
-__device__ __forceinline__ void load_16(const uint16_t *p, float *x) {
+__device__ __forceinline__ void load_16(const uint16_t *p, float *x, bool wide) {
   if constexpr (VEC == 8) {
+    if (!wide) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = to_float<BF16>(p[i]);
+      return;
+    }
     const uint4 v = *reinterpret_cast<const uint4 *>(p);
     to_float2<BF16>(v.x, x[0], x[1]); to_float2<BF16>(v.y, x[2], x[3]);
     to_float2<BF16>(v.z, x[4], x[5]); to_float2<BF16>(v.w, x[6], x[7]);
@@ -64,8 +73,13 @@ __device__ __forceinline__ void load_16(const uint16_t *p, float *x) {
   }
 }
 template <int VEC>
-__device__ __forceinline__ void load_32(const float *p, float *x) {
+__device__ __forceinline__ void load_32(const float *p, float *x, bool wide) {
   if constexpr (VEC == 8) {
+    if (!wide) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = p[i];
+      return;
+    }
     const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
   } else {
@@ -73,21 +87,26 @@ __device__ __forceinline__ void load_32(const float *p, float *x) {
   }
 }
 template <bool BF16, int VEC>
-__device__ __forceinline__ void store_16(uint16_t *p, const float *x) {
-  if constexpr (VEC == 8)
-    *reinterpret_cast<uint4 *>(p) = make_uint4(from_float2<BF16>(x[0], x[1]), from_float2<BF16>(x[2], x[3]), from_float2<BF16>(x[4], x[5]),
-                                               from_float2<BF16>(x[6], x[7]));
-  else
-    *p = from_float<BF16>(x[0]);
+__device__ __forceinline__ void store_16(uint16_t *p, const float *x, bool wide) {
+  if (VEC == 8 && wide) {
+    *reinterpret_cast<uint4 *>(p) = make_uint4(from_float2<BF16>(x[0], x[VEC > 1]), from_float2<BF16>(x[VEC / 4], x[VEC * 3 / 8]),
+                                               from_float2<BF16>(x[VEC / 2], x[VEC * 5 / 8]), from_float2<BF16>(x[VEC * 3 / 4], x[VEC * 7 / 8]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) p[i] = from_float<BF16>(x[i]);
+  }
 }
 template <int VEC>
-__device__ __forceinline__ void store_32(float *p, const float *x) {
+__device__ __forceinline__ void store_32(float *p, const float *x, bool wide) {
   if constexpr (VEC == 8) {
-    *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
-    *reinterpret_cast<float4 *>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
-  } else {
-    *p = x[0];
+    if (wide) {
+      *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
+      *reinterpret_cast<float4 *>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+      return;
+    }
   }
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) p[i] = x[i];
 }
 
 // Sum over the threads of a row; `s` holds a float per warp.  Where a row has more than a warp, it has a block of its own.
@@ -102,7 +121,8 @@ __device__ __forceinline__ float row_sum(float v, int lanes, float *s) {
   return t;
 }
 
-template <bool BF16, bool RES32, bool POST, bool GATE, int VEC, int E>
+// VEC elements at a time; ALL: every array allows 16-byte accesses.
+template <bool BF16, bool RES32, bool POST, bool GATE, int VEC, bool ALL, int E>
 __global__ void __launch_bounds__(1024) add_norm_kernel(const NormArgs a) {
   constexpr int N = E / VEC;
   __shared__ float s_sum[2][32];
@@ -123,17 +143,21 @@ __global__ void __launch_bounds__(1024) add_norm_kernel(const NormArgs a) {
       if (i < a.d) f(i, j * VEC);
     }
   };
-  if (a.y) each([&](int i, int j) { load_16<BF16, VEC>(y + i, u + j); });
+  if (a.y) each([&](int i, int j) { load_16<BF16, VEC>(y + i, u + j, ALL || (a.wide & kWideY)); });
   if (a.res) {
     const char *res = static_cast<const char *>(a.res) + t * a.res_stride * (RES32 ? 4 : 2);
     each([&](int i, int j) {
-      if (RES32) load_32<VEC>(reinterpret_cast<const float *>(res) + i, r + j);
-      else load_16<BF16, VEC>(reinterpret_cast<const uint16_t *>(res) + i, r + j);
+      if (RES32) load_32<VEC>(reinterpret_cast<const float *>(res) + i, r + j, ALL || (a.wide & kWideRes));
+      else load_16<BF16, VEC>(reinterpret_cast<const uint16_t *>(res) + i, r + j, ALL || (a.wide & kWideRes));
     });
   }
   if (GATE) each([&](int i, int j) {
     if constexpr (VEC == 8) {
-      const uint4 v = *reinterpret_cast<const uint4 *>(gate + i);
+      uint4 v;
+      if (ALL || (a.wide & kWideGate)) v = *reinterpret_cast<const uint4 *>(gate + i);
+      else
+        v = make_uint4(gate[i] | (uint32_t)gate[i + 1] << 16, gate[i + 2] | (uint32_t)gate[i + 3] << 16, gate[i + 4] | (uint32_t)gate[i + 5] << 16,
+                       gate[i + 6] | (uint32_t)gate[i + 7] << 16);
       g[j / 2] = v.x; g[j / 2 + 1] = v.y; g[j / 2 + 2] = v.z; g[j / 2 + 3] = v.w;
     } else {
       if (j % 2 == 0) g[j / 2] = gate[i]; else g[j / 2] |= (uint32_t)gate[i] << 16;
@@ -157,7 +181,7 @@ __global__ void __launch_bounds__(1024) add_norm_kernel(const NormArgs a) {
     for (int k = 0; k < VEC; ++k) f[k] = 1.f;
     if (POST) {
       if (a.w_post) {
-        load_16<BF16, VEC>(a.w_post + i, f);
+        load_16<BF16, VEC>(a.w_post + i, f, ALL || (a.wide & kWidePost));
 #pragma unroll
         for (int k = 0; k < VEC; ++k) f[k] = inv * (a.w_offset + f[k]);
       } else {
@@ -181,8 +205,8 @@ __global__ void __launch_bounds__(1024) add_norm_kernel(const NormArgs a) {
       sum = fmaf(r[j + k], r[j + k], sum);
     }
     if (a.res_out) {
-      if (RES32) store_32<VEC>(reinterpret_cast<float *>(res_out) + i, r + j);
-      else store_16<BF16, VEC>(reinterpret_cast<uint16_t *>(res_out) + i, r + j);
+      if (RES32) store_32<VEC>(reinterpret_cast<float *>(res_out) + i, r + j, ALL || (a.wide & kWideResOut));
+      else store_16<BF16, VEC>(reinterpret_cast<uint16_t *>(res_out) + i, r + j, ALL || (a.wide & kWideResOut));
     }
   });
   if (!a.out) return;
@@ -191,14 +215,14 @@ __global__ void __launch_bounds__(1024) add_norm_kernel(const NormArgs a) {
   each([&](int i, int j) {
     float h[VEC];
     if (a.w_pre) {
-      load_16<BF16, VEC>(a.w_pre + i, h);
+      load_16<BF16, VEC>(a.w_pre + i, h, ALL || (a.wide & kWidePre));
 #pragma unroll
       for (int k = 0; k < VEC; ++k) h[k] = r[j + k] * (inv * (a.w_offset + h[k]));
     } else {
 #pragma unroll
       for (int k = 0; k < VEC; ++k) h[k] = r[j + k] * inv;
     }
-    store_16<BF16, VEC>(out + i, h);
+    store_16<BF16, VEC>(out + i, h, ALL || (a.wide & kWideOut));
   });
 }
 

@@ -123,12 +123,13 @@ class FtDense:
         """(address, row stride) of a [rows, cols] tensor with contiguous rows; None is NULL."""
         if t is None:
             return None, 0
-        if t.dtype is not dtype or t.get_device() != self._index or t.shape != (rows, cols):
-            self._fail(where, f"{name}: {dtype} [{rows}, {cols}]")
-        s = t.stride()
-        if cols > 1 and s[1] != 1:
-            self._fail(where, f"{name}: contiguous rows")
-        return t.data_ptr(), (s[0] if rows > 1 else cols)
+        if t.dtype is dtype and t.get_device() == self._index and t.shape == (rows, cols):
+            if t.is_contiguous():
+                return t.data_ptr(), cols
+            stride, step = t.stride()
+            if cols == 1 or step == 1:
+                return t.data_ptr(), (stride if rows > 1 else cols)
+        self._fail(where, f"{name}: {dtype} [{rows}, {cols}], contiguous rows,")
 
     def _vec(self, where, name, t, n, dtype):
         """Address of a contiguous vector of n elements; None is NULL."""
