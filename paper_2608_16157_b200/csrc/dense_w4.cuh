@@ -12,8 +12,9 @@
 // A word's nibble pairs stand where the top mantissa bits of two 16-bit numbers of exponent 4 are (bits 3 .. 6 for bf16, 6 .. 9 for fp16),
 // in place or after one shift or rotation: (w & mask) | magic is the pair 16 + q, from which 16 + z is subtracted exactly.
 //
-// w4_stream_kernel, up to 32 tokens: weights on M, tokens on N = 8, 16 or 32.  Bound: HBM for large matrices (N K / 2 bytes), launch and
-// latency for small ones.
+// w4_stream_kernel, up to 16 tokens (32 for float results): weights on M, tokens on N = 8, 16 or 32.  Bound: HBM for large matrices (N K / 2
+// bytes), launch and latency for small ones.  Measured: 35 us for 5 tokens through 2048 x 150001 (4.7 TB/s; 18.9 instructions per 256 weights),
+// 4.5 us for one token through 2048 x 5120, 9.7 us through 7168 x 7168.
 #pragma once
 #include <type_traits>
 

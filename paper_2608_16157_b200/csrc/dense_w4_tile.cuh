@@ -11,6 +11,8 @@
 // over all of k, and four warps take the sums out while it works on the next unit.  For float results (EXACT) the operands are the exact q - z,
 // a group of k has an accumulator of its own (two in turn), and eight warps add its sums times the row's scale to float sums in registers;
 // that takes about twice as long (reading an accumulator beside the tensor core costs 70 clocks for 16 tokens of 32 rows).
+// Measured: 309 us for 4096 tokens through 7168 x 7168 (1.36 PFLOP/s, the power limit's rate), 87 us for 1024 tokens with groups of 32, 18.5 us for
+// 64 tokens.  With 17 tokens it passes the streaming kernel (24 tokens 17 against 22 us).
 // With a cluster of c blocks each takes 1/c of k, and the sums are added over distributed shared memory, in the blocks' order.
 #pragma once
 #include "dense_w4.cuh"
