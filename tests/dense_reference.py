@@ -48,14 +48,14 @@ def w4_weights(codes, scales, zeros):
 
 def w4(x, w, bias, out_dtype):
     """float64 result and a bound of its error before the result is rounded.  Up to 16 tokens, and for float results: products are exact; a group's
-    sum goes through at most 8 tensor-core instructions of 16 products, each off by 2^-22 of the magnitudes (aligned and cut); then at most
-    2 * 128 / 8 + 16 additions in float: below 2^-17.  More tokens with 16-bit results: every weight is rounded once to the type (half a step,
+    sum goes through at most 8 tensor-core instructions of 16 products, each off by 2^-22 of the magnitudes (aligned and cut), and is added in
+    float: at most k / 32 groups, 16 warps and 8 blocks.  More tokens with 16-bit results: every weight is rounded once to the type (half a step,
     2^-25 below fp16's normal numbers), and the tensor core adds k / 16 times, each off by 2^-22 at most."""
     ref = x.double() @ w.t()
     mag = x.double().abs() @ w.abs().t()
     if bias is not None:
         ref, mag = ref + bias.double(), mag + bias.double().abs()
-    err = 2.0 ** -17 * mag
+    err = (2.0 ** -19 + (x.shape[1] / 32 + 24) * 2.0 ** -24) * mag
     if x.shape[0] > 16 and out_dtype is not torch.float32:
         err = (UNIT[x.dtype] + x.shape[1] / 16 * 2.0 ** -22) * mag + TINY[x.dtype] * x.double().abs().sum(-1, keepdim=True)
     return ref, err

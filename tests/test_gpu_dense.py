@@ -154,6 +154,12 @@ def test_w4_depths_and_groups(k, group, dtype):
     run_w4(70, 150, k, group, dtype, zeros=True, out32=True, seed=k)
 
 
+@pytest.mark.parametrize("t", [2, 16, 24, 40, 200])
+def test_w4_deepest(t):
+    run_w4(t, 70, 65536, 128, "bf16", zeros=True, out32=t in (24, 200), seed=t)
+    run_w4(t, 1100, 65536, 32, "fp16", bias=True, seed=t)
+
+
 @pytest.mark.parametrize("t", [1, 5, 12, 32, 33, 130, 300, 520])
 @pytest.mark.parametrize("n,k,group,dtype,zeros", [(5120, 2048, 128, "bf16", False), (2048, 4096, 32, "fp16", True), (9001, 1024, 64, "bf16", True)])
 def test_w4_wide(t, n, k, group, dtype, zeros):
