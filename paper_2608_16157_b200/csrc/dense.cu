@@ -122,15 +122,18 @@ cudaError_t launch_w4(const ft_dense *h, const W4Args &a, bool zero, cudaStream_
   }
 }
 
-// A row to a cluster of blocks of 512 threads while one a SM takes them all, as many as leave a thread some pieces; more rows to smaller blocks,
-// whose ends overlap with the others' passes; short rows to the smallest.
+// A row to a cluster of blocks of 512 threads while one a SM takes them all, as many as leave a thread some pieces; more rows to blocks of 256,
+// four a SM, whose ends overlap with the others' passes (two to a row while all fit at once); short rows to the smallest.
 template <int TY>
 cudaError_t launch_logprobs(const ft_dense *h, const LogpArgs &a, cudaStream_t st) {
-  const long long pieces = a.vocab / LogpType<TY>::kVec, places = h->sm_count;
-  if (pieces <= 1024 && a.T > places) return launch(logprobs_kernel<TY, 128>, dim3((unsigned)a.T), 128, sizeof(LogpSmem<4>), st, a, 1);
-  if (a.T > places) return launch(logprobs_kernel<TY, 256>, dim3((unsigned)a.T), 256, sizeof(LogpSmem<8>), st, a, 1);
+  const long long pieces = a.vocab / LogpType<TY>::kVec, sms = h->sm_count;
+  if (pieces <= 1024 && a.T > sms) return launch(logprobs_kernel<TY, 128>, dim3((unsigned)a.T), 128, sizeof(LogpSmem<4>), st, a, 1);
   int cluster = 1;
-  while (cluster < kLogpCluster && 2ll * a.T * cluster <= places && pieces >= 1024 * cluster) cluster *= 2;
+  if (a.T > sms) {
+    if (2ll * a.T <= 4 * sms && pieces >= 2048) cluster = 2;
+    return launch_clusters(logprobs_kernel<TY, 256>, dim3((unsigned)a.T * cluster), 256, sizeof(LogpSmem<8>), cluster, st, a, cluster);
+  }
+  while (cluster < kLogpCluster && 2ll * a.T * cluster <= sms && pieces >= 1024 * cluster) cluster *= 2;
   return launch_clusters(logprobs_kernel<TY, 512>, dim3((unsigned)a.T * cluster), 512, sizeof(LogpSmem<16>), cluster, st, a, cluster);
 }
 
