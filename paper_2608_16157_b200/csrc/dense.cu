@@ -335,7 +335,8 @@ ft_status_t ft_dense_logprobs(ft_dense_t *h, int T, int64_t vocab, int dtype, co
   DeviceScope dev(h->device);
   FD_CUDA(dev.err);
   LogpArgs a;
-  a.logits = logits; a.stride = stride; a.T = T; a.vocab = (int32_t)vocab; a.n_tokens = given ? n_tokens : 0; a.top_k = top_k; a.scale = scale;
+  a.logits = logits; a.stride = stride; a.T = T; a.vocab = (int32_t)vocab; a.n_tokens = given ? n_tokens : 0; a.top_k = top_k;
+  logp_scale(a, scale);
   a.tokens = given ? tokens : nullptr; a.tokens_stride = tokens_stride;
   a.logprob = logprob; a.entropy = entropy; a.top_logprobs = top_logprobs; a.top_ids = top_ids;
   a.status = h->status_dev;

@@ -25,13 +25,21 @@ struct LogpArgs {
   const void *logits;
   long long stride;
   int32_t T, vocab, n_tokens, top_k;
-  float scale;                       // c
+  float scale, c2, plain_below;      // c; c log2 e; see logp_scale
   const int32_t *tokens;
   long long tokens_stride;
   float *logprob, *entropy, *top_logprobs;
   int32_t *top_ids;
   uint32_t *status;
 };
+
+// The scale, and below which magnitude of the maximum m exponents may be taken from the rounded product m c2: no product overflows, and |m c2| < 2^31, so
+// that what the product lost in rounding, which is the maximum's own exponent, stays within 64 (it is some hundreds for -1e10: sums of 0 or infinity).
+inline void logp_scale(LogpArgs &a, float scale) {
+  a.scale = scale;
+  a.c2 = scale * 1.44269504088896f;
+  a.plain_below = a.c2 >= 1e8f ? 0.f : a.c2 < 2147483648.f / 1e29f ? 1e29f : 2147483648.f / a.c2;
+}
 
 enum { kLogpBf16 = 0, kLogpFp16 = 1, kLogpFp32 = 2 };
 template <int TY>
@@ -91,6 +99,12 @@ struct LogpType {
   }
 };
 
+// The larger of both; NaN where one is.
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -159,7 +173,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
   if (cluster > 1) cluster_arrive();
   grid_wait();
   const uint8_t *base = static_cast<const uint8_t *>(a.logits) + row * a.stride * Y::kBytes;
-  const float c2 = a.scale * 1.44269504088896f;
+  const float c2 = a.c2;
 
   // the row: `head` elements up to a 16-byte boundary, n_vec pieces, the rest
   const int head = min(a.vocab, (int)(((16 - ((uintptr_t)base & 15)) & 15) / Y::kBytes));
@@ -173,21 +187,20 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
     tok = a.tokens[row * a.tokens_stride + tid];
     if (tok >= 0 && tok < a.vocab) x_tok = Y::at(base, tok);
   }
-  // `plain`: exponents in one instruction from the rounded product ref = m c2, -infinities at the floor; not while the maximum is so small or the
-  // scale so large that the floor would count, or a product overflow
+  // `plain`: exponents in one instruction from the rounded product ref = m c2, -infinities at the floor; not where the floor would count, or beyond
+  // plain_below.  Else the difference is taken first.
   LogpAcc acc;
   float ref = 0.f;
   bool plain = false;
   auto raise = [&](float to) {
-    plain = fabsf(to) < 1e29f && c2 < 1e8f && (Y::floor_value() - to) * c2 < -200.f;
+    plain = fabsf(to) < a.plain_below && (Y::floor_value() - to) * c2 < -200.f;
     ref = plain ? to * c2 : 0.f;
     acc.rescale(to, plain ? -fmaf(to, c2, -ref) : 0.f, c2);
   };
-  auto add_one = [&](float x) {                  // any x, not above the maximum
-    if (x == -INFINITY) return;
-    const float t = plain ? fmaf(x, c2, -ref) : (x - acc.m) * c2, e = exp2_approx(t);
+  auto add_one = [&](float x) {                  // any x, not above the maximum, which is not -infinity (x = -infinity counts nothing)
+    const float t = max_or_nan(plain ? fmaf(x, c2, -ref) : (x - acc.m) * c2, -1000.f), e = exp2_approx(t);
     acc.s += e;
-    acc.u = fmaf(e, fmaxf(t, -1000.f), acc.u);
+    acc.u = fmaf(e, t, acc.u);
   };
   // plain: two logits at a time, in packed arithmetic
   auto add_pair = [&](float x, float y, uint64_t c22, uint64_t ref2, uint64_t &s2, uint64_t &u2) {
@@ -203,7 +216,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
   const float x_edge = has_edge ? Y::at(base, edge_index(tid)) : -INFINITY;
   if (has_edge) {
     if (x_edge > acc.m) raise(x_edge);
-    add_one(x_edge);
+    if (x_edge != -INFINITY) add_one(x_edge);
   }
   // fours of pieces; several fours to a mark where a thread has many
   const int fours = (v1 - v0 + kAhead * THREADS - 1) / (kAhead * THREADS);
@@ -259,14 +272,12 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
       if (x != x || y != y) acc.s = NAN;
     } else {
 #pragma unroll 1
-      for (int i = 0; i < kAhead * 4; ++i) {
-        uint32_t w = 0;
+      for (int i = 0; i < kAhead; ++i) {
+        const uint4 p = i == 0 ? q[0] : i == 1 ? q[1] : i == 2 ? q[2] : q[3];
+        float x[E];
+        Y::unpack(p, x);
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) w = i == 4 * j ? q[j].x : i == 4 * j + 1 ? q[j].y : i == 4 * j + 2 ? q[j].z : i == 4 * j + 3 ? q[j].w : w;
-        float x, y;
-        Y::split(w, x, y);
-        add_one(x);
-        if (TY != kLogpFp32) add_one(y);
+        for (int j = 0; j < E; ++j) add_one(x[j]);
       }
     }
   };
