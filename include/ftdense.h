@@ -66,7 +66,7 @@ ft_status_t ft_dense_w4_forward(ft_dense_t *h, int T, int64_t n, int64_t k, int 
                                 int64_t x_stride, const void *image, const void *bias, void *y, int64_t y_stride, int out_dtype,
                                 void *stream);
 
-/* With l_i = scale * logits[t][i] (scale > 0) and lse = log(sum_i exp(l_i)):
+/* With l_i = scale * logits[t][i] (0 < scale <= 2^126) and lse = log(sum_i exp(l_i)):
  *   logprob[t][j] = l_i - lse for i = tokens[t][j], j < n_tokens   (a negative token is none: 0)
  *   entropy[t]    = -sum_i p_i log(p_i),  p_i = exp(l_i - lse)
  *   top_ids[t][j], top_logprobs[t][j], j < top_k <= 32: the largest logits in descending order, the lowest id first among equals,

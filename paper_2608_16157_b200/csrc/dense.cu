@@ -323,7 +323,7 @@ ft_status_t ft_dense_w4_forward(ft_dense_t *h, int T, int64_t n, int64_t k, int 
 ft_status_t ft_dense_logprobs(ft_dense_t *h, int T, int64_t vocab, int dtype, const void *logits, int64_t stride, float scale,
                               const int32_t *tokens, int64_t tokens_stride, int n_tokens, float *logprob, float *entropy, int top_k,
                               int32_t *top_ids, float *top_logprobs, void *stream) {
-  if (!h || T < 0 || vocab < 1 || vocab > (1 << 30) || (!type16(dtype) && dtype != FT_DENSE_FP32) || !(scale > 0.f) || !(scale < INFINITY) ||
+  if (!h || T < 0 || vocab < 1 || vocab > (1 << 30) || (!type16(dtype) && dtype != FT_DENSE_FP32) || !(scale > 0.f) || !(scale <= kLogpMaxScale) ||
       n_tokens < 0 || top_k < 0 || top_k > kLogpTop)
     return FT_ERR_INVALID_ARG;
   if (T == 0) return FT_OK;

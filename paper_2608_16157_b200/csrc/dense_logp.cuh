@@ -25,7 +25,7 @@ struct LogpArgs {
   const void *logits;
   long long stride;
   int32_t T, vocab, n_tokens, top_k;
-  float scale, c2, plain_below;      // c; c log2 e; see logp_scale
+  float scale, c2, twice_c2, plain_below;      // c; c log2 e; see logp_scale
   const int32_t *tokens;
   long long tokens_stride;
   float *logprob, *entropy, *top_logprobs;
@@ -33,11 +33,14 @@ struct LogpArgs {
   uint32_t *status;
 };
 
+constexpr float kLogpMaxScale = 8.507059173023462e37f;   // 2^126: twice c log2 e is finite
+
 // The scale, and below which magnitude of the maximum m exponents may be taken from the rounded product m c2: no product overflows, and |m c2| < 2^31, so
 // that what the product lost in rounding, which is the maximum's own exponent, stays within 64 (it is some hundreds for -1e10: sums of 0 or infinity).
 inline void logp_scale(LogpArgs &a, float scale) {
   a.scale = scale;
   a.c2 = scale * 1.44269504088896f;
+  a.twice_c2 = 2.f * a.c2;
   a.plain_below = a.c2 >= 1e8f ? 0.f : a.c2 < 2147483648.f / 1e29f ? 1e29f : 2147483648.f / a.c2;
 }
 
@@ -118,12 +121,15 @@ __device__ __forceinline__ uint32_t logp_order(float x) {
 }
 __device__ __forceinline__ float logp_value(uint32_t o) { return __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o); }
 
+// Half of x - m: the difference itself may pass the largest float.
+__device__ __forceinline__ float half_less(float x, float m) { return fmaf(x, 0.5f, -0.5f * m); }
+
 // Of some logits: the largest, m, and the sums of 2^t and 2^t t with t = x c2 - (m c2 + del); del is what the product m c2 lost when it was
 // rounded, so that sums with different references can be joined exactly.  m = -infinity: none yet (s then is 0, or NaN).
 struct LogpAcc {
   float m = -INFINITY, del = 0.f, s = 0.f, u = 0.f;
-  __device__ __forceinline__ void rescale(float to_m, float to_del, float c2) {
-    const float d = fmaf(m - to_m, c2, del - to_del);
+  __device__ __forceinline__ void rescale(float to_m, float to_del, float twice_c2) {
+    const float d = fmaf(half_less(m, to_m), twice_c2, del - to_del);
     if (!(d >= -200.f)) {                 // (-infinity and NaN too: what there is, a NaN stays)
       if (s == s) s = 0.f;
       u = 0.f;
@@ -195,10 +201,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
   auto raise = [&](float to) {
     plain = fabsf(to) < a.plain_below && (Y::floor_value() - to) * c2 < -200.f;
     ref = plain ? to * c2 : 0.f;
-    acc.rescale(to, plain ? -fmaf(to, c2, -ref) : 0.f, c2);
+    acc.rescale(to, plain ? -fmaf(to, c2, -ref) : 0.f, a.twice_c2);
   };
   auto add_one = [&](float x) {                  // any x, not above the maximum, which is not -infinity (x = -infinity counts nothing)
-    const float t = max_or_nan(plain ? fmaf(x, c2, -ref) : (x - acc.m) * c2, -1000.f), e = exp2_approx(t);
+    const float t = max_or_nan(plain ? fmaf(x, c2, -ref) : half_less(x, acc.m) * a.twice_c2, -1000.f), e = exp2_approx(t);
     acc.s += e;
     acc.u = fmaf(e, t, acc.u);
   };
@@ -447,7 +453,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
     }
   };
   auto value = [](uint32_t o) { return o ? logp_value(o) : -INFINITY; };
-  acc.rescale(value(block_top), 0.f, c2);
+  acc.rescale(value(block_top), 0.f, a.twice_c2);
   sum_lanes(acc.s, acc.u);
   if (lane == 0) { sm.sum[0][warp] = acc.s; sm.sum[1][warp] = acc.u; }
   __syncthreads();
@@ -479,13 +485,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
     const bool mine_too = lane < cluster;
     const uint32_t o = mine_too ? sm.part_top[lane] : 0u, top = __reduce_max_sync(0xffffffffu, o);
     if (mine_too) { all.m = value(o); all.s = sm.part[lane][0]; all.u = sm.part[lane][1]; }
-    all.rescale(value(top), 0.f, c2);
+    all.rescale(value(top), 0.f, a.twice_c2);
     sum_lanes(all.s, all.u);
   }
   constexpr float kLn2 = 0.693147180559945f;
   const bool bad = !(all.s < INFINITY), none = all.s == 0.f;
   const float log2_s = log2f(all.s), rest = log2_s * kLn2;
-  auto logprob = [&](float x) { return bad ? NAN : none ? -INFINITY : fmaf(x - all.m, a.scale, -rest); };
+  auto logprob = [&](float x) { return bad ? NAN : none ? -INFINITY : fmaf(half_less(x, all.m), 2.f * a.scale, -rest); };
   if (tid == 0 && a.entropy) a.entropy[row] = bad ? NAN : none ? 0.f : fmaxf((log2_s - all.u / all.s) * kLn2, 0.f);
   if (a.tokens)
     for (int i = tid; i < a.n_tokens; i += THREADS) {

@@ -1,7 +1,10 @@
-"""GPU tests of the operators of ``dense`` at the ends of what their arguments may hold: products of logit and scale far beyond the logits' usual ones."""
+"""GPU tests of the operators of ``dense`` at the ends of what their arguments may hold: products of logit and scale far beyond the logits' usual ones,
+scales and logits next to the smallest and the largest floats."""
 import pytest
 import torch
 
+from paper_2608_16157_b200 import binding as B
+from paper_2608_16157_b200 import dense as D
 from tests import dense_reference as R
 from tests.test_gpu_dense import DEV, gen, run_logp
 
@@ -44,3 +47,35 @@ def test_logp_maxima_far_from_zero(dtype, big, t, v):
         x = sign * big + step * torch.randint(-4, 5, (t, v), generator=gen(3), device=DEV)
         for scale in (1.0, 1.0 / step, 3.0 / big):
             run_logp(x.to(dt), 12, scale=scale, seed=v)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("exponent", [-149, -131, -128, -126, -120])
+@pytest.mark.parametrize("t,v", [(1, 60000), (4, 801), (300, 5000)])
+def test_logp_differences_beyond_the_largest_float(dtype, exponent, t, v):
+    """Logits over the whole range of the type, the largest and the lowest value among them, times a scale that leaves ordinary differences."""
+    low, high = torch.finfo(R.DT[dtype]).min, torch.finfo(R.DT[dtype]).max
+    x = (2 * torch.rand(t, v, generator=gen(4), device=DEV) - 1) * 3e38
+    x[:, 5], x[:, v - 9] = low, high
+    x[0, v // 2:] = low
+    run_logp(x.to(R.DT[dtype]), 9, scale=2.0 ** exponent, seed=t)
+
+
+@pytest.mark.parametrize("dtype,size,exponent", [("fp32", 2.0 ** -125, 126), ("fp32", 2.0 ** -140, 126), ("bf16", 2.0 ** -124, 126), ("fp32", 1.0, 100), ("fp16", 1.0, 100),
+                                                 ("bf16", 2.0 ** -100, 105)])
+@pytest.mark.parametrize("t,v", [(1, 60000), (4, 801), (300, 5000)])
+def test_logp_the_largest_scales(dtype, size, exponent, t, v):
+    run_logp((size * torch.randn(t, v, generator=gen(5), device=DEV)).to(R.DT[dtype]), 9, scale=2.0 ** exponent, seed=t)
+
+
+def test_logp_scales_beyond_the_largest_are_refused():
+    h = D.FtDense()
+    x, e = torch.zeros(2, 100, device=DEV), torch.full((2,), -77.0, device=DEV)
+    for scale in (1.01 * 2.0 ** 126, 2.0 ** 127, 3e38):
+        with pytest.raises(D.FtDenseError) as err:
+            h.logprobs(x, entropy=e, scale=scale)
+        assert err.value.code == B.FT_ERR_INVALID_ARG
+    assert h.launch_count() == 0 and (e == -77).all()
+    h.logprobs(x, entropy=e, scale=2.0 ** 126)
+    assert (e - 4.605170186).abs().max() < 1e-5
+    h.destroy()
