@@ -103,7 +103,7 @@ cudaError_t launch_w4_tile(const ft_dense *h, const W4Args &a, W4Tile p, cudaStr
   CUtensorMap tm;
   if (!make_x_map(h, &tm, a, p.bn)) return cudaErrorInvalidValue;
   const int smem = w4_tile_memory<EXACT>(a.g, p), units = p.row_tiles * p.tok_tiles, fit = h->clusters[p.cluster];
-  return launch_clusters(w4_tile_kernel<BF16, ZERO, EXACT>, dim3((p.cluster > 1 || units < fit ? units : fit) * p.cluster), W4TileCfg<EXACT>::kThreads, smem, p.cluster, st, tm, a, p);
+  return launch_clusters(w4_tile_kernel<BF16, ZERO, EXACT>, dim3((p.cluster > 1 || units < fit ? units : fit) * p.cluster), W4TileCfg<EXACT>::kThreads, smem, p.cluster, st, tm, a, p, W4Again{a, p});
 }
 
 template <bool BF16, bool ZERO>

@@ -11,6 +11,8 @@
 // over all of k, and four warps take the sums out while it works on the next unit.  For float results (EXACT) the operands are the exact q - z,
 // a group of k has an accumulator of its own (two in turn), and eight warps add its sums times the row's scale to float sums in registers;
 // that takes about twice as long (reading an accumulator beside the tensor core costs 70 clocks for 16 tokens of 32 rows).
+// A weight that the type cannot hold (a scale above a fifteenth of its largest value may give one) makes every sum of its row infinite or NaN, whatever
+// the token: a block that has seen one computes the results of those rows again in the end, one a thread, in the exact form.  Right, and slow.
 // Measured: 309 us for 4096 tokens through 7168 x 7168 (1.36 PFLOP/s, the power limit's rate), 87 us for 1024 tokens with groups of 32, 18.5 us for
 // 64 tokens.  With 17 tokens it passes the streaming kernel (24 tokens 17 against 22 us).
 // With a cluster of c blocks each takes 1/c of k, and the sums are added over distributed shared memory, in the blocks' order.
@@ -74,11 +76,69 @@ inline W4Tile w4_tile_share(const W4Geom &g, int T, bool exact, const int *clust
   return best;
 }
 
+// Whether a weight of row n may be beyond the type's largest value.
+template <bool BF16>
+__device__ __forceinline__ bool w4_row_over(const W4Args &a, int n) {
+  const W4Geom &g = a.g;
+  const int quad = n >> 6, m = g.tiles_of(quad), per = kW4Block / g.group;
+  const uint8_t *sc = a.image + g.quad_at(quad) + m * 2 * kW4TileBytes + (n & 7) * 16 + (n >> 4 & 3) * 4 + (n >> 3 & 1) * 2;
+  bool over = false;
+  for (int i = 0; i < g.nb * per; ++i)
+    over |= fabsf(to_float<BF16>(*reinterpret_cast<const uint16_t *>(sc + (long long)(i / per) * g.record(m) + i % per * 128))) >
+            (BF16 ? 3.3895313892515355e38f : 65504.f) / 15.f;
+  return over;
+}
+// The sum of row n and token t in the exact form: a group's products with q - z, then the scale, in float.
+template <bool BF16>
+__device__ __forceinline__ float w4_one(const W4Args &a, long long t, int n) {
+  const W4Geom &g = a.g;
+  const int quad = n >> 6, m = g.tiles_of(quad), tile = n >> 4 & 3, gr = n & 7, high = n >> 3 & 1, per = kW4Block / g.group;
+  const uint16_t *x = a.x + t * a.x_stride;
+  float sum = 0.f;
+  for (int k0 = 0; k0 < g.k; k0 += g.group) {
+    const uint8_t *rec = a.image + g.quad_at(quad) + (long long)(k0 / kW4Block) * g.record(m), *sc = rec + m * 2 * kW4TileBytes;
+    const int s = k0 % kW4Block / g.group;
+    const float scale = to_float<BF16>(*reinterpret_cast<const uint16_t *>(sc + s * 128 + gr * 16 + tile * 4 + high * 2));
+    const float zero = g.zeros ? (float)sc[per * 128 + s * 64 + gr * 8 + tile * 2 + high] : 8.f;
+    float part = 0.f;
+    for (int k = k0; k < k0 + g.group; k += 4) {          // a word: pairs `high` and 2 + high are the row's
+      const int i = k % kW4Block;
+      const uint32_t w = *reinterpret_cast<const uint32_t *>(rec + ((i >> 6) * m + tile) * kW4TileBytes + (gr * 4 + (i >> 2 & 3)) * 16 + (i >> 4 & 3) * 4);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const uint32_t c = rotl32(w, 32 - (high ? w4_bit<BF16>(2 * b + 1) : w4_bit<BF16>(2 * b)));
+        part = fmaf(to_float<BF16>(x[k + 2 * b]), (float)(c & 15u) - zero, part);
+        part = fmaf(to_float<BF16>(x[k + 2 * b + 1]), (float)(c >> 16 & 15u) - zero, part);
+      }
+    }
+    sum = fmaf(scale, part, sum);
+  }
+  return sum;
+}
+
+// A block's results in rows whose weights may be beyond the type's largest value.  Not inlined and with arguments of its own: an address of the kernel's
+// own ones costs it 2 us of 14 (512 tokens x 2048 x 5120), a copy of them 30 of 310 (4096 tokens x 7168 x 7168).
+struct W4Again { W4Args a; W4Tile p; };
+template <bool BF16>
+__device__ __noinline__ void w4_again(const W4Again &args, int threads) {
+  const W4Args &a = args.a;
+  const W4Tile &p = args.p;
+  const int rank = blockIdx.x % p.cluster, n_cl = gridDim.x / p.cluster, share = (p.bn + p.cluster - 1) / p.cluster;
+  for (int u = blockIdx.x / p.cluster; u < p.row_tiles * p.tok_tiles; u += n_cl) {
+    const int tok0 = u / p.row_tiles * p.bn + rank * share, n = u % p.row_tiles * 128 + (threadIdx.x & 127);
+    const int n_tok = min(min(share, p.bn - rank * share), a.T - tok0);
+    if (n >= a.g.n || !w4_row_over<BF16>(a, n)) continue;
+#pragma unroll 1
+    for (int t = threadIdx.x >> 7; t < n_tok; t += threads / 128) w4_store<BF16>(a, tok0 + t, n, w4_one<BF16>(a, tok0 + t, n));
+  }
+}
+
 template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 template <bool BF16, bool ZERO, bool EXACT>
-__global__ void __launch_bounds__(W4TileCfg<EXACT>::kThreads, 1) w4_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const W4Args a, const W4Tile p) {
+__global__ void __launch_bounds__(W4TileCfg<EXACT>::kThreads, 1) w4_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const W4Args a, const W4Tile p,
+                                                                                   const __grid_constant__ W4Again args) {
   using Cfg = W4TileCfg<EXACT>;
   constexpr int kRaw = Cfg::kRaw;
   extern __shared__ unsigned char smem_raw[];
@@ -126,6 +186,7 @@ __global__ void __launch_bounds__(W4TileCfg<EXACT>::kThreads, 1) w4_tile_kernel(
   const int cluster = p.cluster, rank = blockIdx.x % cluster, units = p.row_tiles * p.tok_tiles, n_cl = gridDim.x / cluster, cl = blockIdx.x / cluster;
   const int b0 = (int)((long long)g.nb * rank / cluster), b1 = (int)((long long)g.nb * (rank + 1) / cluster);
   const int per = kW4Block / g.group, rec4 = g.record(4);       // groups of a record
+  float odd = 0.f;                                              // NaN once a row's sum (of any token) is not finite
   constexpr int kFirstAdd = Cfg::kThreads / 32 - Cfg::kAdd, kFirstExpand = 4;
 
   if (warp < 4) {
@@ -402,6 +463,7 @@ __global__ void __launch_bounds__(W4TileCfg<EXACT>::kThreads, 1) w4_tile_kernel(
           uint32_t v[16];
           tmem_ld16(out_tmem + c, v);
           tmem_ld_wait();
+          if (!EXACT && c == 0) odd = fmaf(__uint_as_float(v[0]), 0.f, odd);
 #pragma unroll
           for (int j = 0; j < 16; ++j, out += a.y_stride)
             if (store && c + j < n_tok) {
@@ -451,16 +513,17 @@ __global__ void __launch_bounds__(W4TileCfg<EXACT>::kThreads, 1) w4_tile_kernel(
         const int t = i >> 7, n = row0 + (i & 127);
         float v = 0.f;
         for (int r = 0; r < cluster; ++r) v += part[(r * share) * 128 + i];
+        if (!EXACT) odd = fmaf(v, 0.f, odd);
         if (n < g.n) w4_store<BF16>(a, tok0 + t, n, v);
       }
-  } else {
-    __syncthreads();
   }
+  const bool again = __syncthreads_or(!EXACT && odd != odd) && !*s_abort;
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
+  if (!EXACT && again) w4_again<BF16>(args, Cfg::kThreads);
 }
 
 }  // namespace ftmoe
