@@ -180,7 +180,7 @@ class FtDense:
     def w4_pack(self, codes, scales, zeros=None, image=None, stream=None) -> W4Weight:
         """Lays a matrix out once (``ft_dense_w4_pack``): codes uint8 ``[n, k / 2]`` (the even k in the low half of a byte), scales bf16 or fp16
         ``[n, k / group]``, zeros uint8 of the same shape or None (8).  ``image``: uint8 tensor of :func:`w4_bytes` elements to
-        write to, or None (one is made)."""
+        write to, or None: one is made on the current stream, whose work so far another ``stream`` then waits for."""
         w = "ft_dense_w4_pack"
         if codes.dim() != 2 or scales.dim() != 2 or scales.shape[0] != codes.shape[0] or scales.shape[1] < 1 or scales.dtype not in (torch.bfloat16, torch.float16):
             self._fail(w, "codes: uint8 [n, k / 2], scales: bfloat16 or float16 [n, k / group]")
@@ -194,6 +194,13 @@ class FtDense:
             self._fail(w, f"zeros: uint8 {list(scales.shape)}")
         if image is None:
             image = torch.empty(size, dtype=torch.uint8, device=self._device)
+            if stream is not None:
+                # the memory may have been another tensor's, which work queued on the current stream still uses
+                at, own = torch.cuda.current_stream(self._device), self._stream(stream)
+                if own != at.cuda_stream:
+                    own = torch.cuda.ExternalStream(own, device=self._device)
+                    own.wait_stream(at)
+                    image.record_stream(own)
         elif image.dtype is not torch.uint8 or image.get_device() != self._index or not image.is_contiguous() or image.numel() < size:
             self._fail(w, f"image: contiguous uint8 tensor of >= {size} elements")
         _check(self._lib.ft_dense_w4_pack(self._h, n, k, group, _CODE[scales.dtype], cp, cs, self._vec(w, "scales", scales, scales.numel(), scales.dtype),
