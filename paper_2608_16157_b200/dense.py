@@ -89,13 +89,26 @@ class W4Weight:
         self.image, self.n, self.k, self.group, self.dtype, self.zeros = image, n, k, group, dtype, zeros
 
 
+def _device_index(device):
+    """Index of a device; None and a CUDA device without an index are the current one."""
+    if isinstance(device, int):
+        return device
+    index = None
+    if device is not None:
+        device = torch.device(device)
+        if device.type != "cuda":
+            raise FtDenseError(FT_ERR_INVALID_ARG, "ft_dense_create", f"{device} is no CUDA device")
+        index = device.index
+    return torch.cuda.current_device() if index is None else index
+
+
 class FtDense:
-    """Handle of the operators on one device (the current one if none is given).  Methods mirror the C entry points."""
+    """Handle of the operators on one device (the current one if none, or none by number, is given).  Methods mirror the C entry points."""
 
     def __init__(self, device=None):
         self._lib = load()
         self._h = C.c_void_p()
-        index = torch.cuda.current_device() if device is None else device if isinstance(device, int) else torch.device(device).index or 0
+        index = _device_index(device)
         _check(self._lib.ft_dense_create(index, C.byref(self._h)), "ft_dense_create")
         self._index, self._device = index, torch.device("cuda", index)
 
