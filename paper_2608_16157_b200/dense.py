@@ -163,9 +163,10 @@ class FtDense:
         stream_t = res if res is not None else res_out
         if one is None:
             one = stream_t
-        shape = (y if y is not None else stream_t if stream_t is not None else out).shape
-        if len(shape) != 2:
+        first = y if y is not None else stream_t if stream_t is not None else out
+        if first is None or first.dim() != 2:
             self._fail(w, "y, res: [T, d]")
+        shape = first.shape
         t, d = shape
         dt = one.dtype
         rt = stream_t.dtype if stream_t is not None else dt
@@ -223,6 +224,8 @@ class FtDense:
     def w4(self, x, weight: W4Weight, y, bias=None, stream=None):
         """``y = x @ w.T + bias`` with 4-bit weights (``ft_dense_w4_forward``): x ``[T, k]`` of the scales' type, y ``[T, n]`` of it or float32."""
         w = "ft_dense_w4_forward"
+        if x.dim() != 2:
+            self._fail(w, f"x: {weight.dtype} [T, {weight.k}]")
         t, n, k, dt = x.shape[0], weight.n, weight.k, weight.dtype
         out_dt = y.dtype
         if out_dt is not dt and out_dt is not torch.float32:

@@ -30,3 +30,24 @@ def test_a_device_that_is_none(device):
     with pytest.raises(D.FtDenseError) as e:
         D.FtDense(device)
     assert e.value.code == B.FT_ERR_INVALID_ARG
+
+
+@pytest.fixture
+def handle():
+    """A handle of CPU tensors' "device": its checks run, its library must not be reached."""
+    h = D.FtDense.__new__(D.FtDense)
+    h._h, h._lib, h._index, h._device = None, None, -1, torch.device("cpu")
+    return h
+
+
+def test_calls_without_a_tensor_are_refused(handle):
+    z = lambda *s, d=torch.bfloat16: torch.zeros(*s, dtype=d)
+    w = D.W4Weight(z(64, d=torch.uint8), 16, 32, 32, torch.bfloat16, False)
+    for call in (lambda: handle.add_norm(None, None, None, None), lambda: handle.add_norm(None, None, None, None, w_pre=z(8)),
+                 lambda: handle.add_norm(None, None, None, None, w_post=z(8), post=True), lambda: handle.add_norm(z(8), None, None, z(8)),
+                 lambda: handle.add_norm(torch.zeros(()), None, None, None), lambda: handle.w4(torch.zeros((), dtype=torch.bfloat16), w, z(1, 16)),
+                 lambda: handle.w4(z(32), w, z(16)), lambda: handle.w4(z(1, 1, 32), w, z(1, 16)), lambda: handle.logprobs(z(8)),
+                 lambda: handle.logprobs(torch.zeros(()))):
+        with pytest.raises(D.FtDenseError) as e:
+            call()
+        assert e.value.code == B.FT_ERR_INVALID_ARG
