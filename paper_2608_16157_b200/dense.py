@@ -168,7 +168,7 @@ class FtDense:
             self._fail(w, "y, res: [T, d]")
         shape = first.shape
         t, d = shape
-        dt = one.dtype
+        dt = torch.bfloat16 if one is stream_t and one.dtype is torch.float32 else one.dtype       # (no tensor of the 16-bit type: any)
         rt = stream_t.dtype if stream_t is not None else dt
         if dt not in _CODE or rt not in _CODE:
             self._fail(w, "y, out: bfloat16 or float16; res: the same or float32")
