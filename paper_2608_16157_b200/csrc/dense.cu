@@ -47,7 +47,7 @@ bool w4_ok(int64_t n, int64_t k, int group) {
 template <bool BF16, bool RES32, bool POST, bool GATE, int E>
 cudaError_t launch_norm_form(const NormArgs &a, bool wide, cudaStream_t st) {
   const int threads = a.lanes > 32 ? a.lanes : 128, rows = threads / a.lanes;
-  const unsigned grid = (unsigned)((a.T + rows - 1) / rows);
+  const unsigned grid = (unsigned)(((long long)a.T + rows - 1) / rows);
   if (!wide) return launch(add_norm_kernel<BF16, RES32, POST, GATE, 1, false, E>, grid, threads, 0, st, a);
   return a.wide == kWideAll ? launch(add_norm_kernel<BF16, RES32, POST, GATE, 8, true, E>, grid, threads, 0, st, a)
                             : launch(add_norm_kernel<BF16, RES32, POST, GATE, 8, false, E>, grid, threads, 0, st, a);

@@ -24,3 +24,15 @@ def test_a_stream_alone(res, t, d):
     assert ((r.double() - want).abs() <= 2.0 ** -23 * want.abs() + R.rounding(want, r.dtype)).all()
     assert h.sync_status() == 0 and h.launch_count() == 2
     h.destroy()
+
+
+def test_as_many_rows_as_there_can_be():
+    h = D.FtDense()
+    t = 2 ** 31 - 1
+    y = torch.empty(t, 1, dtype=torch.bfloat16, device=DEV)
+    y[::2], y[1::2] = 3.0, -2.0
+    out = torch.zeros_like(y)
+    h.add_norm(y, None, None, out, eps=0.0, y_scale=2.0)
+    assert h.sync_status() == 0
+    assert (out[::2] == 1).all() and (out[1::2] == -1).all()
+    h.destroy()
