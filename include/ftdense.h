@@ -34,7 +34,8 @@ ft_status_t ft_dense_destroy(ft_dense_t *h);
  * r' = res_scale * res + y_scale * gate * u                                   -> res_out (if given)
  * h  = r' * rsqrt(mean(r'^2) + eps) * (w_offset + w_pre)                      -> out (if given)
  * over rows of d <= 16384 elements.  y, w_post, gate, w_pre and out are of `dtype` (bf16 or fp16), res and res_out of `res_dtype`
- * (the same, or fp32).  Computed in float, r' and h each rounded once (h from the r' that is not rounded yet).
+ * (the same, or fp32).  Computed in float, r' and h each rounded once (h from the r' that is not rounded yet);
+ * a mean whose squares leave the range of float is taken of the row times a power of two.
  *   y [T][d] or NULL (then r' = res_scale * res);  res [T][d] or NULL (then r' = y_scale * gate * u); not both
  *   gate NULL (one), else its element (t, i) stands at gate[t * gate_stride + i * gate_step], gate_step 0 or 1: a gate per element,
  *        per token (gate_step 0), per channel (gate_stride 0)

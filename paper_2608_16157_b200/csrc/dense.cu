@@ -260,6 +260,7 @@ ft_status_t ft_dense_add_norm(ft_dense_t *h, int T, int d, int dtype, int res_dt
   a.res = res; a.res_out = res_out; a.out = static_cast<uint16_t *>(out);
   a.y_stride = y_stride; a.res_stride = res_stride; a.gate_stride = gate_stride; a.res_out_stride = res_out_stride; a.out_stride = out_stride;
   a.w_offset = w_offset; a.eps = eps; a.res_scale = res_scale; a.y_scale = y_scale;
+  a.mean_low = eps > 1.3e-23f ? 0u : (127u - 100u) << 23;          // (2^-76), 2^-100
   auto rows16 = [&](const void *p, int64_t stride, int bytes) { return aligned(p, 16) && (T == 1 || stride * bytes % 16 == 0); };
   a.wide = (rows16(y, y_stride, 2) ? kWideY : 0u) | (rows16(res, res_stride, res32 ? 4 : 2) ? kWideRes : 0u) | (rows16(gate, gate_stride, 2) ? kWideGate : 0u) |
            (aligned(w_post, 16) ? kWidePost : 0u) | (aligned(w_pre, 16) ? kWidePre : 0u) | (rows16(res_out, res_out_stride, res32 ? 4 : 2) ? kWideResOut : 0u) |

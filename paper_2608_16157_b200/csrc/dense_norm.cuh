@@ -26,6 +26,7 @@ struct NormArgs {
   uint16_t *out;
   long long y_stride, res_stride, gate_stride, res_out_stride, out_stride;
   float w_offset, eps, res_scale, y_scale;
+  uint32_t mean_low;                 // bits of the float below which a mean of squares counts as lost
 };
 
 template <bool BF16>
@@ -122,11 +123,50 @@ __device__ __forceinline__ float row_sum(float v, int lanes, float *s) {
   return t;
 }
 
+__device__ __forceinline__ float row_max(float v, int lanes, float *s) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  if (lanes == 32) return v;
+  if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
+  __syncthreads();
+  float t = 0.f;
+  for (int i = 0; i < lanes >> 5; ++i) t = fmaxf(t, s[i]);
+  return t;
+}
+// 1 / sqrt(mean(x^2) + eps) of a row from the sum of its squares.  Where the squares have left the floats' range (a sum that is infinite, or below 2^-100
+// with an eps that does not cover what is lost), x becomes x f and what is returned belongs to that, f a power of two: then the larger of the
+// largest element and the root of eps is near one.
+template <int E>
+__device__ __forceinline__ float row_inv_rms(const NormArgs &a, float (&x)[E], float sum, float (*s)[32]) {
+  float mean = sum / (float)a.d, eps = a.eps;
+  // (the same for all of a row's threads; one comparison of the bits, beyond which infinity and NaN stand too)
+  if (__builtin_expect(__float_as_uint(mean) - a.mean_low >= 0x7f800000u - a.mean_low, 0)) {
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) top = fmaxf(top, fabsf(x[i]));
+    top = row_max(top, a.lanes, s[0]);
+    if (top > 0.f && top < INFINITY) {
+      int e = -ilogbf(top);
+      if (eps > 0.f) e = min(e, -ilogbf(eps) / 2);
+      const float f = ldexpf(1.f, min(e, 126));
+      sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        x[i] *= f;
+        sum = fmaf(x[i], x[i], sum);
+      }
+      mean = row_sum(sum, a.lanes, s[1]) / (float)a.d;
+      eps = eps * f * f;
+    }
+  }
+  return rsqrtf(mean + eps);
+}
+
 // VEC elements at a time; ALL: every array allows 16-byte accesses.
 template <bool BF16, bool RES32, bool POST, bool GATE, int VEC, bool ALL, int E>
 __global__ void __launch_bounds__(1024) add_norm_kernel(const NormArgs a) {
   constexpr int N = E / VEC;
-  __shared__ float s_sum[2][32];
+  __shared__ float s_sum[6][32];
   grid_let_next();
   const int lane = threadIdx.x & (a.lanes - 1);
   const long long t = (long long)blockIdx.x * (blockDim.x / a.lanes) + threadIdx.x / a.lanes;
@@ -172,7 +212,7 @@ __global__ void __launch_bounds__(1024) add_norm_kernel(const NormArgs a) {
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < E; ++i) sum = fmaf(u[i], u[i], sum);
-    inv = rsqrtf(row_sum(sum, a.lanes, s_sum[0]) / (float)a.d + a.eps);
+    inv = row_inv_rms<E>(a, u, row_sum(sum, a.lanes, s_sum[0]), s_sum + 2);
   }
   float sum = 0.f;
   char *res_out = static_cast<char *>(a.res_out) + t * a.res_out_stride * (RES32 ? 4 : 2);
@@ -211,7 +251,7 @@ __global__ void __launch_bounds__(1024) add_norm_kernel(const NormArgs a) {
     }
   });
   if (!a.out) return;
-  inv = rsqrtf(row_sum(sum, a.lanes, s_sum[1]) / (float)a.d + a.eps);
+  inv = row_inv_rms<E>(a, r, row_sum(sum, a.lanes, s_sum[1]), s_sum + 4);
   uint16_t *out = a.out + t * a.out_stride;
   each([&](int i, int j) {
     float h[VEC];
