@@ -12,7 +12,7 @@
 // a group of k has an accumulator of its own (two in turn), and eight warps add its sums times the row's scale to float sums in registers;
 // that takes about twice as long (reading an accumulator beside the tensor core costs 70 clocks for 16 tokens of 32 rows).
 // A weight that the type cannot hold (a scale above a fifteenth of its largest value may give one) makes every sum of its row infinite or NaN, whatever
-// the token: a block that has seen one computes the results of those rows again in the end, one a thread, in the exact form.  Right, and slow.
+// the token: a block that has seen one computes the results of those rows again in the end, a warp each, in the exact form.  Right, and slow.
 // Measured: 309 us for 4096 tokens through 7168 x 7168 (1.36 PFLOP/s, the power limit's rate), 87 us for 1024 tokens with groups of 32, 18.5 us for
 // 64 tokens.  With 17 tokens it passes the streaming kernel (24 tokens 17 against 22 us).
 // With a cluster of c blocks each takes 1/c of k, and the sums are added over distributed shared memory, in the blocks' order.
@@ -83,53 +83,62 @@ __device__ __forceinline__ bool w4_row_over(const W4Args &a, int n) {
   const int quad = n >> 6, m = g.tiles_of(quad), per = kW4Block / g.group;
   const uint8_t *sc = a.image + g.quad_at(quad) + m * 2 * kW4TileBytes + (n & 7) * 16 + (n >> 4 & 3) * 4 + (n >> 3 & 1) * 2;
   bool over = false;
-  for (int i = 0; i < g.nb * per; ++i)
-    over |= fabsf(to_float<BF16>(*reinterpret_cast<const uint16_t *>(sc + (long long)(i / per) * g.record(m) + i % per * 128))) >
-            (BF16 ? 3.3895313892515355e38f : 65504.f) / 15.f;
+  for (int b = 0; b < g.nb; ++b, sc += g.record(m))
+    for (int i = 0; i < per; ++i) over |= fabsf(to_float<BF16>(*reinterpret_cast<const uint16_t *>(sc + i * 128))) > (BF16 ? 3.3895313892515355e38f : 65504.f) / 15.f;
   return over;
 }
-// The sum of row n and token t in the exact form: a group's products with q - z, then the scale, in float.
+// The sum of row n and token t in the exact form, by a warp: a lane has 4 of 128 k, their products with q - z, then the scale, in float.
 template <bool BF16>
 __device__ __forceinline__ float w4_one(const W4Args &a, long long t, int n) {
   const W4Geom &g = a.g;
-  const int quad = n >> 6, m = g.tiles_of(quad), tile = n >> 4 & 3, gr = n & 7, high = n >> 3 & 1, per = kW4Block / g.group;
+  const int lane = threadIdx.x & 31, quad = n >> 6, m = g.tiles_of(quad), tile = n >> 4 & 3, gr = n & 7, high = n >> 3 & 1, s = lane * 4 / g.group;
+  const uint8_t *rec = a.image + g.quad_at(quad), *sc = rec + m * 2 * kW4TileBytes + s * 128 + gr * 16 + tile * 4 + high * 2;
+  const uint8_t *word = rec + ((lane >> 4) * m + tile) * kW4TileBytes + (gr * 4 + (lane & 3)) * 16 + (lane >> 2 & 3) * 4;
+  const uint8_t *zero = rec + m * 2 * kW4TileBytes + kW4Block / g.group * 128 + s * 64 + gr * 8 + tile * 2 + high;
   const uint16_t *x = a.x + t * a.x_stride;
   float sum = 0.f;
-  for (int k0 = 0; k0 < g.k; k0 += g.group) {
-    const uint8_t *rec = a.image + g.quad_at(quad) + (long long)(k0 / kW4Block) * g.record(m), *sc = rec + m * 2 * kW4TileBytes;
-    const int s = k0 % kW4Block / g.group;
-    const float scale = to_float<BF16>(*reinterpret_cast<const uint16_t *>(sc + s * 128 + gr * 16 + tile * 4 + high * 2));
-    const float zero = g.zeros ? (float)sc[per * 128 + s * 64 + gr * 8 + tile * 2 + high] : 8.f;
+  for (int k = lane * 4; k < g.k; k += kW4Block) {
+    const uint2 v = *reinterpret_cast<const uint2 *>(x + k);
+    const uint32_t w = *reinterpret_cast<const uint32_t *>(word), pair[2] = {v.x, v.y};
+    const float z = g.zeros ? (float)*zero : 8.f;
     float part = 0.f;
-    for (int k = k0; k < k0 + g.group; k += 4) {          // a word: pairs `high` and 2 + high are the row's
-      const int i = k % kW4Block;
-      const uint32_t w = *reinterpret_cast<const uint32_t *>(rec + ((i >> 6) * m + tile) * kW4TileBytes + (gr * 4 + (i >> 2 & 3)) * 16 + (i >> 4 & 3) * 4);
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const uint32_t c = rotl32(w, 32 - (high ? w4_bit<BF16>(2 * b + 1) : w4_bit<BF16>(2 * b)));
-        part = fmaf(to_float<BF16>(x[k + 2 * b]), (float)(c & 15u) - zero, part);
-        part = fmaf(to_float<BF16>(x[k + 2 * b + 1]), (float)(c >> 16 & 15u) - zero, part);
-      }
+    for (int b = 0; b < 2; ++b) {                  // (of a word, pairs `high` and 2 + high are the row's)
+      const uint32_t c = rotl32(w, 32 - (high ? w4_bit<BF16>(2 * b + 1) : w4_bit<BF16>(2 * b)));
+      float x0, x1;
+      to_float2<BF16>(pair[b], x0, x1);
+      part = fmaf(x0, (float)(c & 15u) - z, part);
+      part = fmaf(x1, (float)(c >> 16 & 15u) - z, part);
     }
-    sum = fmaf(scale, part, sum);
+    sum = fmaf(to_float<BF16>(*reinterpret_cast<const uint16_t *>(sc)), part, sum);
+    word += g.record(m);
+    sc += g.record(m);
+    zero += g.record(m);
   }
-  return sum;
+  return warp_sum(sum);
 }
 
-// A block's results in rows whose weights may be beyond the type's largest value.  Not inlined and with arguments of its own: an address of the kernel's
-// own ones costs it 2 us of 14 (512 tokens x 2048 x 5120), a copy of them 30 of 310 (4096 tokens x 7168 x 7168).
+// A block's results in rows whose weights may be beyond the type's largest value, a warp each.  Not inlined and with arguments of its own: an address of the
+// kernel's own ones costs it 2 us of 14 (512 tokens x 2048 x 5120), a copy of them 30 of 310 (4096 tokens x 7168 x 7168).
 struct W4Again { W4Args a; W4Tile p; };
 template <bool BF16>
 __device__ __noinline__ void w4_again(const W4Again &args, int threads) {
   const W4Args &a = args.a;
   const W4Tile &p = args.p;
-  const int rank = blockIdx.x % p.cluster, n_cl = gridDim.x / p.cluster, share = (p.bn + p.cluster - 1) / p.cluster;
+  const int rank = blockIdx.x % p.cluster, n_cl = gridDim.x / p.cluster, share = (p.bn + p.cluster - 1) / p.cluster, lane = threadIdx.x & 31;
   for (int u = blockIdx.x / p.cluster; u < p.row_tiles * p.tok_tiles; u += n_cl) {
-    const int tok0 = u / p.row_tiles * p.bn + rank * share, n = u % p.row_tiles * 128 + (threadIdx.x & 127);
+    const int tok0 = u / p.row_tiles * p.bn + rank * share, row0 = u % p.row_tiles * 128;
     const int n_tok = min(min(share, p.bn - rank * share), a.T - tok0);
-    if (n >= a.g.n || !w4_row_over<BF16>(a, n)) continue;
-#pragma unroll 1
-    for (int t = threadIdx.x >> 7; t < n_tok; t += threads / 128) w4_store<BF16>(a, tok0 + t, n, w4_one<BF16>(a, tok0 + t, n));
+    for (int r = 0; r < 128; r += 32) {
+      uint32_t rows = __ballot_sync(0xffffffffu, row0 + r + lane < a.g.n && w4_row_over<BF16>(a, row0 + r + lane));
+      for (; rows; rows &= rows - 1) {
+        const int n = row0 + r + __ffs(rows) - 1;
+        for (int t = threadIdx.x >> 5; t < n_tok; t += threads / 32) {
+          const float v = w4_one<BF16>(a, tok0 + t, n);
+          if (lane == 0) w4_store<BF16>(a, tok0 + t, n, v);
+        }
+      }
+    }
   }
 }
 
