@@ -9,7 +9,7 @@
 // in 16 bits, reaches it.  The four with a thread's maximum waits in shared memory (read again from
 // global memory it took 2.4 us a row, the rows under way being more than L2 holds).  The main loop thus does next to nothing for them.
 // Candidates are ranked by counting, as keys (logit, then lowest id).
-// Measured: 126 us for 2048 rows of 150000 in bf16 (4.87 TB/s, 0.76 of a copy's rate), 77 us for 1024 rows of 100000 floats (5.3 TB/s), 7.5 us for one
+// Measured: 127 us for 2048 rows of 150000 in bf16 (4.8 TB/s, 0.75 of a copy's rate), 77 us for 1024 rows of 100000 floats (5.3 TB/s), 7.4 us for one
 // row of 150000.
 #pragma once
 #include "async.cuh"

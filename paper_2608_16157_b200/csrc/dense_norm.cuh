@@ -5,8 +5,8 @@
 // a row is read once, whatever is written over it.  All loads of y, r and the gate go out before the first sum.  E = 16, or 8 for few rows, where
 // latency counts.  Where d is a multiple of 8 a thread has 8 neighbouring elements at a time, in one access for each array whose rows all
 // start on 16 bytes; else single elements, neighbouring threads on neighbouring elements (twice the time: the load and store units are
-// then the bound).  Measured: 60 us for 16384 tokens of 2048 with a float stream (6.7 TB/s), 61 us in bf16 with norms on both sides and a
-// gate per channel (4.4 TB/s), 2.1 us for 8 tokens.
+// then the bound).  Measured: 60 us for 16384 tokens of 2048 with a float stream (6.7 TB/s), 62 us in bf16 with norms on both sides and a
+// gate per channel (4.3 TB/s), 2.1 us for 8 tokens.
 #pragma once
 #include "async.cuh"
 #include "common.cuh"

@@ -13,8 +13,8 @@
 // in place or after one shift or rotation: (w & mask) | magic is the pair 16 + q, from which 16 + z is subtracted exactly.
 //
 // w4_stream_kernel, up to 16 tokens (32 for float results): weights on M, tokens on N = 8, 16 or 32.  Bound: HBM for large matrices (N K / 2
-// bytes), launch and latency for small ones.  Measured: 35 us for 5 tokens through 2048 x 150001 (4.7 TB/s; 18.9 instructions per 256 weights),
-// 4.5 us for one token through 2048 x 5120, 9.7 us through 7168 x 7168.
+// bytes), launch and latency for small ones.  Measured: 37 us for 5 tokens through 2048 x 150001 (4.5 TB/s; 18.5 instructions per 256 weights)
+// and 55 for 16, 4.7 us for one token through 2048 x 5120, 9.9 us through 7168 x 7168.
 #pragma once
 #include <type_traits>
 

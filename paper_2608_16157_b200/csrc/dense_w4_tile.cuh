@@ -7,14 +7,15 @@
 //   expanding     turn codes into 16-bit numbers and leave them in tensor memory
 //   mma warp      rows on M = 128 (A from tensor memory), tokens on N (B from shared memory)
 // Two forms.  For 16-bit results the operands are the weights s (q - z), rounded once to the type (8 or 11 bits of scale times 4 of code do
-// not fit it): an error of the size of the result's own rounding, 0.0013 of the result in bf16 where that is 0.0017.  The tensor core adds
+// not fit it): an error of the size of the result's own rounding, 0.0014 of the result in bf16 where that is 0.0017.  The tensor core adds
 // over all of k, and four warps take the sums out while it works on the next unit.  For float results (EXACT) the operands are the exact q - z,
 // a group of k has an accumulator of its own (two in turn), and eight warps add its sums times the row's scale to float sums in registers;
-// that takes about twice as long (reading an accumulator beside the tensor core costs 70 clocks for 16 tokens of 32 rows).
+// that takes 1.3 to 2.3 times as long (reading an accumulator beside the tensor core costs 70 clocks for 16 tokens of 32 rows): 22 against 17 us for 24
+// tokens through 7168 x 7168, 26 against 18.5 for 64, 448 against 310 for 4096; 144 against 62 for 64 tokens through 2048 x 150001 in groups of 64.
 // A weight that the type cannot hold (a scale above a fifteenth of its largest value may give one) makes every sum of its row infinite or NaN, whatever
 // the token: a block that has seen one computes the results of those rows again in the end, a warp each, in the exact form.  Right, and slow.
-// Measured: 309 us for 4096 tokens through 7168 x 7168 (1.36 PFLOP/s, the power limit's rate), 87 us for 1024 tokens with groups of 32, 18.5 us for
-// 64 tokens.  With 17 tokens it passes the streaming kernel (24 tokens 17 against 22 us).
+// Measured: 310 us for 4096 tokens through 7168 x 7168 (1.36 PFLOP/s, 0.82 of a library product's rate for as short a run; 365 in a long one, 0.83 of the rate
+// that holds there), 88 us for 1024 tokens with groups of 32, 18.5 us for 64 tokens.  With 17 tokens it passes the streaming kernel (24 tokens 17 against 22 us).
 // With a cluster of c blocks each takes 1/c of k, and the sums are added over distributed shared memory, in the blocks' order.
 #pragma once
 #include "dense_w4.cuh"
