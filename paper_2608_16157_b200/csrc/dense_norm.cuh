@@ -148,7 +148,7 @@ __device__ __forceinline__ float row_inv_rms(const NormArgs &a, float (&x)[E], f
     if (top > 0.f && top < INFINITY) {
       int e = -ilogbf(top);
       if (eps > 0.f) e = min(e, -ilogbf(eps) / 2);
-      const float f = ldexpf(1.f, min(e, 126));
+      const float f = ldexpf(1.f, max(min(e, 126), -127));
       sum = 0.f;
 #pragma unroll
       for (int i = 0; i < E; ++i) {

@@ -78,3 +78,15 @@ def test_a_row_of_zeros_without_an_eps_is_not_a_number():
     h.add_norm(None, torch.zeros(2, 64, device=DEV), None, out, eps=0.0)
     assert torch.isnan(out).all()
     h.destroy()
+
+
+@pytest.mark.parametrize("t,d", [(4, 320), (700, 2048)])
+def test_an_infinite_eps_leaves_nothing(t, d):
+    h = D.FtDense()
+    y = (1e30 * torch.randn(t, d, generator=gen(1), device=DEV)).bfloat16()
+    out, ro = torch.ones_like(y), torch.ones_like(y)
+    h.add_norm(y, None, ro, out, eps=float("inf"))
+    assert (out == 0).all() and torch.equal(ro, y)
+    h.add_norm(y, None, ro, out, eps=float("inf"), post=True)
+    assert (out == 0).all() and (ro == 0).all()
+    h.destroy()
