@@ -35,13 +35,14 @@ struct LogpArgs {
 
 constexpr float kLogpMaxScale = 8.507059173023462e37f;   // 2^126: twice c log2 e is finite
 
-// The scale, and below which magnitude of the maximum m exponents may be taken from the rounded product m c2: no product overflows, and |m c2| < 2^31, so
-// that what the product lost in rounding, which is the maximum's own exponent, stays within 64 (it is some hundreds for -1e10: sums of 0 or infinity).
+// The scale, and below which magnitude of the maximum m exponents may be taken from the rounded product m c2: no product overflows, and |m c2| < 2^25, so
+// that what the product lost in rounding, which is the maximum's own exponent, stays within 1.  (It is 64 for -1e9, where the weighted sum loses as many times
+// its own rounding when that is taken out again, and some hundreds for -1e10: sums of 0 or infinity.)
 inline void logp_scale(LogpArgs &a, float scale) {
   a.scale = scale;
   a.c2 = scale * 1.44269504088896f;
   a.twice_c2 = 2.f * a.c2;
-  a.plain_below = a.c2 >= 1e8f ? 0.f : a.c2 < 2147483648.f / 1e29f ? 1e29f : 2147483648.f / a.c2;
+  a.plain_below = a.c2 >= 1e8f ? 0.f : a.c2 < 33554432.f / 1e29f ? 1e29f : 33554432.f / a.c2;
 }
 
 enum { kLogpBf16 = 0, kLogpFp16 = 1, kLogpFp32 = 2 };
@@ -75,6 +76,13 @@ struct LogpType {
     if (TY == kLogpFp32) asm("max.NaN.f32 %0, %1, %2;" : "=f"(reinterpret_cast<float &>(d)) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)));
     else if (TY == kLogpBf16) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+  }
+  static __device__ __forceinline__ uint32_t min_nan(uint32_t a, uint32_t b) {
+    uint32_t d;
+    if (TY == kLogpFp32) asm("min.NaN.f32 %0, %1, %2;" : "=f"(reinterpret_cast<float &>(d)) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)));
+    else if (TY == kLogpBf16) asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    else asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
   }
   static __device__ __forceinline__ uint32_t raise_word(uint32_t a) { return max_nan(a, floor_bits()); }
@@ -277,13 +285,23 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
       Y::split(any, x, y);
       if (x != x || y != y) acc.s = NAN;
     } else {
-#pragma unroll 1
-      for (int i = 0; i < kAhead; ++i) {
-        const uint4 p = i == 0 ? q[0] : i == 1 ? q[1] : i == 2 ? q[2] : q[3];
-        float x[E];
-        Y::unpack(p, x);
+      // (where a mask's value is all that a thread has seen, as a rule all elements are that)
+      uint32_t least = Y::min_nan(Y::min_nan(q[0].x, q[0].y), Y::min_nan(q[0].z, q[0].w));
 #pragma unroll
-        for (int j = 0; j < E; ++j) add_one(x[j]);
+      for (int i = 1; i < kAhead; ++i) least = Y::min_nan(least, Y::min_nan(Y::min_nan(q[i].x, q[i].y), Y::min_nan(q[i].z, q[i].w)));
+      float lo, hi;
+      Y::split(least, lo, hi);
+      if (lo == acc.m && hi == acc.m && lo < INFINITY) {
+        acc.s += (float)(kAhead * E);
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < kAhead; ++i) {
+          const uint4 p = i == 0 ? q[0] : i == 1 ? q[1] : i == 2 ? q[2] : q[3];
+          float x[E];
+          Y::unpack(p, x);
+#pragma unroll
+          for (int j = 0; j < E; ++j) add_one(x[j]);
+        }
       }
     }
   };

@@ -79,3 +79,11 @@ def test_logp_scales_beyond_the_largest_are_refused():
     h.logprobs(x, entropy=e, scale=2.0 ** 126)
     assert (e - 4.605170186).abs().max() < 1e-5
     h.destroy()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("t,v", [(300, 87103), (20, 60001)])
+def test_logp_entropy_of_rows_of_one_far_value(dtype, t, v):
+    """Every row holds one value of its own between -1e7 and -1e9: the logarithm of the vocabulary to float's accuracy, whatever the products lost."""
+    x = -(10.0 ** torch.linspace(7, 9, t, device=DEV))[:, None].expand(t, v)
+    run_logp(x.to(R.DT[dtype]).contiguous(), 3, seed=t)
