@@ -61,9 +61,10 @@ ft_status_t ft_dense_w4_pack(ft_dense_t *h, int64_t n, int64_t k, int group, int
 /* y[t][i] = sum_k x[t][k] * w[i][k] + bias[i].  x DEVICE [T][k] of `dtype`, 16-byte aligned, x_stride a multiple of 8 and < 2^38; T <= 2^20; bias
  * DEVICE [n] of `dtype` or NULL; y DEVICE [T][n] of out_dtype (`dtype` or fp32), any alignment of whole elements.  Up to 16 tokens, and for fp32
  * results at any number, the codes less their zero point are multiplied exactly, sums are float, and scales are applied to the sums of a
- * group in float (a group's sum without its scale has to be a float too: x beyond 10^35 may give infinities).  For 16-bit results of more tokens each weight is rounded once to `dtype` before it is multiplied (an error of the size of
- * the result's own rounding); rows with a scale above 1/15 of the type's largest value, whose weights it may not hold, are then computed in the exact
- * form all the same, slowly.  y is rounded once; it overlaps none of the inputs.  n, k, group, dtype and has_zeros must be those of the image. */
+ * group in float (a group's sum without its scale has to be a float too: x beyond 10^35 may give infinities).  For 16-bit results of more tokens
+ * each weight is rounded once to `dtype` before it is multiplied (an error of the size of the result's own rounding); rows with a scale above 1/15 of
+ * the type's largest value, whose weights it may not hold, are then computed in the exact form all the same, slowly.  y is rounded once; it overlaps
+ * none of the inputs.  n, k, group, dtype and has_zeros must be those of the image. */
 ft_status_t ft_dense_w4_forward(ft_dense_t *h, int T, int64_t n, int64_t k, int group, int dtype, int has_zeros, const void *x,
                                 int64_t x_stride, const void *image, const void *bias, void *y, int64_t y_stride, int out_dtype,
                                 void *stream);
